@@ -136,6 +136,9 @@ def prepare(case, seed):
     S, H = case["S"], case["H"]
     if case["kind"] == "append":
         at = _lengths(case, g, case["old"]) if case["old"] else torch.zeros(S, dtype=torch.int32, device="cuda")
+        # every pass writes the same tokens again, as a rejected draft is written over: the rows before them in their
+        # block have to be staged still, so the write ends in the block that it begins in, or begins with a block
+        at = at // B * B + torch.clamp(at % B, max=max(0, B - case["n"]))
         cap = -(-(case["old"] + case["n"]) // B) * B
         c = _filled(g, S, H, cap, at, False)
         dt = torch.bfloat16 if case["src"] == "bf16" else torch.float32
