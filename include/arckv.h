@@ -73,6 +73,8 @@ typedef enum {
 /* Flags (arckv_config.flags). */
 #define ARCKV_FLAG_NONBLOCKING 0x1u /* do not synchronise; see arckv_query_status */
 #define ARCKV_FLAG_COMPACT_BF16 0x2u /* arckv_attend_joint: C_k, C_v are bf16, not fp32 */
+#define ARCKV_FLAG_F32 0x4u /* arckv_cache_append: K, V are fp32, not bf16; arckv_cache_read: so are the outputs */
+#define ARCKV_FLAG_CAUSAL 0x8u /* arckv_cache_attend, arckv_cache_select: position p of n_pos is token len - n_pos + p */
 
 /*
  * Problem description for one layer.  Sizes:
@@ -295,6 +297,129 @@ size_t arckv_attend_static_floats(int32_t H_kv, int32_t n, int32_t t, int32_t d)
 arckv_status arckv_attend_static(int32_t H_kv, int32_t n, int32_t t, int32_t d, float logit_scale,
                                  const void* Q, const float* C_k, const float* beta, const float* C_v,
                                  float* O, void* stream);
+
+/*
+ * Caches held in 8 bits.  The paper has no counterpart: these calls keep a
+ * full or a compact cache at half the bytes of bf16 and serve the decode loop
+ * from it.
+ *
+ * Tokens are cut into blocks of ARCKV_CACHE_BLOCK = 64.  A block of one
+ * (sequence, KV head) with rows x_i holds, for K and for V each,
+ *     a     = max(max_{i,e} |x_ie|, 2^-100)           its magnitude
+ *     scale = a * fl(1/127)                           fp32
+ *     c_ie  = rint(x_ie * fl(127 / a))  in [-127, 127]   stored as c + 128
+ * and stands for the values c_ie * scale (products rounded to fp32).  For K it
+ * also holds the least and largest code of every dimension, from which
+ * arckv_cache_select bounds the block's logits.  Rows are quantised as they
+ * are written: the rows of the newest block stay staged in fp32, and when a new
+ * row raises the block's magnitude its earlier rows are quantised again, so the
+ * cache's content depends on its tokens alone, not on how they were cut into
+ * calls.
+ *
+ * All arrays are device memory of the caller, 16-byte aligned and dense; the
+ * cache is empty when len is zero, and `state` and `len` must be zeroed before
+ * the first call (the other arrays may hold anything):
+ *   S sequences, H KV heads, cap tokens of capacity (a multiple of 64), d = 128
+ *   K, V        uint8 [S][H][cap][d]        codes
+ *   k_scale, v_scale  fp32 [S][H][cap/64]
+ *   bounds      int8 [S][H][cap/64][2][d]   least, largest code of K
+ *   bias        fp32 [S][H][cap] or NULL    added to the logits of a token (beta of a compact cache)
+ *   tail        fp32 [S][H][2][64][d]       staged rows of the newest block (K, V)
+ *   tail_amax   fp32 [S][H][2][64]          their magnitudes
+ *   len         int32 [S]                   tokens held
+ *   state       256 bytes: the status word of append and read, and a counter
+ * Lengths live on the device only: a decode loop can be captured in a CUDA
+ * graph and replayed while the caches grow.
+ *
+ * Status: append and read record device errors in `state`, attend and select
+ * in the first word of `ws`.  Unlike the calls above, these do not clear the
+ * word when they start: with ARCKV_FLAG_NONBLOCKING an error stays until
+ * arckv_query_status(state or ws) reads and clears it, and a blocking call
+ * reads and clears it.
+ */
+#define ARCKV_CACHE_BLOCK 64
+typedef struct {
+  int32_t S, H, cap, d;
+  uint8_t *K, *V;
+  float *k_scale, *v_scale;
+  int8_t* bounds;
+  float* bias;
+  float *tail, *tail_amax;
+  int32_t* len;
+  void* state;
+} arckv_cache8;
+
+/*
+ * Write n new rows of every sequence and head at its end, and advance len.
+ *   K, V      bf16 (fp32 with ARCKV_FLAG_F32); the row of token i of head h of
+ *             sequence s begins strides[0] s + strides[1] h + strides[2] i
+ *             elements after the base (NULL: dense [S][H][n][d]).  Base and
+ *             strides are multiples of 16 bytes.
+ *   bias      fp32 [S][H][n] or NULL (zeros); NULL when the cache has none
+ *   at        int32 [S] device or NULL: first token written instead of len[s],
+ *             which writes over rejected tokens.  It must be a multiple of 64
+ *             or in the newest block, and at most len[s].
+ *   counts    int32 [S] device or NULL (n): rows of sequence s that are written,
+ *             the first counts[s] of its n (0 leaves the sequence as it is)
+ * A sequence whose at, count or end (above cap) is out of range is left as it
+ * is and records ARCKV_ERR_SHAPE.  Non-finite elements are written as zero and
+ * record ARCKV_ERR_NONFINITE.
+ */
+arckv_status arckv_cache_append(const arckv_cache8* c, int32_t n, const void* K, const int64_t* k_strides,
+                                const void* V, const int64_t* v_strides, const float* bias, const int32_t* at,
+                                const int32_t* counts, uint32_t flags, void* stream);
+
+/*
+ * Read back `count` tokens of every sequence from token `start` on (a negative
+ * start counts from the sequence's length), as the values the codes stand for:
+ *   K_out, V_out  bf16 (fp32 with ARCKV_FLAG_F32) [S][H][count][d]; either may
+ *   be NULL.  Tokens outside [0, len[s]) read as zero.
+ */
+arckv_status arckv_cache_read(const arckv_cache8* c, int32_t start, int32_t count, void* K_out, void* V_out,
+                              uint32_t flags, void* stream);
+
+/* Workspace bytes of arckv_cache_attend and arckv_cache_select (0 if the sizes
+ * are invalid).  Host-only.  The first ARCKV_CACHE_WS_HEADER bytes of the
+ * workspace must be zeroed once before its first use; calls leave them zero
+ * (but for the status word). */
+#define ARCKV_CACHE_WS_HEADER 4096
+size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G);
+
+/*
+ * Attention over the cache:
+ *   O[s,h,p,g] = softmax_j(logit_scale q . k_j + bias_j) v_j  over the visible tokens j,
+ * j < len[s], or with ARCKV_FLAG_CAUSAL j <= len[s] - n_pos + p (the query
+ * positions are the newest n_pos tokens).  A row that sees no token, or only
+ * biases of -inf, is zero.
+ *   Q  bf16, n_pos positions of the G query heads of each KV head: row (p, g)
+ *      begins q_strides[0] s + q_strides[1] h + q_strides[2] p + 128 g elements
+ *      after the base (NULL: dense [S][H][n_pos][G][d]); base and strides are
+ *      multiples of 16 bytes
+ *   O  out fp32, addressed in the same way with o_strides
+ *   blocks  NULL: all tokens; else int32 [S][H][n_pos][m] block indices, the
+ *      only ones that position p of head h reads (arckv_cache_select writes
+ *      them; distinct, in any order, -1 for none; an index past the cache
+ *      records ARCKV_ERR_INVALID_ARG and is passed over)
+ */
+arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G, float logit_scale, const void* Q,
+                                const int64_t* q_strides, const int32_t* blocks, int32_t m, float* O,
+                                const int64_t* o_strides, void* ws, size_t ws_bytes, uint32_t flags, void* stream);
+
+/*
+ * The m blocks that each query position reads, by a bound of their logits: with
+ * the query row quantised like a block of one row (code qc, scale s_q),
+ *   I(b) = sum_e max(qc_e lo_be, qc_e hi_be)         an exact integer
+ *   score(b) = max_g fl(fl(s_q I(b)) k_scale[b])
+ * The first keep_first and the newest keep_last blocks that the position sees
+ * are always taken, then the highest scores, ties to the lower block.
+ *   blocks  out int32 [S][H][n_pos][m], ascending; -1 after the last when the
+ *           position sees fewer than m
+ * 1 <= m <= 8192, keep_first + keep_last <= m.  Q as for arckv_cache_attend.
+ * Biases play no part.
+ */
+arckv_status arckv_cache_select(const arckv_cache8* c, int32_t n_pos, int32_t G, int32_t m, int32_t keep_first,
+                                int32_t keep_last, const void* Q, const int64_t* q_strides, int32_t* blocks, void* ws,
+                                size_t ws_bytes, uint32_t flags, void* stream);
 
 /* Read (and clear) the device status word of a workspace after a
  * non-blocking call; synchronises `stream`. */

@@ -18,7 +18,8 @@ __all__ = [
     "attend_workspace_bytes", "arckv_compact", "arckv_attend", "arckv_query_status", "status_string",
     "compact_layer", "attend", "INDEXER_FIELDS", "attend_joint", "arckv_attend_joint",
     "attend_joint_workspace_bytes", "FLAG_COMPACT_BF16", "truncated_error", "arckv_truncated_error", "SELECTOR_INDEXER", "SELECTOR_HA", "SELECTOR_VI",
-    "arckv_wait_probe",
+    "arckv_wait_probe", "Cache8", "cache_alloc", "cache_workspace", "cache_append", "cache_read", "cache_attend",
+    "cache_select", "CACHE_BLOCK", "FLAG_F32", "FLAG_CAUSAL",
 ]
 
 _LIB_PATH = Path(__file__).resolve().parent / "libarckv.so"
@@ -31,6 +32,10 @@ STATUS = {
 }
 FLAG_NONBLOCKING = 0x1
 FLAG_COMPACT_BF16 = 0x2
+FLAG_F32 = 0x4
+FLAG_CAUSAL = 0x8
+CACHE_BLOCK = 64
+CACHE_WS_HEADER = 4096
 SELECTOR_INDEXER, SELECTOR_HA, SELECTOR_VI = 0, 1, 2
 NUM_STAGES = 11
 STAGE_NAMES = ("indexer_features", "index_logits", "pool_top_t", "reference_attention", "column_profiles",
@@ -59,6 +64,12 @@ class _Indexer(ctypes.Structure):
 class _Aux(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("scores", "anchors", "assign", "anchors_in", "assign_in", "stage_events", "launches")]
+
+
+class _Cache8(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("S", "H", "cap", "d")] +
+                [(n, ctypes.c_void_p) for n in ("K", "V", "k_scale", "v_scale", "bounds", "bias", "tail", "tail_amax",
+                                                "len", "state")])
 
 
 @dataclasses.dataclass
@@ -127,6 +138,18 @@ def load_library():
     lib.arckv_truncated_error.argtypes = [ctypes.c_int32] * 5 + [ctypes.c_float] + [P] * 5 + [P, ctypes.c_size_t,
                                                                                               ctypes.c_uint32, P]
     lib.arckv_truncated_error.restype = ctypes.c_int
+    I, L3, C = ctypes.c_int32, ctypes.POINTER(ctypes.c_int64 * 3), ctypes.POINTER(_Cache8)
+    lib.arckv_cache_workspace_bytes.argtypes = [I] * 6
+    lib.arckv_cache_workspace_bytes.restype = ctypes.c_size_t
+    lib.arckv_cache_append.argtypes = [C, I, P, L3, P, L3, P, P, P, ctypes.c_uint32, P]
+    lib.arckv_cache_append.restype = ctypes.c_int
+    lib.arckv_cache_read.argtypes = [C, I, I, P, P, ctypes.c_uint32, P]
+    lib.arckv_cache_read.restype = ctypes.c_int
+    lib.arckv_cache_attend.argtypes = [C, I, I, ctypes.c_float, P, L3, P, I, P, L3, P, ctypes.c_size_t,
+                                       ctypes.c_uint32, P]
+    lib.arckv_cache_attend.restype = ctypes.c_int
+    lib.arckv_cache_select.argtypes = [C, I, I, I, I, I, P, L3, P, P, ctypes.c_size_t, ctypes.c_uint32, P]
+    lib.arckv_cache_select.restype = ctypes.c_int
     lib.arckv_query_status.argtypes = [P, P]
     lib.arckv_query_status.restype = ctypes.c_int
     lib.arckv_wait_probe.argtypes = [P, ctypes.c_size_t, ctypes.c_uint32, P]
@@ -410,3 +433,218 @@ def truncated_error(Q_eval, K, V, S, logit_scale: float = 0.0, *, stream=None, c
     if check and st != 0:
         raise ArckvError(st, "arckv_truncated_error")
     return E
+
+
+# ------------------------------------------------------- caches held in 8 bits
+
+@dataclasses.dataclass(frozen=True, eq=False)
+class Cache8:
+    """An 8-bit KV cache of S sequences and H KV heads (mirrors ``arckv_cache8``; the header has the layout and what
+    the codes stand for).  ``cache_alloc`` makes an empty one; the tensors stay the caller's and are not replaced."""
+    K: object                     # uint8 [S, H, cap, 128]
+    V: object
+    k_scale: object               # fp32 [S, H, cap / 64]
+    v_scale: object
+    bounds: object                # int8 [S, H, cap / 64, 2, 128]
+    tail: object                  # fp32 [S, H, 2, 64, 128]
+    tail_amax: object             # fp32 [S, H, 2, 64]
+    len: object                   # int32 [S], tokens held
+    bias: object = None           # fp32 [S, H, cap] or None
+    state: object = None          # uint8 [256], made here unless given
+
+    def __post_init__(self):
+        import torch
+        u8, f32 = (torch.uint8,), (torch.float32,)
+        _expect("K", self.K, u8, (None, None, None, 128))
+        S, H, cap, d = self.K.shape
+        if cap < CACHE_BLOCK or cap % CACHE_BLOCK:
+            raise ValueError("arckv: the capacity must be a positive multiple of %d, got %d" % (CACHE_BLOCK, cap))
+        nb = cap // CACHE_BLOCK
+        _expect("V", self.V, u8, (S, H, cap, d))
+        _expect("k_scale", self.k_scale, f32, (S, H, nb))
+        _expect("v_scale", self.v_scale, f32, (S, H, nb))
+        _expect("bounds", self.bounds, (torch.int8,), (S, H, nb, 2, d))
+        _expect("tail", self.tail, f32, (S, H, 2, CACHE_BLOCK, d))
+        _expect("tail_amax", self.tail_amax, f32, (S, H, 2, CACHE_BLOCK))
+        _expect("len", self.len, (torch.int32,), (S,))
+        if self.bias is not None:
+            _expect("bias", self.bias, f32, (S, H, cap))
+        if self.state is None:
+            object.__setattr__(self, "state", torch.zeros(256, dtype=torch.uint8, device=self.K.device))
+        _expect("state", self.state, u8, (256,))
+        _on_one_cuda_device(K=self.K, V=self.V, k_scale=self.k_scale, v_scale=self.v_scale, bounds=self.bounds,
+                            tail=self.tail, tail_amax=self.tail_amax, len=self.len, bias=self.bias, state=self.state)
+        object.__setattr__(self, "_c", _Cache8(S, H, cap, d, *[_ptr(getattr(self, n)) for n, _ in _Cache8._fields_[4:]]))
+
+    @property
+    def capacity(self) -> int:
+        return self._c.cap
+
+
+def cache_alloc(S: int, H: int, capacity: int, *, bias: bool = False, device="cuda") -> Cache8:
+    """An empty cache of at least `capacity` tokens for S sequences and H KV heads; with `bias` it holds a logit bias
+    for each token (the beta of a compact cache)."""
+    import torch
+    cap = max(1, -(-capacity // CACHE_BLOCK)) * CACHE_BLOCK
+    nb = cap // CACHE_BLOCK
+    def e(*shape, dt=torch.float32, f=torch.empty):
+        return f(*shape, dtype=dt, device=device)
+    return Cache8(K=e(S, H, cap, 128, dt=torch.uint8), V=e(S, H, cap, 128, dt=torch.uint8), k_scale=e(S, H, nb),
+                  v_scale=e(S, H, nb), bounds=e(S, H, nb, 2, 128, dt=torch.int8), tail=e(S, H, 2, CACHE_BLOCK, 128),
+                  tail_amax=e(S, H, 2, CACHE_BLOCK), len=e(S, dt=torch.int32, f=torch.zeros),
+                  bias=e(S, H, cap) if bias else None)
+
+
+def cache_workspace(cache: Cache8, n_pos: int, G: int):
+    """A workspace for ``cache_attend`` and ``cache_select`` with up to n_pos positions of G query heads.  Calls that
+    may run at the same time need one each."""
+    import torch
+    c = cache._c
+    need = int(load_library().arckv_cache_workspace_bytes(c.S, c.H, c.cap, c.d, n_pos, G))
+    if need == 0:
+        raise ArckvError(2, "arckv_cache_workspace_bytes")
+    ws = torch.empty(need, dtype=torch.uint8, device=cache.K.device)
+    ws[:CACHE_WS_HEADER].zero_()
+    return ws
+
+
+def _strides3(name: str, x, dense_from: int):
+    """The first three strides of x, whose dimensions from `dense_from` on must be dense."""
+    st = x.stride()
+    want = 1
+    for i in range(x.dim() - 1, dense_from - 1, -1):
+        if st[i] != want and x.shape[i] != 1:
+            raise ValueError("arckv: the last %d dimensions of %s must be dense, got strides %s"
+                             % (x.dim() - dense_from, name, st))
+        want *= x.shape[i]
+    return (ctypes.c_int64 * 3)(*[st[i] if x.shape[i] != 1 else 0 for i in range(3)])
+
+
+def _on_stream(stream, device, *tensors):
+    """The raw handle of `stream` (None: the current one) and a context in which new tensors belong to it; tensors in
+    use on a stream other than the current one are recorded there, so that their memory is not reused too early."""
+    import contextlib
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    if stream != torch.cuda.current_stream(device):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream=None, check: bool = True) -> None:
+    """Write the rows K, V [S, H, n, 128] (bf16 or fp32, dense in the last dimension) at the end of every sequence.
+    bias [S, H, n]: their logit biases (zeros when not given).  at [S] int32: first token written instead of the end,
+    over rejected tokens of the newest block.  counts [S] int32: how many of the n rows each sequence takes.
+    With check=False the call only enqueues, and ``arckv_query_status(cache.state)`` reports errors."""
+    import torch
+    c = cache._c
+    n = K.shape[2] if K.dim() == 4 else -1
+    for name, x in (("K", K), ("V", V)):
+        if x.dtype != K.dtype or x.dtype not in (torch.bfloat16, torch.float32) or tuple(x.shape) != (c.S, c.H, n, 128):
+            raise ValueError("arckv: %s must be bfloat16 or float32 (K and V alike) of shape %s, got %s %s"
+                             % (name, (c.S, c.H, "n", 128), x.dtype, tuple(x.shape)))
+    if bias is not None:
+        if cache.bias is None:
+            raise ValueError("arckv: this cache holds no bias")
+        _expect("bias", bias, (torch.float32,), (c.S, c.H, n))
+    for name, x in (("at", at), ("counts", counts)):
+        if x is not None:
+            _expect(name, x, (torch.int32,), (c.S,))
+    _on_one_cuda_device(cache=cache.K, K=K, V=V, bias=bias, at=at, counts=counts)
+    if n == 0:
+        return
+    handle, _ = _on_stream(stream, K.device, K, V, bias, at, counts, cache.K, cache.V)
+    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if K.dtype == torch.float32 else 0)
+    st = load_library().arckv_cache_append(ctypes.byref(c), n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
+                                           _strides3("V", V, 3), _ptr(bias), _ptr(at), _ptr(counts), flags, handle)
+    if st != 0:
+        raise ArckvError(st, "arckv_cache_append")
+
+
+def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None, check: bool = True):
+    """The values that `count` tokens from `start` on stand for (negative: from each sequence's end), as a pair
+    K, V [S, H, count, 128] in bf16 (or dtype=torch.float32); tokens that a sequence does not hold are zero."""
+    import torch
+    c = cache._c
+    dtype = torch.bfloat16 if dtype is None else dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
+    handle, ctx = _on_stream(stream, cache.K.device, cache.K, cache.V)
+    with ctx:
+        K = torch.empty(c.S, c.H, max(count, 0), 128, dtype=dtype, device=cache.K.device)
+        V = torch.empty_like(K)
+    if count == 0:
+        return K, V
+    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
+    st = load_library().arckv_cache_read(ctypes.byref(c), start, count, K.data_ptr(), V.data_ptr(), flags, handle)
+    if st != 0:
+        raise ArckvError(st, "arckv_cache_read")
+    return K, V
+
+
+def _check_queries(cache: Cache8, Q):
+    import torch
+    c = cache._c
+    if Q.dim() != 5 or Q.dtype != torch.bfloat16 or Q.shape[0] != c.S or Q.shape[1] != c.H or Q.shape[4] != 128:
+        raise ValueError("arckv: Q must be bfloat16 of shape %s, got %s %s"
+                         % ((c.S, c.H, "n_pos", "G", 128), Q.dtype, tuple(Q.shape)))
+    if Q.device != cache.K.device:
+        raise ValueError("arckv: Q is on %s but the cache on %s" % (Q.device, cache.K.device))
+
+
+def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, causal: bool = False, out=None, ws=None,
+                 stream=None, check: bool = True):
+    """O = softmax(scale Q K^T + bias) V over the cache for Q [S, H, n_pos, G, 128] bf16 (the last two dimensions
+    dense); returns fp32 of the same shape, or fills `out`.  causal: the positions are the newest n_pos tokens, and
+    each sees the tokens up to itself.  blocks [S, H, n_pos, m] int32: the only blocks that each position reads
+    (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often."""
+    import torch
+    _check_queries(cache, Q)
+    c = cache._c
+    n_pos, G = Q.shape[2], Q.shape[3]
+    if blocks is not None:
+        _expect("blocks", blocks, (torch.int32,), (c.S, c.H, n_pos, None))
+        _on_one_cuda_device(cache=cache.K, blocks=blocks)
+    handle, ctx = _on_stream(stream, Q.device, Q, blocks, out, ws, cache.K, cache.V)
+    with ctx:
+        if ws is None:
+            ws = cache_workspace(cache, n_pos, G)
+        if out is None:
+            out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
+        elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
+            raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
+    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
+    st = load_library().arckv_cache_attend(ctypes.byref(c), n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3),
+                                           _ptr(blocks), 0 if blocks is None else blocks.shape[3], out.data_ptr(),
+                                           _strides3("out", out, 3), ws.data_ptr(), ws.numel(), flags, handle)
+    if st != 0:
+        raise ArckvError(st, "arckv_cache_attend")
+    return out
+
+
+def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: int = 1, causal: bool = False, ws=None,
+                 stream=None, check: bool = True):
+    """The m blocks of 64 tokens that each query position reads, [S, H, n_pos, m] int32 ascending, -1 for none: the
+    first keep_first, the newest keep_last and those whose logits can be largest.  Q, causal and ws as for
+    ``cache_attend``."""
+    import torch
+    _check_queries(cache, Q)
+    c = cache._c
+    n_pos, G = Q.shape[2], Q.shape[3]
+    handle, ctx = _on_stream(stream, Q.device, Q, ws, cache.K, cache.V)
+    with ctx:
+        if ws is None:
+            ws = cache_workspace(cache, n_pos, G)
+        blocks = torch.empty(c.S, c.H, n_pos, max(m, 0), dtype=torch.int32, device=Q.device)
+    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
+    st = load_library().arckv_cache_select(ctypes.byref(c), n_pos, G, m, keep_first, keep_last, Q.data_ptr(),
+                                           _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags,
+                                           handle)
+    if st != 0:
+        raise ArckvError(st, "arckv_cache_select")
+    return blocks

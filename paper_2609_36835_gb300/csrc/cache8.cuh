@@ -1,0 +1,45 @@
+// Shared definitions of the 8-bit cache kernels (arckv_cache8 in arckv.h).
+#pragma once
+#include <algorithm>
+
+#include "kernels.h"
+
+namespace arckv {
+
+constexpr int kCB = ARCKV_CACHE_BLOCK;   // tokens of a block
+constexpr float kCacheFloor = 7.888609052210118e-31f;   // 2^-100: least block magnitude, so that 127 / a stays finite
+constexpr float kInv127 = 0.007874015718698502f;        // fl(1 / 127)
+
+// Rows addressed by (sequence, head, position), in elements from the base.
+struct RowStrides {
+  long long s, h, i;
+};
+
+// First counter of a cache's `state` after the status word.
+__device__ __forceinline__ unsigned int* state_ticket(DevStatus* st) { return &st->pad[0]; }
+
+// Tokens that position p of n_pos sees in a sequence of len tokens.
+__device__ __forceinline__ int visible_tokens(int len, int n_pos, int p, bool causal) {
+  return causal ? max(0, len - n_pos + 1 + p) : len;
+}
+__device__ __forceinline__ int cache_len(const arckv_cache8& c, int s) { return min(max(c.len[s], 0), c.cap); }
+
+// ---- launchers (each returns the kernels it enqueued, or -1) ---------------
+int launch_cache_append(const arckv_cache8& c, int n, bool f32, const void* K, RowStrides ks, const void* V,
+                        RowStrides vs, const float* bias, const int* at, const int* counts, cudaStream_t st);
+int launch_cache_read(const arckv_cache8& c, int start, int count, bool f32, void* K, void* V, cudaStream_t st);
+
+struct CacheQuery {
+  int n_pos, G;
+  bool causal;
+  const bf16* Q;
+  RowStrides qs;
+};
+size_t cache_attend_scratch(int S, int H, int cap, int n_pos, int G);
+int launch_cache_attend(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
+                        RowStrides os, void* ws, cudaStream_t st);
+size_t cache_select_scratch(int S, int H, int cap, int n_pos);
+int launch_cache_select(const arckv_cache8& c, const CacheQuery& q, int m, int keep_first, int keep_last, int* blocks,
+                        void* ws, cudaStream_t st);
+
+}  // namespace arckv
