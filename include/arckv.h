@@ -380,8 +380,8 @@ arckv_status arckv_cache_read(const arckv_cache8* c, int32_t start, int32_t coun
 
 /* Workspace bytes of arckv_cache_attend and arckv_cache_select (0 if the sizes
  * are invalid).  Host-only.  The first ARCKV_CACHE_WS_HEADER bytes of the
- * workspace must be zeroed once before its first use; calls leave them zero
- * (but for the status word). */
+ * workspace must be zeroed once before its first use (and after
+ * ARCKV_ERR_TIMEOUT); calls leave them zero (but for the status word). */
 #define ARCKV_CACHE_WS_HEADER 4096
 size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G);
 

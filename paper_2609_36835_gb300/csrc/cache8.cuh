@@ -24,6 +24,12 @@ __device__ __forceinline__ int visible_tokens(int len, int n_pos, int p, bool ca
 }
 __device__ __forceinline__ int cache_len(const arckv_cache8& c, int s) { return min(max(c.len[s], 0), c.cap); }
 
+// Workspace of cache_attend: the header (status word, then one ticket for each
+// CTA of the split kernels), then partial results.
+constexpr int kCacheMaxCtas = 160;   // CTAs of the persistent kernels, at most one for each SM
+__host__ __device__ inline int* ws_tickets(void* ws) { return (int*)((char*)ws + sizeof(DevStatus)); }
+static_assert(sizeof(DevStatus) + kCacheMaxCtas * sizeof(int) <= ARCKV_CACHE_WS_HEADER, "tickets fit the header");
+
 // ---- launchers (each returns the kernels it enqueued, or -1) ---------------
 int launch_cache_append(const arckv_cache8& c, int n, bool f32, const void* K, RowStrides ks, const void* V,
                         RowStrides vs, const float* bias, const int* at, const int* counts, cudaStream_t st);

@@ -1,74 +1,612 @@
-// Attention over an 8-bit cache: O = softmax_j(scale q . k_j + bias_j) v_j over
-// all visible tokens of a row, or over the blocks listed for its position.
+// Attention of few query rows over an 8-bit cache (decode and draft steps, and
+// every sparse call):
+//
+//   O_r = sum_j e^{x_rj} v_j / sum_j e^{x_rj},  x_rj = scale q_r . k_j + bias_j
+//
+// over all visible tokens j, or over the listed blocks.  256 bytes of codes a
+// token and head are read once: the call is bound by HBM, and the work per byte
+// has to stay small.  So:
+//  - Work is the list of (item, block) pairs, an item being (sequence, KV head,
+//    up to 16 query rows[, position]).  One CTA on each SM takes an equal share
+//    of it, whatever the lengths; an item cut by a share's end is finished by
+//    the CTA that comes last (a ticket), which adds the parts up in CTA order.
+//  - A producer warp streams blocks (64 x 128 codes of K and of V, 8 KB each,
+//    128-byte swizzle) through a ring in shared memory by TMA.  Each consumer
+//    warp takes whole blocks of its own, with its own running maximum, sum and
+//    output: no barrier between warps until the item ends.
+//  - Products run on mma.sync m16n8k16 with f16 operands: keys (dims for V) are
+//    the 16 rows and the query rows the 8 columns, so four to eight rows fill
+//    an instruction; tcgen05 would want 64 to 128 rows and a pass of the
+//    codes through shared memory as f16.  A code becomes an f16 with one byte permute
+//    and one subtraction a pair (1024 + u is 0x6400 | u); codes are exact in f16.
+//    So are bf16 queries once each row is scaled by a power of two (elements
+//    under 2^-32 of the row's largest lose bits, far below fp32 rounding).
+//    Softmax weights, scaled by 2^15, enter as f16 pairs hi + lo: 22 bits.  With
+//    four rows, hi and lo are columns 0-3 and 4-7 of the same instruction.
+//  - S^T and O^T are what the instructions give (keys x rows, dims x rows), so
+//    weights go from one product to the other by an 8 x 8 transpose in registers.
 #include "cache8.cuh"
+#include "tc.cuh"
+
+#include <cuda_fp16.h>
 
 namespace arckv {
 namespace {
 
-// One warp per query row, lane l dims 4l .. 4l+3, one key a step.
-__global__ void __launch_bounds__(128) cache_attend_rows_kernel(const arckv_cache8 c, CacheQuery q, float scale,
-                                                                const int* blocks, int m, float* O, RowStrides os,
-                                                                long long rows, DevStatus* stt) {
-  const long long row = blockIdx.x * 4ll + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= rows) return;
-  const int g = (int)(row % q.G);
-  const long long item = row / q.G;
-  const int p = (int)(item % q.n_pos);
-  const long long sh = item / q.n_pos;
-  const int h = (int)(sh % c.H), s = (int)(sh / c.H);
-  const int see = visible_tokens(cache_len(c, s), q.n_pos, p, q.causal), nblk = c.cap / kCB;
-  float x[4];
-  const bf16* qr = q.Q + s * q.qs.s + h * q.qs.h + p * q.qs.i + g * 128 + lane * 4;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = scale * __bfloat162float(qr[e]);
-  float top = -INFINITY, z = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const int nb = blocks ? m : (see + kCB - 1) / kCB;
-  for (int i = 0; i < nb; ++i) {
-    const int b = blocks ? blocks[item * m + i] : i;
-    if (b < 0) continue;
-    if (b >= nblk) {
-      if (lane == 0) set_status(stt, ARCKV_ERR_INVALID_ARG);
-      continue;
+constexpr int kTileBytes = kCB * 128;        // codes of one block, K or V
+
+struct RowsShape {
+  int H, n_pos, G, nblk, cap;   // nblk: blocks of the capacity
+  int groups;                   // row groups of an item's rows
+  int m;                        // blocks listed for an item (sparse)
+  bool causal;
+};
+
+template <int kR>
+struct RowsCfg {
+  // consumer warps: with the producer a multiple of four, as registers are dealt out to the SM's quarters
+  static constexpr int kWarps = kR == 16 ? 7 : 11;
+  static constexpr int kStages = kR == 16 ? 9 : kR == 8 ? 10 : 11;
+  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kMerge = kWarps * kR * 128 * 4;         // their outputs at an item's end
+  static constexpr int kSmem = kStages * (2 * kTileBytes + kCB * 4) + kMerge + 1024;
+};
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Bytes (0, 1) or (2, 3) of w, codes + 128, as two f16 codes.
+template <int kHi>
+__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
+  const uint32_t y = __byte_perm(w, 0x64646464u, kHi ? 0x4342 : 0x4140);
+  const __half2 z = __hsub2(*(const __half2*)&y, __half2{__half_raw{0x6480}, __half_raw{0x6480}});
+  return *(const uint32_t*)&z;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *(const uint32_t*)&h;
+}
+__device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+// Equal shares of `total` units: CTA c has [start(c), start(c + 1)).
+struct Shares {
+  long long total;
+  int ctas;
+  __device__ long long start(int c) const { return total * c / ctas; }
+  __device__ int owner(long long u) const {   // the CTA that has unit u
+    int c = (int)((u * ctas + ctas - 1) / total);
+    while (c > 0 && start(c) > u) --c;
+    while (c + 1 < ctas && start(c + 1) <= u) ++c;
+    return c;
+  }
+};
+
+// The item and block of unit u, and the units left in the item.
+struct Place {
+  long long item_first;   // unit at which the item begins
+  long long sh;           // sequence x KV head
+  long long list;         // sparse: row of the block lists
+  int s, pos, group, blk, count;   // blk of count blocks (list entries)
+};
+
+// Dense: units run over s, then head and row group, then blocks; pre[s] are
+// the blocks before sequence s (at least one block for each sequence).
+template <bool kSparse>
+__device__ __forceinline__ Place place_of(long long u, const RowsShape& d, int S, const int* pre) {
+  Place p;
+  if (kSparse) {
+    const long long item = u / d.m;
+    p.blk = (int)(u - item * d.m);
+    p.count = d.m;
+    p.item_first = item * d.m;
+    p.group = (int)(item % d.groups);
+    p.list = item / d.groups;
+    p.pos = (int)(p.list % d.n_pos);
+    p.sh = p.list / d.n_pos;
+    p.s = (int)(p.sh / d.H);
+  } else {
+    const long long per = (long long)d.H * d.groups;
+    int lo = 0, hi = S;   // last s with pre[s] * per <= u
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] * per <= u) lo = mid;
+      else hi = mid;
     }
-    if (b * kCB >= see) continue;
-    const float ks = c.k_scale[sh * nblk + b], vs = c.v_scale[sh * nblk + b];
-    for (int j = b * kCB; j < min(see, (b + 1) * kCB); ++j) {
-      const long long tok = sh * c.cap + j;
-      const unsigned int kw = *(const unsigned int*)(c.K + tok * 128 + lane * 4);
-      float a = 0.f;
+    p.s = lo;
+    p.count = pre[lo + 1] - pre[lo];
+    const long long rest = u - pre[lo] * per, it = rest / p.count;
+    p.blk = (int)(rest - it * p.count);
+    p.item_first = pre[lo] * per + it * p.count;
+    p.group = (int)(it % d.groups);
+    p.sh = (long long)lo * d.H + it / d.groups;
+    p.pos = 0;
+    p.list = 0;
+  }
+  return p;
+}
+
+template <int kR, bool kBias, bool kSparse>
+__global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
+    cache_rows_kernel(const __grid_constant__ CUtensorMap mK, const __grid_constant__ CUtensorMap mV,
+                      const arckv_cache8 c, RowsShape d, const bf16* Q, RowStrides qs, float scale, const int* blocks,
+                      float* O, RowStrides os, float* parts, int* tickets, DevStatus* stt) {
+  using Cfg = RowsCfg<kR>;
+  constexpr int kNT = kR == 16 ? 2 : 1;   // column tiles of 8 rows
+  constexpr int kW = Cfg::kWarps, kSt = Cfg::kStages;
+  extern __shared__ __align__(1024) unsigned char smraw[];
+  unsigned char* ring = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
+  float* sBias = (float*)(ring + kSt * 2 * kTileBytes);
+  float* sO = sBias + kSt * kCB;                                 // [warp][row][128]
+  __shared__ __align__(8) uint64_t full[kSt], empty[kSt];
+  __shared__ float sKs[kSt], sVs[kSt];
+  __shared__ int sBlk[kSt];
+  __shared__ float sM[kW][kR], sL[kW][kR];
+  __shared__ int abort_flag, last_flag, stop_flag;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int* pre = (int*)(sO + kW * kR * 128);                         // dense: [S + 1]
+  volatile int* abortp = &abort_flag;
+
+  if (tid == 0) {
+    for (int s = 0; s < kSt; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    abort_flag = 0;
+    tc::mbar_fence_init();
+  }
+  if (warp == kW) {   // blocks before each sequence, by warp scan
+    if (lane == 0) {
+      tc::tma_prefetch(&mK);
+      tc::tma_prefetch(&mV);
+    }
+    if (!kSparse) {
+      int run = 0;
+      for (int s0 = 0; s0 < c.S; s0 += 32) {
+        int x = s0 + lane < c.S ? max(1, (cache_len(c, s0 + lane) + kCB - 1) / kCB) : 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) a = fmaf(x[e], (float)((int)((kw >> (8 * e)) & 0xffu) - 128), a);
-      a = warp_sum(a) * ks;
-      if (c.bias) a += c.bias[tok];
-      if (a == -INFINITY) continue;
-      const float up = fmaxf(top, a), f = expf(top - up), pr = expf(a - up);
-      z = z * f + pr;
-      top = up;
-      const unsigned int vw = *(const unsigned int*)(c.V + tok * 128 + lane * 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        acc[e] = fmaf(pr * vs, (float)((int)((vw >> (8 * e)) & 0xffu) - 128), acc[e] * f);
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        if (s0 + lane < c.S) pre[s0 + lane + 1] = run + x;
+        run += __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) pre[0] = 0;
     }
   }
-  const float inv = z == 0.f ? 0.f : 1.f / z;   // NaN stays NaN
-  const float4 o = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-  if (!(fabsf(o.x) <= 3.402823466e38f) || !(fabsf(o.y) <= 3.402823466e38f) || !(fabsf(o.z) <= 3.402823466e38f) ||
-      !(fabsf(o.w) <= 3.402823466e38f))
-    set_status(stt, ARCKV_ERR_NONFINITE);
-  *(float4*)(O + s * os.s + h * os.h + p * os.i + g * 128 + lane * 4) = o;
+  __syncthreads();
+  Shares sh;
+  sh.total = kSparse ? (long long)c.S * d.H * d.n_pos * d.groups * d.m
+                     : (long long)pre[c.S] * d.H * d.groups;
+  sh.ctas = (int)min((long long)gridDim.x, sh.total);
+  if ((int)blockIdx.x >= sh.ctas) return;
+  const long long u0 = sh.start(blockIdx.x), u1 = sh.start(blockIdx.x + 1);
+
+  if (warp == kW) {
+    // ------------------------------------------------------------- producer
+    int it = 0;   // blocks issued
+    bool ok = true;
+    for (long long u = u0; u < u1 && ok;) {
+      const Place p = place_of<kSparse>(u, d, c.S, pre);
+      const int n = (int)min((long long)(p.count - p.blk), u1 - u), len = cache_len(c, p.s);
+      for (int k0 = 0; k0 < n && ok; k0 += 32) {
+        const int k = k0 + lane;
+        int b = -1;
+        if (k < n) {
+          b = kSparse ? blocks[p.list * d.m + p.blk + k] : p.blk + k;
+          if (kSparse && b >= d.nblk) {
+            set_status(stt, ARCKV_ERR_INVALID_ARG);
+            b = -1;
+          }
+          if (b >= 0 && b * kCB >= len) b = -1;   // nothing of it is held
+        }
+        const long long at = p.sh * d.nblk + b;
+        float ks = 0.f, vs = 0.f;
+        if (b >= 0) {
+          ks = c.k_scale[at];
+          vs = c.v_scale[at];
+        }
+        const int cnt = min(32, n - k0);
+        auto load = [&](int st) {   // this lane's block into stage st
+          unsigned char* dst = ring + st * 2 * kTileBytes;
+          tc::tma_load_3d(dst, &mK, 0, b * kCB, (int)p.sh, &full[st]);
+          tc::tma_load_3d(dst + kTileBytes, &mV, 0, b * kCB, (int)p.sh, &full[st]);
+          if (kBias) tc::bulk_load(sBias + st * kCB, c.bias + p.sh * c.cap + b * kCB, kCB * 4, &full[st]);
+        };
+        auto announce = [&](int st) {
+          sKs[st] = ks;
+          sVs[st] = vs;
+          sBlk[st] = b;
+          if (b >= 0) tc::mbar_arrive_expect_tx(&full[st], 2 * kTileBytes + (kBias ? kCB * 4 : 0));
+          else tc::mbar_arrive(&full[st]);
+        };
+        int j = 0;
+        if (it < kSt) {   // the ring's first round: copies start before the scales have come
+          const int first = min(cnt, kSt - it);
+          if (lane < first && b >= 0) load(it + lane);
+          if (lane < first) announce(it + lane);
+          __syncwarp();
+          j = first;
+        }
+        for (; j < cnt && ok; ++j) {
+          const int q = it + j, st = q % kSt;
+          ok = tc::mbar_wait(&empty[st], ((q / kSt) - 1) & 1, abortp, stt);
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok && lane == j) {
+            if (b >= 0) load(st);
+            announce(st);
+          }
+        }
+        it += j;
+      }
+      u += n;
+    }
+    if (!ok) {   // let the copies in flight land before the CTA's memory goes
+      volatile int never = 0;
+      for (int q = max(0, it - 1 - kSt); q < it - 1; ++q) tc::mbar_wait(&full[q % kSt], (q / kSt) & 1, &never, stt);
+    }
+    return;
+  }
+
+  // --------------------------------------------------------------- consumers
+  const int g = lane >> 2, t = lane & 3;
+  constexpr float kP15 = 15.f;   // weights carry a factor of 2^15
+  int base = 0;                  // blocks of earlier segments
+  bool ok = true;
+  for (long long u = u0; u < u1;) {
+    const Place p = place_of<kSparse>(u, d, c.S, pre);
+    const int n = (int)min((long long)(p.count - p.blk), u1 - u), len = cache_len(c, p.s);
+    const int h = (int)(p.sh - (long long)p.s * d.H), nrows = kSparse ? d.G : d.n_pos * d.G;
+    // query rows: column n of tile nt is row nt * 8 + n of the group (four rows: twice the same four)
+    uint32_t qf[kNT][8][2];
+    float fac[kNT][2];           // 2^e scale (log2 e) of rows 2t, 2t + 1
+    int see[kNT][2];             // tokens that they see
+    int see_min = 0x7fffffff;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int r = p.group * kR + (kR == 4 ? (g & 3) : nt * 8 + g);
+      const int pos = kSparse ? p.pos : r / d.G, gq = kSparse ? r : r - pos * d.G;
+      float x[32], amax = 0.f;
+      if (r < nrows) {
+        const uint4* src = (const uint4*)(Q + p.s * qs.s + h * qs.h + pos * qs.i + gq * 128 + 32 * t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint4 v = __ldg(src + e);
+          const __nv_bfloat162* y = (const __nv_bfloat162*)&v;
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const float2 z = __bfloat1622float2(y[f]);
+            x[8 * e + 2 * f] = z.x;
+            x[8 * e + 2 * f + 1] = z.y;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) amax = fmaxf(amax, fabsf(x[e]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = 0.f;
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      // exponent of the row's largest element, kept where 2^(14 - e) and 2^(e - 14) are normal
+      const int e = max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100);
+      const float up = __uint_as_float((unsigned)(14 - e + 127) << 23), down = __uint_as_float((unsigned)(e - 14 + 127) << 23);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        qf[nt][k][0] = pack_f16(x[4 * k] * up, x[4 * k + 1] * up);
+        qf[nt][k][1] = pack_f16(x[4 * k + 2] * up, x[4 * k + 3] * up);
+      }
+      const float f = down * scale * (kBias ? 1.f : kLog2e);
+      const int sees = r < nrows ? visible_tokens(len, d.n_pos, pos, d.causal) : 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fac[nt][i] = __shfl_sync(0xffffffffu, f, (2 * t + i) * 4);
+        see[nt][i] = __shfl_sync(0xffffffffu, sees, (2 * t + i) * 4);
+      }
+      see_min = min(see_min, __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff));
+    }
+    float o[kNT][8][4], mx[kNT][2], l[kNT][2];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mx[nt][i] = -INFINITY;
+        l[nt][i] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][k][e] = 0.f;
+    }
+    // blocks base + i of the CTA belong to warp (base + i) % kW
+    for (int i = (warp - base % kW + kW) % kW; i < n; i += kW) {
+      const int q = base + i, st = q % kSt;
+      ok = tc::mbar_wait(&full[st], (q / kSt) & 1, abortp, stt);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const int b = sBlk[st];
+      if (b >= 0) {
+        const float ks = sKs[st], vs = sVs[st];
+        const unsigned char* Kt = ring + st * 2 * kTileBytes;
+        const unsigned char* Vt = Kt + kTileBytes;
+        // ---- S^T = K Q^T: lane (g, t) has keys g, g + 8 and dims 32t .. 32t + 31
+        float s[kNT][4][4];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][mt][e] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+          for (int ch = 0; ch < 2; ++ch) {
+            const int off = (mt * 16 + g) * 128 + (((2 * t + ch) ^ g) << 4);
+            const uint4 a = *(const uint4*)(Kt + off), a8 = *(const uint4*)(Kt + off + 8 * 128);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w}, w8[4] = {a8.x, a8.y, a8.z, a8.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t f0 = codes_f16<0>(w[k]), f1 = codes_f16<0>(w8[k]), f2 = codes_f16<1>(w[k]),
+                             f3 = codes_f16<1>(w8[k]);
+#pragma unroll
+              for (int nt = 0; nt < kNT; ++nt)
+                mma_f16(s[nt][mt], f0, f1, f2, f3, qf[nt][4 * ch + k][0], qf[nt][4 * ch + k][1]);
+            }
+          }
+        }
+        // ---- softmax of the block
+        const bool edge = (b + 1) * kCB > see_min;
+        uint32_t ph[kNT][4][2], pl[kNT][4][2];
+        float alpha[kNT][2];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+          for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
+            const float f = fac[nt][e2] * ks;
+            float top = -INFINITY;
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                float& x = s[nt][mt][2 * hf + e2];
+                const int kk = mt * 16 + hf * 8 + g;
+                x = kBias ? fmaf(x, f, sBias[st * kCB + kk]) : x * f;
+                if (edge && b * kCB + kk >= see[nt][e2]) x = -INFINITY;
+                top = fmaxf(top, x);
+              }
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+            const float old = mx[nt][e2];
+            top = fmaxf(top, old);
+            mx[nt][e2] = top;
+            const float ref = top == -INFINITY ? 0.f : top;   // nothing visible yet: weights e^{-inf} = 0
+            alpha[nt][e2] = ex2_approx(kBias ? (old - ref) * kLog2e : old - ref);
+            float sum = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                float& x = s[nt][mt][2 * hf + e2];
+                // a bias of the type's lowest value cancels against itself before the factor log2 e
+                x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kP15) : (x - ref) + kP15);
+                sum += x;
+              }
+            l[nt][e2] = fmaf(l[nt][e2], alpha[nt][e2], sum);
+          }
+          // f16 pairs, transposed to (keys, row) operands
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const float x0 = s[nt][mt][2 * hf], x1 = s[nt][mt][2 * hf + 1];
+              const uint32_t hi = pack_f16(x0, x1);
+              const float2 hf2 = __half22float2(*(const __half2*)&hi);
+              const uint32_t lo = pack_f16(x0 - hf2.x, x1 - hf2.y);
+              if (kR == 4) {   // columns 4 .. 7 carry lo of the same rows
+                ph[nt][mt][hf] = transpose8x8(t >= 2 ? lo : hi);
+              } else {
+                ph[nt][mt][hf] = transpose8x8(hi);
+                pl[nt][mt][hf] = transpose8x8(lo);
+              }
+            }
+        }
+        // ---- O^T += V^T P^T: lane (g, t) has dims 16g .. 16g + 15 of keys 2t, 2t + 1, 2t + 8, 2t + 9
+        float acc[kNT][8][4];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[nt][k][e] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+          const unsigned char* row = Vt + (mt * 16 + 2 * t) * 128;
+          const int c0 = (g ^ (2 * t)) << 4, c1 = (g ^ (2 * t + 1)) << 4;
+          const uint4 v0 = *(const uint4*)(row + c0), v1 = *(const uint4*)(row + 128 + c1);
+          const uint4 v8 = *(const uint4*)(row + 8 * 128 + c0), v9 = *(const uint4*)(row + 9 * 128 + c1);
+          const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+          const uint32_t w8[4] = {v8.x, v8.y, v8.z, v8.w}, w9[4] = {v9.x, v9.y, v9.z, v9.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {   // dims 16g + 4k + 2z, + 1
+              const uint32_t y = __byte_perm(w0[k], w1[k], z ? 0x7362 : 0x5140);
+              const uint32_t y8 = __byte_perm(w8[k], w9[k], z ? 0x7362 : 0x5140);
+              const uint32_t f0 = codes_f16<0>(y), f1 = codes_f16<1>(y), f2 = codes_f16<0>(y8), f3 = codes_f16<1>(y8);
+#pragma unroll
+              for (int nt = 0; nt < kNT; ++nt) {
+                mma_f16(acc[nt][2 * k + z], f0, f1, f2, f3, ph[nt][mt][0], ph[nt][mt][1]);
+                if (kR != 4) mma_f16(acc[nt][2 * k + z], f0, f1, f2, f3, pl[nt][mt][0], pl[nt][mt][1]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nt][k][e] = fmaf(o[nt][k][e], alpha[nt][e & 1], vs * acc[nt][k][e]);
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&empty[st]);
+    }
+    base += n;
+    // ---- the item's end (or this CTA's part of it): add the warps up
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], w);
+        const int r = nt * 8 + 2 * t + i;
+        if (g == 0 && r < kR) {
+          sM[warp][r] = mx[nt][i];
+          sL[warp][r] = l[nt][i];
+        }
+        if (kR == 4) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+              o[nt][k][2 * z + i] += __shfl_xor_sync(0xffffffffu, o[nt][k][2 * z + i], 2);   // hi + lo
+        }
+        if (r < kR) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            *(float4*)(sO + (warp * kR + r) * 128 + 16 * g + 4 * k) =
+                make_float4(o[nt][2 * k][i], o[nt][2 * k][2 + i], o[nt][2 * k + 1][i], o[nt][2 * k + 1][2 + i]);
+        }
+      }
+    }
+    if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
+    bar_consumers(kW * 32);
+    if (stop_flag) break;   // a wait gave up: write nothing
+    const bool whole = p.blk == 0 && n == p.count;
+    const int c_first = whole ? blockIdx.x : sh.owner(p.item_first);
+    const int c_last = whole ? blockIdx.x : sh.owner(p.item_first + p.count - 1);
+    auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
+      return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
+    };
+    auto store = [&](int r, int dim, float4 v, float z) {
+      const float inv = z == 0.f ? 0.f : 1.f / z;
+      v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      const float big = 3.402823466e38f;
+      if (!(fabsf(v.x) <= big && fabsf(v.y) <= big && fabsf(v.z) <= big && fabsf(v.w) <= big))
+        set_status(stt, ARCKV_ERR_NONFINITE);
+      const int row = p.group * kR + r, pos = kSparse ? p.pos : row / d.G, gq = kSparse ? row : row - pos * d.G;
+      if (row < nrows) *(float4*)(O + p.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
+    };
+    // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
+    constexpr int kSlot = kR * 132;   // 128 outputs, m, l (and two unused) for each row
+    for (int x = tid; x < kR * 32; x += kW * 32) {
+      const int r = x >> 5, dim = (x & 31) * 4;
+      float top = -INFINITY, z = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) top = fmaxf(top, sM[w][r]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float f = weight(sM[w][r], top);
+        const float4 y = *(const float4*)(sO + (w * kR + r) * 128 + dim);
+        z = fmaf(sL[w][r], f, z);
+        v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
+      }
+      if (whole) store(r, dim, v, z);
+      else {
+        float* slot = parts + (2ll * blockIdx.x + (p.blk == 0 ? 1 : 0)) * kSlot + r * 132;
+        __stcg((float4*)(slot + dim), v);
+        if (dim == 0) __stcg((float2*)(slot + 128), make_float2(top, z));
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      bar_consumers(kW * 32);
+      if (tid == 0) {
+        last_flag = atomicAdd(&tickets[c_first], 1) == c_last - c_first;
+        if (last_flag) tickets[c_first] = 0;
+        __threadfence();
+      }
+      bar_consumers(kW * 32);
+      if (last_flag) {
+        for (int x = tid; x < kR * 32; x += kW * 32) {
+          const int r = x >> 5, dim = (x & 31) * 4;
+          float top = -INFINITY, z = 0.f;
+          for (int cc = c_first; cc <= c_last; ++cc)
+            top = fmaxf(top, __ldcg(parts + (2ll * cc + (cc == c_first)) * kSlot + r * 132 + 128));
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int cc = c_first; cc <= c_last; ++cc) {
+            const float* slot = parts + (2ll * cc + (cc == c_first)) * kSlot + r * 132;
+            const float2 ml = __ldcg((const float2*)(slot + 128));
+            const float4 y = __ldcg((const float4*)(slot + dim));
+            const float f = weight(ml.x, top);
+            z = fmaf(ml.y, f, z);
+            v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
+          }
+          store(r, dim, v, z);
+        }
+      }
+    }
+    bar_consumers(kW * 32);   // sO, sM, sL are free
+    u += n;
+  }
+}
+
+template <int kR, bool kBias, bool kSparse>
+int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
+                RowStrides os, void* ws, cudaStream_t st) {
+  using Cfg = RowsCfg<kR>;
+  CUtensorMap mK, mV;
+  if (!encode_u8_map_3d(&mK, c.K, c.cap, (uint64_t)c.S * c.H, kCB) ||
+      !encode_u8_map_3d(&mV, c.V, c.cap, (uint64_t)c.S * c.H, kCB))
+    return -1;
+  RowsShape d;
+  d.H = c.H;
+  d.n_pos = q.n_pos;
+  d.G = q.G;
+  d.cap = c.cap;
+  d.nblk = c.cap / kCB;
+  d.groups = cdiv(kSparse ? q.G : (long long)q.n_pos * q.G, kR);
+  d.m = m;
+  d.causal = q.causal;
+  auto kern = cache_rows_kernel<kR, kBias, kSparse>;
+  const int smem = Cfg::kSmem + (kSparse ? 0 : (c.S + 1) * (int)sizeof(int));
+  if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
+  const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
+  kern<<<ctas, Cfg::kThreads, smem, st>>>(mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
+                                          (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
+  return 1;
+}
+
+template <int kR>
+int launch_rows_r(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
+                  RowStrides os, void* ws, cudaStream_t st) {
+  if (c.bias)
+    return blocks ? launch_rows<kR, true, true>(c, q, scale, blocks, m, O, os, ws, st)
+                  : launch_rows<kR, true, false>(c, q, scale, blocks, m, O, os, ws, st);
+  return blocks ? launch_rows<kR, false, true>(c, q, scale, blocks, m, O, os, ws, st)
+                : launch_rows<kR, false, false>(c, q, scale, blocks, m, O, os, ws, st);
 }
 
 }  // namespace
 
-size_t cache_attend_scratch(int, int, int, int, int) { return 0; }
+size_t cache_attend_scratch(int, int, int, int, int) { return (size_t)2 * kCacheMaxCtas * 16 * 132 * sizeof(float); }
 
 int launch_cache_attend(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
                         RowStrides os, void* ws, cudaStream_t st) {
-  const long long rows = (long long)c.S * c.H * q.n_pos * q.G;
-  cache_attend_rows_kernel<<<(unsigned)((rows + 3) / 4), 128, 0, st>>>(c, q, scale, blocks, m, O, os, rows,
-                                                                       (DevStatus*)ws);
-  return 1;
+  const long long rows = blocks ? q.G : (long long)q.n_pos * q.G;   // rows that read the same blocks
+  if (rows <= 4) return launch_rows_r<4>(c, q, scale, blocks, m, O, os, ws, st);
+  if (rows <= 8) return launch_rows_r<8>(c, q, scale, blocks, m, O, os, ws, st);
+  return launch_rows_r<16>(c, q, scale, blocks, m, O, os, ws, st);
 }
 
 }  // namespace arckv

@@ -236,4 +236,8 @@ bool encode_bf16_map_3d_sw64(CUtensorMap* map, const void* base, uint64_t dim0, 
 bool encode_f32_map_3d(CUtensorMap* map, const void* base, uint64_t dim0, uint64_t dim1, uint64_t dim2,
                        uint32_t box0, uint32_t box1, uint64_t ld = 0, uint64_t bs = 0, bool swz128 = false);
 
+// Host: encode a 3-D tiled TMA map over bytes [dim2][dim1][128] with a box of
+// {128, box1, 1} and 128-byte swizzle (16-byte chunk c of row r at c ^ (r % 8)).
+bool encode_u8_map_3d(CUtensorMap* map, const void* base, uint64_t dim1, uint64_t dim2, uint32_t box1);
+
 }  // namespace arckv

@@ -74,6 +74,19 @@ bool encode_f32_map_3d(CUtensorMap* map, const void* base, uint64_t dim0, uint64
   return r == CUDA_SUCCESS;
 }
 
+bool encode_u8_map_3d(CUtensorMap* map, const void* base, uint64_t dim1, uint64_t dim2, uint32_t box1) {
+  if (!encoder_ready()) return false;
+  if (((uintptr_t)base & 15u) != 0 || box1 == 0 || box1 > 256) return false;
+  const cuuint64_t gdim[3] = {128, dim1, dim2};
+  const cuuint64_t gstride[2] = {128, 128 * dim1};
+  const cuuint32_t box[3] = {128, box1, 1};
+  const cuuint32_t estride[3] = {1, 1, 1};
+  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), gdim, gstride, box,
+                              estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
 cudaError_t set_dyn_smem(const void* kern, int bytes) {
   static std::mutex mu;
   static std::map<std::pair<const void*, int>, int> done;   // (kernel, device) -> bytes already allowed
