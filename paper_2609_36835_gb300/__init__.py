@@ -509,7 +509,9 @@ def cache_workspace(cache: Cache8, n_pos: int, G: int):
 
 
 def _strides3(name: str, x, dense_from: int):
-    """The first three strides of x, whose dimensions from `dense_from` on must be dense."""
+    """The first three strides of x (None when it is dense), whose dimensions from `dense_from` on must be dense."""
+    if x.is_contiguous():
+        return None
     st = x.stride()
     want = 1
     for i in range(x.dim() - 1, dense_from - 1, -1):
@@ -520,20 +522,30 @@ def _strides3(name: str, x, dense_from: int):
     return (ctypes.c_int64 * 3)(*[st[i] if x.shape[i] != 1 else 0 for i in range(3)])
 
 
-def _on_stream(stream, device, *tensors):
-    """The raw handle of `stream` (None: the current one) and a context in which new tensors belong to it; tensors in
-    use on a stream other than the current one are recorded there, so that their memory is not reused too early."""
-    import contextlib
+def _side_stream(stream, device, *tensors):
+    """`stream` as a torch stream.  Tensors in use on a stream other than the current one are recorded there, so that
+    their memory is not reused too early."""
     import torch
-    if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
     if stream != torch.cuda.current_stream(device):
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-    return stream.cuda_stream, torch.cuda.stream(stream)
+    return stream
+
+
+def _current_handle(device) -> int:
+    """The raw handle of the device's current stream, without making a stream object where torch has a call for that."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _same_device(cache: "Cache8", **tensors):
+    for name, x in tensors.items():
+        if x is not None and x.device != cache.K.device:
+            raise ValueError("arckv: %s is on %s but the cache on %s" % (name, x.device, cache.K.device))
 
 
 def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream=None, check: bool = True) -> None:
@@ -555,10 +567,12 @@ def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream
     for name, x in (("at", at), ("counts", counts)):
         if x is not None:
             _expect(name, x, (torch.int32,), (c.S,))
-    _on_one_cuda_device(cache=cache.K, K=K, V=V, bias=bias, at=at, counts=counts)
+    _same_device(cache, K=K, V=V, bias=bias, at=at, counts=counts)
     if n == 0:
         return
-    handle, _ = _on_stream(stream, K.device, K, V, bias, at, counts, cache.K, cache.V)
+    dev = cache.K.device
+    handle = (_current_handle(dev) if stream is None else
+              _side_stream(stream, dev, K, V, bias, at, counts, cache.K, cache.V).cuda_stream)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if K.dtype == torch.float32 else 0)
     st = load_library().arckv_cache_append(ctypes.byref(c), n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
                                            _strides3("V", V, 3), _ptr(bias), _ptr(at), _ptr(counts), flags, handle)
@@ -574,12 +588,16 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
-    handle, ctx = _on_stream(stream, cache.K.device, cache.K, cache.V)
-    with ctx:
-        K = torch.empty(c.S, c.H, max(count, 0), 128, dtype=dtype, device=cache.K.device)
-        V = torch.empty_like(K)
+    dev = cache.K.device
+    if stream is not None:   # the outputs belong to the stream that fills them
+        stream = _side_stream(stream, dev, cache.K, cache.V)
+        with torch.cuda.stream(stream):
+            return cache_read(cache, start, count, dtype=dtype, check=check)
+    K = torch.empty((c.S, c.H, max(count, 0), 128), dtype=dtype, device=dev)
+    V = torch.empty((c.S, c.H, max(count, 0), 128), dtype=dtype, device=dev)
     if count == 0:
         return K, V
+    handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
     st = load_library().arckv_cache_read(ctypes.byref(c), start, count, K.data_ptr(), V.data_ptr(), flags, handle)
     if st != 0:
@@ -595,6 +613,7 @@ def _check_queries(cache: Cache8, Q):
                          % ((c.S, c.H, "n_pos", "G", 128), Q.dtype, tuple(Q.shape)))
     if Q.device != cache.K.device:
         raise ValueError("arckv: Q is on %s but the cache on %s" % (Q.device, cache.K.device))
+    return c
 
 
 def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, causal: bool = False, out=None, ws=None,
@@ -604,20 +623,22 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     each sees the tokens up to itself.  blocks [S, H, n_pos, m] int32: the only blocks that each position reads
     (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often."""
     import torch
-    _check_queries(cache, Q)
-    c = cache._c
-    n_pos, G = Q.shape[2], Q.shape[3]
+    c = _check_queries(cache, Q)
+    if stream is not None:   # a workspace and an output made here belong to the stream that fills them
+        stream = _side_stream(stream, Q.device, Q, blocks, out, ws, cache.K, cache.V)
+        with torch.cuda.stream(stream):
+            return cache_attend(cache, Q, logit_scale, blocks=blocks, causal=causal, out=out, ws=ws, check=check)
+    _, _, n_pos, G, _ = Q.shape
     if blocks is not None:
         _expect("blocks", blocks, (torch.int32,), (c.S, c.H, n_pos, None))
-        _on_one_cuda_device(cache=cache.K, blocks=blocks)
-    handle, ctx = _on_stream(stream, Q.device, Q, blocks, out, ws, cache.K, cache.V)
-    with ctx:
-        if ws is None:
-            ws = cache_workspace(cache, n_pos, G)
-        if out is None:
-            out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
-        elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
-            raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
+        _same_device(cache, blocks=blocks)
+    if ws is None:
+        ws = cache_workspace(cache, n_pos, G)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
+    elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
+        raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
+    handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
     st = load_library().arckv_cache_attend(ctypes.byref(c), n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3),
                                            _ptr(blocks), 0 if blocks is None else blocks.shape[3], out.data_ptr(),
@@ -633,14 +654,17 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: in
     first keep_first, the newest keep_last and those whose logits can be largest.  Q, causal and ws as for
     ``cache_attend``."""
     import torch
-    _check_queries(cache, Q)
-    c = cache._c
-    n_pos, G = Q.shape[2], Q.shape[3]
-    handle, ctx = _on_stream(stream, Q.device, Q, ws, cache.K, cache.V)
-    with ctx:
-        if ws is None:
-            ws = cache_workspace(cache, n_pos, G)
-        blocks = torch.empty(c.S, c.H, n_pos, max(m, 0), dtype=torch.int32, device=Q.device)
+    c = _check_queries(cache, Q)
+    if stream is not None:
+        stream = _side_stream(stream, Q.device, Q, ws, cache.K, cache.V)
+        with torch.cuda.stream(stream):
+            return cache_select(cache, Q, m, keep_first=keep_first, keep_last=keep_last, causal=causal, ws=ws,
+                                check=check)
+    _, _, n_pos, G, _ = Q.shape
+    if ws is None:
+        ws = cache_workspace(cache, n_pos, G)
+    blocks = torch.empty((c.S, c.H, n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
+    handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
     st = load_library().arckv_cache_select(ctypes.byref(c), n_pos, G, m, keep_first, keep_last, Q.data_ptr(),
                                            _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags,
