@@ -30,6 +30,19 @@ constexpr int kCacheMaxCtas = 160;   // CTAs of the persistent kernels, at most 
 __host__ __device__ inline int* ws_tickets(void* ws) { return (int*)((char*)ws + sizeof(DevStatus)); }
 static_assert(sizeof(DevStatus) + kCacheMaxCtas * sizeof(int) <= ARCKV_CACHE_WS_HEADER, "tickets fit the header");
 
+// Equal shares of `total` units: CTA c has [start(c), start(c + 1)).
+struct CacheShares {
+  long long total;
+  int ctas;
+  __device__ long long start(int c) const { return total * c / ctas; }
+  __device__ int owner(long long u) const {   // the CTA that has unit u
+    int c = (int)((u * ctas + ctas - 1) / total);
+    while (c > 0 && start(c) > u) --c;
+    while (c + 1 < ctas && start(c + 1) <= u) ++c;
+    return c;
+  }
+};
+
 // ---- launchers (each returns the kernels it enqueued, or -1) ---------------
 int launch_cache_append(const arckv_cache8& c, int n, bool f32, const void* K, RowStrides ks, const void* V,
                         RowStrides vs, const float* bias, const int* at, const int* counts, cudaStream_t st);
@@ -44,6 +57,10 @@ struct CacheQuery {
 size_t cache_attend_scratch(int S, int H, int cap, int n_pos, int G);
 int launch_cache_attend(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
                         RowStrides os, void* ws, cudaStream_t st);
+// the same for more than 16 rows of a head over all tokens
+size_t cache_tiles_scratch(long long rows);
+int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
+                       cudaStream_t st);
 size_t cache_select_scratch(int S, int H, int cap, int n_pos);
 int launch_cache_select(const arckv_cache8& c, const CacheQuery& q, int m, int keep_first, int keep_last, int* blocks,
                         void* ws, cudaStream_t st);

@@ -33,6 +33,7 @@
 namespace arckv {
 namespace {
 
+constexpr int kRowsMax = 16;                 // more rows of a head go to the tcgen05 kernel
 constexpr int kTileBytes = kCB * 128;        // codes of one block, K or V
 
 struct RowsShape {
@@ -76,19 +77,6 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   return *(const uint32_t*)&h;
 }
 __device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
-
-// Equal shares of `total` units: CTA c has [start(c), start(c + 1)).
-struct Shares {
-  long long total;
-  int ctas;
-  __device__ long long start(int c) const { return total * c / ctas; }
-  __device__ int owner(long long u) const {   // the CTA that has unit u
-    int c = (int)((u * ctas + ctas - 1) / total);
-    while (c > 0 && start(c) > u) --c;
-    while (c + 1 < ctas && start(c + 1) <= u) ++c;
-    return c;
-  }
-};
 
 // The item and block of unit u, and the units left in the item.
 struct Place {
@@ -184,7 +172,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     }
   }
   __syncthreads();
-  Shares sh;
+  CacheShares sh;
   sh.total = kSparse ? (long long)c.S * d.H * d.n_pos * d.groups * d.m
                      : (long long)pre[c.S] * d.H * d.groups;
   sh.ctas = (int)min((long long)gridDim.x, sh.total);
@@ -599,14 +587,18 @@ int launch_rows_r(const arckv_cache8& c, const CacheQuery& q, float scale, const
 
 }  // namespace
 
-size_t cache_attend_scratch(int, int, int, int, int) { return (size_t)2 * kCacheMaxCtas * 16 * 132 * sizeof(float); }
+size_t cache_attend_scratch(int, int, int, int n_pos, int G) {
+  const size_t rows = (size_t)2 * kCacheMaxCtas * 16 * 132 * sizeof(float);
+  return (long long)n_pos * G > kRowsMax ? std::max(rows, cache_tiles_scratch((long long)n_pos * G)) : rows;
+}
 
 int launch_cache_attend(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
                         RowStrides os, void* ws, cudaStream_t st) {
   const long long rows = blocks ? q.G : (long long)q.n_pos * q.G;   // rows that read the same blocks
   if (rows <= 4) return launch_rows_r<4>(c, q, scale, blocks, m, O, os, ws, st);
   if (rows <= 8) return launch_rows_r<8>(c, q, scale, blocks, m, O, os, ws, st);
-  return launch_rows_r<16>(c, q, scale, blocks, m, O, os, ws, st);
+  if (blocks || rows <= kRowsMax) return launch_rows_r<16>(c, q, scale, blocks, m, O, os, ws, st);
+  return launch_cache_tiles(c, q, scale, O, os, ws, st);
 }
 
 }  // namespace arckv
