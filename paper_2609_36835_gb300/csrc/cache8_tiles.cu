@@ -22,6 +22,9 @@
 // far apart the blocks' scales lie.  ref follows the running maximum of x_j +
 // log2 vs_b only when that has grown by more than 8 (weights then stay below
 // 2^15, in the range of f16): O is read, scaled and written back on few steps.
+//
+// The pipe's fp32 sums round towards zero, and O would shrink by 1.4e-7 a step:
+// after 16 steps it is added to sums in the workspace (L2) and starts again.
 #include "cache8.cuh"
 #include "tc.cuh"
 
@@ -32,6 +35,8 @@ namespace {
 
 constexpr int kStep = 128;                    // keys of a step (two blocks)
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
+constexpr int kFlush = 16;                    // steps that O is summed up over in TMEM
+constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
 constexpr float kVsUnit = 0x1p-20f;           // sums are in units of kVsUnit / vs: the least vs, 2^-107, stays in range
 
@@ -44,7 +49,11 @@ template <int kT>
 struct TileCfg {
   static constexpr int kRows = 128 * kT;
   static constexpr int kSoft = 4 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
-  static constexpr int kThreads = 32 * (kSoft + 5);
+  static constexpr int kThreads = 32 * (kSoft + 8);      // (whole warpgroups: three warps idle)
+  // registers at launch (65536 / kThreads, a multiple of 8), and how the warpgroups share them:
+  // kT kRegsSoft + 2 kRegsRest = (kT + 2) kRegs
+  static constexpr int kRegs = kT == 2 ? 128 : 168, kRegsRest = kT == 2 ? 72 : 136, kRegsSoft = kT == 2 ? 184 : 232;
+  static_assert(kT * kRegsSoft + 2 * kRegsRest == (kT + 2) * kRegs && kRegs * kThreads <= 65536, "register shares");
   static constexpr int kSmem = kT * 2 * kHalf + 2 * 4 * kHalf + 1024;   // Q, then two stages of (K, V)
   static constexpr int kSlot = 131 * kRows;              // floats of a partial result: O, ref, log2 vs of ref, sum
 };
@@ -67,6 +76,59 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
       "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// 32 columns of this warp's lanes, not waited for.
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+        "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+        "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Nothing that uses v moves above this point (behind a wait).
+__device__ __forceinline__ void settle32(float* v) {
+  asm volatile(""
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                 "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]),
+                 "+f"(v[30]), "+f"(v[31]));
+}
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+template <int kN>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
+template <int kN>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN)); }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -210,7 +272,12 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   const bool active = (int)blockIdx.x < sh.ctas;
   const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
 
-  if (warp == kSoft + 4) {
+  if (warp >= kSoft) regs_dec<Cfg::kRegsRest>();
+  else regs_inc<Cfg::kRegsSoft>();
+
+  if (warp > kSoft + 4) {
+    // idle
+  } else if (warp == kSoft + 4) {
     // ------------------------------------------------------------ MMA issuer
     bool ok = true;
     int it = 0, seg = 0;   // steps and items so far
@@ -236,7 +303,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
               for (int ks = 0; ks < 8; ++ks) {
                 const uint64_t bd = tc::sdesc_k128(v + (ks >> 2) * kHalf + (ks & 3) * 32);
                 const uint32_t a = S + (ks >> 1) * 32 + (ks & 1) * 8;   // hi; lo is 16 columns on
-                mma_f16_ts(Ot, a, bd, kIdescF16, (i > 1 || ks > 0) ? 1u : 0u);
+                mma_f16_ts(Ot, a, bd, kIdescF16, ((i - 1) % kFlush != 0 || ks > 0) ? 1u : 0u);
                 mma_f16_ts(Ot, a + 16, bd, kIdescF16, 1u);
               }
               if (i == n) tc::mma_commit(&odone[t]);
@@ -282,37 +349,36 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const uint8_t* Kh = c.K + g.sh * c.cap * 128;
       const uint8_t* Vh = c.V + g.sh * c.cap * 128;
       const uint4 zero = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-      uint4 rk[8], rv[8];
+      uint4 raw[8];
       auto load_k = [&](int i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int key = (g.step + i) * kStep + kr + 4 * j;
-          rk[j] = key < c.cap ? __ldg((const uint4*)(Kh + (long long)key * 128 + kc * 16)) : zero;
+          raw[j] = key < c.cap ? __ldg((const uint4*)(Kh + (long long)key * 128 + kc * 16)) : zero;
         }
       };
       auto load_v = [&](int i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int key = (g.step + i) * kStep + ko * 8 + j;
-          rv[j] = key < c.cap ? __ldg((const uint4*)(Vh + (long long)key * 128 + dg * 16)) : zero;
+          raw[j] = key < c.cap ? __ldg((const uint4*)(Vh + (long long)key * 128 + dg * 16)) : zero;
         }
       };
-      load_k(0);
-      load_v(0);
       for (int i = 0; i < n && ok; ++i) {
         const int q = it + i, st = q & 1;
         unsigned char* Ks = sKV + st * 4 * kHalf;
         unsigned char* Vs = Ks + 2 * kHalf;
+        load_k(i);   // in flight while the stage is waited for
         if (q >= 2) ok = tc::mbar_wait(&kempty[st], ((q >> 1) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int r = kr + 4 * j;
-          const uint4 x = make_uint4(codes_f16<0>(rk[j].x), codes_f16<1>(rk[j].x), codes_f16<0>(rk[j].y),
-                                     codes_f16<1>(rk[j].y));
-          const uint4 y = make_uint4(codes_f16<0>(rk[j].z), codes_f16<1>(rk[j].z), codes_f16<0>(rk[j].w),
-                                     codes_f16<1>(rk[j].w));
+          const uint4 x = make_uint4(codes_f16<0>(raw[j].x), codes_f16<1>(raw[j].x), codes_f16<0>(raw[j].y),
+                                     codes_f16<1>(raw[j].y));
+          const uint4 y = make_uint4(codes_f16<0>(raw[j].z), codes_f16<1>(raw[j].z), codes_f16<0>(raw[j].w),
+                                     codes_f16<1>(raw[j].w));
           unsigned char* row = Ks + (kc >> 2) * kHalf + r * 128;
           // the two chunks in an order that keeps the eight lanes of a row on different banks
           const int q0 = (kc & 3) * 2 + (kc >> 2), q1 = (kc & 3) * 2 + 1 - (kc >> 2);
@@ -331,9 +397,9 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           m.lv[ct] = log2f(vs);
           m.iv[ct] = kVsUnit / vs;
         }
-        if (i + 1 < n) load_k(i + 1);
         tc::fence_proxy_async_smem();
         tc::mbar_arrive(&kfull[st]);
+        load_v(i);
         if (q >= 2) ok = tc::mbar_wait(&vempty[st], ((q >> 1) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
@@ -342,8 +408,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           uint32_t f[4][4];             // [dim][key pair]
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            const uint32_t a = w == 0 ? rv[2 * p].x : w == 1 ? rv[2 * p].y : w == 2 ? rv[2 * p].z : rv[2 * p].w;
-            const uint32_t b = w == 0 ? rv[2 * p + 1].x : w == 1 ? rv[2 * p + 1].y : w == 2 ? rv[2 * p + 1].z : rv[2 * p + 1].w;
+            const uint32_t a = w == 0 ? raw[2 * p].x : w == 1 ? raw[2 * p].y : w == 2 ? raw[2 * p].z : raw[2 * p].w;
+            const uint32_t b = w == 0 ? raw[2 * p + 1].x : w == 1 ? raw[2 * p + 1].y : w == 2 ? raw[2 * p + 1].z : raw[2 * p + 1].w;
             const uint32_t y = __byte_perm(a, b, 0x5140), z = __byte_perm(a, b, 0x7362);
             f[0][p] = codes_f16<0>(y);
             f[1][p] = codes_f16<1>(y);
@@ -357,7 +423,6 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
                 make_uint4(f[e][0], f[e][1], f[e][2], f[e][3]);
           }
         }
-        if (i + 1 < n) load_v(i + 1);
         tc::fence_proxy_async_smem();
         tc::mbar_arrive(&vfull[st]);
       }
@@ -415,6 +480,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tc::fence_proxy_async_smem();
         tc::mbar_arrive(&qfull);
       }
+      float* sums = parts + 2ll * kCacheMaxCtas * Cfg::kSlot + (long long)blockIdx.x * kRows * 128 + t * 128 + row_t;
+      float bref = -INFINITY, brefv = 0.f;          // reference of the flushed sums
       float ref = -INFINITY, refv = 0.f, l = 0.f;   // with biases ref is the logit and refv the log2 vs that came with it
       const float* bias = kBias ? c.bias + g.sh * c.cap : nullptr;
       for (int i = 0; i < n; ++i) {
@@ -425,40 +492,72 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         if (!ok) break;
         tc::fence_after_sync();
         const Meta m = meta[q & 3];
-        const bool edge = __any_sync(0xffffffffu, j0 + kStep > see);
-        // x' = logit (+ bias): largest of each block
+        if (i > 0 && i % kFlush == 0) {
+          // O goes to this row's sums in memory and starts again at zero (see above)
+          const float d = kBias ? fmaf(ref - bref, kLog2e, refv - brefv) : ref - bref;   // NaN, inf: nothing there yet
+          const bool none = bref == -INFINITY, far = !none && d > kFar;
+          const float up = none || far ? 1.f : ex2_approx(d), down = far ? ex2_approx(-d) : 1.f;
+          const bool redo = __any_sync(0xffffffffu, none || far);
+#pragma unroll 1
+          for (int ch = 0; ch < 8; ++ch) {
+            float o[16];
+            tc::tmem_ld16(Ot + ch * 16, o);
+            float* b = sums + ch * 16 * kRows;
+            if (redo) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float old = none ? 0.f : __ldcg(b + e * kRows);
+                __stcg(b + e * kRows, fmaf(old, down, o[e] * up));
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                asm volatile("red.global.add.f32 [%0], %1;" ::"l"(b + e * kRows), "f"(o[e] * up) : "memory");
+            }
+          }
+          if (none || far) {
+            bref = ref;
+            brefv = refv;
+          }
+          tc::fence_before_sync();
+        }
+        float v[128];
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) tmem_ld32_async(S + ch * 32, v + ch * 32);
+        tmem_wait_ld();
+#pragma unroll
+        for (int ch = 0; ch < 4; ++ch) settle32(v + ch * 32);
+        const int lim = see - j0;   // keys of the step that the row sees
+        const bool edge = __any_sync(0xffffffffu, lim < kStep);
+        const float f[2] = {fac * m.ks[0], fac * m.ks[1]};
+        if (kBias) {   // logits; biases are read four at a time where the row sees something, within the capacity
+#pragma unroll
+          for (int e = 0; e < kStep; e += 4) {
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (e < lim) x = __ldg((const float4*)(bias + j0 + e));
+            v[e] = fmaf(v[e], f[e >> 6], x.x);
+            v[e + 1] = fmaf(v[e + 1], f[e >> 6], x.y);
+            v[e + 2] = fmaf(v[e + 2], f[e >> 6], x.z);
+            v[e + 3] = fmaf(v[e + 3], f[e >> 6], x.w);
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < kStep; ++e)
+            if (e >= lim) v[e] = -INFINITY;
+        }
+        // largest of each block
         float top[2];
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-          float best = -INFINITY;
-          const float f = fac * m.ks[hb];
+          float a = v[hb * 64], b = v[hb * 64 + 1];
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            float v[32];
-            tc::tmem_ld32(S + hb * 64 + ch * 32, v);
-            const int j = j0 + hb * 64 + ch * 32;
-            if (kBias) {
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                if (j + e < see) {   // bias is read where the row sees something: within the capacity
-                  const float4 bb = __ldg((const float4*)(bias + j + e));
-                  const float x[4] = {bb.x, bb.y, bb.z, bb.w};
-#pragma unroll
-                  for (int k = 0; k < 4; ++k)
-                    if (j + e + k < see) best = fmaxf(best, fmaf(v[e + k], f, x[k]));
-                }
-              }
-            } else if (edge) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (j + e < see) best = fmaxf(best, v[e]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) best = fmaxf(best, v[e]);
-            }
+          for (int e = 2; e < 64; e += 2) {
+            a = fmaxf(a, v[hb * 64 + e]);
+            b = fmaxf(b, v[hb * 64 + e + 1]);
           }
-          top[hb] = kBias ? best : fmaf(best, f, m.lv[hb]);   // f > 0: the largest product is the largest logit
-          if (!kBias && best == -INFINITY) top[hb] = -INFINITY;
+          a = fmaxf(a, b);
+          top[hb] = kBias ? a : fmaf(a, f[hb], m.lv[hb]);   // f > 0: the largest product is the largest logit
         }
         float alpha = 1.f;
         bool grow;
@@ -486,15 +585,14 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             ref = nr;
           }
         }
-        if (i > 0 && __any_sync(0xffffffffu, grow)) {
+        if (i % kFlush != 0 && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+          for (int ch = 0; ch < 8; ++ch) {
+            float o[16];
+            tc::tmem_ld16(Ot + ch * 16, o);
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            float v[32];
-            uint32_t r[32];
-            tc::tmem_ld32(Ot + ch * 32, v);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(v[e] * alpha);
-            tmem_st32(Ot + ch * 32, r);
+            for (int e = 0; e < 16; ++e) o[e] *= alpha;
+            tmem_st16(Ot + ch * 16, o);
           }
           tmem_wait_st();
         }
@@ -502,46 +600,34 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const float base = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-          const float f = fac * m.ks[hb];
           const float add = kBias ? m.lv[hb] - refv + kLift : m.lv[hb] - base + kLift;
-          float sum = 0.f;
+          const float2 add_2 = make_float2(add, add);
+          float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
           for (int ch = 0; ch < 2; ++ch) {
-            float v[32];
             uint32_t r[32];
-            tc::tmem_ld32(S + hb * 64 + ch * 32, v);
-            const int j = j0 + hb * 64 + ch * 32;
-            if (kBias) {
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                float4 bb = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (j + e < see) bb = __ldg((const float4*)(bias + j + e));
-                const float x[4] = {bb.x, bb.y, bb.z, bb.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  v[e + k] = j + e + k < see ? ex2_approx(fmaf(fmaf(v[e + k], f, x[k]) - base, kLog2e, add)) : 0.f;
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = ex2_approx(fmaf(v[e], f, add));
-              if (edge) {
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (j + e >= see) v[e] = 0.f;
-              }
-            }
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              sum += v[e] + v[e + 1];
-              const __half2 hi = __floats2half2_rn(v[e], v[e + 1]);
-              const float2 back = __half22float2(hi);
-              const __half2 lo = __floats2half2_rn(v[e] - back.x, v[e + 1] - back.y);
-              r[e >> 1] = *(const uint32_t*)&hi;
-              r[16 + (e >> 1)] = *(const uint32_t*)&lo;
+              const int k = hb * 64 + ch * 32 + e;
+              float2 x = make_float2(v[k], v[k + 1]);
+              if (kBias)
+                x = fma2(add2(x, make_float2(-base, -base)), make_float2(kLog2e, kLog2e), add_2);
+              else
+                x = fma2(x, make_float2(f[hb], f[hb]), add_2);
+              x.x = ex2_approx(x.x);
+              x.y = ex2_approx(x.y);
+              sum = add2(sum, x);
+              // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
+              const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
+                                            __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
+              const float2 lo = add2(x, make_float2(-hi.x, -hi.y));
+              const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
+              r[e >> 1] = *(const uint32_t*)&h2;
+              r[16 + (e >> 1)] = *(const uint32_t*)&l2;
             }
             tmem_st32(S + hb * 64 + ch * 32, r);
           }
-          l = fmaf(sum, m.iv[hb], l);
+          l = fmaf(sum.x + sum.y, m.iv[hb], l);
         }
         tmem_wait_st();
         tc::fence_before_sync();
@@ -562,11 +648,17 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         *(float4*)(O + g.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
       };
       const float inv = l == 0.f ? 0.f : kVsUnit / l;
+      const bool flushed = bref != -INFINITY;
+      const float bw = flushed ? ex2_approx(kBias ? fmaf(bref - ref, kLog2e, brefv - refv) : bref - ref) : 0.f;
       float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + t * 128 + row_t;
 #pragma unroll
       for (int ch = 0; ch < 4; ++ch) {
         float v[32];
         tc::tmem_ld32(Ot + ch * 32, v);
+        if (flushed) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(__ldcg(sums + (ch * 32 + e) * kRows), bw, v[e]);
+        }
         if (whole) {
           if (mine)
 #pragma unroll
@@ -656,7 +748,8 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
 }  // namespace
 
 size_t cache_tiles_scratch(long long rows) {
-  return (size_t)2 * kCacheMaxCtas * (rows <= 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot) * sizeof(float);
+  const size_t slot = rows <= 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot;
+  return kCacheMaxCtas * (2 * slot + (rows <= 128 ? TileCfg<1>::kRows : TileCfg<2>::kRows) * 128) * sizeof(float);
 }
 
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
