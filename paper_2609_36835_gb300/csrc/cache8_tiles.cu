@@ -3,18 +3,19 @@
 //
 // With n rows a head every code is used n times, so the call is bound by the
 // tensor pipe.  A CTA takes 128 or 256 rows of one head (one or two M = 128
-// tiles) and goes over the keys 128 at a time:
-//   converters (4 warps)  read the codes of K and V from HBM and leave them in
-//                         shared memory as f16 operands, V transposed; a code
-//                         costs about one instruction for 256 rows
-//   MMA warp              S = Q K^T (f16, exact products, fp32 sums in TMEM), O += P V
+// tiles) and goes over the keys a block of 64 at a time:
+//   converters (4 warps)  read the codes of K and V and leave them in shared
+//                         memory as f16 operands, V transposed, four blocks
+//                         ahead; a code costs about one instruction for 256 rows
+//   MMA warp              S = Q K^T (exact products, fp32 sums in TMEM), O += P V
 //   softmax (4 warps a tile, one row a thread)  turn S into weights in place: the
 //                         f16 pair hi + lo of 32 keys takes the 32 columns that
 //                         their logits had; P is the MMA's operand from TMEM
-// P V runs once for hi and once for lo, which keeps 22 bits of a weight: three
+// P V runs once for hi and once for lo, which keeps 21 bits of a weight: three
 // units of MMA work where f16 weights would do with two, so 2/3 of the pipe's
-// peak is the most that the fp32 output allows.  With two tiles the pipe works
-// on one while the other's softmax runs.
+// peak is the most that the fp32 output allows.  A tile has two buffers of S in
+// TMEM: the logits of the next block come in while the softmax of this one runs,
+// and the pipe has the other tile's products meanwhile.
 //
 // The weight of key j of block b carries the block's scale of V:
 //   w_j = 2^{x_j + log2 vs_b - ref + 7},  O = sum_j w_j c_j / sum_b (sum_{j in b} w_j) / vs_b
@@ -23,8 +24,8 @@
 // log2 vs_b only when that has grown by more than 8 (weights then stay below
 // 2^15, in the range of f16): O is read, scaled and written back on few steps.
 //
-// The pipe's fp32 sums round towards zero, and O would shrink by 1.4e-7 a step:
-// after 16 steps it is added to sums in the workspace (L2) and starts again.
+// The pipe's fp32 sums round towards zero, and O would shrink by 7e-8 a block:
+// after 32 blocks it is added to sums in the workspace (L2) and starts again.
 #include "cache8.cuh"
 #include "tc.cuh"
 
@@ -33,9 +34,10 @@
 namespace arckv {
 namespace {
 
-constexpr int kStep = 128;                    // keys of a step (two blocks)
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
-constexpr int kFlush = 16;                    // steps that O is summed up over in TMEM
+constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
+constexpr int kStages = 4, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
+constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
 constexpr float kVsUnit = 0x1p-20f;           // sums are in units of kVsUnit / vs: the least vs, 2^-107, stays in range
@@ -49,34 +51,79 @@ template <int kT>
 struct TileCfg {
   static constexpr int kRows = 128 * kT;
   static constexpr int kSoft = 4 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
-  static constexpr int kThreads = 32 * (kSoft + 8);      // (whole warpgroups: three warps idle)
-  // registers at launch (65536 / kThreads, a multiple of 8), and how the warpgroups share them:
-  // kT kRegsSoft + 2 kRegsRest = (kT + 2) kRegs
-  static constexpr int kRegs = kT == 2 ? 128 : 168, kRegsRest = kT == 2 ? 72 : 136, kRegsSoft = kT == 2 ? 184 : 232;
-  static_assert(kT * kRegsSoft + 2 * kRegsRest == (kT + 2) * kRegs && kRegs * kThreads <= 65536, "register shares");
-  static constexpr int kSmem = kT * 2 * kHalf + 2 * 4 * kHalf + 1024;   // Q, then two stages of (K, V)
-  static constexpr int kSlot = 131 * kRows;              // floats of a partial result: O, ref, log2 vs of ref, sum
+  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: three warps idle
+  // registers at launch, and how the warpgroups share them: softmax (kT groups), converters, MMA
+  static constexpr int kRegs = kT == 2 ? 128 : 168;
+  static constexpr int kRegsSoft = kT == 2 ? 184 : 232, kRegsRest = kT == 2 ? 72 : 136;
+  static_assert(kT * kRegsSoft + 2 * kRegsRest == (kT + 2) * kRegs && kRegs * kThreads <= 65536,
+                "the shares add up to what the block was launched with");
+  static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + 1024;   // Q, then the stages
+  static constexpr int kSlot = 132 * kRows;              // floats of a partial result: O, then ref, log2 vs of ref and sum of the rows
 };
 
-// D[tmem] (+)= A[tmem] * B[smem]^T, kind::f16, one CTA.
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+// The products of one block and row tile, issued by one elected lane of a converged warp with warp-uniform operands
+// (from one lane of a divergent branch each MMA took 90 to 125 cycles to issue, twice what it runs).  A descriptor's
+// low bits are the address in units of 16 bytes, so K steps are added to the tile's descriptor.
+//
+// S = Q K^T: Q 128 x 128 and K 64 x 128 in halves of 64 dims (16 KB and 8 KB apart).
+__device__ __forceinline__ void mma_qk(uint32_t s, uint64_t q, uint64_t k, uint32_t idesc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
-      "r"(a), "l"(bdesc), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred e, z, c;\n\t.reg .b64 a, b;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 z, 0, 0;\n\tsetp.eq.b32 c, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1024;\n\tadd.s64 b, %2, 512;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1026;\n\tadd.s64 b, %2, 514;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1028;\n\tadd.s64 b, %2, 516;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1030;\n\tadd.s64 b, %2, 518;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t}\n" ::"r"(s),
+      "l"(q), "l"(k), "r"(idesc)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+// O (+)= P V: P in TMEM, 16 keys in 8 columns, hi and then lo 16 columns on, 32 keys in 32 columns; V^T 128 x 64.
+__device__ __forceinline__ void mma_pv(uint32_t o, uint32_t p, uint64_t v, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      "{\n\t.reg .pred e, c, y;\n\t.reg .b64 b;\n\t.reg .b32 a;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 c, %4, 0;\n\tsetp.eq.b32 y, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, c;\n\t"
+      "add.u32 a, %1, 16;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], %2, %3, y;\n\t"
+      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 2;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t"
+      "add.u32 a, %1, 24;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t"
+      "add.u32 a, %1, 32;\n\tadd.s64 b, %2, 4;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t"
+      "add.u32 a, %1, 48;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t"
+      "add.u32 a, %1, 40;\n\tadd.s64 b, %2, 6;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t"
+      "add.u32 a, %1, 56;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, y;\n\t}\n" ::"r"(o),
+      "r"(p), "l"(v), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// tc::mma_commit by one elected lane of a converged warp.
+__device__ __forceinline__ void commit_elected(uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(tc::smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 // 32 columns of this warp's lanes, not waited for.
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* v) {
@@ -123,18 +170,21 @@ template <int kN>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
 template <int kN>
 __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN)); }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]),
+      "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]),
+      "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]),
+      "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31])
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// kind::f16 with A = B = f16, D = fp32, both K-major, M = 128, N = 128.
-constexpr uint32_t kIdescF16 = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+// kind::f16 with A = B = f16, D = fp32, both K-major, M = 128, N = n.
+__host__ __device__ constexpr uint32_t idesc_f16(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 
 template <int kHi>
 __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {   // bytes (0, 1) or (2, 3), codes + 128, as two f16 codes
@@ -143,10 +193,10 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {   // bytes (0, 1) or
   return *(const uint32_t*)&z;
 }
 
-// Steps of a row tile: as far as its last row sees (one at least).
+// Blocks of a row tile: as far as its last row sees (one at least).
 __device__ __forceinline__ int tile_steps(const TileShape& d, int len, int tile, int rows) {
   const int last = min((tile + 1) * rows, d.n_pos * d.G) - 1;
-  return max(1, (visible_tokens(len, d.n_pos, last / d.G, d.causal) + kStep - 1) / kStep);
+  return max(1, (visible_tokens(len, d.n_pos, last / d.G, d.causal) + kCB - 1) / kCB);
 }
 
 struct Segment {
@@ -198,8 +248,8 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   return g;
 }
 
-struct Meta {   // of a step's two blocks
-  float ks[2], lv[2], iv[2];   // scale of K, log2 and inverse (in units of kVsUnit) of V's
+struct Meta {   // of a block
+  float ks, lv, iv;   // scale of K, log2 and inverse (in units of kVsUnit) of V's
 };
 
 template <int kT, bool kBias>
@@ -210,11 +260,11 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows;
   extern __shared__ unsigned char smraw[];
   unsigned char* sQ = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [tile][half][128][128 B]
-  unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K, V][half]
-  long long* pre = (long long*)(sKV + 8 * kHalf);                                  // [S + 1] steps of a head
-  __shared__ __align__(8) uint64_t qfull, kfull[2], vfull[2], kempty[2], vempty[2], sfull[kT], pfull[kT], odone[kT],
-      drain;
-  __shared__ Meta meta[4];
+  unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K halves, V]
+  long long* pre = (long long*)(sKV + kStages * kStageBytes);                      // [S + 1] blocks of a head's tiles
+  __shared__ __align__(8) uint64_t qfull, kfull[kStages], vfull[kStages], kempty[kStages], vempty[kStages],
+      sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
+  __shared__ Meta meta[2 * kStages];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, stop_flag, last_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -222,17 +272,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
 
   if (tid == 0) {
     tc::mbar_init(&qfull, kRows);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kStages; ++i) {
       tc::mbar_init(&kfull[i], 128);
       tc::mbar_init(&vfull[i], 128);
       tc::mbar_init(&kempty[i], 1);
       tc::mbar_init(&vempty[i], 1);
     }
-    for (int t = 0; t < kT; ++t) {
-      tc::mbar_init(&sfull[t], 1);
-      tc::mbar_init(&pfull[t], 128);
-      tc::mbar_init(&odone[t], 1);
-    }
+    for (int t = 0; t < kT; ++t)
+      for (int i = 0; i < 2; ++i) {
+        tc::mbar_init(&sfull[t][i], 1);
+        tc::mbar_init(&pfull[t][i], 128);
+        tc::mbar_init(&odone[t][i], 1);
+      }
     tc::mbar_init(&drain, 1);
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -265,152 +316,131 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = tmem_slot;   // tile t: S / P at columns 256 t, O at 256 t + 128
+  const uint32_t tmem = tmem_slot;   // tile t: two buffers of S / P at columns 256 t, O at 256 t + 128
   CacheShares sh;
   sh.total = pre[c.S] * d.H;
   sh.ctas = (int)min((long long)gridDim.x, sh.total);
   const bool active = (int)blockIdx.x < sh.ctas;
   const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
 
-  if (warp >= kSoft) regs_dec<Cfg::kRegsRest>();
-  else regs_inc<Cfg::kRegsSoft>();
-
   if (warp > kSoft + 4) {
-    // idle
+    regs_dec<Cfg::kRegsRest>();   // idle
   } else if (warp == kSoft + 4) {
     // ------------------------------------------------------------ MMA issuer
+    regs_dec<Cfg::kRegsRest>();
     bool ok = true;
-    int it = 0, seg = 0;   // steps and items so far
+    int q = 0;   // blocks so far
+    // warp-wide reductions leave their result in uniform registers
+    const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
+    const uint64_t q_desc = tc::sdesc_k128(tc::smem_u32(sQ)), kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
+    int seg = 0;
     for (long long u = u0; u < u1 && ok; ++seg) {
       const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = (int)min((long long)(g.count - g.step), u1 - u);
-      ok = tc::mbar_wait(&qfull, seg & 1, abortp, stt);
+      const int n = __reduce_max_sync(0xffffffffu, (int)min((long long)(g.count - g.step), u1 - u));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&qfull, seg & 1, abortp, stt));
+      // S of block i, then P V of block i - 1: the softmax of i runs beside the products of its neighbours
       for (int i = 0; i <= n && ok; ++i) {
-        const int q = it + i;
-        if (i < n) ok = tc::mbar_wait(&kfull[q & 1], (q >> 1) & 1, abortp, stt);
-        if (ok && i > 0) ok = tc::mbar_wait(&vfull[(q - 1) & 1], ((q - 1) >> 1) & 1, abortp, stt);
-#pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          if (ok && i > 0) ok = tc::mbar_wait(&pfull[t], (q - 1) & 1, abortp, stt);
-          ok = __all_sync(0xffffffffu, ok);
+        if (i < n) {
+          const int st = q % kStages;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&kfull[st], (q / kStages) & 1, abortp, stt));
           if (!ok) break;
           tc::fence_after_sync();
-          if (lane == 0) {
-            const uint32_t S = tmem + 256 * t, Ot = S + 128;
-            if (i > 0) {   // O += P V of the step before
-              const uint32_t v = tc::smem_u32(sKV + ((q - 1) & 1) * 4 * kHalf + 2 * kHalf);
 #pragma unroll
-              for (int ks = 0; ks < 8; ++ks) {
-                const uint64_t bd = tc::sdesc_k128(v + (ks >> 2) * kHalf + (ks & 3) * 32);
-                const uint32_t a = S + (ks >> 1) * 32 + (ks & 1) * 8;   // hi; lo is 16 columns on
-                mma_f16_ts(Ot, a, bd, kIdescF16, ((i - 1) % kFlush != 0 || ks > 0) ? 1u : 0u);
-                mma_f16_ts(Ot, a + 16, bd, kIdescF16, 1u);
-              }
-              if (i == n) tc::mma_commit(&odone[t]);
-            }
-            if (i < n) {   // S = Q K^T
-              const uint32_t a = tc::smem_u32(sQ + t * 2 * kHalf), k = tc::smem_u32(sKV + (q & 1) * 4 * kHalf);
-#pragma unroll
-              for (int ks = 0; ks < 8; ++ks)
-                tc::mma_f16(S, tc::sdesc_k128(a + (ks >> 2) * kHalf + (ks & 3) * 32),
-                            tc::sdesc_k128(k + (ks >> 2) * kHalf + (ks & 3) * 32), kIdescF16, ks > 0 ? 1u : 0u);
-              tc::mma_commit(&sfull[t]);
-            }
+          for (int t = 0; t < kT; ++t) {
+            mma_qk(tm + 256 * t + (q & 1) * 64, q_desc + t * (2 * kHalf >> 4), kv_desc + st * (kStageBytes >> 4),
+                   idesc_f16(64));
+            commit_elected(&sfull[t][q & 1]);
           }
-          __syncwarp();
+          commit_elected(&kempty[st]);
         }
-        if (ok && lane == 0) {
-          if (i < n) tc::mma_commit(&kempty[q & 1]);
-          if (i > 0) tc::mma_commit(&vempty[(q - 1) & 1]);
+        if (i > 0) {
+          const int p = q - 1, st = p % kStages;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&vfull[st], (p / kStages) & 1, abortp, stt));
+          if (!ok) break;
+#pragma unroll
+          for (int t = 0; t < kT; ++t) {
+            ok = __all_sync(0xffffffffu, ok && tc::mbar_wait(&pfull[t][p & 1], (p >> 1) & 1, abortp, stt));
+            if (!ok) break;
+            tc::fence_after_sync();
+            mma_pv(tm + 256 * t + 128, tm + 256 * t + (p & 1) * 64, kv_desc + ((st * kStageBytes + 2 * kKTile) >> 4),
+                   idesc_f16(128), (i - 1) % kFlush != 0);
+            commit_elected(&odone[t][p & 1]);
+          }
+          if (!ok) break;
+          commit_elected(&vempty[st]);
         }
-        __syncwarp();
+        if (i < n) ++q;
       }
-      it += n;
       u += n;
     }
-    if (lane == 0) {   // every MMA done before TMEM and shared memory go
-      tc::mma_commit(&drain);
+    __syncwarp();
+    {   // every MMA done before TMEM and shared memory go
+      commit_elected(&drain);
       volatile int never = 0;
       tc::mbar_wait(&drain, 0, &never, stt);
     }
     __syncwarp();
   } else if (warp >= kSoft) {
     // ------------------------------------------------------------ converters
+    regs_dec<Cfg::kRegsRest>();
     const int cw = warp - kSoft, ct = tid - kSoft * 32;
-    // K: eight lanes a row, 16 dims each.  V: keys 8 ko .. 8 ko + 7, dims 16 dg .. 16 dg + 15 (eight lanes with
+    // K: eight lanes a row, 16 dims each.  V: keys 8 ko .. 8 ko + 7, dims 8 dg .. 8 dg + 7 (eight lanes with
     // different ko write one dim's chunks: no bank conflicts)
-    const int kc = lane & 7, kr = cw * 32 + (lane >> 3);
-    const int ko = (lane & 7) + 8 * (cw & 1), dg = (lane >> 3) + 4 * (cw >> 1);
+    const int kc = lane & 7, kr = cw * 16 + (lane >> 3);
+    const int ko = lane & 7, dg = (lane >> 3) + 4 * cw;
     bool ok = true;
     int it = 0;
     for (long long u = u0; u < u1 && ok;) {
       const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = (int)min((long long)(g.count - g.step), u1 - u);
-      const uint8_t* Kh = c.K + g.sh * c.cap * 128;
-      const uint8_t* Vh = c.V + g.sh * c.cap * 128;
-      const uint4 zero = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
-      uint4 raw[8];
-      auto load_k = [&](int i) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key = (g.step + i) * kStep + kr + 4 * j;
-          raw[j] = key < c.cap ? __ldg((const uint4*)(Kh + (long long)key * 128 + kc * 16)) : zero;
-        }
-      };
-      auto load_v = [&](int i) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int key = (g.step + i) * kStep + ko * 8 + j;
-          raw[j] = key < c.cap ? __ldg((const uint4*)(Vh + (long long)key * 128 + dg * 16)) : zero;
-        }
-      };
+      const int n = (int)min((long long)(g.count - g.step), u1 - u), len = cache_len(c, g.s);
       for (int i = 0; i < n && ok; ++i) {
-        const int q = it + i, st = q & 1;
-        unsigned char* Ks = sKV + st * 4 * kHalf;
-        unsigned char* Vs = Ks + 2 * kHalf;
-        load_k(i);   // in flight while the stage is waited for
-        if (q >= 2) ok = tc::mbar_wait(&kempty[st], ((q >> 1) - 1) & 1, abortp, stt);
+        const int q = it + i, st = q % kStages, b = g.step + i;
+        unsigned char* Ks = sKV + st * kStageBytes;
+        unsigned char* Vs = Ks + 2 * kKTile;
+        // in flight while the stage is waited for (b lies within the capacity: `count` does)
+        const long long at = g.sh * c.cap + (long long)b * kCB;
+        uint4 rk[4];
+        uint2 rv[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rk[j] = __ldg((const uint4*)(c.K + (at + kr + 4 * j) * 128 + kc * 16));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rv[j] = __ldg((const uint2*)(c.V + (at + ko * 8 + j) * 128 + dg * 8));
+        if (q >= kStages) ok = tc::mbar_wait(&kempty[st], ((q / kStages) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4; ++j) {
           const int r = kr + 4 * j;
-          const uint4 x = make_uint4(codes_f16<0>(raw[j].x), codes_f16<1>(raw[j].x), codes_f16<0>(raw[j].y),
-                                     codes_f16<1>(raw[j].y));
-          const uint4 y = make_uint4(codes_f16<0>(raw[j].z), codes_f16<1>(raw[j].z), codes_f16<0>(raw[j].w),
-                                     codes_f16<1>(raw[j].w));
-          unsigned char* row = Ks + (kc >> 2) * kHalf + r * 128;
+          const uint4 x = make_uint4(codes_f16<0>(rk[j].x), codes_f16<1>(rk[j].x), codes_f16<0>(rk[j].y),
+                                     codes_f16<1>(rk[j].y));
+          const uint4 y = make_uint4(codes_f16<0>(rk[j].z), codes_f16<1>(rk[j].z), codes_f16<0>(rk[j].w),
+                                     codes_f16<1>(rk[j].w));
+          unsigned char* row = Ks + (kc >> 2) * kKTile + r * 128;
           // the two chunks in an order that keeps the eight lanes of a row on different banks
           const int q0 = (kc & 3) * 2 + (kc >> 2), q1 = (kc & 3) * 2 + 1 - (kc >> 2);
           *(uint4*)(row + ((q0 ^ (r & 7)) << 4)) = (kc >> 2) ? y : x;
           *(uint4*)(row + ((q1 ^ (r & 7)) << 4)) = (kc >> 2) ? x : y;
         }
-        if (ct < 2) {
-          const int b = (g.step + i) * 2 + ct;
-          float ks = 1.f, vs = 1.f;   // of blocks that hold nothing: their keys are masked
-          if (b * kCB < cache_len(c, g.s)) {
+        if (ct == 0) {
+          float ks = 1.f, vs = 1.f;   // of a block that holds nothing: its keys are masked
+          if (b * kCB < len) {
             ks = c.k_scale[g.sh * d.nblk + b];
             vs = c.v_scale[g.sh * d.nblk + b];
           }
-          Meta& m = meta[q & 3];
-          m.ks[ct] = ks;
-          m.lv[ct] = log2f(vs);
-          m.iv[ct] = kVsUnit / vs;
+          meta[q % (2 * kStages)] = Meta{ks, log2f(vs), kVsUnit / vs};
         }
         tc::fence_proxy_async_smem();
         tc::mbar_arrive(&kfull[st]);
-        load_v(i);
-        if (q >= 2) ok = tc::mbar_wait(&vempty[st], ((q >> 1) - 1) & 1, abortp, stt);
+        if (q >= kStages) ok = tc::mbar_wait(&vempty[st], ((q / kStages) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {   // dims 16 dg + 4 w ..
+        for (int w = 0; w < 2; ++w) {   // dims 8 dg + 4 w ..
           uint32_t f[4][4];             // [dim][key pair]
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            const uint32_t a = w == 0 ? raw[2 * p].x : w == 1 ? raw[2 * p].y : w == 2 ? raw[2 * p].z : raw[2 * p].w;
-            const uint32_t b = w == 0 ? raw[2 * p + 1].x : w == 1 ? raw[2 * p + 1].y : w == 2 ? raw[2 * p + 1].z : raw[2 * p + 1].w;
-            const uint32_t y = __byte_perm(a, b, 0x5140), z = __byte_perm(a, b, 0x7362);
+            const uint32_t a = w ? rv[2 * p].y : rv[2 * p].x, e = w ? rv[2 * p + 1].y : rv[2 * p + 1].x;
+            const uint32_t y = __byte_perm(a, e, 0x5140), z = __byte_perm(a, e, 0x7362);
             f[0][p] = codes_f16<0>(y);
             f[1][p] = codes_f16<1>(y);
             f[2][p] = codes_f16<0>(z);
@@ -418,9 +448,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int dim = dg * 16 + w * 4 + e;
-            *(uint4*)(Vs + (ko >> 3) * kHalf + dim * 128 + (((ko & 7) ^ (dim & 7)) << 4)) =
-                make_uint4(f[e][0], f[e][1], f[e][2], f[e][3]);
+            const int dim = dg * 8 + w * 4 + e;
+            *(uint4*)(Vs + dim * 128 + ((ko ^ (dim & 7)) << 4)) = make_uint4(f[e][0], f[e][1], f[e][2], f[e][3]);
           }
         }
         tc::fence_proxy_async_smem();
@@ -431,12 +460,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     }
   } else {
     // --------------------------------------------------------------- softmax
+    regs_inc<Cfg::kRegsSoft>();
     const int t = warp >> 2, row_t = (warp & 3) * 32 + lane;   // this thread's row of its tile
-    const uint32_t S = tmem + 256 * t + ((uint32_t)(warp & 3) * 32 << 16), Ot = S + 128;
+    const uint32_t Sb = tmem + 256 * t + ((uint32_t)(warp & 3) * 32 << 16), Ot = Sb + 128;
     const int nrows = d.n_pos * d.G;
     bool ok = true;
-    int it = 0, seg = 0;
-    for (long long u = u0; u < u1; ++seg) {
+    int it = 0;
+    for (long long u = u0; u < u1;) {
       const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
       const int row = g.tile * kRows + t * 128 + row_t, pos = row / d.G, gq = row - pos * d.G;
@@ -445,201 +475,195 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const int see = mine ? visible_tokens(cache_len(c, g.s), d.n_pos, pos, d.causal) : 0;
       float fac;   // of this row's products, in powers of two without biases, of e with them
       {            // the query row as f16, scaled by a power of two
-        const uint4* src = (const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128);
+        uint4 v[16];
         float amax = 0.f;
-        if (mine)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint4 v = __ldg(src + e);
-            const __nv_bfloat162* y = (const __nv_bfloat162*)&v;
+        for (int e = 0; e < 16; ++e) {
+          v[e] = make_uint4(0u, 0u, 0u, 0u);
+          if (mine) v[e] = __ldg((const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128) + e);
+        }
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              const float2 z = __bfloat1622float2(y[f]);
-              amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
-            }
+        for (int e = 0; e < 16; ++e) {
+          const __nv_bfloat162* y = (const __nv_bfloat162*)&v[e];
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const float2 z = __bfloat1622float2(y[f]);
+            amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
           }
+        }
         const int ex = max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100);
         const float up = __uint_as_float((unsigned)(14 - ex + 127) << 23);
         fac = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (mine) {
-            v = __ldg(src + e);
-            const __nv_bfloat162* y = (const __nv_bfloat162*)&v;
-            __half2 z[4];
+          const __nv_bfloat162* y = (const __nv_bfloat162*)&v[e];
+          __half2 z[4];
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              const float2 a = __bfloat1622float2(y[f]);
-              z[f] = __floats2half2_rn(a.x * up, a.y * up);
-            }
-            v = *(const uint4*)&z[0];
+          for (int f = 0; f < 4; ++f) {
+            const float2 a = __bfloat1622float2(y[f]);
+            z[f] = __floats2half2_rn(a.x * up, a.y * up);
           }
-          *(uint4*)(sQ + (t * 2 + (e >> 3)) * kHalf + row_t * 128 + (((e & 7) ^ (row_t & 7)) << 4)) = v;
+          *(uint4*)(sQ + (t * 2 + (e >> 3)) * kHalf + row_t * 128 + (((e & 7) ^ (row_t & 7)) << 4)) =
+              *(const uint4*)&z[0];
         }
         tc::fence_proxy_async_smem();
         tc::mbar_arrive(&qfull);
       }
-      float* sums = parts + 2ll * kCacheMaxCtas * Cfg::kSlot + (long long)blockIdx.x * kRows * 128 + t * 128 + row_t;
+      // this row's sums in memory, [dims / 4][row][4]
+      const long long row_at = (long long)(t * 128 + row_t) * 4;
+      float* sums = parts + 2ll * kCacheMaxCtas * Cfg::kSlot + (long long)blockIdx.x * kRows * 128 + row_at;
       float bref = -INFINITY, brefv = 0.f;          // reference of the flushed sums
       float ref = -INFINITY, refv = 0.f, l = 0.f;   // with biases ref is the logit and refv the log2 vs that came with it
       const float* bias = kBias ? c.bias + g.sh * c.cap : nullptr;
       for (int i = 0; i < n; ++i) {
-        const int q = it + i, j0 = (g.step + i) * kStep;
-        // S is in; so are the product of the step before (issued earlier by the same thread) and the step's scales
-        // (written before kfull, which the MMA warp waited for)
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t], q & 1, abortp, stt));
+        const int q = it + i, j0 = (g.step + i) * kCB;
+        const uint32_t S = Sb + (q & 1) * 64;
+        // S is in, and with it the block's scales (written before kfull, which the MMA warp waited for)
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q & 1], (q >> 1) & 1, abortp, stt));
         if (!ok) break;
         tc::fence_after_sync();
-        const Meta m = meta[q & 3];
         if (i > 0 && i % kFlush == 0) {
           // O goes to this row's sums in memory and starts again at zero (see above)
-          const float d = kBias ? fmaf(ref - bref, kLog2e, refv - brefv) : ref - bref;   // NaN, inf: nothing there yet
-          const bool none = bref == -INFINITY, far = !none && d > kFar;
-          const float up = none || far ? 1.f : ex2_approx(d), down = far ? ex2_approx(-d) : 1.f;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(q - 1) & 1], ((q - 1) >> 1) & 1, abortp, stt));
+          if (!ok) break;
+          tc::fence_after_sync();
+          const float dd = kBias ? fmaf(ref - bref, kLog2e, refv - brefv) : ref - bref;   // unused while there are none
+          const bool none = bref == -INFINITY, far = !none && dd > kFar;
+          const float up = none || far ? 1.f : ex2_approx(dd), down = far ? ex2_approx(-dd) : 1.f;
           const bool redo = __any_sync(0xffffffffu, none || far);
 #pragma unroll 1
-          for (int ch = 0; ch < 8; ++ch) {
-            float o[16];
-            tc::tmem_ld16(Ot + ch * 16, o);
-            float* b = sums + ch * 16 * kRows;
-            if (redo) {
+          for (int ch = 0; ch < 4; ++ch) {
+            float o[32];
+            tc::tmem_ld32(Ot + ch * 32, o);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float old = none ? 0.f : __ldcg(b + e * kRows);
-                __stcg(b + e * kRows, fmaf(old, down, o[e] * up));
+            for (int e = 0; e < 8; ++e) {
+              float* b = sums + (long long)(ch * 8 + e) * kRows * 4;
+              const float4 x = make_float4(o[4 * e] * up, o[4 * e + 1] * up, o[4 * e + 2] * up, o[4 * e + 3] * up);
+              if (redo) {
+                float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!none) old = __ldcg((const float4*)b);
+                __stcg((float4*)b, make_float4(fmaf(old.x, down, x.x), fmaf(old.y, down, x.y), fmaf(old.z, down, x.z),
+                                               fmaf(old.w, down, x.w)));
+              } else {
+                asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(b), "f"(x.x), "f"(x.y),
+                             "f"(x.z), "f"(x.w)
+                             : "memory");
               }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                asm volatile("red.global.add.f32 [%0], %1;" ::"l"(b + e * kRows), "f"(o[e] * up) : "memory");
             }
           }
           if (none || far) {
             bref = ref;
             brefv = refv;
           }
-          tc::fence_before_sync();
         }
-        float v[128];
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) tmem_ld32_async(S + ch * 32, v + ch * 32);
+        float v[64];
+        tmem_ld32_async(S, v);
+        tmem_ld32_async(S + 32, v + 32);
+        const Meta m = meta[q % (2 * kStages)];
+        const float f = fac * m.ks;
         tmem_wait_ld();
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch) settle32(v + ch * 32);
-        const int lim = see - j0;   // keys of the step that the row sees
-        const bool edge = __any_sync(0xffffffffu, lim < kStep);
-        const float f[2] = {fac * m.ks[0], fac * m.ks[1]};
+        settle32(v);
+        settle32(v + 32);
+        const int lim = see - j0;   // keys of the block that the row sees
         if (kBias) {   // logits; biases are read four at a time where the row sees something, within the capacity
 #pragma unroll
-          for (int e = 0; e < kStep; e += 4) {
+          for (int e = 0; e < kCB; e += 4) {
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
             if (e < lim) x = __ldg((const float4*)(bias + j0 + e));
-            v[e] = fmaf(v[e], f[e >> 6], x.x);
-            v[e + 1] = fmaf(v[e + 1], f[e >> 6], x.y);
-            v[e + 2] = fmaf(v[e + 2], f[e >> 6], x.z);
-            v[e + 3] = fmaf(v[e + 3], f[e >> 6], x.w);
+            v[e] = fmaf(v[e], f, x.x);
+            v[e + 1] = fmaf(v[e + 1], f, x.y);
+            v[e + 2] = fmaf(v[e + 2], f, x.z);
+            v[e + 3] = fmaf(v[e + 3], f, x.w);
           }
         }
-        if (edge) {
+        if (__any_sync(0xffffffffu, lim < kCB)) {
 #pragma unroll
-          for (int e = 0; e < kStep; ++e)
+          for (int e = 0; e < kCB; ++e)
             if (e >= lim) v[e] = -INFINITY;
         }
-        // largest of each block
-        float top[2];
+        float top = v[0], b = v[1], aa = v[2], bb = v[3];
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-          float a = v[hb * 64], b = v[hb * 64 + 1];
-#pragma unroll
-          for (int e = 2; e < 64; e += 2) {
-            a = fmaxf(a, v[hb * 64 + e]);
-            b = fmaxf(b, v[hb * 64 + e + 1]);
-          }
-          a = fmaxf(a, b);
-          top[hb] = kBias ? a : fmaf(a, f[hb], m.lv[hb]);   // f > 0: the largest product is the largest logit
+        for (int e = 4; e < kCB; e += 4) {
+          top = fmaxf(top, v[e]);
+          b = fmaxf(b, v[e + 1]);
+          aa = fmaxf(aa, v[e + 2]);
+          bb = fmaxf(bb, v[e + 3]);
         }
+        top = fmaxf(fmaxf(top, b), fmaxf(aa, bb));
         float alpha = 1.f;
         bool grow;
         if (kBias) {
           // in units of log2: (x - ref) log2 e + lv - refv; differences of logits first, so that the type's lowest
           // value cancels against itself
-          float nr = ref, nv = refv;
-#pragma unroll
-          for (int hb = 0; hb < 2; ++hb)
-            if (top[hb] != -INFINITY && (nr == -INFINITY || fmaf(top[hb] - nr, kLog2e, m.lv[hb] - nv) > 0.f)) {
-              nr = top[hb];
-              nv = m.lv[hb];
-            }
-          grow = nr != -INFINITY && (ref == -INFINITY || fmaf(nr - ref, kLog2e, nv - refv) > kGrow);
+          grow = top != -INFINITY && (ref == -INFINITY || fmaf(top - ref, kLog2e, m.lv - refv) > kGrow);
           if (grow) {
-            alpha = ref == -INFINITY ? 0.f : ex2_approx(fmaf(ref - nr, kLog2e, refv - nv));
-            ref = nr;
-            refv = nv;
+            alpha = ref == -INFINITY ? 0.f : ex2_approx(fmaf(ref - top, kLog2e, refv - m.lv));
+            ref = top;
+            refv = m.lv;
           }
         } else {
-          const float nr = fmaxf(top[0], top[1]);
-          grow = nr > ref + kGrow || (ref == -INFINITY && nr != -INFINITY);
+          top = fmaf(top, f, m.lv);   // f > 0: the largest product is the largest logit
+          grow = top > ref + kGrow || (ref == -INFINITY && top != -INFINITY);
           if (grow) {
-            alpha = ref == -INFINITY ? 0.f : ex2_approx(ref - nr);
-            ref = nr;
+            alpha = ref == -INFINITY ? 0.f : ex2_approx(ref - top);
+            ref = top;
           }
         }
-        if (i % kFlush != 0 && __any_sync(0xffffffffu, grow)) {
+        if (i % kFlush != 0 && __any_sync(0xffffffffu, grow)) {   // scale O once the product of the block before is in
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(q - 1) & 1], ((q - 1) >> 1) & 1, abortp, stt));
+          if (!ok) break;
+          tc::fence_after_sync();
 #pragma unroll 1
-          for (int ch = 0; ch < 8; ++ch) {
-            float o[16];
-            tc::tmem_ld16(Ot + ch * 16, o);
+          for (int ch = 0; ch < 4; ++ch) {
+            float o[32];
+            tc::tmem_ld32(Ot + ch * 32, o);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] *= alpha;
-            tmem_st16(Ot + ch * 16, o);
+            for (int e = 0; e < 32; ++e) o[e] *= alpha;
+            tmem_st32(Ot + ch * 32, o);
           }
-          tmem_wait_st();
         }
-        l *= alpha;
         const float base = ref == -INFINITY ? 0.f : ref;
+        const float add = (kBias ? m.lv - refv : m.lv - base) + kLift;
+        const float2 add_2 = make_float2(add, add);
+        float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-          const float add = kBias ? m.lv[hb] - refv + kLift : m.lv[hb] - base + kLift;
-          const float2 add_2 = make_float2(add, add);
-          float2 sum = make_float2(0.f, 0.f);
+        for (int ch = 0; ch < 4; ++ch) {   // 16 keys: eight columns of hi, eight of lo
+          uint32_t hr[8], lr[8];
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
-            uint32_t r[32];
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const int k = hb * 64 + ch * 32 + e;
-              float2 x = make_float2(v[k], v[k + 1]);
-              if (kBias)
-                x = fma2(add2(x, make_float2(-base, -base)), make_float2(kLog2e, kLog2e), add_2);
-              else
-                x = fma2(x, make_float2(f[hb], f[hb]), add_2);
-              x.x = ex2_approx(x.x);
-              x.y = ex2_approx(x.y);
-              sum = add2(sum, x);
-              // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
-              const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
-                                            __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
-              const float2 lo = add2(x, make_float2(-hi.x, -hi.y));
-              const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
-              r[e >> 1] = *(const uint32_t*)&h2;
-              r[16 + (e >> 1)] = *(const uint32_t*)&l2;
-            }
-            tmem_st32(S + hb * 64 + ch * 32, r);
+          for (int e = 0; e < 16; e += 2) {
+            float2 x = make_float2(v[ch * 16 + e], v[ch * 16 + e + 1]);
+            if (kBias)
+              x = fma2(add2(x, make_float2(-base, -base)), make_float2(kLog2e, kLog2e), add_2);
+            else
+              x = fma2(x, make_float2(f, f), add_2);
+            x.x = ex2_approx(x.x);
+            x.y = ex2_approx(x.y);
+            sum = add2(sum, x);
+            // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
+            const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
+                                          __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
+            const float2 lo = add2(x, make_float2(-hi.x, -hi.y));
+            const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
+            hr[e >> 1] = *(const uint32_t*)&h2;
+            lr[e >> 1] = *(const uint32_t*)&l2;
           }
-          l = fmaf(sum.x + sum.y, m.iv[hb], l);
+          tmem_st8(S + (ch >> 1) * 32 + (ch & 1) * 8, hr);
+          tmem_st8(S + (ch >> 1) * 32 + (ch & 1) * 8 + 16, lr);
         }
+        l = fmaf(l, alpha, (sum.x + sum.y) * m.iv);
         tmem_wait_st();
         tc::fence_before_sync();
-        tc::mbar_arrive(&pfull[t]);
+        tc::mbar_arrive(&pfull[t][q & 1]);
       }
       it += n;
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t], seg & 1, abortp, stt));
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(it - 1) & 1], ((it - 1) >> 1) & 1, abortp, stt));
       tc::fence_after_sync();
       if (tid == 0) stop_flag = *abortp;   // one reading for all
       asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
       if (stop_flag) break;
       const bool whole = g.step == 0 && n == g.count;
+      const bool flushed = bref != -INFINITY;
+      const float bw = flushed ? ex2_approx(kBias ? fmaf(bref - ref, kLog2e, brefv - refv) : bref - ref) : 0.f;
       auto store4 = [&](int dim, float4 v, float inv) {
         v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
         const float big = 3.402823466e38f;
@@ -648,31 +672,29 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         *(float4*)(O + g.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
       };
       const float inv = l == 0.f ? 0.f : kVsUnit / l;
-      const bool flushed = bref != -INFINITY;
-      const float bw = flushed ? ex2_approx(kBias ? fmaf(bref - ref, kLog2e, brefv - refv) : bref - ref) : 0.f;
-      float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + t * 128 + row_t;
-#pragma unroll
+      // partial results: laid out as `sums`, then (ref, refv, l) of the rows
+      float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot;
+#pragma unroll 1
       for (int ch = 0; ch < 4; ++ch) {
         float v[32];
         tc::tmem_ld32(Ot + ch * 32, v);
-        if (flushed) {
+        float4 y[8];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = fmaf(__ldcg(sums + (ch * 32 + e) * kRows), bw, v[e]);
+        for (int e = 0; e < 8; ++e) {
+          y[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (flushed) y[e] = __ldcg((const float4*)(sums + (long long)(ch * 8 + e) * kRows * 4));
         }
-        if (whole) {
-          if (mine)
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) store4(ch * 32 + e, make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), inv);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) __stcg(slot + (ch * 32 + e) * kRows, v[e]);
+        for (int e = 0; e < 8; ++e) {
+          const float4 x = make_float4(fmaf(y[e].x, bw, v[4 * e]), fmaf(y[e].y, bw, v[4 * e + 1]),
+                                       fmaf(y[e].z, bw, v[4 * e + 2]), fmaf(y[e].w, bw, v[4 * e + 3]));
+          if (!whole) __stcg((float4*)(slot + row_at + (long long)(ch * 8 + e) * kRows * 4), x);
+          else if (mine) store4(ch * 32 + 4 * e, x, inv);
         }
       }
       tc::fence_before_sync();
       if (!whole) {
-        __stcg(slot + 128 * kRows, ref);
-        __stcg(slot + 129 * kRows, refv);
-        __stcg(slot + 130 * kRows, l);
+        __stcg((float4*)(slot + 128 * kRows + row_at), make_float4(ref, refv, l, 0.f));
         const int c_first = sh.owner(g.first), c_last = sh.owner(g.first + g.count - 1);
         __threadfence();
         asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
@@ -683,34 +705,45 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         }
         asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
         if (last_flag && mine) {
-          auto part = [&](int cc) { return parts + (2ll * cc + (cc == c_first)) * Cfg::kSlot + t * 128 + row_t; };
-          float top = -INFINITY, topv = 0.f, z = 0.f;
-          for (int cc = c_first; cc <= c_last; ++cc) {
-            const float r = __ldcg(part(cc) + 128 * kRows), rv = __ldcg(part(cc) + 129 * kRows);
-            if (r != -INFINITY && (top == -INFINITY || (kBias ? fmaf(r - top, kLog2e, rv - topv) : r - top) > 0.f)) {
-              top = r;
-              topv = rv;
-            }
-          }
-          auto weight = [&](int cc) {
-            const float r = __ldcg(part(cc) + 128 * kRows), rv = __ldcg(part(cc) + 129 * kRows);
-            return r == -INFINITY ? 0.f : ex2_approx(kBias ? fmaf(r - top, kLog2e, rv - topv) : r - top);
-          };
-          for (int cc = c_first; cc <= c_last; ++cc) z = fmaf(__ldcg(part(cc) + 130 * kRows), weight(cc), z);
-          const float zinv = z == 0.f ? 0.f : kVsUnit / z;
+          // the parts in CTA order, with a running reference; 32 dims at a time
+#pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
-            float v[32];
+            float top = -INFINITY, topv = 0.f, z = 0.f;
+            float4 a[8];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = 0.f;
+            for (int e = 0; e < 8; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
             for (int cc = c_first; cc <= c_last; ++cc) {
-              const float w = weight(cc);
-              const float* p = part(cc) + ch * 32 * kRows;
+              const float* p = parts + (2ll * cc + (cc == c_first)) * Cfg::kSlot + row_at;
+              const float4 st4 = __ldcg((const float4*)(p + 128 * kRows));
+              float4 x[8];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) v[e] = fmaf(__ldcg(p + e * kRows), w, v[e]);
+              for (int e = 0; e < 8; ++e) x[e] = __ldcg((const float4*)(p + (long long)(ch * 8 + e) * kRows * 4));
+              if (st4.x == -INFINITY) continue;   // a part that saw nothing
+              float w = 1.f, down = 0.f;          // of the new part, of the sums
+              if (top == -INFINITY) {
+                top = st4.x;
+                topv = st4.y;
+              } else {
+                const float up = kBias ? fmaf(st4.x - top, kLog2e, st4.y - topv) : st4.x - top;
+                if (up > 0.f) {
+                  down = ex2_approx(-up);
+                  top = st4.x;
+                  topv = st4.y;
+                } else {
+                  down = 1.f;
+                  w = ex2_approx(up);
+                }
+              }
+              z = fmaf(z, down, st4.z * w);
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                a[e] = make_float4(fmaf(a[e].x, down, x[e].x * w), fmaf(a[e].y, down, x[e].y * w),
+                                   fmaf(a[e].z, down, x[e].z * w), fmaf(a[e].w, down, x[e].w * w));
             }
+            const float zinv = z == 0.f ? 0.f : kVsUnit / z;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              store4(ch * 32 + e, make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]), zinv);
+            for (int e = 0; e < 8; ++e) store4(ch * 32 + 4 * e, a[e], zinv);
           }
         }
       }
