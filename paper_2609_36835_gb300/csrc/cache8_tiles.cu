@@ -5,17 +5,19 @@
 // tensor pipe.  A CTA takes 128 or 256 rows of one head (one or two M = 128
 // tiles) and goes over the keys a block of 64 at a time:
 //   converters (4 warps)  read the codes of K and V and leave them in shared
-//                         memory as f16 operands, V transposed, four blocks
+//                         memory as f16 operands, V transposed, six blocks
 //                         ahead; a code costs about one instruction for 256 rows
 //   MMA warp              S = Q K^T (exact products, fp32 sums in TMEM), O += P V
-//   softmax (4 warps a tile, one row a thread)  turn S into weights in place: the
-//                         f16 pair hi + lo of 32 keys takes the 32 columns that
-//                         their logits had; P is the MMA's operand from TMEM
+//   softmax (8 warps a tile, 16 rows each, four lanes a row)  turn S into weights
+//                         in place: the f16 pair hi + lo of 32 keys takes the 32
+//                         columns that their logits had; P is the MMA's operand
+//                         from TMEM
+// Q is an operand from TMEM too: read from shared memory for each block, Q and K
+// would take 1.5 times the pipe's time for S.
 // P V runs once for hi and once for lo, which keeps 21 bits of a weight: three
 // units of MMA work where f16 weights would do with two, so 2/3 of the pipe's
-// peak is the most that the fp32 output allows.  A tile has two buffers of S in
-// TMEM: the logits of the next block come in while the softmax of this one runs,
-// and the pipe has the other tile's products meanwhile.
+// peak is the most that the fp32 output allows.  With two tiles the pipe works on
+// one while the other's softmax runs.
 //
 // The weight of key j of block b carries the block's scale of V:
 //   w_j = 2^{x_j + log2 vs_b - ref + 7},  O = sum_j w_j c_j / sum_b (sum_{j in b} w_j) / vs_b
@@ -36,7 +38,7 @@ namespace {
 
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
-constexpr int kStages = 4, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
+constexpr int kStages = 6, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
 constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
@@ -50,43 +52,45 @@ struct TileShape {
 template <int kT>
 struct TileCfg {
   static constexpr int kRows = 128 * kT;
-  static constexpr int kSoft = 4 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
-  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: three warps idle
-  // registers at launch, and how the warpgroups share them: softmax (kT groups), converters, MMA
-  static constexpr int kRegs = kT == 2 ? 128 : 168;
-  static constexpr int kRegsSoft = kT == 2 ? 184 : 232, kRegsRest = kT == 2 ? 72 : 136;
-  static_assert(kT * kRegsSoft + 2 * kRegsRest == (kT + 2) * kRegs && kRegs * kThreads <= 65536,
+  static constexpr int kSoft = 8 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
+  static constexpr int kSoftThreads = 32 * kSoft;
+  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: MMA, scales, two idle warps
+  // registers at launch, and how the warpgroups share them: softmax (2 kT groups), converters, MMA
+  static constexpr int kRegs = kT == 2 ? 80 : 128;
+  static constexpr int kRegsSoft = kT == 2 ? 96 : 176, kRegsConv = kT == 2 ? 64 : 96, kRegsMma = kT == 2 ? 32 : 64;
+  static_assert(2 * kT * kRegsSoft + kRegsConv + kRegsMma == (2 * kT + 2) * kRegs && kRegs * kThreads <= 65536,
                 "the shares add up to what the block was launched with");
-  static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + 1024;   // Q, then the stages
-  static constexpr int kSlot = 132 * kRows;              // floats of a partial result: O, then ref, log2 vs of ref and sum of the rows
+  static constexpr int kSmem = kStages * kStageBytes + 1024;
+  // floats of a partial result: 64 outputs and twice (ref, log2 vs of ref, sum, unused) of each softmax thread
+  static constexpr int kSlot = 72 * kSoftThreads;
 };
 
 // The products of one block and row tile, issued by one elected lane of a converged warp with warp-uniform operands
 // (from one lane of a divergent branch each MMA took 90 to 125 cycles to issue, twice what it runs).  A descriptor's
 // low bits are the address in units of 16 bytes, so K steps are added to the tile's descriptor.
 //
-// S = Q K^T: Q 128 x 128 and K 64 x 128 in halves of 64 dims (16 KB and 8 KB apart).
-__device__ __forceinline__ void mma_qk(uint32_t s, uint64_t q, uint64_t k, uint32_t idesc) {
+// S = Q K^T: Q in TMEM, 16 dims in 8 columns; K 64 x 128 in halves of 64 dims, 8 KB apart.
+__device__ __forceinline__ void mma_qk(uint32_t s, uint32_t q, uint64_t k, uint32_t idesc) {
   asm volatile(
-      "{\n\t.reg .pred e, z, c;\n\t.reg .b64 a, b;\n\t"
+      "{\n\t.reg .pred e, z, c;\n\t.reg .b64 b;\n\t.reg .b32 a;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
       "setp.ne.b32 z, 0, 0;\n\tsetp.eq.b32 c, 0, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n\t"
-      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 1024;\n\tadd.s64 b, %2, 512;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 1026;\n\tadd.s64 b, %2, 514;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 1028;\n\tadd.s64 b, %2, 516;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
-      "add.s64 a, %1, 1030;\n\tadd.s64 b, %2, 518;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t}\n" ::"r"(s),
-      "l"(q), "l"(k), "r"(idesc)
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, z;\n\t"
+      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 2;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 16;\n\tadd.s64 b, %2, 4;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 24;\n\tadd.s64 b, %2, 6;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 32;\n\tadd.s64 b, %2, 512;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 40;\n\tadd.s64 b, %2, 514;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 48;\n\tadd.s64 b, %2, 516;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
+      "add.u32 a, %1, 56;\n\tadd.s64 b, %2, 518;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t}\n" ::"r"(s),
+      "r"(q), "l"(k), "r"(idesc)
       : "memory");
 }
 // O (+)= P V: P in TMEM, 16 keys in 8 columns, hi and then lo 16 columns on, 32 keys in 32 columns; V^T 128 x 64.
@@ -120,15 +124,12 @@ __device__ __forceinline__ void commit_elected(uint64_t* bar) {
       "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(tc::smem_u32(bar))
       : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
-               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-// 32 columns of this warp's lanes, not waited for.
-__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* v) {
+// 16 lanes of TMEM spread over a warp: lane l has rows l / 4 and l / 4 + 8.
+//   loads and stores of fp32 columns: v[4 j + 2 i + e] is row l / 4 + 8 i, column 8 j + 2 (l % 4) + e
+//   stores of 16 columns of f16 pairs: r[2 j + i] is row l / 4 + 8 i, column 4 j + l % 4
+__device__ __forceinline__ void tmem_ld_rows64(uint32_t taddr, float (&v)[32]) {   // not waited for
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
@@ -137,15 +138,50 @@ __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float* v) {
         "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
       : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_ld_rows32(uint32_t taddr, float (&v)[16]) {   // not waited for
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st_rows32(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_pairs16(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 32 columns of this warp's 32 lanes, a lane each.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Nothing that uses v moves above this point (behind a wait).
-__device__ __forceinline__ void settle32(float* v) {
-  asm volatile(""
-               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
-                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
-                 "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]),
-                 "+f"(v[30]), "+f"(v[31]));
+template <int kN>
+__device__ __forceinline__ void settle(float (&v)[kN]) {
+#pragma unroll
+  for (int i = 0; i < kN; i += 16)
+    asm volatile(""
+                 : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                   "+f"(v[i + 6]), "+f"(v[i + 7]), "+f"(v[i + 8]), "+f"(v[i + 9]), "+f"(v[i + 10]), "+f"(v[i + 11]),
+                   "+f"(v[i + 12]), "+f"(v[i + 13]), "+f"(v[i + 14]), "+f"(v[i + 15]));
 }
 // Two fp32 operations an instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -170,18 +206,6 @@ template <int kN>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
 template <int kN>
 __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kN)); }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]),
-      "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]),
-      "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]),
-      "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // kind::f16 with A = B = f16, D = fp32, both K-major, M = 128, N = n.
 __host__ __device__ constexpr uint32_t idesc_f16(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
@@ -259,31 +283,27 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   using Cfg = TileCfg<kT>;
   constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows;
   extern __shared__ unsigned char smraw[];
-  unsigned char* sQ = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [tile][half][128][128 B]
-  unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K halves, V]
-  long long* pre = (long long*)(sKV + kStages * kStageBytes);                      // [S + 1] blocks of a head's tiles
-  __shared__ __align__(8) uint64_t qfull, kfull[kStages], vfull[kStages], kempty[kStages], vempty[kStages],
-      sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
+  unsigned char* sKV = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [stage][K halves, V]
+  long long* pre = (long long*)(sKV + kStages * kStageBytes);                       // [S + 1] blocks of a head's tiles
+  __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT], pfull[kT], odone[kT], drain;
   __shared__ Meta meta[2 * kStages];
+  __shared__ float s_row[kT][2][128];   // of a row: largest |q| of each half, then its factor
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, stop_flag, last_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abortp = &abort_flag;
 
   if (tid == 0) {
-    tc::mbar_init(&qfull, kRows);
+    tc::mbar_init(&qfull, kSoft);
     for (int i = 0; i < kStages; ++i) {
-      tc::mbar_init(&kfull[i], 128);
-      tc::mbar_init(&vfull[i], 128);
-      tc::mbar_init(&kempty[i], 1);
-      tc::mbar_init(&vempty[i], 1);
+      tc::mbar_init(&full[i], 5);   // four converters and the scales
+      tc::mbar_init(&empty[i], 1);
     }
-    for (int t = 0; t < kT; ++t)
-      for (int i = 0; i < 2; ++i) {
-        tc::mbar_init(&sfull[t][i], 1);
-        tc::mbar_init(&pfull[t][i], 128);
-        tc::mbar_init(&odone[t][i], 1);
-      }
+    for (int t = 0; t < kT; ++t) {
+      tc::mbar_init(&sfull[t], 1);
+      tc::mbar_init(&pfull[t], 8);
+      tc::mbar_init(&odone[t], 1);
+    }
     tc::mbar_init(&drain, 1);
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -316,61 +336,90 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = tmem_slot;   // tile t: two buffers of S / P at columns 256 t, O at 256 t + 128
+  const uint32_t tmem = tmem_slot;   // tile t: Q at columns 256 t, S / P at 256 t + 64, O at 256 t + 128
   CacheShares sh;
   sh.total = pre[c.S] * d.H;
   sh.ctas = (int)min((long long)gridDim.x, sh.total);
   const bool active = (int)blockIdx.x < sh.ctas;
   const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
 
-  if (warp > kSoft + 4) {
-    regs_dec<Cfg::kRegsRest>();   // idle
+  if (warp > kSoft + 5) {
+    regs_dec<Cfg::kRegsMma>();   // idle
+  } else if (warp == kSoft + 5) {
+    // ---------------------------------------------------------------- scales
+    regs_dec<Cfg::kRegsMma>();
+    bool ok = true;
+    int it = 0;
+    for (long long u = u0; u < u1 && ok;) {
+      const Segment g = segment_of(u, d, c, pre, kRows);
+      const int n = (int)min((long long)(g.count - g.step), u1 - u), len = cache_len(c, g.s);
+      Meta m;
+      for (int i = 0; i < n && ok; ++i) {
+        const int q = it + i, st = q % kStages;
+        if ((i & 31) == 0) {   // of the next 32 blocks, a lane each
+          const int b = g.step + i + lane;
+          float ks = 1.f, vs = 1.f;   // of a block that holds nothing: its keys are masked
+          if (i + lane < n && b * kCB < len) {
+            ks = c.k_scale[g.sh * d.nblk + b];
+            vs = c.v_scale[g.sh * d.nblk + b];
+          }
+          m = Meta{ks, log2f(vs), kVsUnit / vs};
+        }
+        if (q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && lane == (i & 31)) {
+          meta[q % (2 * kStages)] = m;
+          tc::mbar_arrive(&full[st]);
+        }
+      }
+      it += n;
+      u += n;
+    }
   } else if (warp == kSoft + 4) {
     // ------------------------------------------------------------ MMA issuer
-    regs_dec<Cfg::kRegsRest>();
+    regs_dec<Cfg::kRegsMma>();
     bool ok = true;
-    int q = 0;   // blocks so far
+    int q = 0, st = 0, sp = 0, phase = 0;   // blocks so far; stages of this block and of the one before
     // warp-wide reductions leave their result in uniform registers
     const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
-    const uint64_t q_desc = tc::sdesc_k128(tc::smem_u32(sQ)), kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
-    int seg = 0;
-    for (long long u = u0; u < u1 && ok; ++seg) {
+    const uint64_t kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
+    int seg = 0, left = __reduce_max_sync(0xffffffffu, (int)(u1 - u0));   // blocks to come
+    for (long long u = u0; left > 0 && ok; ++seg) {
       const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = __reduce_max_sync(0xffffffffu, (int)min((long long)(g.count - g.step), u1 - u));
+      const int n = __reduce_max_sync(0xffffffffu, min(g.count - g.step, left));
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&qfull, seg & 1, abortp, stt));
-      // S of block i, then P V of block i - 1: the softmax of i runs beside the products of its neighbours
+      // for each tile P V of block i - 1, then S of block i in its place: the softmax of one tile runs beside the
+      // other's products
       for (int i = 0; i <= n && ok; ++i) {
-        if (i < n) {
-          const int st = q % kStages;
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&kfull[st], (q / kStages) & 1, abortp, stt));
+        if (i < n) ok = tc::mbar_wait(&full[st], phase, abortp, stt);
+#pragma unroll
+        for (int t = 0; t < kT; ++t) {
+          if (i > 0) ok = ok && tc::mbar_wait(&pfull[t], (q - 1) & 1, abortp, stt);
+          ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc::fence_after_sync();
-#pragma unroll
-          for (int t = 0; t < kT; ++t) {
-            mma_qk(tm + 256 * t + (q & 1) * 64, q_desc + t * (2 * kHalf >> 4), kv_desc + st * (kStageBytes >> 4),
-                   idesc_f16(64));
-            commit_elected(&sfull[t][q & 1]);
-          }
-          commit_elected(&kempty[st]);
-        }
-        if (i > 0) {
-          const int p = q - 1, st = p % kStages;
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&vfull[st], (p / kStages) & 1, abortp, stt));
-          if (!ok) break;
-#pragma unroll
-          for (int t = 0; t < kT; ++t) {
-            ok = __all_sync(0xffffffffu, ok && tc::mbar_wait(&pfull[t][p & 1], (p >> 1) & 1, abortp, stt));
-            if (!ok) break;
-            tc::fence_after_sync();
-            mma_pv(tm + 256 * t + 128, tm + 256 * t + (p & 1) * 64, kv_desc + ((st * kStageBytes + 2 * kKTile) >> 4),
+          if (i > 0)
+            mma_pv(tm + 256 * t + 128, tm + 256 * t + 64, kv_desc + ((sp * kStageBytes + 2 * kKTile) >> 4),
                    idesc_f16(128), (i - 1) % kFlush != 0);
-            commit_elected(&odone[t][p & 1]);
+          if (i < n) {
+            mma_qk(tm + 256 * t + 64, tm + 256 * t, kv_desc + (st * kStageBytes >> 4), idesc_f16(64));
+            commit_elected(&sfull[t]);
+          } else {
+            commit_elected(&odone[t]);
           }
-          if (!ok) break;
-          commit_elected(&vempty[st]);
         }
-        if (i < n) ++q;
+        if (!ok) break;
+        if (i > 0) commit_elected(&empty[sp]);
+        if (i < n) {
+          sp = st;
+          if (++st == kStages) {
+            st = 0;
+            phase ^= 1;
+          }
+          ++q;
+        }
       }
+      left -= n;
       u += n;
     }
     __syncwarp();
@@ -382,58 +431,49 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     __syncwarp();
   } else if (warp >= kSoft) {
     // ------------------------------------------------------------ converters
-    regs_dec<Cfg::kRegsRest>();
-    const int cw = warp - kSoft, ct = tid - kSoft * 32;
-    // K: eight lanes a row, 16 dims each.  V: keys 8 ko .. 8 ko + 7, dims 8 dg .. 8 dg + 7 (eight lanes with
-    // different ko write one dim's chunks: no bank conflicts)
-    const int kc = lane & 7, kr = cw * 16 + (lane >> 3);
+    regs_dec<Cfg::kRegsConv>();
+    const int cw = warp - kSoft;
+    // K: 16 dims of a row; eight lanes write alternate chunks of half a row and of the next row's.  V: keys 8 ko ..
+    // 8 ko + 7, dims 8 dg .. 8 dg + 7; eight lanes write one dim's chunks.  Neither meets bank conflicts.
+    const int kc = (lane & 3) + 4 * (lane >> 4), kr = cw * 16 + ((lane >> 2) & 3);
     const int ko = lane & 7, dg = (lane >> 3) + 4 * cw;
     bool ok = true;
     int it = 0;
     for (long long u = u0; u < u1 && ok;) {
       const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = (int)min((long long)(g.count - g.step), u1 - u), len = cache_len(c, g.s);
+      const int n = (int)min((long long)(g.count - g.step), u1 - u);
+      // loads run ahead by one block (blocks lie within the capacity: `count` does)
+      const uint8_t* Kh = c.K + (g.sh * c.cap + (long long)g.step * kCB + kr) * 128 + kc * 16;
+      const uint8_t* Vh = c.V + (g.sh * c.cap + (long long)g.step * kCB + ko * 8) * 128 + dg * 8;
+      uint4 rk[4];
+      uint2 rv[8];
+      auto load_k = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rk[j] = __ldg((const uint4*)(Kh + (long long)i * (kCB * 128) + 4 * j * 128));
+      };
+      auto load_v = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rv[j] = __ldg((const uint2*)(Vh + (long long)i * (kCB * 128) + j * 128));
+      };
+      load_k(0);
+      load_v(0);
       for (int i = 0; i < n && ok; ++i) {
-        const int q = it + i, st = q % kStages, b = g.step + i;
+        const int q = it + i, st = q % kStages;
         unsigned char* Ks = sKV + st * kStageBytes;
         unsigned char* Vs = Ks + 2 * kKTile;
-        // in flight while the stage is waited for (b lies within the capacity: `count` does)
-        const long long at = g.sh * c.cap + (long long)b * kCB;
-        uint4 rk[4];
-        uint2 rv[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) rk[j] = __ldg((const uint4*)(c.K + (at + kr + 4 * j) * 128 + kc * 16));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) rv[j] = __ldg((const uint2*)(c.V + (at + ko * 8 + j) * 128 + dg * 8));
-        if (q >= kStages) ok = tc::mbar_wait(&kempty[st], ((q / kStages) - 1) & 1, abortp, stt);
+        if (q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int r = kr + 4 * j;
-          const uint4 x = make_uint4(codes_f16<0>(rk[j].x), codes_f16<1>(rk[j].x), codes_f16<0>(rk[j].y),
-                                     codes_f16<1>(rk[j].y));
-          const uint4 y = make_uint4(codes_f16<0>(rk[j].z), codes_f16<1>(rk[j].z), codes_f16<0>(rk[j].w),
-                                     codes_f16<1>(rk[j].w));
           unsigned char* row = Ks + (kc >> 2) * kKTile + r * 128;
-          // the two chunks in an order that keeps the eight lanes of a row on different banks
-          const int q0 = (kc & 3) * 2 + (kc >> 2), q1 = (kc & 3) * 2 + 1 - (kc >> 2);
-          *(uint4*)(row + ((q0 ^ (r & 7)) << 4)) = (kc >> 2) ? y : x;
-          *(uint4*)(row + ((q1 ^ (r & 7)) << 4)) = (kc >> 2) ? x : y;
+          *(uint4*)(row + ((((kc & 3) * 2) ^ (r & 7)) << 4)) =
+              make_uint4(codes_f16<0>(rk[j].x), codes_f16<1>(rk[j].x), codes_f16<0>(rk[j].y), codes_f16<1>(rk[j].y));
+          *(uint4*)(row + ((((kc & 3) * 2 + 1) ^ (r & 7)) << 4)) =
+              make_uint4(codes_f16<0>(rk[j].z), codes_f16<1>(rk[j].z), codes_f16<0>(rk[j].w), codes_f16<1>(rk[j].w));
         }
-        if (ct == 0) {
-          float ks = 1.f, vs = 1.f;   // of a block that holds nothing: its keys are masked
-          if (b * kCB < len) {
-            ks = c.k_scale[g.sh * d.nblk + b];
-            vs = c.v_scale[g.sh * d.nblk + b];
-          }
-          meta[q % (2 * kStages)] = Meta{ks, log2f(vs), kVsUnit / vs};
-        }
-        tc::fence_proxy_async_smem();
-        tc::mbar_arrive(&kfull[st]);
-        if (q >= kStages) ok = tc::mbar_wait(&vempty[st], ((q / kStages) - 1) & 1, abortp, stt);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
+        if (i + 1 < n) load_k(i + 1);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {   // dims 8 dg + 4 w ..
           uint32_t f[4][4];             // [dim][key pair]
@@ -452,98 +492,133 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             *(uint4*)(Vs + dim * 128 + ((ko ^ (dim & 7)) << 4)) = make_uint4(f[e][0], f[e][1], f[e][2], f[e][3]);
           }
         }
+        if (i + 1 < n) load_v(i + 1);
         tc::fence_proxy_async_smem();
-        tc::mbar_arrive(&vfull[st]);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&full[st]);
       }
       it += n;
       u += n;
     }
   } else {
     // --------------------------------------------------------------- softmax
+    // a warp has 16 rows of its tile: lane l rows l / 4 and l / 4 + 8 of them, two columns of eight
     regs_inc<Cfg::kRegsSoft>();
-    const int t = warp >> 2, row_t = (warp & 3) * 32 + lane;   // this thread's row of its tile
-    const uint32_t Sb = tmem + 256 * t + ((uint32_t)(warp & 3) * 32 << 16), Ot = Sb + 128;
+    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;   // (a warp reaches the lanes of its quarter)
+    const int r_warp = quarter * 32 + half * 16, cl = 2 * (lane & 3);
+    const uint32_t S = tmem + 256 * t + 64 + ((uint32_t)r_warp << 16), Ot = S + 64;
     const int nrows = d.n_pos * d.G;
+    auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
     bool ok = true;
-    int it = 0;
-    for (long long u = u0; u < u1;) {
+    int it = 0, seg = 0;
+    for (long long u = u0; u < u1; ++seg) {
       const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
-      const int row = g.tile * kRows + t * 128 + row_t, pos = row / d.G, gq = row - pos * d.G;
-      const int h = (int)(g.sh - (long long)g.s * d.H);
-      const bool mine = row < nrows;
-      const int see = mine ? visible_tokens(cache_len(c, g.s), d.n_pos, pos, d.causal) : 0;
-      float fac;   // of this row's products, in powers of two without biases, of e with them
-      {            // the query row as f16, scaled by a power of two
-        uint4 v[16];
+      const int row0 = g.tile * kRows + t * 128, h = (int)(g.sh - (long long)g.s * d.H), len = cache_len(c, g.s);
+      {   // the queries as f16, each row scaled by a power of two, into TMEM: here a lane is a row, and has 64 dims
+        const int r = quarter * 32 + lane, row = row0 + r, pos = row / d.G, gq = row - pos * d.G;
+        uint4 x[8];
         float amax = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          v[e] = make_uint4(0u, 0u, 0u, 0u);
-          if (mine) v[e] = __ldg((const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128) + e);
+        for (int e = 0; e < 8; ++e) {
+          x[e] = make_uint4(0u, 0u, 0u, 0u);
+          if (row < nrows)
+            x[e] = __ldg((const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128 + half * 64) + e);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const __nv_bfloat162* y = (const __nv_bfloat162*)&v[e];
+        for (int e = 0; e < 8; ++e) {
+          const __nv_bfloat162* y = (const __nv_bfloat162*)&x[e];
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const float2 z = __bfloat1622float2(y[f]);
+          for (int k = 0; k < 4; ++k) {
+            const float2 z = __bfloat1622float2(y[k]);
             amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
           }
         }
+        s_row[t][half][r] = amax;
+        tile_sync();
+        amax = fmaxf(amax, s_row[t][half ^ 1][r]);
+        tile_sync();
         const int ex = max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100);
         const float up = __uint_as_float((unsigned)(14 - ex + 127) << 23);
-        fac = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
+        if (half == 0) s_row[t][0][r] = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
+        uint32_t w[32];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const __nv_bfloat162* y = (const __nv_bfloat162*)&v[e];
-          __half2 z[4];
+        for (int e = 0; e < 8; ++e) {
+          const __nv_bfloat162* y = (const __nv_bfloat162*)&x[e];
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const float2 a = __bfloat1622float2(y[f]);
-            z[f] = __floats2half2_rn(a.x * up, a.y * up);
+          for (int k = 0; k < 4; ++k) {
+            const float2 a = __bfloat1622float2(y[k]);
+            const __half2 z = __floats2half2_rn(a.x * up, a.y * up);
+            w[4 * e + k] = *(const uint32_t*)&z;
           }
-          *(uint4*)(sQ + (t * 2 + (e >> 3)) * kHalf + row_t * 128 + (((e & 7) ^ (row_t & 7)) << 4)) =
-              *(const uint4*)&z[0];
         }
-        tc::fence_proxy_async_smem();
-        tc::mbar_arrive(&qfull);
+        tmem_st32(tmem + 256 * t + half * 32 + ((uint32_t)quarter * 32 << 16), w);
+        tmem_wait_st();
+        tc::fence_before_sync();
+        tile_sync();   // the rows' factors are there
+        if (lane == 0) tc::mbar_arrive(&qfull);
       }
-      // this row's sums in memory, [dims / 4][row][4]
-      const long long row_at = (long long)(t * 128 + row_t) * 4;
-      float* sums = parts + 2ll * kCacheMaxCtas * Cfg::kSlot + (long long)blockIdx.x * kRows * 128 + row_at;
-      float bref = -INFINITY, brefv = 0.f;          // reference of the flushed sums
-      float ref = -INFINITY, refv = 0.f, l = 0.f;   // with biases ref is the logit and refv the log2 vs that came with it
+      // products' factors (powers of two without biases, of e with them) and sight of this thread's two rows
+      float fac[2];
+      int see[2], pos[2], gq[2];
+      bool mine[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = r_warp + (lane >> 2) + 8 * i, row = row0 + r;
+        fac[i] = s_row[t][0][r];
+        pos[i] = row / d.G;
+        gq[i] = row - pos[i] * d.G;
+        mine[i] = row < nrows;
+        see[i] = mine[i] ? visible_tokens(len, d.n_pos, pos[i], d.causal) : 0;
+      }
+      const int see_min = __reduce_min_sync(0xffffffffu, min(see[0], see[1]));
+      // this thread's sums in memory, 16 bytes of all threads together
+      float* sums = parts + 2ll * kCacheMaxCtas * Cfg::kSlot + (long long)blockIdx.x * 64 * Cfg::kSoftThreads + tid * 4;
+      // references of the flushed sums and of O (with biases the logit, and the log2 vs that came with it), sums of weights
+      float bref[2] = {-INFINITY, -INFINITY}, brefv[2] = {0.f, 0.f}, ref[2] = {-INFINITY, -INFINITY};
+      float refv[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
       const float* bias = kBias ? c.bias + g.sh * c.cap : nullptr;
       for (int i = 0; i < n; ++i) {
-        const int q = it + i, j0 = (g.step + i) * kCB;
-        const uint32_t S = Sb + (q & 1) * 64;
-        // S is in, and with it the block's scales (written before kfull, which the MMA warp waited for)
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q & 1], (q >> 1) & 1, abortp, stt));
+        const int q = it + i, j0 = (g.step + i) * kCB + cl;
+        // S is in; so are the product of the block before (issued earlier by the same thread) and the block's scales
+        // (written before `full`, which the MMA warp waited for)
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t], q & 1, abortp, stt));
         if (!ok) break;
         tc::fence_after_sync();
         if (i > 0 && i % kFlush == 0) {
-          // O goes to this row's sums in memory and starts again at zero (see above)
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(q - 1) & 1], ((q - 1) >> 1) & 1, abortp, stt));
-          if (!ok) break;
-          tc::fence_after_sync();
-          const float dd = kBias ? fmaf(ref - bref, kLog2e, refv - brefv) : ref - bref;   // unused while there are none
-          const bool none = bref == -INFINITY, far = !none && dd > kFar;
-          const float up = none || far ? 1.f : ex2_approx(dd), down = far ? ex2_approx(-dd) : 1.f;
-          const bool redo = __any_sync(0xffffffffu, none || far);
+          // O goes to the sums in memory and starts again at zero (see above)
+          float up[2], down[2];
+          bool redo = false;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float dd = kBias ? fmaf(ref[k] - bref[k], kLog2e, refv[k] - brefv[k]) : ref[k] - bref[k];
+            const bool none = bref[k] == -INFINITY, far = !none && dd > kFar;
+            up[k] = none || far ? 1.f : ex2_approx(dd);
+            down[k] = none ? 0.f : far ? ex2_approx(-dd) : 1.f;
+            if (none || far) {
+              redo = true;
+              bref[k] = ref[k];
+              brefv[k] = refv[k];
+            }
+          }
+          redo = __any_sync(0xffffffffu, redo);
 #pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
-            float o[32];
-            tc::tmem_ld32(Ot + ch * 32, o);
+            float o[16];
+            tmem_ld_rows32(Ot + ch * 32, o);
+            tmem_wait_ld();
+            settle(o);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float* b = sums + (long long)(ch * 8 + e) * kRows * 4;
-              const float4 x = make_float4(o[4 * e] * up, o[4 * e + 1] * up, o[4 * e + 2] * up, o[4 * e + 3] * up);
+            for (int e = 0; e < 4; ++e) {
+              float* b = sums + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4;
+              float4 x = make_float4(o[4 * e] * up[0], o[4 * e + 1] * up[0], o[4 * e + 2] * up[1], o[4 * e + 3] * up[1]);
               if (redo) {
-                float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!none) old = __ldcg((const float4*)b);
-                __stcg((float4*)b, make_float4(fmaf(old.x, down, x.x), fmaf(old.y, down, x.y), fmaf(old.z, down, x.z),
-                                               fmaf(old.w, down, x.w)));
+                if (i > kFlush) {
+                  const float4 old = __ldcg((const float4*)b);
+                  x = make_float4(fmaf(old.x, down[0], x.x), fmaf(old.y, down[0], x.y), fmaf(old.z, down[1], x.z),
+                                  fmaf(old.w, down[1], x.w));
+                }
+                __stcg((float4*)b, x);
               } else {
                 asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(b), "f"(x.x), "f"(x.y),
                              "f"(x.z), "f"(x.w)
@@ -551,199 +626,223 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
               }
             }
           }
-          if (none || far) {
-            bref = ref;
-            brefv = refv;
-          }
         }
-        float v[64];
-        tmem_ld32_async(S, v);
-        tmem_ld32_async(S + 32, v + 32);
+        float v[32];
+        tmem_ld_rows64(S, v);
         const Meta m = meta[q % (2 * kStages)];
-        const float f = fac * m.ks;
+        const float f[2] = {fac[0] * m.ks, fac[1] * m.ks};
         tmem_wait_ld();
-        settle32(v);
-        settle32(v + 32);
-        const int lim = see - j0;   // keys of the block that the row sees
-        if (kBias) {   // logits; biases are read four at a time where the row sees something, within the capacity
+        settle(v);
+        const bool edge = j0 - cl + kCB > see_min;
+        if (kBias) {   // logits; biases are read in pairs where a row sees something, within the capacity
 #pragma unroll
-          for (int e = 0; e < kCB; e += 4) {
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (e < lim) x = __ldg((const float4*)(bias + j0 + e));
-            v[e] = fmaf(v[e], f, x.x);
-            v[e + 1] = fmaf(v[e + 1], f, x.y);
-            v[e + 2] = fmaf(v[e + 2], f, x.z);
-            v[e + 3] = fmaf(v[e + 3], f, x.w);
+          for (int j = 0; j < 8; ++j) {
+            float2 x = make_float2(0.f, 0.f);
+            if (j0 + 8 * j < max(see[0], see[1])) x = __ldg((const float2*)(bias + j0 + 8 * j));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              v[4 * j + 2 * k] = fmaf(v[4 * j + 2 * k], f[k], x.x);
+              v[4 * j + 2 * k + 1] = fmaf(v[4 * j + 2 * k + 1], f[k], x.y);
+            }
           }
         }
-        if (__any_sync(0xffffffffu, lim < kCB)) {
+        if (edge) {
 #pragma unroll
-          for (int e = 0; e < kCB; ++e)
-            if (e >= lim) v[e] = -INFINITY;
-        }
-        float top = v[0], b = v[1], aa = v[2], bb = v[3];
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 4; e < kCB; e += 4) {
-          top = fmaxf(top, v[e]);
-          b = fmaxf(b, v[e + 1]);
-          aa = fmaxf(aa, v[e + 2]);
-          bb = fmaxf(bb, v[e + 3]);
+            for (int k = 0; k < 4; ++k)
+              if (j0 + 8 * j + (k & 1) >= see[k >> 1]) v[4 * j + k] = -INFINITY;
         }
-        top = fmaxf(fmaxf(top, b), fmaxf(aa, bb));
-        float alpha = 1.f;
-        bool grow;
-        if (kBias) {
-          // in units of log2: (x - ref) log2 e + lv - refv; differences of logits first, so that the type's lowest
-          // value cancels against itself
-          grow = top != -INFINITY && (ref == -INFINITY || fmaf(top - ref, kLog2e, m.lv - refv) > kGrow);
-          if (grow) {
-            alpha = ref == -INFINITY ? 0.f : ex2_approx(fmaf(ref - top, kLog2e, refv - m.lv));
-            ref = top;
-            refv = m.lv;
+        float alpha[2];
+        bool grows = false;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float top = fmaxf(v[2 * k], v[2 * k + 1]), b = fmaxf(v[4 + 2 * k], v[4 + 2 * k + 1]);
+#pragma unroll
+          for (int j = 2; j < 8; j += 2) {
+            top = fmaxf(fmaxf(top, v[4 * j + 2 * k]), v[4 * j + 2 * k + 1]);
+            b = fmaxf(fmaxf(b, v[4 * j + 4 + 2 * k]), v[4 * j + 4 + 2 * k + 1]);
           }
-        } else {
-          top = fmaf(top, f, m.lv);   // f > 0: the largest product is the largest logit
-          grow = top > ref + kGrow || (ref == -INFINITY && top != -INFINITY);
-          if (grow) {
-            alpha = ref == -INFINITY ? 0.f : ex2_approx(ref - top);
-            ref = top;
+          top = fmaxf(top, b);
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          alpha[k] = 1.f;
+          if (kBias) {
+            // in units of log2: (x - ref) log2 e + lv - refv; differences of logits first, so that the type's lowest
+            // value cancels against itself
+            if (top != -INFINITY && (ref[k] == -INFINITY || fmaf(top - ref[k], kLog2e, m.lv - refv[k]) > kGrow)) {
+              alpha[k] = ref[k] == -INFINITY ? 0.f : ex2_approx(fmaf(ref[k] - top, kLog2e, refv[k] - m.lv));
+              ref[k] = top;
+              refv[k] = m.lv;
+              grows = true;
+            }
+          } else {
+            top = fmaf(top, f[k], m.lv);   // f > 0: the largest product is the largest logit
+            if (top > ref[k] + kGrow || (ref[k] == -INFINITY && top != -INFINITY)) {
+              alpha[k] = ref[k] == -INFINITY ? 0.f : ex2_approx(ref[k] - top);
+              ref[k] = top;
+              grows = true;
+            }
           }
         }
-        if (i % kFlush != 0 && __any_sync(0xffffffffu, grow)) {   // scale O once the product of the block before is in
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(q - 1) & 1], ((q - 1) >> 1) & 1, abortp, stt));
-          if (!ok) break;
-          tc::fence_after_sync();
+        if (i % kFlush != 0 && __any_sync(0xffffffffu, grows)) {   // scale O
 #pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
-            float o[32];
-            tc::tmem_ld32(Ot + ch * 32, o);
+            float o[16];
+            tmem_ld_rows32(Ot + ch * 32, o);
+            tmem_wait_ld();
+            settle(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] *= alpha;
-            tmem_st32(Ot + ch * 32, o);
+            for (int e = 0; e < 16; ++e) o[e] *= alpha[(e >> 1) & 1];
+            tmem_st_rows32(Ot + ch * 32, o);
           }
         }
-        const float base = ref == -INFINITY ? 0.f : ref;
-        const float add = (kBias ? m.lv - refv : m.lv - base) + kLift;
-        const float2 add_2 = make_float2(add, add);
-        float2 sum = make_float2(0.f, 0.f);
+        float2 base[2], add[2], sum[2];
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {   // 16 keys: eight columns of hi, eight of lo
+        for (int k = 0; k < 2; ++k) {
+          const float b = ref[k] == -INFINITY ? 0.f : ref[k], a = (kBias ? m.lv - refv[k] : m.lv - b) + kLift;
+          base[k] = make_float2(-b, -b);
+          add[k] = make_float2(a, a);
+          sum[k] = make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch) {   // 32 keys: 16 columns of hi, 16 of lo
           uint32_t hr[8], lr[8];
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            float2 x = make_float2(v[ch * 16 + e], v[ch * 16 + e + 1]);
+          for (int e = 0; e < 8; ++e) {
+            const int k = e & 1, j = ch * 4 + (e >> 1);
+            float2 x = make_float2(v[4 * j + 2 * k], v[4 * j + 2 * k + 1]);
             if (kBias)
-              x = fma2(add2(x, make_float2(-base, -base)), make_float2(kLog2e, kLog2e), add_2);
+              x = fma2(add2(x, base[k]), make_float2(kLog2e, kLog2e), add[k]);
             else
-              x = fma2(x, make_float2(f, f), add_2);
+              x = fma2(x, make_float2(f[k], f[k]), add[k]);
             x.x = ex2_approx(x.x);
             x.y = ex2_approx(x.y);
-            sum = add2(sum, x);
+            sum[k] = add2(sum[k], x);
             // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
             const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
                                           __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
             const float2 lo = add2(x, make_float2(-hi.x, -hi.y));
             const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
-            hr[e >> 1] = *(const uint32_t*)&h2;
-            lr[e >> 1] = *(const uint32_t*)&l2;
+            hr[e] = *(const uint32_t*)&h2;
+            lr[e] = *(const uint32_t*)&l2;
           }
-          tmem_st8(S + (ch >> 1) * 32 + (ch & 1) * 8, hr);
-          tmem_st8(S + (ch >> 1) * 32 + (ch & 1) * 8 + 16, lr);
+          tmem_st_pairs16(S + ch * 32, hr);
+          tmem_st_pairs16(S + ch * 32 + 16, lr);
         }
-        l = fmaf(l, alpha, (sum.x + sum.y) * m.iv);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) l[k] = fmaf(l[k], alpha[k], (sum[k].x + sum[k].y) * m.iv);
         tmem_wait_st();
         tc::fence_before_sync();
-        tc::mbar_arrive(&pfull[t][q & 1]);
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&pfull[t]);
       }
       it += n;
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][(it - 1) & 1], ((it - 1) >> 1) & 1, abortp, stt));
+      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t], seg & 1, abortp, stt));
       tc::fence_after_sync();
       if (tid == 0) stop_flag = *abortp;   // one reading for all
-      asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
+      asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
       if (stop_flag) break;
-      const bool whole = g.step == 0 && n == g.count;
-      const bool flushed = bref != -INFINITY;
-      const float bw = flushed ? ex2_approx(kBias ? fmaf(bref - ref, kLog2e, brefv - refv) : bref - ref) : 0.f;
-      auto store4 = [&](int dim, float4 v, float inv) {
-        v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      const bool whole = g.step == 0 && n == g.count, flushed = n > kFlush;
+      float bw[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+        bw[k] = bref[k] == -INFINITY ? 0.f
+                                     : ex2_approx(kBias ? fmaf(bref[k] - ref[k], kLog2e, brefv[k] - refv[k]) : bref[k] - ref[k]);
+      }
+      // outputs of one 16-byte unit of this thread: columns 8 j + cl, + 1 of its two rows
+      auto store = [&](int j, float4 x, float inv0, float inv1) {
+        x = make_float4(x.x * inv0, x.y * inv0, x.z * inv1, x.w * inv1);
         const float big = 3.402823466e38f;
-        if (!(fabsf(v.x) <= big && fabsf(v.y) <= big && fabsf(v.z) <= big && fabsf(v.w) <= big))
+        float* o = O + g.s * os.s + h * os.h + 8 * j + cl;
+        if (mine[0]) *(float2*)(o + pos[0] * os.i + gq[0] * 128) = make_float2(x.x, x.y);
+        if (mine[1]) *(float2*)(o + pos[1] * os.i + gq[1] * 128) = make_float2(x.z, x.w);
+        if ((mine[0] && !(fabsf(x.x) <= big && fabsf(x.y) <= big)) ||
+            (mine[1] && !(fabsf(x.z) <= big && fabsf(x.w) <= big)))
           set_status(stt, ARCKV_ERR_NONFINITE);
-        *(float4*)(O + g.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
       };
-      const float inv = l == 0.f ? 0.f : kVsUnit / l;
-      // partial results: laid out as `sums`, then (ref, refv, l) of the rows
-      float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot;
+      const float inv0 = l[0] == 0.f ? 0.f : kVsUnit / l[0], inv1 = l[1] == 0.f ? 0.f : kVsUnit / l[1];
+      float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + tid * 4;
 #pragma unroll 1
       for (int ch = 0; ch < 4; ++ch) {
-        float v[32];
-        tc::tmem_ld32(Ot + ch * 32, v);
-        float4 y[8];
+        float v[16];
+        tmem_ld_rows32(Ot + ch * 32, v);
+        float4 y[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
           y[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (flushed) y[e] = __ldcg((const float4*)(sums + (long long)(ch * 8 + e) * kRows * 4));
+          if (flushed) y[e] = __ldcg((const float4*)(sums + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4));
         }
+        tmem_wait_ld();
+        settle(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float4 x = make_float4(fmaf(y[e].x, bw, v[4 * e]), fmaf(y[e].y, bw, v[4 * e + 1]),
-                                       fmaf(y[e].z, bw, v[4 * e + 2]), fmaf(y[e].w, bw, v[4 * e + 3]));
-          if (!whole) __stcg((float4*)(slot + row_at + (long long)(ch * 8 + e) * kRows * 4), x);
-          else if (mine) store4(ch * 32 + 4 * e, x, inv);
+        for (int e = 0; e < 4; ++e) {
+          const float4 x = make_float4(fmaf(y[e].x, bw[0], v[4 * e]), fmaf(y[e].y, bw[0], v[4 * e + 1]),
+                                       fmaf(y[e].z, bw[1], v[4 * e + 2]), fmaf(y[e].w, bw[1], v[4 * e + 3]));
+          if (!whole) __stcg((float4*)(slot + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4), x);
+          else store(ch * 4 + e, x, inv0, inv1);
         }
       }
       tc::fence_before_sync();
       if (!whole) {
-        __stcg((float4*)(slot + 128 * kRows + row_at), make_float4(ref, refv, l, 0.f));
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          __stcg((float4*)(slot + (long long)(16 + k) * Cfg::kSoftThreads * 4), make_float4(ref[k], refv[k], l[k], 0.f));
         const int c_first = sh.owner(g.first), c_last = sh.owner(g.first + g.count - 1);
         __threadfence();
-        asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
+        asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
         if (tid == 0) {
           last_flag = atomicAdd(&tickets[c_first], 1) == c_last - c_first;
           if (last_flag) tickets[c_first] = 0;
           __threadfence();
         }
-        asm volatile("bar.sync 1, %0;" ::"r"(kRows) : "memory");
-        if (last_flag && mine) {
-          // the parts in CTA order, with a running reference; 32 dims at a time
+        asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
+        if (last_flag) {
+          // the parts in CTA order, with a running reference; 32 columns at a time
 #pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
-            float top = -INFINITY, topv = 0.f, z = 0.f;
-            float4 a[8];
+            float top[2] = {-INFINITY, -INFINITY}, topv[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
+            float4 a[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int e = 0; e < 4; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
             for (int cc = c_first; cc <= c_last; ++cc) {
-              const float* p = parts + (2ll * cc + (cc == c_first)) * Cfg::kSlot + row_at;
-              const float4 st4 = __ldcg((const float4*)(p + 128 * kRows));
-              float4 x[8];
+              const float* p = parts + (2ll * cc + (cc == c_first)) * Cfg::kSlot + tid * 4;
+              float4 st4[2], x[4];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = __ldcg((const float4*)(p + (long long)(ch * 8 + e) * kRows * 4));
-              if (st4.x == -INFINITY) continue;   // a part that saw nothing
-              float w = 1.f, down = 0.f;          // of the new part, of the sums
-              if (top == -INFINITY) {
-                top = st4.x;
-                topv = st4.y;
-              } else {
-                const float up = kBias ? fmaf(st4.x - top, kLog2e, st4.y - topv) : st4.x - top;
+              for (int k = 0; k < 2; ++k) st4[k] = __ldcg((const float4*)(p + (long long)(16 + k) * Cfg::kSoftThreads * 4));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                x[e] = __ldcg((const float4*)(p + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4));
+              float w[2], down[2];   // of the new part, of the sums
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                w[k] = 0.f;
+                down[k] = 1.f;
+                if (st4[k].x == -INFINITY) continue;   // a part that saw nothing
+                const float up = top[k] == -INFINITY ? 1.f
+                                 : kBias             ? fmaf(st4[k].x - top[k], kLog2e, st4[k].y - topv[k])
+                                                     : st4[k].x - top[k];
                 if (up > 0.f) {
-                  down = ex2_approx(-up);
-                  top = st4.x;
-                  topv = st4.y;
+                  w[k] = 1.f;
+                  down[k] = top[k] == -INFINITY ? 0.f : ex2_approx(-up);
+                  top[k] = st4[k].x;
+                  topv[k] = st4[k].y;
                 } else {
-                  down = 1.f;
-                  w = ex2_approx(up);
+                  w[k] = ex2_approx(up);
                 }
+                z[k] = fmaf(z[k], down[k], st4[k].z * w[k]);
               }
-              z = fmaf(z, down, st4.z * w);
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                a[e] = make_float4(fmaf(a[e].x, down, x[e].x * w), fmaf(a[e].y, down, x[e].y * w),
-                                   fmaf(a[e].z, down, x[e].z * w), fmaf(a[e].w, down, x[e].w * w));
+              for (int e = 0; e < 4; ++e)
+                a[e] = make_float4(fmaf(a[e].x, down[0], x[e].x * w[0]), fmaf(a[e].y, down[0], x[e].y * w[0]),
+                                   fmaf(a[e].z, down[1], x[e].z * w[1]), fmaf(a[e].w, down[1], x[e].w * w[1]));
             }
-            const float zinv = z == 0.f ? 0.f : kVsUnit / z;
+            const float i0 = z[0] == 0.f ? 0.f : kVsUnit / z[0], i1 = z[1] == 0.f ? 0.f : kVsUnit / z[1];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) store4(ch * 32 + 4 * e, a[e], zinv);
+            for (int e = 0; e < 4; ++e) store(ch * 4 + e, a[e], i0, i1);
           }
         }
       }
@@ -782,7 +881,7 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
 
 size_t cache_tiles_scratch(long long rows) {
   const size_t slot = rows <= 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot;
-  return kCacheMaxCtas * (2 * slot + (rows <= 128 ? TileCfg<1>::kRows : TileCfg<2>::kRows) * 128) * sizeof(float);
+  return kCacheMaxCtas * (2 * slot + 64 * (rows <= 128 ? TileCfg<1>::kSoftThreads : TileCfg<2>::kSoftThreads)) * sizeof(float);
 }
 
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
