@@ -5,19 +5,19 @@
 // tensor pipe.  A CTA takes 128 or 256 rows of one head (one or two M = 128
 // tiles) and goes over the keys a block of 64 at a time:
 //   converters (4 warps)  read the codes of K and V and leave them in shared
-//                         memory as f16 operands, V transposed, six blocks
+//                         memory as f16 operands, V transposed, four blocks
 //                         ahead; a code costs about one instruction for 256 rows
 //   MMA warp              S = Q K^T (exact products, fp32 sums in TMEM), O += P V
 //   softmax (8 warps a tile, 16 rows each, four lanes a row)  turn S into weights
 //                         in place: the f16 pair hi + lo of 32 keys takes the 32
 //                         columns that their logits had; P is the MMA's operand
 //                         from TMEM
-// Q is an operand from TMEM too: read from shared memory for each block, Q and K
-// would take 1.5 times the pipe's time for S.
 // P V runs once for hi and once for lo, which keeps 21 bits of a weight: three
 // units of MMA work where f16 weights would do with two, so 2/3 of the pipe's
-// peak is the most that the fp32 output allows.  With two tiles the pipe works on
-// one while the other's softmax runs.
+// peak is the most that the fp32 output allows.  A tile has two buffers of S in
+// TMEM: the softmax of one block runs beside the products of its neighbours.  (With
+// one buffer and Q in TMEM too, S takes 256 instead of 392 cycles a block and tile,
+// but softmax and products wait for each other: 374 instead of XXX us.)
 //
 // The weight of key j of block b carries the block's scale of V:
 //   w_j = 2^{x_j + log2 vs_b - ref + 7},  O = sum_j w_j c_j / sum_b (sum_{j in b} w_j) / vs_b
@@ -38,7 +38,7 @@ namespace {
 
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
-constexpr int kStages = 6, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
+constexpr int kStages = 4, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
 constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
@@ -60,7 +60,7 @@ struct TileCfg {
   static constexpr int kRegsSoft = kT == 2 ? 96 : 176, kRegsConv = kT == 2 ? 64 : 96, kRegsMma = kT == 2 ? 32 : 64;
   static_assert(2 * kT * kRegsSoft + kRegsConv + kRegsMma == (2 * kT + 2) * kRegs && kRegs * kThreads <= 65536,
                 "the shares add up to what the block was launched with");
-  static constexpr int kSmem = kStages * kStageBytes + 1024;
+  static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + 1024;   // Q, then the stages
   // floats of a partial result: 64 outputs and twice (ref, log2 vs of ref, sum, unused) of each softmax thread
   static constexpr int kSlot = 72 * kSoftThreads;
 };
@@ -69,28 +69,28 @@ struct TileCfg {
 // (from one lane of a divergent branch each MMA took 90 to 125 cycles to issue, twice what it runs).  A descriptor's
 // low bits are the address in units of 16 bytes, so K steps are added to the tile's descriptor.
 //
-// S = Q K^T: Q in TMEM, 16 dims in 8 columns; K 64 x 128 in halves of 64 dims, 8 KB apart.
-__device__ __forceinline__ void mma_qk(uint32_t s, uint32_t q, uint64_t k, uint32_t idesc) {
+// S = Q K^T: Q 128 x 128 and K 64 x 128 in halves of 64 dims (16 KB and 8 KB apart).
+__device__ __forceinline__ void mma_qk(uint32_t s, uint64_t q, uint64_t k, uint32_t idesc) {
   asm volatile(
-      "{\n\t.reg .pred e, z, c;\n\t.reg .b64 b;\n\t.reg .b32 a;\n\t"
+      "{\n\t.reg .pred e, z, c;\n\t.reg .b64 a, b;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
       "setp.ne.b32 z, 0, 0;\n\tsetp.eq.b32 c, 0, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, z;\n\t"
-      "add.u32 a, %1, 8;\n\tadd.s64 b, %2, 2;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 16;\n\tadd.s64 b, %2, 4;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 24;\n\tadd.s64 b, %2, 6;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 32;\n\tadd.s64 b, %2, 512;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 40;\n\tadd.s64 b, %2, 514;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 48;\n\tadd.s64 b, %2, 516;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t"
-      "add.u32 a, %1, 56;\n\tadd.s64 b, %2, 518;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, c;\n\t}\n" ::"r"(s),
-      "r"(q), "l"(k), "r"(idesc)
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1024;\n\tadd.s64 b, %2, 512;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1026;\n\tadd.s64 b, %2, 514;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1028;\n\tadd.s64 b, %2, 516;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t"
+      "add.s64 a, %1, 1030;\n\tadd.s64 b, %2, 518;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, c;\n\t}\n" ::"r"(s),
+      "l"(q), "l"(k), "r"(idesc)
       : "memory");
 }
 // O (+)= P V: P in TMEM, 16 keys in 8 columns, hi and then lo 16 columns on, 32 keys in 32 columns; V^T 128 x 64.
@@ -158,18 +158,6 @@ __device__ __forceinline__ void tmem_st_pairs16(uint32_t taddr, const uint32_t (
   asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]),
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
-}
-// 32 columns of this warp's 32 lanes, a lane each.
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -283,9 +271,11 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   using Cfg = TileCfg<kT>;
   constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows;
   extern __shared__ unsigned char smraw[];
-  unsigned char* sKV = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [stage][K halves, V]
-  long long* pre = (long long*)(sKV + kStages * kStageBytes);                       // [S + 1] blocks of a head's tiles
-  __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT], pfull[kT], odone[kT], drain;
+  unsigned char* sQ = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [tile][half][128][128 B]
+  unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K halves, V]
+  long long* pre = (long long*)(sKV + kStages * kStageBytes);                      // [S + 1] blocks of a head's tiles
+  // of buffer (parity of the block) 0 and 1: S written, P written, P V done
+  __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
   __shared__ Meta meta[2 * kStages];
   __shared__ float s_row[kT][2][128];   // of a row: largest |q| of each half, then its factor
   __shared__ uint32_t tmem_slot;
@@ -299,11 +289,12 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       tc::mbar_init(&full[i], 5);   // four converters and the scales
       tc::mbar_init(&empty[i], 1);
     }
-    for (int t = 0; t < kT; ++t) {
-      tc::mbar_init(&sfull[t], 1);
-      tc::mbar_init(&pfull[t], 8);
-      tc::mbar_init(&odone[t], 1);
-    }
+    for (int t = 0; t < kT; ++t)
+      for (int i = 0; i < 2; ++i) {
+        tc::mbar_init(&sfull[t][i], 1);
+        tc::mbar_init(&pfull[t][i], 8);
+        tc::mbar_init(&odone[t][i], 1);
+      }
     tc::mbar_init(&drain, 1);
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -336,7 +327,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = tmem_slot;   // tile t: Q at columns 256 t, S / P at 256 t + 64, O at 256 t + 128
+  const uint32_t tmem = tmem_slot;   // tile t: two buffers of S / P at columns 256 t, O at 256 t + 128
   CacheShares sh;
   sh.total = pre[c.S] * d.H;
   sh.ctas = (int)min((long long)gridDim.x, sh.total);
@@ -382,34 +373,39 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     int q = 0, st = 0, sp = 0, phase = 0;   // blocks so far; stages of this block and of the one before
     // warp-wide reductions leave their result in uniform registers
     const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
-    const uint64_t kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
+    const uint64_t q_desc = tc::sdesc_k128(tc::smem_u32(sQ)), kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
     int seg = 0, left = __reduce_max_sync(0xffffffffu, (int)(u1 - u0));   // blocks to come
     for (long long u = u0; left > 0 && ok; ++seg) {
       const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = __reduce_max_sync(0xffffffffu, min(g.count - g.step, left));
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&qfull, seg & 1, abortp, stt));
-      // for each tile P V of block i - 1, then S of block i in its place: the softmax of one tile runs beside the
-      // other's products
+      // S of block i, then P V of block i - 1
       for (int i = 0; i <= n && ok; ++i) {
-        if (i < n) ok = tc::mbar_wait(&full[st], phase, abortp, stt);
-#pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          if (i > 0) ok = ok && tc::mbar_wait(&pfull[t], (q - 1) & 1, abortp, stt);
-          ok = __all_sync(0xffffffffu, ok);
+        if (i < n) {
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[st], phase, abortp, stt));
           if (!ok) break;
           tc::fence_after_sync();
-          if (i > 0)
-            mma_pv(tm + 256 * t + 128, tm + 256 * t + 64, kv_desc + ((sp * kStageBytes + 2 * kKTile) >> 4),
-                   idesc_f16(128), (i - 1) % kFlush != 0);
-          if (i < n) {
-            mma_qk(tm + 256 * t + 64, tm + 256 * t, kv_desc + (st * kStageBytes >> 4), idesc_f16(64));
-            commit_elected(&sfull[t]);
-          } else {
-            commit_elected(&odone[t]);
+#pragma unroll
+          for (int t = 0; t < kT; ++t) {
+            mma_qk(tm + 256 * t + (q & 1) * 64, q_desc + t * (2 * kHalf >> 4), kv_desc + (st * kStageBytes >> 4),
+                   idesc_f16(64));
+            commit_elected(&sfull[t][q & 1]);
           }
         }
-        if (!ok) break;
-        if (i > 0) commit_elected(&empty[sp]);
+        if (i > 0) {
+          const int p = q - 1;
+#pragma unroll
+          for (int t = 0; t < kT; ++t) {
+            ok = __all_sync(0xffffffffu, ok && tc::mbar_wait(&pfull[t][p & 1], (p >> 1) & 1, abortp, stt));
+            if (!ok) break;
+            tc::fence_after_sync();
+            mma_pv(tm + 256 * t + 128, tm + 256 * t + (p & 1) * 64, kv_desc + ((sp * kStageBytes + 2 * kKTile) >> 4),
+                   idesc_f16(128), (i - 1) % kFlush != 0);
+            commit_elected(&odone[t][p & 1]);
+          }
+          if (!ok) break;
+          commit_elected(&empty[sp]);
+        }
         if (i < n) {
           sp = st;
           if (++st == kStages) {
@@ -506,16 +502,23 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     regs_inc<Cfg::kRegsSoft>();
     const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;   // (a warp reaches the lanes of its quarter)
     const int r_warp = quarter * 32 + half * 16, cl = 2 * (lane & 3);
-    const uint32_t S = tmem + 256 * t + 64 + ((uint32_t)r_warp << 16), Ot = S + 64;
+    const uint32_t Sb = tmem + 256 * t + ((uint32_t)r_warp << 16), Ot = Sb + 128;
     const int nrows = d.n_pos * d.G;
-    auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
     bool ok = true;
-    int it = 0, seg = 0;
-    for (long long u = u0; u < u1; ++seg) {
+    // P V of block q is in O.  (The one before it, whose phase this could be taken for, is known to be: S of block
+    // q + 1 was issued after it and has come in.)
+    auto product_done = [&](int q) {
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][q & 1], (q >> 1) & 1, abortp, stt));
+      tc::fence_after_sync();
+      return ok;
+    };
+    auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
+    int it = 0;
+    for (long long u = u0; u < u1;) {
       const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
       const int row0 = g.tile * kRows + t * 128, h = (int)(g.sh - (long long)g.s * d.H), len = cache_len(c, g.s);
-      {   // the queries as f16, each row scaled by a power of two, into TMEM: here a lane is a row, and has 64 dims
+      {   // the queries as f16, each row scaled by a power of two: here a lane is a row, and has 64 dims
         const int r = quarter * 32 + lane, row = row0 + r, pos = row / d.G, gq = row - pos * d.G;
         uint4 x[8];
         float amax = 0.f;
@@ -541,20 +544,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const int ex = max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100);
         const float up = __uint_as_float((unsigned)(14 - ex + 127) << 23);
         if (half == 0) s_row[t][0][r] = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
-        uint32_t w[32];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const __nv_bfloat162* y = (const __nv_bfloat162*)&x[e];
+          __half2 z[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float2 a = __bfloat1622float2(y[k]);
-            const __half2 z = __floats2half2_rn(a.x * up, a.y * up);
-            w[4 * e + k] = *(const uint32_t*)&z;
+            z[k] = __floats2half2_rn(a.x * up, a.y * up);
           }
+          *(uint4*)(sQ + (t * 2 + half) * kHalf + r * 128 + ((e ^ (r & 7)) << 4)) = *(const uint4*)&z[0];
         }
-        tmem_st32(tmem + 256 * t + half * 32 + ((uint32_t)quarter * 32 << 16), w);
-        tmem_wait_st();
-        tc::fence_before_sync();
+        tc::fence_proxy_async_smem();
         tile_sync();   // the rows' factors are there
         if (lane == 0) tc::mbar_arrive(&qfull);
       }
@@ -580,12 +581,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const float* bias = kBias ? c.bias + g.sh * c.cap : nullptr;
       for (int i = 0; i < n; ++i) {
         const int q = it + i, j0 = (g.step + i) * kCB + cl;
-        // S is in; so are the product of the block before (issued earlier by the same thread) and the block's scales
-        // (written before `full`, which the MMA warp waited for)
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t], q & 1, abortp, stt));
+        const uint32_t S = Sb + (q & 1) * 64;
+        // S is in, and with it the block's scales (written before `full`, which the MMA warp waited for)
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q & 1], (q >> 1) & 1, abortp, stt));
         if (!ok) break;
         tc::fence_after_sync();
         if (i > 0 && i % kFlush == 0) {
+          if (!product_done(q - 1)) break;
           // O goes to the sums in memory and starts again at zero (see above)
           float up[2], down[2];
           bool redo = false;
@@ -686,6 +688,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           }
         }
         if (i % kFlush != 0 && __any_sync(0xffffffffu, grows)) {   // scale O
+          if (!product_done(q - 1)) break;
 #pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
             float o[16];
@@ -735,11 +738,10 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tmem_wait_st();
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&pfull[t]);
+        if (lane == 0) tc::mbar_arrive(&pfull[t][q & 1]);
       }
       it += n;
-      if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t], seg & 1, abortp, stt));
-      tc::fence_after_sync();
+      if (ok) product_done(it - 1);
       if (tid == 0) stop_flag = *abortp;   // one reading for all
       asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
       if (stop_flag) break;
