@@ -181,6 +181,11 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 d;
   asm("{\n\t.reg .b64 a, b, d;\n\t"
@@ -662,8 +667,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           float top = fmaxf(v[2 * k], v[2 * k + 1]), b = fmaxf(v[4 + 2 * k], v[4 + 2 * k + 1]);
 #pragma unroll
           for (int j = 2; j < 8; j += 2) {
-            top = fmaxf(fmaxf(top, v[4 * j + 2 * k]), v[4 * j + 2 * k + 1]);
-            b = fmaxf(fmaxf(b, v[4 * j + 4 + 2 * k]), v[4 * j + 4 + 2 * k + 1]);
+            top = max3(top, v[4 * j + 2 * k], v[4 * j + 2 * k + 1]);
+            b = max3(b, v[4 * j + 4 + 2 * k], v[4 * j + 4 + 2 * k + 1]);
           }
           top = fmaxf(top, b);
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -725,7 +730,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
             const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
                                           __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
-            const float2 lo = add2(x, make_float2(-hi.x, -hi.y));
+            const float2 lo = fma2(hi, make_float2(-1.f, -1.f), x);
             const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
             hr[e] = *(const uint32_t*)&h2;
             lr[e] = *(const uint32_t*)&l2;
