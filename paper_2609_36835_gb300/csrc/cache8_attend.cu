@@ -45,9 +45,12 @@ struct RowsShape {
 
 template <int kR>
 struct RowsCfg {
-  // consumer warps: with the producer a multiple of four, as registers are dealt out to the SM's quarters
-  static constexpr int kWarps = kR == 16 ? 7 : 11;
-  static constexpr int kStages = kR == 16 ? 9 : kR == 8 ? 10 : 11;
+  // consumer warps: with the producer at most a multiple of four, as registers are dealt out to the SM's quarters
+  static constexpr int kWarps = kR == 16 ? 7 : kR == 8 ? 10 : 11;
+  // Stages of the ring: one for each consumer warp, so that a stage is always consumed by the same warp.  A warp that
+  // came to a stage while an earlier block of another warp was still on its way there would take the phase before
+  // that one for its own (a wait sees a phase's parity only).
+  static constexpr int kStages = kWarps;
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kMerge = kWarps * kR * 128 * 4;         // their outputs at an item's end
   static constexpr int kSmem = kStages * (2 * kTileBytes + kCB * 4) + kMerge + 1024;
@@ -334,17 +337,23 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
           for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[nt][mt][e] = 0.f;
+        // (four independent chains of products: the 16-key tiles)
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int ch = 0; ch < 2; ++ch) {
+          uint4 a[4], a8[4];
 #pragma unroll
-          for (int ch = 0; ch < 2; ++ch) {
+          for (int mt = 0; mt < 4; ++mt) {
             const int off = (mt * 16 + g) * 128 + (((2 * t + ch) ^ g) << 4);
-            const uint4 a = *(const uint4*)(Kt + off), a8 = *(const uint4*)(Kt + off + 8 * 128);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w}, w8[4] = {a8.x, a8.y, a8.z, a8.w};
+            a[mt] = *(const uint4*)(Kt + off);
+            a8[mt] = *(const uint4*)(Kt + off + 8 * 128);
+          }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t f0 = codes_f16<0>(w[k]), f1 = codes_f16<0>(w8[k]), f2 = codes_f16<1>(w[k]),
-                             f3 = codes_f16<1>(w8[k]);
+          for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+              const uint32_t w = k == 0 ? a[mt].x : k == 1 ? a[mt].y : k == 2 ? a[mt].z : a[mt].w;
+              const uint32_t w8 = k == 0 ? a8[mt].x : k == 1 ? a8[mt].y : k == 2 ? a8[mt].z : a8[mt].w;
+              const uint32_t f0 = codes_f16<0>(w), f1 = codes_f16<0>(w8), f2 = codes_f16<1>(w), f3 = codes_f16<1>(w8);
 #pragma unroll
               for (int nt = 0; nt < kNT; ++nt)
                 mma_f16(s[nt][mt], f0, f1, f2, f3, qf[nt][4 * ch + k][0], qf[nt][4 * ch + k][1]);

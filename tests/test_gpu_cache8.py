@@ -307,6 +307,17 @@ def test_long_sequences_split_over_the_device(G, n_pos):
     assert torch.equal(pk.cache_attend(c, Q, causal=True), pk.cache_attend(c, Q, causal=True))
 
 
+@pytest.mark.parametrize("G,n_pos,bias", [(4, 1, False), (8, 1, False), (4, 3, True), (16, 1, False), (3, 2, True)])
+def test_rings_go_round(G, n_pos, bias):
+    """Many blocks for each SM, for every number of rows of the decode kernel: the shared-memory ring is refilled."""
+    lens = [24000, 19937, 23041]
+    c, _, _ = filled(75, lens, 4, bias=bias)
+    Q = queries(76, c, n_pos, G)
+    O = pk.cache_attend(c, Q, causal=True)
+    check_attend(c, Q, O, True, heads=[(0, 0), (1, 2), (2, 3)])
+    assert torch.equal(O, pk.cache_attend(c, Q, causal=True))
+
+
 def test_offsets_past_32_bits():
     """More than 2^32 bytes of codes: the last head of the last sequence, whose rows lie behind them."""
     S, H, cap = 5, 9, 1 << 20
