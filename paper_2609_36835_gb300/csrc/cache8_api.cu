@@ -110,7 +110,9 @@ arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G,
   if (e != ARCKV_OK) return e;
   RowStrides os;
   if (!O || !row_strides(O, o_strides, c->H, n_pos, (int64_t)G * 128, 4, &os)) return ARCKV_ERR_INVALID_ARG;
-  if (blocks && (m < 1 || m > c->cap / kCB + 8192)) return ARCKV_ERR_SHAPE;
+  // blocks read in all are counted in 32 bits
+  if (blocks && (m < 1 || m > c->cap / kCB + 8192 || (long long)c->S * c->H * n_pos * ((G + 3) / 4) * m >= (1LL << 31)))
+    return ARCKV_ERR_SHAPE;
   if (!(logit_scale >= 0.f) || !isfinite(logit_scale)) return ARCKV_ERR_INVALID_ARG;
   const float scale = logit_scale > 0.f ? logit_scale : 1.0f / sqrtf((float)c->d);
   cudaGetLastError();

@@ -7,9 +7,11 @@
 // token and head are read once: the call is bound by HBM, and the work per byte
 // has to stay small.  So:
 //  - Work is the list of (item, block) pairs, an item being (sequence, KV head,
-//    up to 16 query rows[, position]).  One CTA on each SM takes an equal share
-//    of it, whatever the lengths; an item cut by a share's end is finished by
-//    the CTA that comes last (a ticket), which adds the parts up in CTA order.
+//    up to 16 query rows[, position]).  With more items than SMs each SM's CTA
+//    takes an equal share of it, whatever the lengths; with fewer, items are cut
+//    into equal parts, a CTA each, as many as there are SMs for: a CTA then meets
+//    one item only.  An item in several CTAs is finished by the one that comes
+//    last (a ticket), which adds the parts up in CTA order.
 //  - A producer warp streams blocks (64 x 128 codes of K and of V, 8 KB each,
 //    128-byte swizzle) through a ring in shared memory by TMA.  Each consumer
 //    warp takes whole blocks of its own, with its own running maximum, sum and
@@ -38,7 +40,7 @@ constexpr int kTileBytes = kCB * 128;        // codes of one block, K or V
 
 struct RowsShape {
   int H, n_pos, G, nblk, cap;   // nblk: blocks of the capacity
-  int groups;                   // row groups of an item's rows
+  int groups;                   // sparse: row groups of a position
   int m;                        // blocks listed for an item (sparse)
   bool causal;
 };
@@ -81,49 +83,97 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 }
 __device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
-// The item and block of unit u, and the units left in the item.
-struct Place {
-  long long item_first;   // unit at which the item begins
-  long long sh;           // sequence x KV head
-  long long list;         // sparse: row of the block lists
-  int s, pos, group, blk, count;   // blk of count blocks (list entries)
+// A CTA's run of blocks (entries of the block list) of one item.
+struct Run {
+  int s, h, sh;           // sequence, head, both
+  int pos, group, list;   // sparse: position, row group, row of the block lists
+  int blk, n;             // blocks blk .. blk + n - 1
+  int first, last;        // the CTAs that share the item
 };
 
-// Dense: units run over s, then head and row group, then blocks; pre[s] are
-// the blocks before sequence s (at least one block for each sequence).
+// Smallest number of blocks that are worth a CTA of their own: joining two CTAs' parts takes about as long as this
+// many blocks, which the warps of one CTA have at the same time.
+constexpr int kPartMin = 6;
+
+// The runs of a CTA, in order.  Items are numbered over sequences, then heads (sparse: positions, row groups); dense,
+// pre[s] are the blocks (or parts) before sequence s of one head.
 template <bool kSparse>
-__device__ __forceinline__ Place place_of(long long u, const RowsShape& d, int S, const int* pre) {
-  Place p;
-  if (kSparse) {
-    const long long item = u / d.m;
-    p.blk = (int)(u - item * d.m);
-    p.count = d.m;
-    p.item_first = item * d.m;
-    p.group = (int)(item % d.groups);
-    p.list = item / d.groups;
-    p.pos = (int)(p.list % d.n_pos);
-    p.sh = p.list / d.n_pos;
-    p.s = (int)(p.sh / d.H);
-  } else {
-    const long long per = (long long)d.H * d.groups;
-    int lo = 0, hi = S;   // last s with pre[s] * per <= u
+struct Walk {
+  const RowsShape& d;
+  const int* pre;
+  int S, cta;
+  bool parts;             // items are cut into equal parts
+  int u, u1;              // parts: this CTA's part of all; else units (blocks) of its share
+  int q, r;               // shares: q units each, one more for the first r CTAs
+  int per;                // sparse: parts of an item
+  const int* len;
+
+  __device__ int owner(int unit) const {
+    const int big = r * (q + 1);
+    return unit < big ? unit / (q + 1) : r + (unit - big) / q;
+  }
+  __device__ int blocks_of(int s) const { return max(1, (min(max(len[s], 0), d.cap) + kCB - 1) / kCB); }
+  // last s with pre[s] * H <= x
+  __device__ int sequence_of(int x) const {
+    int lo = 0, hi = S;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (pre[mid] * per <= u) lo = mid;
+      if (pre[mid] * d.H <= x) lo = mid;
       else hi = mid;
     }
-    p.s = lo;
-    p.count = pre[lo + 1] - pre[lo];
-    const long long rest = u - pre[lo] * per, it = rest / p.count;
-    p.blk = (int)(rest - it * p.count);
-    p.item_first = pre[lo] * per + it * p.count;
-    p.group = (int)(it % d.groups);
-    p.sh = (long long)lo * d.H + it / d.groups;
-    p.pos = 0;
-    p.list = 0;
+    return lo;
   }
-  return p;
-}
+  __device__ bool next(Run& p) {
+    if (u >= u1) return false;
+    if (kSparse) {
+      const int cut = parts ? per : d.m, item = u / cut, k = u - item * cut;
+      p.group = item % d.groups;
+      p.list = item / d.groups;
+      p.pos = p.list % d.n_pos;
+      p.sh = p.list / d.n_pos;
+      p.s = p.sh / d.H;
+      p.h = p.sh - p.s * d.H;
+      if (parts) {
+        p.blk = (int)((long long)d.m * k / per);
+        p.n = (int)((long long)d.m * (k + 1) / per) - p.blk;
+        p.first = item * per;
+        p.last = p.first + per - 1;
+        ++u;
+      } else {
+        take(p, k, d.m);
+      }
+      return true;
+    }
+    p.s = sequence_of(u);
+    const int cut = pre[p.s + 1] - pre[p.s], rest = u - pre[p.s] * d.H;
+    p.h = rest / cut;
+    p.sh = p.s * d.H + p.h;
+    p.pos = p.group = p.list = 0;
+    const int k = rest - p.h * cut;
+    if (parts) {
+      const int nb = blocks_of(p.s);
+      p.blk = (int)((long long)nb * k / cut);
+      p.n = (int)((long long)nb * (k + 1) / cut) - p.blk;
+      p.first = u - k;
+      p.last = p.first + cut - 1;
+      ++u;
+    } else {
+      take(p, k, cut);
+    }
+    return true;
+  }
+  // block k of an item of `count`, and as many as the share holds
+  __device__ void take(Run& p, int k, int count) {
+    p.blk = k;
+    p.n = min(count - k, u1 - u);
+    p.first = p.last = cta;
+    if (p.n < count) {
+      p.first = owner(u - k);
+      p.last = owner(u - k + count - 1);
+    }
+    u += p.n;
+  }
+};
 
 template <int kR, bool kBias, bool kSparse>
 __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
@@ -154,53 +204,79 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     abort_flag = 0;
     tc::mbar_fence_init();
   }
-  if (warp == kW) {   // blocks before each sequence, by warp scan
+  __shared__ int s_cut;   // blocks of a part (0: equal shares)
+  if (warp == kW) {   // blocks, or parts, before each sequence, by warp scan
     if (lane == 0) {
       tc::tma_prefetch(&mK);
       tc::tma_prefetch(&mV);
     }
     if (!kSparse) {
-      int run = 0;
-      for (int s0 = 0; s0 < c.S; s0 += 32) {
-        int x = s0 + lane < c.S ? max(1, (cache_len(c, s0 + lane) + kCB - 1) / kCB) : 0;
+      int cut = 0;
+      auto scan = [&] {
+        int run = 0;
+        for (int s0 = 0; s0 < c.S; s0 += 32) {
+          int x = s0 + lane < c.S ? max(1, (cache_len(c, s0 + lane) + kCB - 1) / kCB) : 0;
+          if (cut > 0) x = (x + cut - 1) / cut;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, x, o);
-          if (lane >= o) x += y;
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+          }
+          if (s0 + lane < c.S) pre[s0 + lane + 1] = run + x;
+          run += __shfl_sync(0xffffffffu, x, 31);
         }
-        if (s0 + lane < c.S) pre[s0 + lane + 1] = run + x;
-        run += __shfl_sync(0xffffffffu, x, 31);
+        return run;
+      };
+      int all = scan();
+      if (c.S * d.H <= (int)gridDim.x) {   // the smallest parts that the CTAs suffice for
+        cut = max(kPartMin, (all * d.H + (int)gridDim.x - 1) / (int)gridDim.x);
+        for (all = scan(); all * d.H > (int)gridDim.x; all = scan())
+          cut = max(cut + 1, (int)((long long)cut * all * d.H / (int)gridDim.x));
       }
-      if (lane == 0) pre[0] = 0;
+      if (lane == 0) {
+        pre[0] = 0;
+        s_cut = cut;
+      }
     }
   }
   __syncthreads();
-  CacheShares sh;
-  sh.total = kSparse ? (long long)c.S * d.H * d.n_pos * d.groups * d.m
-                     : (long long)pre[c.S] * d.H * d.groups;
-  sh.ctas = (int)min((long long)gridDim.x, sh.total);
-  if ((int)blockIdx.x >= sh.ctas) return;
-  const long long u0 = sh.start(blockIdx.x), u1 = sh.start(blockIdx.x + 1);
+  Walk<kSparse> walk{d, pre, c.S, (int)blockIdx.x};
+  walk.len = c.len;
+  int total;
+  if (kSparse) {
+    const int items = c.S * d.H * d.n_pos * d.groups;
+    walk.parts = items <= (int)gridDim.x;
+    walk.per = walk.parts ? max(1, min((int)gridDim.x / items, d.m / kPartMin)) : 1;
+    total = items * (walk.parts ? walk.per : d.m);
+  } else {
+    walk.parts = s_cut > 0;
+    total = pre[c.S] * d.H;
+  }
+  const int ctas = min((int)gridDim.x, total), me = blockIdx.x;
+  if (me >= ctas) return;
+  walk.q = total / ctas;
+  walk.r = total - walk.q * ctas;
+  walk.u = walk.q * me + min(me, walk.r);
+  walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
 
   if (warp == kW) {
     // ------------------------------------------------------------- producer
     int it = 0;   // blocks issued
     bool ok = true;
-    for (long long u = u0; u < u1 && ok;) {
-      const Place p = place_of<kSparse>(u, d, c.S, pre);
-      const int n = (int)min((long long)(p.count - p.blk), u1 - u), len = cache_len(c, p.s);
+    for (Run p; ok && walk.next(p);) {
+      const int n = p.n, len = cache_len(c, p.s);
       for (int k0 = 0; k0 < n && ok; k0 += 32) {
         const int k = k0 + lane;
         int b = -1;
         if (k < n) {
-          b = kSparse ? blocks[p.list * d.m + p.blk + k] : p.blk + k;
+          b = kSparse ? blocks[(long long)p.list * d.m + p.blk + k] : p.blk + k;
           if (kSparse && b >= d.nblk) {
             set_status(stt, ARCKV_ERR_INVALID_ARG);
             b = -1;
           }
           if (b >= 0 && b * kCB >= len) b = -1;   // nothing of it is held
         }
-        const long long at = p.sh * d.nblk + b;
+        const long long at = (long long)p.sh * d.nblk + b;
         float ks = 0.f, vs = 0.f;
         if (b >= 0) {
           ks = c.k_scale[at];
@@ -209,9 +285,9 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         const int cnt = min(32, n - k0);
         auto load = [&](int st) {   // this lane's block into stage st
           unsigned char* dst = ring + st * 2 * kTileBytes;
-          tc::tma_load_3d(dst, &mK, 0, b * kCB, (int)p.sh, &full[st]);
-          tc::tma_load_3d(dst + kTileBytes, &mV, 0, b * kCB, (int)p.sh, &full[st]);
-          if (kBias) tc::bulk_load(sBias + st * kCB, c.bias + p.sh * c.cap + b * kCB, kCB * 4, &full[st]);
+          tc::tma_load_3d(dst, &mK, 0, b * kCB, p.sh, &full[st]);
+          tc::tma_load_3d(dst + kTileBytes, &mV, 0, b * kCB, p.sh, &full[st]);
+          if (kBias) tc::bulk_load(sBias + st * kCB, c.bias + (long long)p.sh * c.cap + b * kCB, kCB * 4, &full[st]);
         };
         auto announce = [&](int st) {
           sKs[st] = ks;
@@ -239,7 +315,6 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         }
         it += j;
       }
-      u += n;
     }
     if (!ok) {   // let the copies in flight land before the CTA's memory goes
       volatile int never = 0;
@@ -253,10 +328,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   constexpr float kP15 = 15.f;   // weights carry a factor of 2^15
   int base = 0;                  // blocks of earlier segments
   bool ok = true;
-  for (long long u = u0; u < u1;) {
-    const Place p = place_of<kSparse>(u, d, c.S, pre);
-    const int n = (int)min((long long)(p.count - p.blk), u1 - u), len = cache_len(c, p.s);
-    const int h = (int)(p.sh - (long long)p.s * d.H), nrows = kSparse ? d.G : d.n_pos * d.G;
+  for (Run p; walk.next(p);) {
+    const int n = p.n, len = cache_len(c, p.s), h = p.h, nrows = kSparse ? d.G : d.n_pos * d.G;
     // query rows: column n of tile nt is row nt * 8 + n of the group (four rows: twice the same four)
     uint32_t qf[kNT][8][2];
     float fac[kNT][2];           // 2^e scale (log2 e) of rows 2t, 2t + 1
@@ -488,9 +561,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
     bar_consumers(kW * 32);
     if (stop_flag) break;   // a wait gave up: write nothing
-    const bool whole = p.blk == 0 && n == p.count;
-    const int c_first = whole ? blockIdx.x : sh.owner(p.item_first);
-    const int c_last = whole ? blockIdx.x : sh.owner(p.item_first + p.count - 1);
+    const bool whole = p.first == p.last;
     auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
       return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
     };
@@ -529,32 +600,32 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       __threadfence();
       bar_consumers(kW * 32);
       if (tid == 0) {
-        last_flag = atomicAdd(&tickets[c_first], 1) == c_last - c_first;
-        if (last_flag) tickets[c_first] = 0;
+        last_flag = atomicAdd(&tickets[p.first], 1) == p.last - p.first;
+        if (last_flag) tickets[p.first] = 0;
         __threadfence();
       }
       bar_consumers(kW * 32);
       if (last_flag) {
         for (int x = tid; x < kR * 32; x += kW * 32) {
           const int r = x >> 5, dim = (x & 31) * 4;
+          // with a running maximum, so that a part's loads wait for nothing
           float top = -INFINITY, z = 0.f;
-          for (int cc = c_first; cc <= c_last; ++cc)
-            top = fmaxf(top, __ldcg(parts + (2ll * cc + (cc == c_first)) * kSlot + r * 132 + 128));
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int cc = c_first; cc <= c_last; ++cc) {
-            const float* slot = parts + (2ll * cc + (cc == c_first)) * kSlot + r * 132;
+#pragma unroll 4
+          for (int cc = p.first; cc <= p.last; ++cc) {
+            const float* slot = parts + (2ll * cc + (cc == p.first)) * kSlot + r * 132;
             const float2 ml = __ldcg((const float2*)(slot + 128));
             const float4 y = __ldcg((const float4*)(slot + dim));
-            const float f = weight(ml.x, top);
-            z = fmaf(ml.y, f, z);
-            v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
+            const float up = fmaxf(top, ml.x), f = weight(ml.x, up), f0 = weight(top, up);
+            top = up;
+            z = fmaf(z, f0, ml.y * f);
+            v = make_float4(fmaf(v.x, f0, y.x * f), fmaf(v.y, f0, y.y * f), fmaf(v.z, f0, y.z * f), fmaf(v.w, f0, y.w * f));
           }
           store(r, dim, v, z);
         }
       }
     }
     bar_consumers(kW * 32);   // sO, sM, sL are free
-    u += n;
   }
 }
 
@@ -572,7 +643,7 @@ int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const i
   d.G = q.G;
   d.cap = c.cap;
   d.nblk = c.cap / kCB;
-  d.groups = cdiv(kSparse ? q.G : (long long)q.n_pos * q.G, kR);
+  d.groups = kSparse ? cdiv(q.G, kR) : 1;   // dense calls with more rows go elsewhere
   d.m = m;
   d.causal = q.causal;
   auto kern = cache_rows_kernel<kR, kBias, kSparse>;
