@@ -12,10 +12,12 @@
 //    into equal parts, a CTA each, as many as there are SMs for: a CTA then meets
 //    one item only.  An item in several CTAs is finished by the one that comes
 //    last (a ticket), which adds the parts up in CTA order.
-//  - A producer warp streams blocks (64 x 128 codes of K and of V, 8 KB each,
-//    128-byte swizzle) through a ring in shared memory by TMA.  Each consumer
-//    warp takes whole blocks of its own, with its own running maximum, sum and
-//    output: no barrier between warps until the item ends.
+//  - Two producer warps stream the blocks' keys and values (64 x 128 codes, 8 KB
+//    each, 128-byte swizzle) through rings in shared memory by TMA.  Each of ten
+//    consumer warps takes whole blocks of its own, with its own running maximum,
+//    sum and output: no barrier between warps until the item ends.  A warp gives
+//    its keys' stage back before the softmax, so that the next block's keys come
+//    in while it works on the values, and its values while on those keys.
 //  - Products run on mma.sync m16n8k16 with f16 operands: keys (dims for V) are
 //    the 16 rows and the query rows the 8 columns, so four to eight rows fill
 //    an instruction; tcgen05 would want 64 to 128 rows and a pass of the
@@ -45,17 +47,19 @@ struct RowsShape {
   bool causal;
 };
 
+constexpr int kW = 10;   // consumer warps; with the producers a multiple of four, as registers are dealt out to the SM's quarters
+// Stages of a ring: one for each consumer warp (two for each pair of warps that share blocks), so that a stage is
+// always consumed by the same warps.  A warp that came to a stage while an earlier block of another warp was still on
+// its way there would take the phase before that one for its own (a wait sees a phase's parity only).
+constexpr int kSt = kW;
+constexpr int kRowsThreads = 32 * (kW + 2);
+
 template <int kR>
 struct RowsCfg {
-  // consumer warps: with the producer at most a multiple of four, as registers are dealt out to the SM's quarters
-  static constexpr int kWarps = kR == 16 ? 7 : kR == 8 ? 10 : 11;
-  // Stages of the ring: one for each consumer warp, so that a stage is always consumed by the same warp.  A warp that
-  // came to a stage while an earlier block of another warp was still on its way there would take the phase before
-  // that one for its own (a wait sees a phase's parity only).
-  static constexpr int kStages = kWarps;
-  static constexpr int kThreads = 32 * (kWarps + 1);
-  static constexpr int kMerge = kWarps * kR * 128 * 4;         // their outputs at an item's end
-  static constexpr int kSmem = kStages * (2 * kTileBytes + kCB * 4) + kMerge + 1024;
+  static constexpr int kTiles = kR == 16 ? 2 : 1;   // tiles of 8 rows; warps w and w + kW / 2 share blocks, a tile each
+  static constexpr int kTeams = kW / kTiles;        // warps, or pairs, that take blocks in turn
+  static constexpr int kTileRows = kR < 8 ? kR : 8;
+  static constexpr int kSmem = kSt * (2 * kTileBytes + kCB * 4) + kW * kTileRows * 128 * 4 + 1024;
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -176,30 +180,32 @@ struct Walk {
 };
 
 template <int kR, bool kBias, bool kSparse>
-__global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
+__global__ void __launch_bounds__(kRowsThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap mK, const __grid_constant__ CUtensorMap mV,
                       const arckv_cache8 c, RowsShape d, const bf16* Q, RowStrides qs, float scale, const int* blocks,
                       float* O, RowStrides os, float* parts, int* tickets, DevStatus* stt) {
   using Cfg = RowsCfg<kR>;
-  constexpr int kNT = kR == 16 ? 2 : 1;   // column tiles of 8 rows
-  constexpr int kW = Cfg::kWarps, kSt = Cfg::kStages;
+  constexpr int kTR = Cfg::kTileRows, kTeams = Cfg::kTeams;
   extern __shared__ __align__(1024) unsigned char smraw[];
-  unsigned char* ring = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
-  float* sBias = (float*)(ring + kSt * 2 * kTileBytes);
-  float* sO = sBias + kSt * kCB;                                 // [warp][row][128]
-  __shared__ __align__(8) uint64_t full[kSt], empty[kSt];
+  unsigned char* ringK = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
+  unsigned char* ringV = ringK + kSt * kTileBytes;
+  float* sBias = (float*)(ringV + kSt * kTileBytes);
+  float* sO = sBias + kSt * kCB;                                 // [warp][row of its tile][128]
+  int* pre = (int*)(sO + kW * kTR * 128);                        // dense: [S + 1]
+  __shared__ __align__(8) uint64_t fullK[kSt], emptyK[kSt], fullV[kSt], emptyV[kSt];
   __shared__ float sKs[kSt], sVs[kSt];
   __shared__ int sBlk[kSt];
-  __shared__ float sM[kW][kR], sL[kW][kR];
+  __shared__ float sM[kW][kTR], sL[kW][kTR];
   __shared__ int abort_flag, last_flag, stop_flag;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int* pre = (int*)(sO + kW * kR * 128);                         // dense: [S + 1]
   volatile int* abortp = &abort_flag;
 
   if (tid == 0) {
     for (int s = 0; s < kSt; ++s) {
-      tc::mbar_init(&full[s], 1);
-      tc::mbar_init(&empty[s], 1);
+      tc::mbar_init(&fullK[s], 1);
+      tc::mbar_init(&emptyK[s], Cfg::kTiles);
+      tc::mbar_init(&fullV[s], 1);
+      tc::mbar_init(&emptyV[s], Cfg::kTiles);
     }
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -259,8 +265,14 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   walk.u = walk.q * me + min(me, walk.r);
   walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
 
-  if (warp == kW) {
-    // ------------------------------------------------------------- producer
+  if (warp >= kW) {
+    // ------------------------------------- producers: keys (with scales and biases) and values
+    const bool keys = warp == kW;
+    uint64_t *full = keys ? fullK : fullV, *empty = keys ? emptyK : emptyV;
+    unsigned char* ring = keys ? ringK : ringV;
+    const CUtensorMap* map = keys ? &mK : &mV;
+    const float* scales = keys ? c.k_scale : c.v_scale;
+    float* sScale = keys ? sKs : sVs;
     int it = 0;   // blocks issued
     bool ok = true;
     for (Run p; ok && walk.next(p);) {
@@ -276,24 +288,18 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
           }
           if (b >= 0 && b * kCB >= len) b = -1;   // nothing of it is held
         }
-        const long long at = (long long)p.sh * d.nblk + b;
-        float ks = 0.f, vs = 0.f;
-        if (b >= 0) {
-          ks = c.k_scale[at];
-          vs = c.v_scale[at];
-        }
+        const float sc = b >= 0 ? scales[(long long)p.sh * d.nblk + b] : 0.f;
         const int cnt = min(32, n - k0);
+        const bool with_bias = kBias && keys;
         auto load = [&](int st) {   // this lane's block into stage st
-          unsigned char* dst = ring + st * 2 * kTileBytes;
-          tc::tma_load_3d(dst, &mK, 0, b * kCB, p.sh, &full[st]);
-          tc::tma_load_3d(dst + kTileBytes, &mV, 0, b * kCB, p.sh, &full[st]);
-          if (kBias) tc::bulk_load(sBias + st * kCB, c.bias + (long long)p.sh * c.cap + b * kCB, kCB * 4, &full[st]);
+          tc::tma_load_3d(ring + st * kTileBytes, map, 0, b * kCB, p.sh, &full[st]);
+          if (with_bias)
+            tc::bulk_load(sBias + st * kCB, c.bias + (long long)p.sh * c.cap + b * kCB, kCB * 4, &full[st]);
         };
         auto announce = [&](int st) {
-          sKs[st] = ks;
-          sVs[st] = vs;
-          sBlk[st] = b;
-          if (b >= 0) tc::mbar_arrive_expect_tx(&full[st], 2 * kTileBytes + (kBias ? kCB * 4 : 0));
+          sScale[st] = sc;
+          if (keys) sBlk[st] = b;
+          if (b >= 0) tc::mbar_arrive_expect_tx(&full[st], kTileBytes + (with_bias ? kCB * 4 : 0));
           else tc::mbar_arrive(&full[st]);
         };
         int j = 0;
@@ -325,19 +331,18 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 
   // --------------------------------------------------------------- consumers
   const int g = lane >> 2, t = lane & 3;
+  const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
   constexpr float kP15 = 15.f;   // weights carry a factor of 2^15
-  int base = 0;                  // blocks of earlier segments
+  int base = 0;                  // blocks of earlier runs
   bool ok = true;
   for (Run p; walk.next(p);) {
     const int n = p.n, len = cache_len(c, p.s), h = p.h, nrows = kSparse ? d.G : d.n_pos * d.G;
-    // query rows: column n of tile nt is row nt * 8 + n of the group (four rows: twice the same four)
-    uint32_t qf[kNT][8][2];
-    float fac[kNT][2];           // 2^e scale (log2 e) of rows 2t, 2t + 1
-    int see[kNT][2];             // tokens that they see
-    int see_min = 0x7fffffff;
-#pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) {
-      const int r = p.group * kR + (kR == 4 ? (g & 3) : nt * 8 + g);
+    // query rows: column n is row n of the tile (four rows: twice the same four)
+    uint32_t qf[8][2];
+    float fac[2];           // 2^e scale (log2 e) of rows 2t, 2t + 1
+    int see[2], see_min;    // tokens that they see
+    {
+      const int r = p.group * kR + tile0 + (kR == 4 ? (g & 3) : g);
       const int pos = kSparse ? p.pos : r / d.G, gq = kSparse ? r : r - pos * d.G;
       float x[32], amax = 0.f;
       if (r < nrows) {
@@ -366,51 +371,39 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       const float up = __uint_as_float((unsigned)(14 - e + 127) << 23), down = __uint_as_float((unsigned)(e - 14 + 127) << 23);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        qf[nt][k][0] = pack_f16(x[4 * k] * up, x[4 * k + 1] * up);
-        qf[nt][k][1] = pack_f16(x[4 * k + 2] * up, x[4 * k + 3] * up);
+        qf[k][0] = pack_f16(x[4 * k] * up, x[4 * k + 1] * up);
+        qf[k][1] = pack_f16(x[4 * k + 2] * up, x[4 * k + 3] * up);
       }
       const float f = down * scale * (kBias ? 1.f : kLog2e);
       const int sees = r < nrows ? visible_tokens(len, d.n_pos, pos, d.causal) : 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        fac[nt][i] = __shfl_sync(0xffffffffu, f, (2 * t + i) * 4);
-        see[nt][i] = __shfl_sync(0xffffffffu, sees, (2 * t + i) * 4);
+        fac[i] = __shfl_sync(0xffffffffu, f, (2 * t + i) * 4);
+        see[i] = __shfl_sync(0xffffffffu, sees, (2 * t + i) * 4);
       }
-      see_min = min(see_min, __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff));
+      see_min = __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff);
     }
-    float o[kNT][8][4], mx[kNT][2], l[kNT][2];
+    float o[8][4], mx[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) {
+    for (int k = 0; k < 8; ++k)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        mx[nt][i] = -INFINITY;
-        l[nt][i] = 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[nt][k][e] = 0.f;
-    }
-    // blocks base + i of the CTA belong to warp (base + i) % kW
-    for (int i = (warp - base % kW + kW) % kW; i < n; i += kW) {
+      for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
+    // block base + i of the CTA belongs to team (base + i) % kTeams
+    for (int i = (team - base % kTeams + kTeams) % kTeams; i < n; i += kTeams) {
       const int q = base + i, st = q % kSt;
-      ok = tc::mbar_wait(&full[st], (q / kSt) & 1, abortp, stt);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullK[st], (q / kSt) & 1, abortp, stt));
       if (!ok) break;
       const int b = sBlk[st];
       if (b >= 0) {
-        const float ks = sKs[st], vs = sVs[st];
-        const unsigned char* Kt = ring + st * 2 * kTileBytes;
-        const unsigned char* Vt = Kt + kTileBytes;
+        const float ks = sKs[st];
+        const unsigned char* Kt = ringK + st * kTileBytes;
         // ---- S^T = K Q^T: lane (g, t) has keys g, g + 8 and dims 32t .. 32t + 31
-        float s[kNT][4][4];
-#pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-          for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[nt][mt][e] = 0.f;
         // (four independent chains of products: the 16-key tiles)
+        float s[4][4];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[mt][e] = 0.f;
 #pragma unroll
         for (int ch = 0; ch < 2; ++ch) {
           uint4 a[4], a8[4];
@@ -426,77 +419,78 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
             for (int mt = 0; mt < 4; ++mt) {
               const uint32_t w = k == 0 ? a[mt].x : k == 1 ? a[mt].y : k == 2 ? a[mt].z : a[mt].w;
               const uint32_t w8 = k == 0 ? a8[mt].x : k == 1 ? a8[mt].y : k == 2 ? a8[mt].z : a8[mt].w;
-              const uint32_t f0 = codes_f16<0>(w), f1 = codes_f16<0>(w8), f2 = codes_f16<1>(w), f3 = codes_f16<1>(w8);
-#pragma unroll
-              for (int nt = 0; nt < kNT; ++nt)
-                mma_f16(s[nt][mt], f0, f1, f2, f3, qf[nt][4 * ch + k][0], qf[nt][4 * ch + k][1]);
+              mma_f16(s[mt], codes_f16<0>(w), codes_f16<0>(w8), codes_f16<1>(w), codes_f16<1>(w8), qf[4 * ch + k][0],
+                      qf[4 * ch + k][1]);
             }
           }
         }
         // ---- softmax of the block
         const bool edge = (b + 1) * kCB > see_min;
-        uint32_t ph[kNT][4][2], pl[kNT][4][2];
-        float alpha[kNT][2];
+        float top[2], alpha[2];
 #pragma unroll
-        for (int nt = 0; nt < kNT; ++nt) {
-#pragma unroll
-          for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
-            const float f = fac[nt][e2] * ks;
-            float top = -INFINITY;
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-              for (int hf = 0; hf < 2; ++hf) {
-                float& x = s[nt][mt][2 * hf + e2];
-                const int kk = mt * 16 + hf * 8 + g;
-                x = kBias ? fmaf(x, f, sBias[st * kCB + kk]) : x * f;
-                if (edge && b * kCB + kk >= see[nt][e2]) x = -INFINITY;
-                top = fmaxf(top, x);
-              }
-#pragma unroll
-            for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-            const float old = mx[nt][e2];
-            top = fmaxf(top, old);
-            mx[nt][e2] = top;
-            const float ref = top == -INFINITY ? 0.f : top;   // nothing visible yet: weights e^{-inf} = 0
-            alpha[nt][e2] = ex2_approx(kBias ? (old - ref) * kLog2e : old - ref);
-            float sum = 0.f;
-#pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-              for (int hf = 0; hf < 2; ++hf) {
-                float& x = s[nt][mt][2 * hf + e2];
-                // a bias of the type's lowest value cancels against itself before the factor log2 e
-                x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kP15) : (x - ref) + kP15);
-                sum += x;
-              }
-            l[nt][e2] = fmaf(l[nt][e2], alpha[nt][e2], sum);
-          }
-          // f16 pairs, transposed to (keys, row) operands
+        for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
+          const float f = fac[e2] * ks;
+          top[e2] = -INFINITY;
 #pragma unroll
           for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              const float x0 = s[nt][mt][2 * hf], x1 = s[nt][mt][2 * hf + 1];
-              const uint32_t hi = pack_f16(x0, x1);
-              const float2 hf2 = __half22float2(*(const __half2*)&hi);
-              const uint32_t lo = pack_f16(x0 - hf2.x, x1 - hf2.y);
-              if (kR == 4) {   // columns 4 .. 7 carry lo of the same rows
-                ph[nt][mt][hf] = transpose8x8(t >= 2 ? lo : hi);
-              } else {
-                ph[nt][mt][hf] = transpose8x8(hi);
-                pl[nt][mt][hf] = transpose8x8(lo);
-              }
+              float& x = s[mt][2 * hf + e2];
+              const int kk = mt * 16 + hf * 8 + g;
+              x = kBias ? fmaf(x, f, sBias[st * kCB + kk]) : x * f;
+              if (edge && b * kCB + kk >= see[e2]) x = -INFINITY;
+              top[e2] = fmaxf(top[e2], x);
             }
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&emptyK[st]);   // the next block's keys may come
+#pragma unroll
+        for (int e2 = 0; e2 < 2; ++e2) {
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) top[e2] = fmaxf(top[e2], __shfl_xor_sync(0xffffffffu, top[e2], w));
+          const float old = mx[e2], up = fmaxf(top[e2], old);
+          mx[e2] = up;
+          const float ref = up == -INFINITY ? 0.f : up;   // nothing visible yet: weights e^{-inf} = 0
+          alpha[e2] = ex2_approx(kBias ? (old - ref) * kLog2e : old - ref);
+          float sum = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              float& x = s[mt][2 * hf + e2];
+              // a bias of the type's lowest value cancels against itself before the factor log2 e
+              x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kP15) : (x - ref) + kP15);
+              sum += x;
+            }
+          l[e2] = fmaf(l[e2], alpha[e2], sum);
+        }
+        // f16 pairs, transposed to (keys, row) operands
+        uint32_t ph[4][2], pl[4][2];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const float x0 = s[mt][2 * hf], x1 = s[mt][2 * hf + 1];
+            const uint32_t hi = pack_f16(x0, x1);
+            const float2 hf2 = __half22float2(*(const __half2*)&hi);
+            const uint32_t lo = pack_f16(x0 - hf2.x, x1 - hf2.y);
+            if (kR == 4) {   // columns 4 .. 7 carry lo of the same rows
+              ph[mt][hf] = transpose8x8(t >= 2 ? lo : hi);
+            } else {
+              ph[mt][hf] = transpose8x8(hi);
+              pl[mt][hf] = transpose8x8(lo);
+            }
+          }
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullV[st], (q / kSt) & 1, abortp, stt));
+        if (!ok) break;
+        const float vs = sVs[st];
+        const unsigned char* Vt = ringV + st * kTileBytes;
         // ---- O^T += V^T P^T: lane (g, t) has dims 16g .. 16g + 15 of keys 2t, 2t + 1, 2t + 8, 2t + 9
-        float acc[kNT][8][4];
+        float acc[8][4];
 #pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
+        for (int k = 0; k < 8; ++k)
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[nt][k][e] = 0.f;
+          for (int e = 0; e < 4; ++e) acc[k][e] = 0.f;
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
           const unsigned char* row = Vt + (mt * 16 + 2 * t) * 128;
@@ -512,53 +506,51 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
               const uint32_t y = __byte_perm(w0[k], w1[k], z ? 0x7362 : 0x5140);
               const uint32_t y8 = __byte_perm(w8[k], w9[k], z ? 0x7362 : 0x5140);
               const uint32_t f0 = codes_f16<0>(y), f1 = codes_f16<1>(y), f2 = codes_f16<0>(y8), f3 = codes_f16<1>(y8);
-#pragma unroll
-              for (int nt = 0; nt < kNT; ++nt) {
-                mma_f16(acc[nt][2 * k + z], f0, f1, f2, f3, ph[nt][mt][0], ph[nt][mt][1]);
-                if (kR != 4) mma_f16(acc[nt][2 * k + z], f0, f1, f2, f3, pl[nt][mt][0], pl[nt][mt][1]);
-              }
+              mma_f16(acc[2 * k + z], f0, f1, f2, f3, ph[mt][0], ph[mt][1]);
+              if (kR != 4) mma_f16(acc[2 * k + z], f0, f1, f2, f3, pl[mt][0], pl[mt][1]);
             }
           }
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&emptyV[st]);
 #pragma unroll
-        for (int nt = 0; nt < kNT; ++nt)
+        for (int k = 0; k < 8; ++k)
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[nt][k][e] = fmaf(o[nt][k][e], alpha[nt][e & 1], vs * acc[nt][k][e]);
+          for (int e = 0; e < 4; ++e) o[k][e] = fmaf(o[k][e], alpha[e & 1], vs * acc[k][e]);
+      } else {   // an entry that names no block
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullV[st], (q / kSt) & 1, abortp, stt));
+        if (!ok) break;
+        if (lane == 0) {
+          tc::mbar_arrive(&emptyK[st]);
+          tc::mbar_arrive(&emptyV[st]);
+        }
       }
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&empty[st]);
     }
     base += n;
     // ---- the item's end (or this CTA's part of it): add the warps up
 #pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) {
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int w = 4; w < 32; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+      const int r = 2 * t + i;
+      if (g == 0 && r < kTR) {
+        sM[warp][r] = mx[i];
+        sL[warp][r] = l[i];
+      }
+      if (kR == 4) {
 #pragma unroll
-        for (int w = 4; w < 32; w <<= 1) l[nt][i] += __shfl_xor_sync(0xffffffffu, l[nt][i], w);
-        const int r = nt * 8 + 2 * t + i;
-        if (g == 0 && r < kR) {
-          sM[warp][r] = mx[nt][i];
-          sL[warp][r] = l[nt][i];
-        }
-        if (kR == 4) {
+        for (int k = 0; k < 8; ++k)
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int z = 0; z < 2; ++z) o[k][2 * z + i] += __shfl_xor_sync(0xffffffffu, o[k][2 * z + i], 2);   // hi + lo
+      }
+      if (r < kTR) {
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
-              o[nt][k][2 * z + i] += __shfl_xor_sync(0xffffffffu, o[nt][k][2 * z + i], 2);   // hi + lo
-        }
-        if (r < kR) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            *(float4*)(sO + (warp * kR + r) * 128 + 16 * g + 4 * k) =
-                make_float4(o[nt][2 * k][i], o[nt][2 * k][2 + i], o[nt][2 * k + 1][i], o[nt][2 * k + 1][2 + i]);
-        }
+        for (int k = 0; k < 4; ++k)
+          *(float4*)(sO + (warp * kTR + r) * 128 + 16 * g + 4 * k) =
+              make_float4(o[2 * k][i], o[2 * k][2 + i], o[2 * k + 1][i], o[2 * k + 1][2 + i]);
       }
     }
-    if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
+    if (tid == 0) stop_flag = *abortp;   // one reading for all: the producers may raise the flag at any time
     bar_consumers(kW * 32);
     if (stop_flag) break;   // a wait gave up: write nothing
     const bool whole = p.first == p.last;
@@ -577,32 +569,33 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
     constexpr int kSlot = kR * 132;   // 128 outputs, m, l (and two unused) for each row
     for (int x = tid; x < kR * 32; x += kW * 32) {
-      const int r = x >> 5, dim = (x & 31) * 4;
-      float top = -INFINITY, z = 0.f;
+      const int r = x >> 5, dim = (x & 31) * 4, w0 = r / kTR * kTeams, rr = r % kTR;
+      float up = -INFINITY, z = 0.f;
 #pragma unroll
-      for (int w = 0; w < kW; ++w) top = fmaxf(top, sM[w][r]);
+      for (int w = 0; w < kTeams; ++w) up = fmaxf(up, sM[w0 + w][rr]);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kW; ++w) {
-        const float f = weight(sM[w][r], top);
-        const float4 y = *(const float4*)(sO + (w * kR + r) * 128 + dim);
-        z = fmaf(sL[w][r], f, z);
+      for (int w = 0; w < kTeams; ++w) {
+        const float f = weight(sM[w0 + w][rr], up);
+        const float4 y = *(const float4*)(sO + ((w0 + w) * kTR + rr) * 128 + dim);
+        z = fmaf(sL[w0 + w][rr], f, z);
         v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
       }
       if (whole) store(r, dim, v, z);
       else {
         float* slot = parts + (2ll * blockIdx.x + (p.blk == 0 ? 1 : 0)) * kSlot + r * 132;
         __stcg((float4*)(slot + dim), v);
-        if (dim == 0) __stcg((float2*)(slot + 128), make_float2(top, z));
+        if (dim == 0) __stcg((float2*)(slot + 128), make_float2(up, z));
       }
     }
     if (!whole) {
-      __threadfence();
       bar_consumers(kW * 32);
       if (tid == 0) {
-        last_flag = atomicAdd(&tickets[p.first], 1) == p.last - p.first;
+        // the CTA's results before the ticket, the others' after it
+        int ticket;
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(&tickets[p.first]) : "memory");
+        last_flag = ticket == p.last - p.first;
         if (last_flag) tickets[p.first] = 0;
-        __threadfence();
       }
       bar_consumers(kW * 32);
       if (last_flag) {
@@ -632,7 +625,6 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 template <int kR, bool kBias, bool kSparse>
 int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const int* blocks, int m, float* O,
                 RowStrides os, void* ws, cudaStream_t st) {
-  using Cfg = RowsCfg<kR>;
   CUtensorMap mK, mV;
   if (!encode_u8_map_3d(&mK, c.K, c.cap, (uint64_t)c.S * c.H, kCB) ||
       !encode_u8_map_3d(&mV, c.V, c.cap, (uint64_t)c.S * c.H, kCB))
@@ -647,10 +639,10 @@ int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const i
   d.m = m;
   d.causal = q.causal;
   auto kern = cache_rows_kernel<kR, kBias, kSparse>;
-  const int smem = Cfg::kSmem + (kSparse ? 0 : (c.S + 1) * (int)sizeof(int));
+  const int smem = RowsCfg<kR>::kSmem + (kSparse ? 0 : (c.S + 1) * (int)sizeof(int));
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
   const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
-  kern<<<ctas, Cfg::kThreads, smem, st>>>(mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
+  kern<<<ctas, kRowsThreads, smem, st>>>(mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
                                           (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
   return 1;
 }
