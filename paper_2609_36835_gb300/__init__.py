@@ -475,6 +475,7 @@ class Cache8:
         _on_one_cuda_device(K=self.K, V=self.V, k_scale=self.k_scale, v_scale=self.v_scale, bounds=self.bounds,
                             tail=self.tail, tail_amax=self.tail_amax, len=self.len, bias=self.bias, state=self.state)
         object.__setattr__(self, "_c", _Cache8(S, H, cap, d, *[_ptr(getattr(self, n)) for n, _ in _Cache8._fields_[4:]]))
+        object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
     @property
     def capacity(self) -> int:
@@ -542,10 +543,15 @@ def _current_handle(device) -> int:
     return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
-def _same_device(cache: "Cache8", **tensors):
-    for name, x in tensors.items():
-        if x is not None and x.device != cache.K.device:
-            raise ValueError("arckv: %s is on %s but the cache on %s" % (name, x.device, cache.K.device))
+def _counts_ptr(name: str, x, cache: "Cache8"):
+    """Address of an int32 [S] argument on the cache's device, None for none."""
+    import torch
+    if x is None:
+        return None
+    if x.dtype != torch.int32 or x.shape != cache.len.shape or x.device != cache.len.device or not x.is_contiguous():
+        raise ValueError("arckv: %s must be a dense int32 tensor of shape %s on %s, got %s %s on %s"
+                         % (name, tuple(cache.len.shape), cache.len.device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr()
 
 
 def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream=None, check: bool = True) -> None:
@@ -554,28 +560,27 @@ def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream
     over rejected tokens of the newest block.  counts [S] int32: how many of the n rows each sequence takes.
     With check=False the call only enqueues, and ``arckv_query_status(cache.state)`` reports errors."""
     import torch
-    c = cache._c
-    n = K.shape[2] if K.dim() == 4 else -1
-    for name, x in (("K", K), ("V", V)):
-        if x.dtype != K.dtype or x.dtype not in (torch.bfloat16, torch.float32) or tuple(x.shape) != (c.S, c.H, n, 128):
-            raise ValueError("arckv: %s must be bfloat16 or float32 (K and V alike) of shape %s, got %s %s"
-                             % (name, (c.S, c.H, "n", 128), x.dtype, tuple(x.shape)))
+    c, dev, shape, dtype = cache._c, cache.K.device, K.shape, K.dtype
+    if (len(shape) != 4 or shape[0] != c.S or shape[1] != c.H or shape[3] != 128 or V.shape != shape or V.dtype != dtype
+            or (dtype != torch.bfloat16 and dtype != torch.float32)):
+        raise ValueError("arckv: K and V must be bfloat16 or float32 of shape %s, got %s %s and %s %s"
+                         % ((c.S, c.H, "n", 128), dtype, tuple(shape), V.dtype, tuple(V.shape)))
+    if K.device != dev or V.device != dev:
+        raise ValueError("arckv: K is on %s, V on %s but the cache on %s" % (K.device, V.device, dev))
+    n = shape[2]
     if bias is not None:
         if cache.bias is None:
             raise ValueError("arckv: this cache holds no bias")
         _expect("bias", bias, (torch.float32,), (c.S, c.H, n))
-    for name, x in (("at", at), ("counts", counts)):
-        if x is not None:
-            _expect(name, x, (torch.int32,), (c.S,))
-    _same_device(cache, K=K, V=V, bias=bias, at=at, counts=counts)
+        _on_one_cuda_device(cache=cache.K, bias=bias)
+    at_ptr, counts_ptr = _counts_ptr("at", at, cache), _counts_ptr("counts", counts, cache)
     if n == 0:
         return
-    dev = cache.K.device
     handle = (_current_handle(dev) if stream is None else
               _side_stream(stream, dev, K, V, bias, at, counts, cache.K, cache.V).cuda_stream)
-    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if K.dtype == torch.float32 else 0)
-    st = load_library().arckv_cache_append(ctypes.byref(c), n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
-                                           _strides3("V", V, 3), _ptr(bias), _ptr(at), _ptr(counts), flags, handle)
+    flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
+    st = load_library().arckv_cache_append(cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
+                                           _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr, flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_append")
 
@@ -584,64 +589,68 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
     """The values that `count` tokens from `start` on stand for (negative: from each sequence's end), as a pair
     K, V [S, H, count, 128] in bf16 (or dtype=torch.float32); tokens that a sequence does not hold are zero."""
     import torch
-    c = cache._c
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
-    dev = cache.K.device
+    c, dev = cache._c, cache.K.device
     if stream is not None:   # the outputs belong to the stream that fills them
         stream = _side_stream(stream, dev, cache.K, cache.V)
         with torch.cuda.stream(stream):
             return cache_read(cache, start, count, dtype=dtype, check=check)
     K = torch.empty((c.S, c.H, max(count, 0), 128), dtype=dtype, device=dev)
-    V = torch.empty((c.S, c.H, max(count, 0), 128), dtype=dtype, device=dev)
+    V = torch.empty_like(K)
     if count == 0:
         return K, V
     handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
-    st = load_library().arckv_cache_read(ctypes.byref(c), start, count, K.data_ptr(), V.data_ptr(), flags, handle)
+    st = load_library().arckv_cache_read(cache._ref, start, count, K.data_ptr(), V.data_ptr(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_read")
     return K, V
 
 
 def _check_queries(cache: Cache8, Q):
+    """Positions and query heads of Q, which must fit the cache."""
     import torch
-    c = cache._c
-    if Q.dim() != 5 or Q.dtype != torch.bfloat16 or Q.shape[0] != c.S or Q.shape[1] != c.H or Q.shape[4] != 128:
+    c, shape = cache._c, Q.shape
+    if len(shape) != 5 or Q.dtype != torch.bfloat16 or shape[0] != c.S or shape[1] != c.H or shape[4] != 128:
         raise ValueError("arckv: Q must be bfloat16 of shape %s, got %s %s"
-                         % ((c.S, c.H, "n_pos", "G", 128), Q.dtype, tuple(Q.shape)))
+                         % ((c.S, c.H, "n_pos", "G", 128), Q.dtype, tuple(shape)))
     if Q.device != cache.K.device:
         raise ValueError("arckv: Q is on %s but the cache on %s" % (Q.device, cache.K.device))
-    return c
+    return shape[2], shape[3]
 
 
 def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, causal: bool = False, out=None, ws=None,
                  stream=None, check: bool = True):
     """O = softmax(scale Q K^T + bias) V over the cache for Q [S, H, n_pos, G, 128] bf16 (the last two dimensions
-    dense); returns fp32 of the same shape, or fills `out`.  causal: the positions are the newest n_pos tokens, and
+    dense); returns fp32 of Q's shape and layout, or fills `out`.  causal: the positions are the newest n_pos tokens, and
     each sees the tokens up to itself.  blocks [S, H, n_pos, m] int32: the only blocks that each position reads
     (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often."""
     import torch
-    c = _check_queries(cache, Q)
+    n_pos, G = _check_queries(cache, Q)
     if stream is not None:   # a workspace and an output made here belong to the stream that fills them
         stream = _side_stream(stream, Q.device, Q, blocks, out, ws, cache.K, cache.V)
         with torch.cuda.stream(stream):
             return cache_attend(cache, Q, logit_scale, blocks=blocks, causal=causal, out=out, ws=ws, check=check)
-    _, _, n_pos, G, _ = Q.shape
+    m = 0
     if blocks is not None:
-        _expect("blocks", blocks, (torch.int32,), (c.S, c.H, n_pos, None))
-        _same_device(cache, blocks=blocks)
+        shape = blocks.shape
+        if (len(shape) != 4 or blocks.dtype != torch.int32 or shape[:3] != Q.shape[:3] or blocks.device != Q.device or
+                not blocks.is_contiguous()):
+            raise ValueError("arckv: blocks must be a dense int32 tensor of shape %s on %s, got %s %s on %s"
+                             % (tuple(Q.shape[:3]) + ("m",), Q.device, blocks.dtype, tuple(shape), blocks.device))
+        m = shape[3]
     if ws is None:
         ws = cache_workspace(cache, n_pos, G)
     if out is None:
-        out = torch.empty(Q.shape, dtype=torch.float32, device=Q.device)
+        out = torch.empty_like(Q, dtype=torch.float32)
     elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
         raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = load_library().arckv_cache_attend(ctypes.byref(c), n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3),
-                                           _ptr(blocks), 0 if blocks is None else blocks.shape[3], out.data_ptr(),
+    st = load_library().arckv_cache_attend(cache._ref, n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3),
+                                           _ptr(blocks), m, out.data_ptr(),
                                            _strides3("out", out, 3), ws.data_ptr(), ws.numel(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_attend")
@@ -654,19 +663,18 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: in
     first keep_first, the newest keep_last and those whose logits can be largest.  Q, causal and ws as for
     ``cache_attend``."""
     import torch
-    c = _check_queries(cache, Q)
+    n_pos, G = _check_queries(cache, Q)
     if stream is not None:
         stream = _side_stream(stream, Q.device, Q, ws, cache.K, cache.V)
         with torch.cuda.stream(stream):
             return cache_select(cache, Q, m, keep_first=keep_first, keep_last=keep_last, causal=causal, ws=ws,
                                 check=check)
-    _, _, n_pos, G, _ = Q.shape
     if ws is None:
         ws = cache_workspace(cache, n_pos, G)
-    blocks = torch.empty((c.S, c.H, n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
+    blocks = torch.empty((Q.shape[0], Q.shape[1], n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = load_library().arckv_cache_select(ctypes.byref(c), n_pos, G, m, keep_first, keep_last, Q.data_ptr(),
+    st = load_library().arckv_cache_select(cache._ref, n_pos, G, m, keep_first, keep_last, Q.data_ptr(),
                                            _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags,
                                            handle)
     if st != 0:

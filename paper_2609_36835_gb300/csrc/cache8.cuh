@@ -43,6 +43,29 @@ struct CacheShares {
   }
 };
 
+// ---- launches that overlap their predecessor's end ---------------------------
+// The kernels of this file's callers start while the kernel before them on the
+// stream is still ending: pdl_wait() comes before their first access to memory
+// that another kernel may write or read, and pdl_trigger() lets the next one in
+// as soon as all CTAs have started.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_pdl(void (*kern)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
 // ---- launchers (each returns the kernels it enqueued, or -1) ---------------
 int launch_cache_append(const arckv_cache8& c, int n, bool f32, const void* K, RowStrides ks, const void* V,
                         RowStrides vs, const float* bias, const int* at, const int* counts, cudaStream_t st);

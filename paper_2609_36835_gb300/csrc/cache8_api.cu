@@ -86,7 +86,8 @@ arckv_status arckv_cache_append(const arckv_cache8* c, int32_t n, const void* K,
       !row_strides(V, v_strides, c->H, n, 128, f32 ? 4 : 2, &vs))
     return ARCKV_ERR_INVALID_ARG;
   cudaGetLastError();
-  launch_cache_append(*c, n, f32, K, ks, V, vs, bias, at, counts, (cudaStream_t)stream);
+  if (launch_cache_append(*c, n, f32, K, ks, V, vs, bias, at, counts, (cudaStream_t)stream) < 0)
+    return ARCKV_ERR_CUDA;
   return finish(c->state, flags, stream);
 }
 
@@ -98,7 +99,8 @@ arckv_status arckv_cache_read(const arckv_cache8* c, int32_t start, int32_t coun
   if (count < 1 || count > (1 << 26) || start < -(1 << 26) || start > (1 << 26)) return ARCKV_ERR_SHAPE;
   if ((!K_out && !V_out) || misaligned(K_out) || misaligned(V_out)) return ARCKV_ERR_INVALID_ARG;
   cudaGetLastError();
-  launch_cache_read(*c, start, count, (flags & ARCKV_FLAG_F32) != 0, K_out, V_out, (cudaStream_t)stream);
+  if (launch_cache_read(*c, start, count, (flags & ARCKV_FLAG_F32) != 0, K_out, V_out, (cudaStream_t)stream) < 0)
+    return ARCKV_ERR_CUDA;
   return finish(c->state, flags, stream);
 }
 
@@ -130,7 +132,7 @@ arckv_status arckv_cache_select(const arckv_cache8* c, int32_t n_pos, int32_t G,
     return ARCKV_ERR_SHAPE;
   if (!blocks || misaligned(blocks, 4)) return ARCKV_ERR_INVALID_ARG;
   cudaGetLastError();
-  launch_cache_select(*c, q, m, keep_first, keep_last, blocks, ws, (cudaStream_t)stream);
+  if (launch_cache_select(*c, q, m, keep_first, keep_last, blocks, ws, (cudaStream_t)stream) < 0) return ARCKV_ERR_CUDA;
   return finish(ws, flags, stream);
 }
 

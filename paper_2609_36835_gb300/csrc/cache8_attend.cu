@@ -210,6 +210,8 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     abort_flag = 0;
     tc::mbar_fence_init();
   }
+  pdl_trigger();
+  pdl_wait();
   __shared__ int s_cut;   // blocks of a part (0: equal shares)
   if (warp == kW) {   // blocks, or parts, before each sequence, by warp scan
     if (lane == 0) {
@@ -642,9 +644,9 @@ int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const i
   const int smem = RowsCfg<kR>::kSmem + (kSparse ? 0 : (c.S + 1) * (int)sizeof(int));
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
   const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
-  kern<<<ctas, kRowsThreads, smem, st>>>(mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
-                                          (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
-  return 1;
+  const cudaError_t e = launch_pdl(kern, dim3(ctas), kRowsThreads, smem, st, mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
+                                   (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
+  return e == cudaSuccess ? 1 : -1;
 }
 
 template <int kR>

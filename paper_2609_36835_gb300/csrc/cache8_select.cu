@@ -23,6 +23,7 @@ constexpr int kScoreRows = 64;       // query rows whose codes a CTA holds at a 
 // score[item][b] of every candidate block; CTA = (sequence x head and 128 blocks, `per` positions).
 __global__ void __launch_bounds__(kScoreThreads) cache_score_kernel(const arckv_cache8 c, CacheQuery q, int per,
                                                                     int tiles, float* score) {
+  pdl_wait();
   const int nblk = c.cap / kCB, p0 = blockIdx.y * per, p1 = min(p0 + per, q.n_pos);
   const long long sh = blockIdx.x / tiles;
   const int h = (int)(sh % c.H), s = (int)(sh / c.H), len = cache_len(c, s);
@@ -117,6 +118,7 @@ __global__ void __launch_bounds__(kT == 32 ? 128 : kT) cache_pick_kernel(const a
   constexpr int kGroups = kT == 32 ? 4 : 1;
   __shared__ int s_part[kT == 32 ? 1 : 2 * (kT / 32)];
   __shared__ int s_scan[kT == 32 ? 1 : kT / 32];
+  pdl_wait();
   const long long item = (long long)blockIdx.x * kGroups + threadIdx.x / kT;
   if (item >= items) return;   // whole warps (kT = 32) or never
   const int tid = threadIdx.x % kT, lane = threadIdx.x & 31, nblk = c.cap / kCB;
@@ -209,11 +211,11 @@ __global__ void __launch_bounds__(kT == 32 ? 128 : kT) cache_pick_kernel(const a
 }
 
 template <int kT, int kPer>
-void launch_pick(const arckv_cache8& c, const CacheQuery& q, const float* score, int m, int keep_first, int keep_last,
+cudaError_t launch_pick(const arckv_cache8& c, const CacheQuery& q, const float* score, int m, int keep_first, int keep_last,
                  long long items, int* blocks, cudaStream_t st) {
   const int groups = kT == 32 ? 4 : 1;
-  cache_pick_kernel<kT, kPer><<<(unsigned)((items + groups - 1) / groups), kT * groups, 0, st>>>(
-      c, q, score, m, keep_first, keep_last, items, blocks);
+  return launch_pdl(cache_pick_kernel<kT, kPer>, dim3((unsigned)((items + groups - 1) / groups)), kT * groups, 0, st, c, q,
+                    score, m, keep_first, keep_last, items, blocks);
 }
 
 }  // namespace
@@ -233,13 +235,15 @@ int launch_cache_select(const arckv_cache8& c, const CacheQuery& q, int m, int k
                                                                     cdiv((long long)q.n_pos * q.G, kScoreRows)));
   const int per = cdiv(q.n_pos, std::min(tiles, q.n_pos));
   const long long heads = (long long)c.S * c.H;
-  cache_score_kernel<<<dim3((unsigned)(heads * bt), cdiv(q.n_pos, per)), kScoreThreads, 0, st>>>(c, q, per, bt, score);
-  if (nblk <= 256) launch_pick<32, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
-  else if (nblk <= 1024) launch_pick<128, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
-  else if (nblk <= 4096) launch_pick<512, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
-  else if (nblk <= 16384) launch_pick<1024, 16>(c, q, score, m, keep_first, keep_last, items, blocks, st);
-  else launch_pick<1024, 0>(c, q, score, m, keep_first, keep_last, items, blocks, st);
-  return 2;
+  cudaError_t e = launch_pdl(cache_score_kernel, dim3((unsigned)(heads * bt), cdiv(q.n_pos, per)), kScoreThreads, 0, st, c,
+                             q, per, bt, score);
+  if (e != cudaSuccess) return -1;
+  if (nblk <= 256) e = launch_pick<32, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
+  else if (nblk <= 1024) e = launch_pick<128, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
+  else if (nblk <= 4096) e = launch_pick<512, 8>(c, q, score, m, keep_first, keep_last, items, blocks, st);
+  else if (nblk <= 16384) e = launch_pick<1024, 16>(c, q, score, m, keep_first, keep_last, items, blocks, st);
+  else e = launch_pick<1024, 0>(c, q, score, m, keep_first, keep_last, items, blocks, st);
+  return e == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace arckv

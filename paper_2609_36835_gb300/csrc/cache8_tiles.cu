@@ -305,7 +305,9 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     tc::mbar_fence_init();
   }
   if (warp == kSoft + 4) tc::tmem_alloc(&tmem_slot, 256 * kT);
-  for (int s = tid; s < c.S; s += Cfg::kThreads) {   // steps of one head of each sequence
+  pdl_trigger();
+  pdl_wait();
+  for (int s = tid; s < c.S; s += Cfg::kThreads) {   // blocks of one head's tiles of each sequence
     const int len = cache_len(c, s);
     long long n = 0;
     if (d.causal)
@@ -879,9 +881,10 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
   auto kern = cache_tiles_kernel<kT, kBias>;
   const int smem = Cfg::kSmem + (c.S + 1) * (int)sizeof(long long);
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
-  kern<<<std::min(tc_gemm_sm_count(), kCacheMaxCtas), Cfg::kThreads, smem, st>>>(
-      c, d, q.Q, q.qs, scale, O, os, (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
-  return 1;
+  const cudaError_t e =
+      launch_pdl(kern, dim3(std::min(tc_gemm_sm_count(), kCacheMaxCtas)), Cfg::kThreads, smem, st, c, d, q.Q, q.qs, scale, O,
+                 os, (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
+  return e == cudaSuccess ? 1 : -1;
 }
 
 }  // namespace
