@@ -71,16 +71,16 @@ __global__ void __launch_bounds__(kScoreThreads) cache_score_kernel(const arckv_
     __syncthreads();
     if (b >= cand) continue;
     for (int r = 0; r < nr; ++r) {
-      int d0 = 0, d1 = 0;   // two chains
+      int d0 = 0, d1 = 0, d2 = 0, d3 = 0;   // four chains
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int4 v = *(const int4*)&s_q[r][4 * e];
         d0 = __dp4a(v.x, w[e].x, d0);
         d1 = __dp4a(v.y, w[e].y, d1);
-        d0 = __dp4a(v.z, w[e].z, d0);
-        d1 = __dp4a(v.w, w[e].w, d1);
+        d2 = __dp4a(v.z, w[e].z, d2);
+        d3 = __dp4a(v.w, w[e].w, d3);
       }
-      best = fmaxf(best, __fmul_rn(__fmul_rn(s_scale[r], (float)(d0 + d1)), ks));
+      best = fmaxf(best, __fmul_rn(__fmul_rn(s_scale[r], (float)(d0 + d1 + (d2 + d3))), ks));
       if (--left == 0) {
         score[(sh * q.n_pos + p) * nblk + b] = best;
         best = -INFINITY;
@@ -118,11 +118,12 @@ __global__ void __launch_bounds__(kT == 32 ? 128 : kT) cache_pick_kernel(const a
   constexpr int kGroups = kT == 32 ? 4 : 1;
   __shared__ int s_part[kT == 32 ? 1 : 2 * (kT / 32)];
   __shared__ int s_scan[kT == 32 ? 1 : kT / 32];
+  __shared__ unsigned int s_ends[2][kT == 32 ? 1 : kT / 32];
   pdl_wait();
   const long long item = (long long)blockIdx.x * kGroups + threadIdx.x / kT;
   if (item >= items) return;   // whole warps (kT = 32) or never
   const int tid = threadIdx.x % kT, lane = threadIdx.x & 31, nblk = c.cap / kCB;
-  const int pos = (int)(item % q.n_pos), s = (int)(item / q.n_pos / c.H);
+  const int sh = (int)item / q.n_pos, pos = (int)item - sh * q.n_pos, s = sh / c.H;   // (items are below 2^31)
   const int cand = (visible_tokens(cache_len(c, s), q.n_pos, pos, q.causal) + kCB - 1) / kCB;
   const float* sc = score + item * nblk;
   int* out = blocks + item * m;
@@ -153,8 +154,33 @@ __global__ void __launch_bounds__(kT == 32 ? 128 : kT) cache_pick_kernel(const a
     return n;
   };
   GroupSum<kT> sum{s_part};
-  // the largest threshold that at least m keys reach: lo is reached by m, hi + 1 is not
-  unsigned int lo = 1u, hi = 0xffffffffu;
+  // the largest threshold that at least m keys reach: lo is reached by m, hi + 1 is not.  It lies between the least and
+  // the largest key that is not forced, or right above (where the forced ones are m).
+  unsigned int lo = 0xffffffffu, hi = 0u;
+  auto span = [&](unsigned int key) {
+    if (key == 0u || key == 0xffffffffu) return;
+    lo = min(lo, key);
+    hi = max(hi, key);
+  };
+  if (kPer > 0) {
+#pragma unroll
+    for (int i = 0; i < (kPer > 0 ? kPer : 1); ++i) span(reg[i]);
+  } else {
+    for (int i = 0; i < per; ++i) span(load(b0 + i));
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (kT > 32) {
+    if (lane == 0) {
+      s_ends[0][tid >> 5] = lo;
+      s_ends[1][tid >> 5] = hi;
+    }
+    __syncthreads();
+    lo = __reduce_min_sync(0xffffffffu, lane < kT / 32 ? s_ends[0][lane] : 0xffffffffu);
+    hi = __reduce_max_sync(0xffffffffu, lane < kT / 32 ? s_ends[1][lane] : 0u);
+  }
+  if (lo > hi) lo = hi = 1u;   // all candidates are forced (and more than m: not with keep_first + keep_last <= m)
+  hi = hi == 0xffffffffu ? hi : hi + 1u;
   bool exact = false;   // exactly m keys reach lo
   while (lo < hi && !exact) {
     const unsigned int mid = lo + ((hi - lo) >> 1) + 1u;
@@ -229,10 +255,11 @@ int launch_cache_select(const arckv_cache8& c, const CacheQuery& q, int m, int k
   const long long items = (long long)c.S * c.H * q.n_pos;
   const int nblk = c.cap / kCB, bt = cdiv(nblk, kScoreThreads);
   float* score = (float*)((char*)ws + ARCKV_CACHE_WS_HEADER);
-  // positions of a CTA: as many as leave four CTAs an SM, but at least 64 rows, which pay for the bounds' loads
+  // positions of a CTA: as many as leave four CTAs an SM, but at least 16 rows, which pay for the bounds' loads (with
+  // 64, 128 positions over 256 blocks of 8 heads took 32 us instead of XXX)
   const long long want = 4ll * tc_gemm_sm_count();
   const int tiles = (int)std::max<long long>(1, std::min<long long>(want / std::max(1ll, (long long)bt * c.S * c.H),
-                                                                    cdiv((long long)q.n_pos * q.G, kScoreRows)));
+                                                                    cdiv((long long)q.n_pos * q.G, kScoreRows / 4)));
   const int per = cdiv(q.n_pos, std::min(tiles, q.n_pos));
   const long long heads = (long long)c.S * c.H;
   cudaError_t e = launch_pdl(cache_score_kernel, dim3((unsigned)(heads * bt), cdiv(q.n_pos, per)), kScoreThreads, 0, st, c,
