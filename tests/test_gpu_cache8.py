@@ -485,3 +485,18 @@ def test_compact_cache_in_8_bits():
     full = pk.attend(Q.view(H, 4, 128), C_k, beta, C_v)
     # a code is off by at most half a step of a / 127 with a near 4.4: about 0.5 % of a value's magnitude
     assert rel(host(O).reshape(H, 4, 128), host(full)) <= 0.03
+
+
+def test_example_runs_them_together():
+    """The decode example: compaction, 8-bit caches, selection and attention in a replayed graph."""
+    import importlib.util
+    from pathlib import Path
+    path = Path(__file__).resolve().parent.parent / "examples" / "decode_8bit.py"
+    spec = importlib.util.spec_from_file_location("decode_8bit", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    f = mod.main(["--context", "1500", "--steps", "70", "--blocks", "24"])
+    assert f["tokens"] == 1570 and f["compact_tokens"] == 220
+    # a code is off by at most half a step: 0.5 / 127 of a block's magnitude, which outlier channels of 8 times the rest
+    # (keys) and single values of 4 deviations (values) set; logits of |q||k|/sqrt(d) up to 60 move by a few tenths
+    assert max(f["full_error"], f["compact_error"], f["sparse_error"]) <= 0.2
