@@ -13,8 +13,8 @@
 //    one item only.  An item in several CTAs is finished by the one that comes
 //    last (a ticket), which adds the parts up in CTA order.
 //  - Two producer warps stream the blocks' keys and values (64 x 128 codes, 8 KB
-//    each, 128-byte swizzle) through rings in shared memory by TMA.  Each of ten
-//    consumer warps takes whole blocks of its own, with its own running maximum,
+//    each, 128-byte swizzle) through rings in shared memory by TMA.  Each
+//    consumer warp takes whole blocks of its own, with its own running maximum,
 //    sum and output: no barrier between warps until the item ends.  A warp gives
 //    its keys' stage back before the softmax, so that the next block's keys come
 //    in while it works on the values, and its values while on those keys.
@@ -47,15 +47,16 @@ struct RowsShape {
   bool causal;
 };
 
-constexpr int kW = 10;   // consumer warps; with the producers a multiple of four, as registers are dealt out to the SM's quarters
+// Consumer warps: with the two producers at most 12 warps, as registers are dealt out to the SM's quarters (168 a
+// thread).  Ten where HBM is the bound; eight for 9 to 16 rows, where the warps' own work is and ten would leave two
+// quarters of the SM a third consumer (12 rows over 64 x 8 compact caches of 1641: 73.6 us with ten, 70.5 with eight;
+// 64 x 8K decode of 4 rows: 123.9 and 127.2).
 // Stages of a ring: one for each consumer warp (two for each pair of warps that share blocks), so that a stage is
 // always consumed by the same warps.  A warp that came to a stage while an earlier block of another warp was still on
 // its way there would take the phase before that one for its own (a wait sees a phase's parity only).
-constexpr int kSt = kW;
-constexpr int kRowsThreads = 32 * (kW + 2);
-
 template <int kR>
 struct RowsCfg {
+  static constexpr int kW = kR == 16 ? 8 : 10, kSt = kW, kThreads = 32 * (kW + 2);
   static constexpr int kTiles = kR == 16 ? 2 : 1;   // tiles of 8 rows; warps w and w + kW / 2 share blocks, a tile each
   static constexpr int kTeams = kW / kTiles;        // warps, or pairs, that take blocks in turn
   static constexpr int kTileRows = kR < 8 ? kR : 8;
@@ -64,14 +65,14 @@ struct RowsCfg {
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 // Bytes (0, 1) or (2, 3) of w, codes + 128, as two f16 codes.
@@ -180,12 +181,12 @@ struct Walk {
 };
 
 template <int kR, bool kBias, bool kSparse>
-__global__ void __launch_bounds__(kRowsThreads, 1)
+__global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap mK, const __grid_constant__ CUtensorMap mV,
                       const arckv_cache8 c, RowsShape d, const bf16* Q, RowStrides qs, float scale, const int* blocks,
                       float* O, RowStrides os, float* parts, int* tickets, DevStatus* stt) {
   using Cfg = RowsCfg<kR>;
-  constexpr int kTR = Cfg::kTileRows, kTeams = Cfg::kTeams;
+  constexpr int kTR = Cfg::kTileRows, kTeams = Cfg::kTeams, kW = Cfg::kW, kSt = Cfg::kSt;
   extern __shared__ __align__(1024) unsigned char smraw[];
   unsigned char* ringK = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
   unsigned char* ringV = ringK + kSt * kTileBytes;
@@ -644,7 +645,7 @@ int launch_rows(const arckv_cache8& c, const CacheQuery& q, float scale, const i
   const int smem = RowsCfg<kR>::kSmem + (kSparse ? 0 : (c.S + 1) * (int)sizeof(int));
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
   const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
-  const cudaError_t e = launch_pdl(kern, dim3(ctas), kRowsThreads, smem, st, mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
+  const cudaError_t e = launch_pdl(kern, dim3(ctas), RowsCfg<kR>::kThreads, smem, st, mK, mV, c, d, q.Q, q.qs, scale, blocks, O, os,
                                    (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
   return e == cudaSuccess ? 1 : -1;
 }
