@@ -12,7 +12,7 @@
 //                         in place: the f16 pair hi + lo of 32 keys takes the 32
 //                         columns that their logits had; P is the MMA's operand
 //                         from TMEM
-// P V runs once for hi and once for lo, which keeps 21 bits of a weight: three
+// P V runs once for hi and once for lo, which keeps 22 bits of a weight: three
 // units of MMA work where f16 weights would do with two, so 2/3 of the pipe's
 // peak is the most that the fp32 output allows.  A tile has two buffers of S in
 // TMEM: the softmax of one block runs beside the products of its neighbours.  (With
@@ -193,6 +193,15 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// x - h, exactly, in one mixed-precision operation each.
+__device__ __forceinline__ float2 minus_f16(float2 x, __half2 h) {
+  float2 d;
+  asm("{\n\t.reg .b16 p, q, m;\n\tmov.b32 {p, q}, %2;\n\tmov.b16 m, 0xBC00;\n\t"   // -1
+      "fma.rn.f32.f16 %0, p, m, %3;\n\tfma.rn.f32.f16 %1, q, m, %4;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "r"(*(const uint32_t*)&h), "f"(x.x), "f"(x.y));
   return d;
 }
 template <int kN>
@@ -729,11 +738,10 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             x.x = ex2_approx(x.x);
             x.y = ex2_approx(x.y);
             sum[k] = add2(sum[k], x);
-            // hi: the leading 11 bits, exact in f16; lo: the rest, at most 2^-10 of w, rounded to 11 bits
-            const float2 hi = make_float2(__uint_as_float(__float_as_uint(x.x) & 0xffffe000u),
-                                          __uint_as_float(__float_as_uint(x.y) & 0xffffe000u));
-            const float2 lo = fma2(hi, make_float2(-1.f, -1.f), x);
-            const __half2 h2 = __floats2half2_rn(hi.x, hi.y), l2 = __floats2half2_rn(lo.x, lo.y);
+            // hi: x rounded to 11 bits; lo: the rest, at most 2^-11 of x, rounded to 11 bits
+            const __half2 h2 = __floats2half2_rn(x.x, x.y);
+            const float2 lo = minus_f16(x, h2);
+            const __half2 l2 = __floats2half2_rn(lo.x, lo.y);
             hr[e] = *(const uint32_t*)&h2;
             lr[e] = *(const uint32_t*)&l2;
           }
