@@ -39,6 +39,7 @@ namespace {
 
 constexpr int kRowsMax = 16;                 // more rows of a head go to the tcgen05 kernel
 constexpr int kTileBytes = kCB * 128;        // codes of one block, K or V
+constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 
 struct RowsShape {
   int H, n_pos, G, nblk, cap;   // nblk: blocks of the capacity
@@ -60,7 +61,7 @@ struct RowsCfg {
   static constexpr int kTiles = kR == 16 ? 2 : 1;   // tiles of 8 rows; warps w and w + kW / 2 share blocks, a tile each
   static constexpr int kTeams = kW / kTiles;        // warps, or pairs, that take blocks in turn
   static constexpr int kTileRows = kR < 8 ? kR : 8;
-  static constexpr int kSmem = kSt * (2 * kTileBytes + kCB * 4) + kW * kTileRows * 128 * 4 + 1024;
+  static constexpr int kSmem = kSt * (2 * kTileBytes + kCB * 4) + kW * kTileRows * kRowO * 4 + 1024;
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -75,12 +76,18 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// Bytes (0, 1) or (2, 3) of w, codes + 128, as two f16 codes.
-template <int kHi>
+// Two bytes of w, codes + 128, as f16 codes: 1024 + u is 0x6400 | u.
+template <unsigned kPick>
 __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
-  const uint32_t y = __byte_perm(w, 0x64646464u, kHi ? 0x4342 : 0x4140);
+  const uint32_t y = __byte_perm(w, 0x64646464u, kPick);
   const __half2 z = __hsub2(*(const __half2*)&y, __half2{__half_raw{0x6480}, __half_raw{0x6480}});
   return *(const uint32_t*)&z;
+}
+// Four 8 x 8 matrices of 16-bit units, transposed; lane 8i + r gives the address of row r of matrix i.
+__device__ __forceinline__ void load_transposed(uint32_t (&w)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(addr));
 }
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -191,8 +198,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   unsigned char* ringK = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
   unsigned char* ringV = ringK + kSt * kTileBytes;
   float* sBias = (float*)(ringV + kSt * kTileBytes);
-  float* sO = sBias + kSt * kCB;                                 // [warp][row of its tile][128]
-  int* pre = (int*)(sO + kW * kTR * 128);                        // dense: [S + 1]
+  float* sO = sBias + kSt * kCB;                                 // [warp][row of its tile][kRowO]
+  int* pre = (int*)(sO + kW * kTR * kRowO);                       // dense: [S + 1]
   __shared__ __align__(8) uint64_t fullK[kSt], emptyK[kSt], fullV[kSt], emptyV[kSt];
   __shared__ float sKs[kSt], sVs[kSt];
   __shared__ int sBlk[kSt];
@@ -335,6 +342,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   // --------------------------------------------------------------- consumers
   const int g = lane >> 2, t = lane & 3;
   const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
+  // this lane's row of a V tile (key lane & 15), and its 16-byte chunk (dims 32j + 16 (lane >> 4)) as stored for j = 0
+  const uint32_t v_row = (lane & 15) * 128, v_chunk = ((lane >> 4) ^ (lane & 7)) << 4;
   constexpr float kP15 = 15.f;   // weights carry a factor of 2^15
   int base = 0;                  // blocks of earlier runs
   bool ok = true;
@@ -422,7 +431,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
             for (int mt = 0; mt < 4; ++mt) {
               const uint32_t w = k == 0 ? a[mt].x : k == 1 ? a[mt].y : k == 2 ? a[mt].z : a[mt].w;
               const uint32_t w8 = k == 0 ? a8[mt].x : k == 1 ? a8[mt].y : k == 2 ? a8[mt].z : a8[mt].w;
-              mma_f16(s[mt], codes_f16<0>(w), codes_f16<0>(w8), codes_f16<1>(w), codes_f16<1>(w8), qf[4 * ch + k][0],
+              mma_f16(s[mt], codes_f16<0x4140>(w), codes_f16<0x4140>(w8), codes_f16<0x4342>(w), codes_f16<0x4342>(w8), qf[4 * ch + k][0],
                       qf[4 * ch + k][1]);
             }
           }
@@ -487,8 +496,9 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullV[st], (q / kSt) & 1, abortp, stt));
         if (!ok) break;
         const float vs = sVs[st];
-        const unsigned char* Vt = ringV + st * kTileBytes;
-        // ---- O^T += V^T P^T: lane (g, t) has dims 16g .. 16g + 15 of keys 2t, 2t + 1, 2t + 8, 2t + 9
+        const uint32_t vt = tc::smem_u32(ringV) + st * kTileBytes + v_row;
+        // ---- O^T += V^T P^T, 16 dims and 16 keys a product: a transposed 16-bit load gives lane (g, t) dims 2g, 2g + 1
+        // of keys 2t, 2t + 1 in one word; even dims are the product's rows 0 .. 7, odd ones 8 .. 15
         float acc[8][4];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
@@ -496,21 +506,16 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
           for (int e = 0; e < 4; ++e) acc[k][e] = 0.f;
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
-          const unsigned char* row = Vt + (mt * 16 + 2 * t) * 128;
-          const int c0 = (g ^ (2 * t)) << 4, c1 = (g ^ (2 * t + 1)) << 4;
-          const uint4 v0 = *(const uint4*)(row + c0), v1 = *(const uint4*)(row + 128 + c1);
-          const uint4 v8 = *(const uint4*)(row + 8 * 128 + c0), v9 = *(const uint4*)(row + 9 * 128 + c1);
-          const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-          const uint32_t w8[4] = {v8.x, v8.y, v8.z, v8.w}, w9[4] = {v9.x, v9.y, v9.z, v9.w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
+          for (int j = 0; j < 4; ++j) {   // dims 32j .. 32j + 31
+            uint32_t w[4];
+            load_transposed(w, vt + mt * (16 * 128) + ((j << 5) ^ v_chunk));
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {   // dims 16g + 4k + 2z, + 1
-              const uint32_t y = __byte_perm(w0[k], w1[k], z ? 0x7362 : 0x5140);
-              const uint32_t y8 = __byte_perm(w8[k], w9[k], z ? 0x7362 : 0x5140);
-              const uint32_t f0 = codes_f16<0>(y), f1 = codes_f16<1>(y), f2 = codes_f16<0>(y8), f3 = codes_f16<1>(y8);
-              mma_f16(acc[2 * k + z], f0, f1, f2, f3, ph[mt][0], ph[mt][1]);
-              if (kR != 4) mma_f16(acc[2 * k + z], f0, f1, f2, f3, pl[mt][0], pl[mt][1]);
+            for (int z = 0; z < 2; ++z) {
+              const uint32_t f0 = codes_f16<0x4240>(w[2 * z]), f1 = codes_f16<0x4341>(w[2 * z]);
+              const uint32_t f2 = codes_f16<0x4240>(w[2 * z + 1]), f3 = codes_f16<0x4341>(w[2 * z + 1]);
+              mma_f16(acc[2 * j + z], f0, f1, f2, f3, ph[mt][0], ph[mt][1]);
+              if (kR != 4) mma_f16(acc[2 * j + z], f0, f1, f2, f3, pl[mt][0], pl[mt][1]);
             }
           }
         }
@@ -548,9 +553,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       }
       if (r < kTR) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *(float4*)(sO + (warp * kTR + r) * 128 + 16 * g + 4 * k) =
-              make_float4(o[2 * k][i], o[2 * k][2 + i], o[2 * k + 1][i], o[2 * k + 1][2 + i]);
+        for (int k = 0; k < 8; ++k)
+          *(float2*)(sO + (warp * kTR + r) * kRowO + 16 * k + 2 * g) = make_float2(o[k][i], o[k][2 + i]);
       }
     }
     if (tid == 0) stop_flag = *abortp;   // one reading for all: the producers may raise the flag at any time
@@ -580,7 +584,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 #pragma unroll
       for (int w = 0; w < kTeams; ++w) {
         const float f = weight(sM[w0 + w][rr], up);
-        const float4 y = *(const float4*)(sO + ((w0 + w) * kTR + rr) * 128 + dim);
+        const float4 y = *(const float4*)(sO + ((w0 + w) * kTR + rr) * kRowO + dim);
         z = fmaf(sL[w0 + w][rr], f, z);
         v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
       }
