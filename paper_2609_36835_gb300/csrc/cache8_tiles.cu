@@ -42,6 +42,7 @@ constexpr int kStages = 4, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, 
 constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
+constexpr float kTiny = -40.f;                // log2 of the scale of a block of tiny values (see below)
 constexpr float kVsUnit = 0x1p-20f;           // sums are in units of kVsUnit / vs: the least vs, 2^-107, stays in range
 
 struct TileShape {
@@ -204,6 +205,11 @@ __device__ __forceinline__ float2 minus_f16(float2 x, __half2 h) {
       : "r"(*(const uint32_t*)&h), "f"(x.x), "f"(x.y));
   return d;
 }
+// x 2^by, where the factor alone may be out of range (a sum of weights beside values 2^126 as large).
+__device__ __forceinline__ float scaled(float x, float by) {
+  const float h = ex2_approx(0.5f * by);
+  return x * h * h;
+}
 template <int kN>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kN)); }
 template <int kN>
@@ -291,7 +297,6 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   // of buffer (parity of the block) 0 and 1: S written, P written, P V done
   __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
   __shared__ Meta meta[2 * kStages];
-  __shared__ float s_row[kT][2][128];   // of a row: largest |q| of each half, then its factor
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, stop_flag, last_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -534,6 +539,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
       const int row0 = g.tile * kRows + t * 128, h = (int)(g.sh - (long long)g.s * d.H), len = cache_len(c, g.s);
+      float row_fac;
       {   // the queries as f16, each row scaled by a power of two: here a lane is a row, and has 64 dims
         const int r = quarter * 32 + lane, row = row0 + r, pos = row / d.G, gq = row - pos * d.G;
         uint4 x[8];
@@ -553,13 +559,14 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             amax = fmaxf(amax, fmaxf(fabsf(z.x), fabsf(z.y)));
           }
         }
-        s_row[t][half][r] = amax;
+        float* half_max = (float*)(sQ + t * 2 * kHalf);   // (the products of the item before have been waited for)
+        half_max[half * 128 + r] = amax;
         tile_sync();
-        amax = fmaxf(amax, s_row[t][half ^ 1][r]);
+        amax = fmaxf(amax, half_max[(half ^ 1) * 128 + r]);
         tile_sync();
         const int ex = max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100);
         const float up = __uint_as_float((unsigned)(14 - ex + 127) << 23);
-        if (half == 0) s_row[t][0][r] = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
+        row_fac = __uint_as_float((unsigned)(ex - 14 + 127) << 23) * scale * (kBias ? 1.f : kLog2e);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const __nv_bfloat162* y = (const __nv_bfloat162*)&x[e];
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           *(uint4*)(sQ + (t * 2 + half) * kHalf + r * 128 + ((e ^ (r & 7)) << 4)) = *(const uint4*)&z[0];
         }
         tc::fence_proxy_async_smem();
-        tile_sync();   // the rows' factors are there
+        __syncwarp();
         if (lane == 0) tc::mbar_arrive(&qfull);
       }
       // products' factors (powers of two without biases, of e with them) and sight of this thread's two rows
@@ -582,7 +589,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = r_warp + (lane >> 2) + 8 * i, row = row0 + r;
-        fac[i] = s_row[t][0][r];
+        fac[i] = __shfl_sync(0xffffffffu, row_fac, half * 16 + (lane >> 2) + 8 * i);   // (r is a row of this warp's lanes)
         pos[i] = row / d.G;
         gq[i] = row - pos[i] * d.G;
         mine[i] = row < nrows;
@@ -648,7 +655,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         float v[32];
         tmem_ld_rows64(S, v);
         const Meta m = meta[q % (2 * kStages)];
-        const float f[2] = {fac[0] * m.ks, fac[1] * m.ks};
+        // (never zero: a masked product is -inf; a row of zeros over a block of zeros would come to 2^-220)
+        const float f[2] = {fmaxf(fac[0] * m.ks, 0x1p-126f), fmaxf(fac[1] * m.ks, 0x1p-126f)};
         tmem_wait_ld();
         settle(v);
         const bool edge = j0 - cl + kCB > see_min;
@@ -689,7 +697,9 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             // in units of log2: (x - ref) log2 e + lv - refv; differences of logits first, so that the type's lowest
             // value cancels against itself
             if (top != -INFINITY && (ref[k] == -INFINITY || fmaf(top - ref[k], kLog2e, m.lv - refv[k]) > kGrow)) {
-              alpha[k] = ref[k] == -INFINITY ? 0.f : ex2_approx(fmaf(ref[k] - top, kLog2e, refv[k] - m.lv));
+              const float by = ref[k] == -INFINITY ? -INFINITY : fmaf(ref[k] - top, kLog2e, refv[k] - m.lv);
+              alpha[k] = ex2_approx(by);
+              l[k] = scaled(l[k], by);
               ref[k] = top;
               refv[k] = m.lv;
               grows = true;
@@ -697,7 +707,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           } else {
             top = fmaf(top, f[k], m.lv);   // f > 0: the largest product is the largest logit
             if (top > ref[k] + kGrow || (ref[k] == -INFINITY && top != -INFINITY)) {
-              alpha[k] = ref[k] == -INFINITY ? 0.f : ex2_approx(ref[k] - top);
+              alpha[k] = ex2_approx(ref[k] - top);
+              l[k] = scaled(l[k], ref[k] - top);
               ref[k] = top;
               grows = true;
             }
@@ -724,6 +735,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           add[k] = make_float2(a, a);
           sum[k] = make_float2(0.f, 0.f);
         }
+        // Beside large values the weights of a block of tiny ones may all be below fp32's range, and their sum with them:
+        // it is then taken with weights 2^64 as large.
+        const bool tiny = m.lv < kTiny;
+        float lifted[2] = {0.f, 0.f};
+        if (tiny) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const int k = (e >> 1) & 1;
+            const float x = kBias ? fmaf(v[e] + base[k].x, kLog2e, add[k].x) : fmaf(v[e], f[k], add[k].x);
+            lifted[k] += ex2_approx(x + 64.f);
+          }
+        }
 #pragma unroll
         for (int ch = 0; ch < 2; ++ch) {   // 32 keys: 16 columns of hi, 16 of lo
           uint32_t hr[8], lr[8];
@@ -749,7 +772,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           tmem_st_pairs16(S + ch * 32 + 16, lr);
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) l[k] = fmaf(l[k], alpha[k], (sum[k].x + sum[k].y) * m.iv);
+        for (int k = 0; k < 2; ++k) l[k] = tiny ? fmaf(lifted[k], m.iv * 0x1p-64f, l[k]) : fmaf(sum[k].x + sum[k].y, m.iv, l[k]);
         tmem_wait_st();
         tc::fence_before_sync();
         __syncwarp();
@@ -833,7 +856,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 x[e] = __ldcg((const float4*)(p + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4));
-              float w[2], down[2];   // of the new part, of the sums
+              float w[2], down[2];   // of the new part, of the outputs so far
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 w[k] = 0.f;
@@ -845,12 +868,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
                 if (up > 0.f) {
                   w[k] = 1.f;
                   down[k] = top[k] == -INFINITY ? 0.f : ex2_approx(-up);
+                  z[k] = top[k] == -INFINITY ? st4[k].z : scaled(z[k], -up) + st4[k].z;
                   top[k] = st4[k].x;
                   topv[k] = st4[k].y;
                 } else {
                   w[k] = ex2_approx(up);
+                  z[k] += scaled(st4[k].z, up);
                 }
-                z[k] = fmaf(z[k], down[k], st4[k].z * w[k]);
               }
 #pragma unroll
               for (int e = 0; e < 4; ++e)

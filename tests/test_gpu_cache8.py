@@ -298,6 +298,73 @@ def test_values_far_apart_in_magnitude():
     check_attend(c, Q, pk.cache_attend(c, Q))
 
 
+@pytest.mark.parametrize("n_pos", [1, 4, 32, 70])
+@pytest.mark.parametrize("bias", [False, True])
+def test_zero_queries_over_zero_keys(n_pos, bias):
+    """All logits are zero, down to products of two factors of 2^-100: rows are means of the visible values."""
+    n = 200
+    k, v = torch.zeros(1, 2, n, 128, device="cuda"), rows(65, 1, 2, n, torch.float32)
+    c = pk.cache_alloc(1, 2, n, bias=bias)
+    pk.cache_append(c, k, v)
+    Q = torch.zeros(1, 2, n_pos, 4, 128, device="cuda", dtype=torch.bfloat16)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=True), True)
+
+
+@pytest.mark.parametrize("n_pos", [4, 32, 70])
+def test_values_far_apart_for_many_rows(n_pos):
+    """As above in causal rows, of which the first see only small values."""
+    n = 320
+    k, v = rows(66, 1, 1, n, torch.float32), rows(67, 1, 1, n, torch.float32, outliers=False)
+    v[0, 0, :64] = 0.0
+    v[0, 0, 64:128] *= 2.0 ** -60
+    v[0, 0, 256:] *= 2.0 ** 60
+    c = pk.cache_alloc(1, 1, n)
+    pk.cache_append(c, k, v)
+    Q = queries(68, c, n_pos, 4)
+    O = pk.cache_attend(c, Q, causal=True)
+    check_attend(c, Q, O, True)
+    K, ks, _, V, vs = held(c, 0, 0)
+    want = ref.attend(host(Q[0, 0]), ref.values(K, ks), ref.values(V, vs), SC, None, True)
+    assert rel(host(O[0, 0, 0]), want[0]) <= TOL      # each row by its own magnitude
+
+
+@pytest.mark.parametrize("n_pos", [1, 4, 32, 70])
+@pytest.mark.parametrize("bias", [False, True])
+def test_zeros_weigh_beside_large_values(n_pos, bias):
+    """Equal logits: a block of zeros takes its share of the weight, whatever the other block's magnitude."""
+    k, v = torch.zeros(1, 1, 128, 128, device="cuda"), rows(69, 1, 1, 128, torch.float32, outliers=False)
+    v[0, 0, :64] = 0.0
+    v[0, 0, 64:] *= 2.0 ** 60
+    c = pk.cache_alloc(1, 1, 128, bias=bias)
+    pk.cache_append(c, k, v)
+    Q = queries(70, c, n_pos, 4)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=False))
+
+
+@pytest.mark.parametrize("n_pos", [1, 4, 32, 70])
+@pytest.mark.parametrize("n", [320, 6400])
+def test_zeros_weigh_behind_large_values(n_pos, n):
+    """As above with the zeros last, in one piece and in parts of several CTAs."""
+    k, v = torch.zeros(1, 1, n, 128, device="cuda"), rows(71, 1, 1, n, torch.float32, outliers=False)
+    v[0, 0, :64] *= 2.0 ** 60
+    v[0, 0, 128:] = 0.0
+    c = pk.cache_alloc(1, 1, n)
+    pk.cache_append(c, k, v)
+    Q = queries(72, c, n_pos, 4)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=True), True)
+
+
+@pytest.mark.parametrize("G,n_pos,bias", [(4, 1, False), (8, 1, False), (16, 1, True), (4, 8, False), (4, 40, True)])
+def test_as_many_sequences_as_are_taken(G, n_pos, bias):
+    S = 4096
+    lens = [(37 * s) % 65 for s in range(S)]
+    c, _, _ = filled(73, lens, 1, cap=64, bias=bias)
+    Q = queries(74, c, n_pos, G)
+    O = pk.cache_attend(c, Q)
+    assert not host(O)[[s for s in range(S) if lens[s] == 0]].any()
+    check_attend(c, Q, O, heads=[(s, 0) for s in (0, 1, 2, 63, 1000, 2047, 2048, 4094, 4095)])
+
+
 @pytest.mark.parametrize("G,n_pos", [(4, 1), (4, 16), (8, 64)])
 def test_long_sequences_split_over_the_device(G, n_pos):
     lens = [20001, 64 * 150, 17]
