@@ -280,6 +280,16 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   return g;
 }
 
+// Two columns of two rows of the output, at o + at0 and o + at1.
+__device__ __forceinline__ void store_rows(float* o, long long at0, long long at1, bool row0, bool row1, float4 x,
+                                           DevStatus* stt) {
+  const float big = 3.402823466e38f;
+  if (row0) *(float2*)(o + at0) = make_float2(x.x, x.y);
+  if (row1) *(float2*)(o + at1) = make_float2(x.z, x.w);
+  if ((row0 && !(fabsf(x.x) <= big && fabsf(x.y) <= big)) || (row1 && !(fabsf(x.z) <= big && fabsf(x.w) <= big)))
+    set_status(stt, ARCKV_ERR_NONFINITE);
+}
+
 struct Meta {   // of a block
   float ks, lv, iv;   // scale of K, log2 and inverse (in units of kVsUnit) of V's
 };
@@ -287,7 +297,7 @@ struct Meta {   // of a block
 template <int kT, bool kBias>
 __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     cache_tiles_kernel(const arckv_cache8 c, TileShape d, const bf16* Q, RowStrides qs, float scale, float* O,
-                       RowStrides os, float* parts, int* tickets, DevStatus* stt) {
+                       RowStrides os, float* parts, int4* cuts, DevStatus* stt) {
   using Cfg = TileCfg<kT>;
   constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows;
   extern __shared__ unsigned char smraw[];
@@ -298,7 +308,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
   __shared__ Meta meta[2 * kStages];
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag, stop_flag, last_flag;
+  __shared__ int abort_flag, stop_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abortp = &abort_flag;
 
@@ -356,7 +366,17 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
 
   if (warp > kSoft + 5) {
-    regs_dec<Cfg::kRegsMma>();   // idle
+    // ------------------------ the item that begins here and goes on in other CTAs
+    regs_dec<Cfg::kRegsMma>();
+    if (warp == kSoft + 6) {
+      int4 cut = make_int4(0, 0, -1, 0);
+      if (active) {
+        const Segment g = segment_of(u1 - 1, d, c, pre, kRows);
+        const long long end = g.first + g.count;
+        if (end > u1 && g.first >= u0) cut = make_int4((int)g.sh, g.tile, sh.owner(end - 1), 0);
+      }
+      if (lane == 0) cuts[blockIdx.x] = cut;
+    }
   } else if (warp == kSoft + 5) {
     // ---------------------------------------------------------------- scales
     regs_dec<Cfg::kRegsMma>();
@@ -584,16 +604,12 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       }
       // products' factors (powers of two without biases, of e with them) and sight of this thread's two rows
       float fac[2];
-      int see[2], pos[2], gq[2];
-      bool mine[2];
+      int see[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = r_warp + (lane >> 2) + 8 * i, row = row0 + r;
         fac[i] = __shfl_sync(0xffffffffu, row_fac, half * 16 + (lane >> 2) + 8 * i);   // (r is a row of this warp's lanes)
-        pos[i] = row / d.G;
-        gq[i] = row - pos[i] * d.G;
-        mine[i] = row < nrows;
-        see[i] = mine[i] ? visible_tokens(len, d.n_pos, pos[i], d.causal) : 0;
+        see[i] = row < nrows ? visible_tokens(len, d.n_pos, row / d.G, d.causal) : 0;
       }
       const int see_min = __reduce_min_sync(0xffffffffu, min(see[0], see[1]));
       // this thread's sums in memory, 16 bytes of all threads together
@@ -783,7 +799,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       if (tid == 0) stop_flag = *abortp;   // one reading for all
       asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
       if (stop_flag) break;
-      const bool whole = g.step == 0 && n == g.count, flushed = n > kFlush;
+      const bool whole = g.step == 0 && n == g.count, flushed = n > kFlush, any_row = row0 + r_warp < nrows;
       float bw[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -792,16 +808,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         bw[k] = bref[k] == -INFINITY ? 0.f
                                      : ex2_approx(kBias ? fmaf(bref[k] - ref[k], kLog2e, brefv[k] - refv[k]) : bref[k] - ref[k]);
       }
-      // outputs of one 16-byte unit of this thread: columns 8 j + cl, + 1 of its two rows
+      int q0 = row0 + r_warp + (lane >> 2);   // (not kept in registers through the loop)
+      asm volatile("" : "+r"(q0));
+      const int q1 = q0 + 8;
+      const long long at0 = (q0 / d.G) * os.i + (q0 % d.G) * 128, at1 = (q1 / d.G) * os.i + (q1 % d.G) * 128;
       auto store = [&](int j, float4 x, float inv0, float inv1) {
-        x = make_float4(x.x * inv0, x.y * inv0, x.z * inv1, x.w * inv1);
-        const float big = 3.402823466e38f;
-        float* o = O + g.s * os.s + h * os.h + 8 * j + cl;
-        if (mine[0]) *(float2*)(o + pos[0] * os.i + gq[0] * 128) = make_float2(x.x, x.y);
-        if (mine[1]) *(float2*)(o + pos[1] * os.i + gq[1] * 128) = make_float2(x.z, x.w);
-        if ((mine[0] && !(fabsf(x.x) <= big && fabsf(x.y) <= big)) ||
-            (mine[1] && !(fabsf(x.z) <= big && fabsf(x.w) <= big)))
-          set_status(stt, ARCKV_ERR_NONFINITE);
+        store_rows(O + g.s * os.s + h * os.h + 8 * j + cl, at0, at1, q0 < nrows, q1 < nrows,
+                   make_float4(x.x * inv0, x.y * inv0, x.z * inv1, x.w * inv1), stt);
       };
       const float inv0 = l[0] == 0.f ? 0.f : kVsUnit / l[0], inv1 = l[1] == 0.f ? 0.f : kVsUnit / l[1];
       float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + tid * 4;
@@ -821,71 +834,15 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         for (int e = 0; e < 4; ++e) {
           const float4 x = make_float4(fmaf(y[e].x, bw[0], v[4 * e]), fmaf(y[e].y, bw[0], v[4 * e + 1]),
                                        fmaf(y[e].z, bw[1], v[4 * e + 2]), fmaf(y[e].w, bw[1], v[4 * e + 3]));
-          if (!whole) __stcg((float4*)(slot + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4), x);
-          else store(ch * 4 + e, x, inv0, inv1);
+          if (whole) store(ch * 4 + e, x, inv0, inv1);
+          else if (any_row) __stcg((float4*)(slot + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4), x);
         }
       }
       tc::fence_before_sync();
-      if (!whole) {
+      if (!whole && any_row) {   // joined by the kernel behind this one
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           __stcg((float4*)(slot + (long long)(16 + k) * Cfg::kSoftThreads * 4), make_float4(ref[k], refv[k], l[k], 0.f));
-        const int c_first = sh.owner(g.first), c_last = sh.owner(g.first + g.count - 1);
-        __threadfence();
-        asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
-        if (tid == 0) {
-          last_flag = atomicAdd(&tickets[c_first], 1) == c_last - c_first;
-          if (last_flag) tickets[c_first] = 0;
-          __threadfence();
-        }
-        asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
-        if (last_flag) {
-          // the parts in CTA order, with a running reference; 32 columns at a time
-#pragma unroll 1
-          for (int ch = 0; ch < 4; ++ch) {
-            float top[2] = {-INFINITY, -INFINITY}, topv[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
-            float4 a[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int cc = c_first; cc <= c_last; ++cc) {
-              const float* p = parts + (2ll * cc + (cc == c_first)) * Cfg::kSlot + tid * 4;
-              float4 st4[2], x[4];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) st4[k] = __ldcg((const float4*)(p + (long long)(16 + k) * Cfg::kSoftThreads * 4));
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[e] = __ldcg((const float4*)(p + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4));
-              float w[2], down[2];   // of the new part, of the outputs so far
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                w[k] = 0.f;
-                down[k] = 1.f;
-                if (st4[k].x == -INFINITY) continue;   // a part that saw nothing
-                const float up = top[k] == -INFINITY ? 1.f
-                                 : kBias             ? fmaf(st4[k].x - top[k], kLog2e, st4[k].y - topv[k])
-                                                     : st4[k].x - top[k];
-                if (up > 0.f) {
-                  w[k] = 1.f;
-                  down[k] = top[k] == -INFINITY ? 0.f : ex2_approx(-up);
-                  z[k] = top[k] == -INFINITY ? st4[k].z : scaled(z[k], -up) + st4[k].z;
-                  top[k] = st4[k].x;
-                  topv[k] = st4[k].y;
-                } else {
-                  w[k] = ex2_approx(up);
-                  z[k] += scaled(st4[k].z, up);
-                }
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                a[e] = make_float4(fmaf(a[e].x, down[0], x[e].x * w[0]), fmaf(a[e].y, down[0], x[e].y * w[0]),
-                                   fmaf(a[e].z, down[1], x[e].z * w[1]), fmaf(a[e].w, down[1], x[e].w * w[1]));
-            }
-            const float i0 = z[0] == 0.f ? 0.f : kVsUnit / z[0], i1 = z[1] == 0.f ? 0.f : kVsUnit / z[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) store(ch * 4 + e, a[e], i0, i1);
-          }
-        }
       }
       u += n;
     }
@@ -895,6 +852,104 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   if (warp == kSoft + 4) {
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, 256 * kT);
+  }
+}
+
+// Adds up the parts of the items that several CTAs of cache_tiles_kernel shared: cuts[c] is {sequence x head, tile, last
+// CTA} of the item that begins in CTA c and goes on, or has a last CTA of -1.  (Left to the CTA that came last, an item's
+// 16 parts of 128 rows took it 30 us, most of them waits for its loads.)  One work unit is the 16 rows that one
+// softmax warp had.
+constexpr int kJoinThreads = 256;
+template <int kT, bool kBias>
+__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_pos, int G, float* O, RowStrides os,
+                                                                  const float* parts, const int4* cuts, int n_cuts,
+                                                                  DevStatus* stt) {
+  using Cfg = TileCfg<kT>;
+  __shared__ int s_item[kCacheMaxCtas];
+  __shared__ int s_items;
+  __shared__ float s_w[kCacheMaxCtas][16], s_inv[16];
+  const int tid = threadIdx.x, lane = tid & 31, nrows = n_pos * G;
+  pdl_trigger();
+  pdl_wait();
+  if (tid < 32) {   // the items, in order
+    int n = 0;
+    for (int c0 = 0; c0 < n_cuts; c0 += 32) {
+      const bool cut = c0 + lane < n_cuts && cuts[c0 + lane].z >= 0;
+      const unsigned int all = __ballot_sync(0xffffffffu, cut);
+      if (cut) s_item[n + __popc(all & ((1u << lane) - 1u))] = c0 + lane;
+      n += __popc(all);
+    }
+    if (lane == 0) s_items = n;
+  }
+  __syncthreads();
+  const int work = s_items * Cfg::kSoft;
+  for (int x = blockIdx.x; x < work; x += gridDim.x) {
+    const int first = s_item[x / Cfg::kSoft], warp = x % Cfg::kSoft;
+    const int4 cut = cuts[first];
+    const int n = cut.z - first + 1;
+    const int row0 = cut.y * Cfg::kRows + (warp >> 3) * 128 + (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
+    if (row0 >= nrows) continue;   // (uniform)
+    auto part = [&](int p) { return parts + (2ll * (first + p) + (p == 0)) * Cfg::kSlot + warp * 128; };
+    {   // weights of the parts for row tid / 16, sixteen parts at a time
+      const int r = tid >> 4, l16 = tid & 15;
+      const long long at = (long long)(16 + (r >> 3)) * Cfg::kSoftThreads * 4 + (r & 7) * 16;
+      // log2 of what separates two references; with biases a logit and the log2 of V's scale that came with it
+      auto beyond = [](float a, float av, float b, float bv) { return kBias ? fmaf(a - b, kLog2e, av - bv) : a - b; };
+      float top = -INFINITY, topv = 0.f;
+      auto raise = [&](float a, float av) {
+        if (a != -INFINITY && (top == -INFINITY || beyond(a, av, top, topv) > 0.f)) {
+          top = a;
+          topv = av;
+        }
+      };
+      for (int p = l16; p < n; p += 16) {
+        const float2 y = __ldcg((const float2*)(part(p) + at));
+        raise(y.x, y.y);
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        const float a = __shfl_xor_sync(0xffffffffu, top, o), av = __shfl_xor_sync(0xffffffffu, topv, o);
+        raise(a, av);
+      }
+      float z = 0.f;
+      for (int p = l16; p < n; p += 16) {
+        const float4 y = __ldcg((const float4*)(part(p) + at));
+        float w = 0.f;
+        if (y.x != -INFINITY) {   // (else a part that saw nothing)
+          const float by = beyond(y.x, y.y, top, topv);
+          w = ex2_approx(by);
+          z += scaled(y.z, by);
+        }
+        s_w[p][r] = w;
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      if (l16 == 0) s_inv[r] = z == 0.f ? 0.f : kVsUnit / z;
+    }
+    __syncthreads();
+    {   // sixteen bytes of two units a thread: columns 8 j + 2 (lane % 4), + 1 of rows lane / 4 and lane / 4 + 8
+      const int r = lane >> 2, j = tid >> 5;
+      float4 a[2];
+      a[0] = a[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int p = 0; p < n; ++p) {
+        const float* src = part(p) + lane * 4;
+        const float w0 = s_w[p][r], w1 = s_w[p][r + 8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 y = __ldcg((const float4*)(src + (long long)(j + 8 * e) * Cfg::kSoftThreads * 4));
+          a[e] = make_float4(fmaf(y.x, w0, a[e].x), fmaf(y.y, w0, a[e].y), fmaf(y.z, w1, a[e].z), fmaf(y.w, w1, a[e].w));
+        }
+      }
+      const int s = cut.x / H, h = cut.x - s * H, q0 = row0 + r, q1 = q0 + 8;
+      const long long at0 = (q0 / G) * os.i + (q0 % G) * 128, at1 = (q1 / G) * os.i + (q1 % G) * 128;
+      const float i0 = s_inv[r], i1 = s_inv[r + 8];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        store_rows(O + s * os.s + h * os.h + 8 * (j + 8 * e) + 2 * (lane & 3), at0, at1, q0 < nrows, q1 < nrows,
+                   make_float4(a[e].x * i0, a[e].y * i0, a[e].z * i1, a[e].w * i1), stt);
+    }
+    __syncthreads();
   }
 }
 
@@ -913,17 +968,23 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
   auto kern = cache_tiles_kernel<kT, kBias>;
   const int smem = Cfg::kSmem + (c.S + 1) * (int)sizeof(long long);
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
-  const cudaError_t e =
-      launch_pdl(kern, dim3(std::min(tc_gemm_sm_count(), kCacheMaxCtas)), Cfg::kThreads, smem, st, c, d, q.Q, q.qs, scale, O,
-                 os, (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
-  return e == cudaSuccess ? 1 : -1;
+  const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
+  float* parts = (float*)((char*)ws + ARCKV_CACHE_WS_HEADER);
+  int4* cuts = (int4*)(parts + kCacheMaxCtas * (2ll * Cfg::kSlot + 64 * Cfg::kSoftThreads));
+  DevStatus* stt = (DevStatus*)ws;
+  cudaError_t e = launch_pdl(kern, dim3(ctas), Cfg::kThreads, smem, st, c, d, q.Q, q.qs, scale, O, os, parts, cuts, stt);
+  if (e != cudaSuccess) return -1;
+  e = launch_pdl(cache_join_kernel<kT, kBias>, dim3(4 * ctas), kJoinThreads, 0, st, c.H, q.n_pos, q.G, O, os, parts, cuts,
+                 ctas, stt);
+  return e == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace
 
 size_t cache_tiles_scratch(long long rows) {
   const size_t slot = rows <= 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot;
-  return kCacheMaxCtas * (2 * slot + 64 * (rows <= 128 ? TileCfg<1>::kSoftThreads : TileCfg<2>::kSoftThreads)) * sizeof(float);
+  const size_t sums = 64 * (rows <= 128 ? TileCfg<1>::kSoftThreads : TileCfg<2>::kSoftThreads);
+  return kCacheMaxCtas * ((2 * slot + sums) * sizeof(float) + sizeof(int4));
 }
 
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
