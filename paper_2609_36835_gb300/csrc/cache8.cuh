@@ -2,11 +2,14 @@
 #pragma once
 #include <algorithm>
 
+#include <cuda_fp16.h>
+
 #include "kernels.h"
 
 namespace arckv {
 
 constexpr int kCB = ARCKV_CACHE_BLOCK;   // tokens of a block
+constexpr int kTileBytes = kCB * 128;    // codes of one block, K or V
 constexpr float kCacheFloor = 7.888609052210118e-31f;   // 2^-100: least block magnitude, so that 127 / a stays finite
 constexpr float kInv127 = 0.007874015718698502f;        // fl(1 / 127)
 
@@ -42,6 +45,21 @@ struct CacheShares {
     return c;
   }
 };
+
+// ---- codes as f16 operands ----------------------------------------------------
+// Two bytes of w, codes + 128, as f16 codes: 1024 + u is 0x6400 | u.
+template <unsigned kPick>
+__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
+  const uint32_t y = __byte_perm(w, 0x64646464u, kPick);
+  const __half2 z = __hsub2(*(const __half2*)&y, __half2{__half_raw{0x6480}, __half_raw{0x6480}});
+  return *(const uint32_t*)&z;
+}
+// Four 8 x 8 matrices of 16-bit units, transposed; lane 8i + r gives the address of row r of matrix i.
+__device__ __forceinline__ void load_transposed(uint32_t (&w)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(addr));
+}
 
 // ---- launches that overlap their predecessor's end ---------------------------
 // The kernels of this file's callers start while the kernel before them on the

@@ -32,13 +32,10 @@
 #include "cache8.cuh"
 #include "tc.cuh"
 
-#include <cuda_fp16.h>
-
 namespace arckv {
 namespace {
 
 constexpr int kRowsMax = 16;                 // more rows of a head go to the tcgen05 kernel
-constexpr int kTileBytes = kCB * 128;        // codes of one block, K or V
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 
 struct RowsShape {
@@ -75,19 +72,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
-}
-// Two bytes of w, codes + 128, as f16 codes: 1024 + u is 0x6400 | u.
-template <unsigned kPick>
-__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
-  const uint32_t y = __byte_perm(w, 0x64646464u, kPick);
-  const __half2 z = __hsub2(*(const __half2*)&y, __half2{__half_raw{0x6480}, __half_raw{0x6480}});
-  return *(const uint32_t*)&z;
-}
-// Four 8 x 8 matrices of 16-bit units, transposed; lane 8i + r gives the address of row r of matrix i.
-__device__ __forceinline__ void load_transposed(uint32_t (&w)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-               : "r"(addr));
 }
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);

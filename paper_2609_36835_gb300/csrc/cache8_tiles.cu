@@ -31,14 +31,13 @@
 #include "cache8.cuh"
 #include "tc.cuh"
 
-#include <cuda_fp16.h>
-
 namespace arckv {
 namespace {
 
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
-constexpr int kStages = 4, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) in shared memory
+constexpr int kStages = 3, kStageBytes = 2 * kKTile + kHalf;   // blocks of (K, V) as operands
+constexpr int kRawBytes = 2 * kTileBytes;                      // of a block as codes
 constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
@@ -61,7 +60,8 @@ struct TileCfg {
   static constexpr int kRegsSoft = kT == 2 ? 96 : 176, kRegsConv = kT == 2 ? 64 : 96, kRegsMma = kT == 2 ? 32 : 64;
   static_assert(2 * kT * kRegsSoft + kRegsConv + kRegsMma == (2 * kT + 2) * kRegs && kRegs * kThreads <= 65536,
                 "the shares add up to what the block was launched with");
-  static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + 1024;   // Q, then the stages
+  static constexpr int kRaw = kT == 2 ? 2 : 4;           // blocks on their way as codes
+  static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + kRaw * kRawBytes + 1024;
   // floats of a partial result: 64 outputs and twice (ref, log2 vs of ref, sum, unused) of each softmax thread
   static constexpr int kSlot = 72 * kSoftThreads;
 };
@@ -218,11 +218,9 @@ __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.a
 // kind::f16 with A = B = f16, D = fp32, both K-major, M = 128, N = n.
 __host__ __device__ constexpr uint32_t idesc_f16(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 
-template <int kHi>
-__device__ __forceinline__ uint32_t codes_f16(uint32_t w) {   // bytes (0, 1) or (2, 3), codes + 128, as two f16 codes
-  const uint32_t y = __byte_perm(w, 0x64646464u, kHi ? 0x4342 : 0x4140);
-  const __half2 z = __hsub2(*(const __half2*)&y, __half2{__half_raw{0x6480}, __half_raw{0x6480}});
-  return *(const uint32_t*)&z;
+__device__ __forceinline__ void store_matrices(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
 }
 
 // Blocks of a row tile: as far as its last row sees (one at least).
@@ -296,16 +294,18 @@ struct Meta {   // of a block
 
 template <int kT, bool kBias>
 __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
-    cache_tiles_kernel(const arckv_cache8 c, TileShape d, const bf16* Q, RowStrides qs, float scale, float* O,
+    cache_tiles_kernel(const __grid_constant__ CUtensorMap mK, const __grid_constant__ CUtensorMap mV, const arckv_cache8 c, TileShape d, const bf16* Q, RowStrides qs, float scale, float* O,
                        RowStrides os, float* parts, int4* cuts, DevStatus* stt) {
   using Cfg = TileCfg<kT>;
-  constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows;
+  constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows, kRaw = Cfg::kRaw;
   extern __shared__ unsigned char smraw[];
   unsigned char* sQ = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [tile][half][128][128 B]
   unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K halves, V]
-  long long* pre = (long long*)(sKV + kStages * kStageBytes);                      // [S + 1] blocks of a head's tiles
+  unsigned char* sRaw = sKV + kStages * kStageBytes;                               // [raw stage][K, V]
+  long long* pre = (long long*)(sRaw + kRaw * kRawBytes);                          // [S + 1] blocks of a head's tiles
   // of buffer (parity of the block) 0 and 1: S written, P written, P V done
   __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
+  __shared__ __align__(8) uint64_t raw_full[kRaw], raw_empty[kRaw];
   __shared__ Meta meta[2 * kStages];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, stop_flag;
@@ -324,6 +324,10 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tc::mbar_init(&pfull[t][i], 8);
         tc::mbar_init(&odone[t][i], 1);
       }
+    for (int i = 0; i < kRaw; ++i) {
+      tc::mbar_init(&raw_full[i], 1);
+      tc::mbar_init(&raw_empty[i], 4);
+    }
     tc::mbar_init(&drain, 1);
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -365,17 +369,39 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   const bool active = (int)blockIdx.x < sh.ctas;
   const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
 
-  if (warp > kSoft + 5) {
+  if (warp == kSoft + 7) {
     // ------------------------ the item that begins here and goes on in other CTAs
     regs_dec<Cfg::kRegsMma>();
-    if (warp == kSoft + 6) {
-      int4 cut = make_int4(0, 0, -1, 0);
-      if (active) {
-        const Segment g = segment_of(u1 - 1, d, c, pre, kRows);
-        const long long end = g.first + g.count;
-        if (end > u1 && g.first >= u0) cut = make_int4((int)g.sh, g.tile, sh.owner(end - 1), 0);
+    int4 cut = make_int4(0, 0, -1, 0);
+    if (active) {
+      const Segment g = segment_of(u1 - 1, d, c, pre, kRows);
+      const long long end = g.first + g.count;
+      if (end > u1 && g.first >= u0) cut = make_int4((int)g.sh, g.tile, sh.owner(end - 1), 0);
+    }
+    if (lane == 0) cuts[blockIdx.x] = cut;
+  } else if (warp == kSoft + 6) {
+    // ---------------------------------------------------------------- codes
+    regs_dec<Cfg::kRegsMma>();
+    bool ok = true;
+    int q = 0;   // blocks issued
+    for (long long u = u0; u < u1 && ok;) {
+      const Segment g = segment_of(u, d, c, pre, kRows);
+      const int n = (int)min((long long)(g.count - g.step), u1 - u);
+      for (int i = 0; i < n; ++i, ++q) {   // (blocks lie within the capacity: `count` does)
+        const int st = q % kRaw;
+        if (q >= kRaw) ok = __all_sync(0xffffffffu, tc::mbar_wait(&raw_empty[st], ((q / kRaw) - 1) & 1, abortp, stt));
+        if (!ok) break;
+        if (lane == 0) {
+          tc::mbar_arrive_expect_tx(&raw_full[st], kRawBytes);
+          tc::tma_load_3d(sRaw + st * kRawBytes, &mK, 0, (g.step + i) * kCB, (int)g.sh, &raw_full[st]);
+          tc::tma_load_3d(sRaw + st * kRawBytes + kTileBytes, &mV, 0, (g.step + i) * kCB, (int)g.sh, &raw_full[st]);
+        }
       }
-      if (lane == 0) cuts[blockIdx.x] = cut;
+      u += n;
+    }
+    if (!ok) {   // let the copies in flight land before the CTA's memory goes
+      volatile int never = 0;
+      for (int p = max(0, q - kRaw); p < q; ++p) tc::mbar_wait(&raw_full[p % kRaw], (p / kRaw) & 1, &never, stt);
     }
   } else if (warp == kSoft + 5) {
     // ---------------------------------------------------------------- scales
@@ -469,73 +495,51 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   } else if (warp >= kSoft) {
     // ------------------------------------------------------------ converters
     regs_dec<Cfg::kRegsConv>();
-    const int cw = warp - kSoft;
-    // K: 16 dims of a row; eight lanes write alternate chunks of half a row and of the next row's.  V: keys 8 ko ..
-    // 8 ko + 7, dims 8 dg .. 8 dg + 7; eight lanes write one dim's chunks.  Neither meets bank conflicts.
-    const int kc = (lane & 3) + 4 * (lane >> 4), kr = cw * 16 + ((lane >> 2) & 3);
-    const int ko = lane & 7, dg = (lane >> 3) + 4 * cw;
-    bool ok = true;
-    int it = 0;
-    for (long long u = u0; u < u1 && ok;) {
-      const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = (int)min((long long)(g.count - g.step), u1 - u);
-      // loads run ahead by one block (blocks lie within the capacity: `count` does)
-      const uint8_t* Kh = c.K + (g.sh * c.cap + (long long)g.step * kCB + kr) * 128 + kc * 16;
-      const uint8_t* Vh = c.V + (g.sh * c.cap + (long long)g.step * kCB + ko * 8) * 128 + dg * 8;
-      uint4 rk[4];
-      uint2 rv[8];
-      auto load_k = [&](int i) {
+    const int cw = warp - kSoft, total = (int)(u1 - u0);
+    // K: 16 dims of a row (chunk kc) at a time.  Eight lanes have four chunks of rows r and r ^ 5, which neither as
+    // codes nor as operands meet in a bank.
+    const int kc = (lane & 3) + 4 * (lane >> 4), kr = cw * 16 + (((lane >> 2) & 1) * 5 ^ ((lane >> 3) & 1) * 2);
+    // V: dims 32 cw .. 32 cw + 31 of 16 keys at a time.  Transposed loads leave dims 2 i, 2 i + 1 of two keys in a word;
+    // the even and odd ones are stored as matrices of 8 dims x 8 keys.
+    const int v_row = (lane & 15) * 128, v_chunk = ((2 * cw + (lane >> 4)) ^ (lane & 7)) << 4;
+    const int m = lane >> 3, dim = 32 * cw + 2 * (lane & 7) + (m & 1);
+    const int o_row = dim * 128, o_chunk = ((m >> 1) ^ (dim & 7)) << 4;
+    const uint32_t raw0 = tc::smem_u32(sRaw), kv0 = tc::smem_u32(sKV);
+    for (int q = 0; q < total; ++q) {
+      const int st = q % kStages, rs = q % kRaw;
+      bool ok = tc::mbar_wait(&raw_full[rs], (q / kRaw) & 1, abortp, stt);
+      if (ok && q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const unsigned char* raw = sRaw + rs * kRawBytes;
+      unsigned char* Ks = sKV + st * kStageBytes;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) rk[j] = __ldg((const uint4*)(Kh + (long long)i * (kCB * 128) + 4 * j * 128));
-      };
-      auto load_v = [&](int i) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) rv[j] = __ldg((const uint2*)(Vh + (long long)i * (kCB * 128) + j * 128));
-      };
-      load_k(0);
-      load_v(0);
-      for (int i = 0; i < n && ok; ++i) {
-        const int q = it + i, st = q % kStages;
-        unsigned char* Ks = sKV + st * kStageBytes;
-        unsigned char* Vs = Ks + 2 * kKTile;
-        if (q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = kr + 4 * j;
-          unsigned char* row = Ks + (kc >> 2) * kKTile + r * 128;
-          *(uint4*)(row + ((((kc & 3) * 2) ^ (r & 7)) << 4)) =
-              make_uint4(codes_f16<0>(rk[j].x), codes_f16<1>(rk[j].x), codes_f16<0>(rk[j].y), codes_f16<1>(rk[j].y));
-          *(uint4*)(row + ((((kc & 3) * 2 + 1) ^ (r & 7)) << 4)) =
-              make_uint4(codes_f16<0>(rk[j].z), codes_f16<1>(rk[j].z), codes_f16<0>(rk[j].w), codes_f16<1>(rk[j].w));
-        }
-        if (i + 1 < n) load_k(i + 1);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {   // dims 8 dg + 4 w ..
-          uint32_t f[4][4];             // [dim][key pair]
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            const uint32_t a = w ? rv[2 * p].y : rv[2 * p].x, e = w ? rv[2 * p + 1].y : rv[2 * p + 1].x;
-            const uint32_t y = __byte_perm(a, e, 0x5140), z = __byte_perm(a, e, 0x7362);
-            f[0][p] = codes_f16<0>(y);
-            f[1][p] = codes_f16<1>(y);
-            f[2][p] = codes_f16<0>(z);
-            f[3][p] = codes_f16<1>(z);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int dim = dg * 8 + w * 4 + e;
-            *(uint4*)(Vs + dim * 128 + ((ko ^ (dim & 7)) << 4)) = make_uint4(f[e][0], f[e][1], f[e][2], f[e][3]);
-          }
-        }
-        if (i + 1 < n) load_v(i + 1);
-        tc::fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&full[st]);
+      for (int j = 0; j < 4; ++j) {
+        const int r = kr ^ (j & 1) ^ (j & 2) << 2;
+        const uint4 x = *(const uint4*)(raw + r * 128 + ((kc ^ (r & 7)) << 4));
+        unsigned char* row = Ks + (kc >> 2) * kKTile + r * 128;
+        *(uint4*)(row + ((((kc & 3) * 2) ^ (r & 7)) << 4)) =
+            make_uint4(codes_f16<0x4140>(x.x), codes_f16<0x4342>(x.x), codes_f16<0x4140>(x.y), codes_f16<0x4342>(x.y));
+        *(uint4*)(row + ((((kc & 3) * 2 + 1) ^ (r & 7)) << 4)) =
+            make_uint4(codes_f16<0x4140>(x.z), codes_f16<0x4342>(x.z), codes_f16<0x4140>(x.w), codes_f16<0x4342>(x.w));
       }
-      it += n;
-      u += n;
+      const uint32_t vs = raw0 + rs * kRawBytes + kTileBytes + v_row + v_chunk;
+      const uint32_t vd = kv0 + st * kStageBytes + 2 * kKTile + o_row;
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) {
+        uint32_t w[4];
+        load_transposed(w, vs + mt * (16 * 128));
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+          store_matrices(vd + z * (16 * 128) + ((mt << 5) ^ o_chunk), codes_f16<0x4240>(w[2 * z]),
+                         codes_f16<0x4341>(w[2 * z]), codes_f16<0x4240>(w[2 * z + 1]), codes_f16<0x4341>(w[2 * z + 1]));
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tc::mbar_arrive(&raw_empty[rs]);
+        tc::mbar_arrive(&full[st]);
+      }
     }
   } else {
     // --------------------------------------------------------------- softmax
@@ -957,6 +961,10 @@ template <int kT, bool kBias>
 int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
                  cudaStream_t st) {
   using Cfg = TileCfg<kT>;
+  CUtensorMap mK, mV;
+  if (!encode_u8_map_3d(&mK, c.K, c.cap, (uint64_t)c.S * c.H, kCB) ||
+      !encode_u8_map_3d(&mV, c.V, c.cap, (uint64_t)c.S * c.H, kCB))
+    return -1;
   TileShape d;
   d.H = c.H;
   d.n_pos = q.n_pos;
@@ -972,7 +980,7 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
   float* parts = (float*)((char*)ws + ARCKV_CACHE_WS_HEADER);
   int4* cuts = (int4*)(parts + kCacheMaxCtas * (2ll * Cfg::kSlot + 64 * Cfg::kSoftThreads));
   DevStatus* stt = (DevStatus*)ws;
-  cudaError_t e = launch_pdl(kern, dim3(ctas), Cfg::kThreads, smem, st, c, d, q.Q, q.qs, scale, O, os, parts, cuts, stt);
+  cudaError_t e = launch_pdl(kern, dim3(ctas), Cfg::kThreads, smem, st, mK, mV, c, d, q.Q, q.qs, scale, O, os, parts, cuts, stt);
   if (e != cudaSuccess) return -1;
   e = launch_pdl(cache_join_kernel<kT, kBias>, dim3(4 * ctas), kJoinThreads, 0, st, c.H, q.n_pos, q.G, O, os, parts, cuts,
                  ctas, stt);
