@@ -61,6 +61,22 @@ __device__ __forceinline__ void load_transposed(uint32_t (&w)[4], uint32_t addr)
                : "r"(addr));
 }
 
+// ---- softmax weights ------------------------------------------------------------
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// x - h, exactly, in one mixed-precision operation each.
+__device__ __forceinline__ float2 minus_f16(float2 x, __half2 h) {
+  float2 d;
+  asm("{\n\t.reg .b16 p, q, m;\n\tmov.b32 {p, q}, %2;\n\tmov.b16 m, 0xBC00;\n\t"   // -1
+      "fma.rn.f32.f16 %0, p, m, %3;\n\tfma.rn.f32.f16 %1, q, m, %4;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "r"(*(const uint32_t*)&h), "f"(x.x), "f"(x.y));
+  return d;
+}
+
 // ---- launches that overlap their predecessor's end ---------------------------
 // The kernels of this file's callers start while the kernel before them on the
 // stream is still ending: pdl_wait() comes before their first access to memory

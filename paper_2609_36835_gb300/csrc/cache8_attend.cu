@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
   // this lane's row of a V tile (key lane & 15), and its 16-byte chunk (dims 32j + 16 (lane >> 4)) as stored for j = 0
   const uint32_t v_row = (lane & 15) * 128, v_chunk = ((lane >> 4) ^ (lane & 7)) << 4;
-  constexpr float kP15 = 15.f;   // weights carry a factor of 2^15
+  constexpr float kGrow = 8.f, kLift = 7.f;   // weights reach 2^15: the range of f16
   int base = 0;                  // blocks of earlier runs
   bool ok = true;
   for (Run p; walk.next(p);) {
@@ -420,34 +420,59 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
             }
           }
         }
-        // ---- softmax of the block
-        const bool edge = (b + 1) * kCB > see_min;
-        float top[2], alpha[2];
-#pragma unroll
-        for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
-          const float f = fac[e2] * ks;
-          top[e2] = -INFINITY;
+        // ---- softmax of the block.  References follow the maximum only when it has grown by more than 2^8 (kGrow), so
+        // that sums are scaled on few blocks.  Without biases the maximum is that of the products, whose factor is
+        // positive (and never zero: a masked product is -inf), and a weight is 2^{product factor - mx}.
+        const float f[2] = {fmaxf(fac[0] * ks, 0x1p-126f), fmaxf(fac[1] * ks, 0x1p-126f)};
+        if (kBias) {
 #pragma unroll
           for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              float& x = s[mt][2 * hf + e2];
-              const int kk = mt * 16 + hf * 8 + g;
-              x = kBias ? fmaf(x, f, sBias[st * kCB + kk]) : x * f;
-              if (edge && b * kCB + kk >= see[e2]) x = -INFINITY;
-              top[e2] = fmaxf(top[e2], x);
+              const float bias = sBias[st * kCB + mt * 16 + hf * 8 + g];
+#pragma unroll
+              for (int e2 = 0; e2 < 2; ++e2) s[mt][2 * hf + e2] = fmaf(s[mt][2 * hf + e2], f[e2], bias);
             }
+        }
+        if ((b + 1) * kCB > see_min) {
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (b * kCB + mt * 16 + (e >> 1) * 8 + g >= see[e & 1]) s[mt][e] = -INFINITY;
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&emptyK[st]);   // the next block's keys may come
+        float alpha[2];
+        bool grows = false;
+#pragma unroll
+        for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
+          float top = max3(s[0][e2], s[0][2 + e2], s[1][e2]);
+          top = max3(top, s[1][2 + e2], s[2][e2]);
+          top = max3(top, s[2][2 + e2], s[3][e2]);
+          top = fmaxf(top, s[3][2 + e2]);
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+          alpha[e2] = 1.f;
+          const float old = mx[e2];
+          if (!kBias) top = fmaf(top, f[e2], -kLift);
+          if (top != -INFINITY && (old == -INFINITY || (kBias ? (top - old) * kLog2e : top - old) > kGrow)) {
+            mx[e2] = top;
+            alpha[e2] = ex2_approx(kBias ? (old - top) * kLog2e : old - top);   // (of -inf: zero)
+            grows = true;
+          }
+        }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int e2 = 0; e2 < 2; ++e2) l[e2] *= alpha[e2];
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][e] *= alpha[e & 1];
+        }
 #pragma unroll
         for (int e2 = 0; e2 < 2; ++e2) {
-#pragma unroll
-          for (int w = 4; w < 32; w <<= 1) top[e2] = fmaxf(top[e2], __shfl_xor_sync(0xffffffffu, top[e2], w));
-          const float old = mx[e2], up = fmaxf(top[e2], old);
-          mx[e2] = up;
-          const float ref = up == -INFINITY ? 0.f : up;   // nothing visible yet: weights e^{-inf} = 0
-          alpha[e2] = ex2_approx(kBias ? (old - ref) * kLog2e : old - ref);
+          const float ref = mx[e2] == -INFINITY ? 0.f : mx[e2];   // nothing visible yet: weights 2^{-inf} = 0
           float sum = 0.f;
 #pragma unroll
           for (int mt = 0; mt < 4; ++mt)
@@ -455,10 +480,10 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
             for (int hf = 0; hf < 2; ++hf) {
               float& x = s[mt][2 * hf + e2];
               // a bias of the type's lowest value cancels against itself before the factor log2 e
-              x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kP15) : (x - ref) + kP15);
+              x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kLift) : fmaf(x, f[e2], -ref));
               sum += x;
             }
-          l[e2] = fmaf(l[e2], alpha[e2], sum);
+          l[e2] += sum;
         }
         // f16 pairs, transposed to (keys, row) operands
         uint32_t ph[4][2], pl[4][2];
@@ -466,10 +491,10 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
-            const float x0 = s[mt][2 * hf], x1 = s[mt][2 * hf + 1];
-            const uint32_t hi = pack_f16(x0, x1);
-            const float2 hf2 = __half22float2(*(const __half2*)&hi);
-            const uint32_t lo = pack_f16(x0 - hf2.x, x1 - hf2.y);
+            const float2 x = make_float2(s[mt][2 * hf], s[mt][2 * hf + 1]);
+            const uint32_t hi = pack_f16(x.x, x.y);
+            const float2 rest = minus_f16(x, *(const __half2*)&hi);
+            const uint32_t lo = pack_f16(rest.x, rest.y);
             if (kR == 4) {   // columns 4 .. 7 carry lo of the same rows
               ph[mt][hf] = transpose8x8(t >= 2 ? lo : hi);
             } else {
@@ -508,7 +533,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 #pragma unroll
         for (int k = 0; k < 8; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[k][e] = fmaf(o[k][e], alpha[e & 1], vs * acc[k][e]);
+          for (int e = 0; e < 4; ++e) o[k][e] = fmaf(vs, acc[k][e], o[k][e]);
       } else {   // an entry that names no block
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullV[st], (q / kSt) & 1, abortp, stt));
         if (!ok) break;

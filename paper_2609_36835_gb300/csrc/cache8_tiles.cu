@@ -182,11 +182,6 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return d;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 d;
   asm("{\n\t.reg .b64 a, b, d;\n\t"
@@ -194,15 +189,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-// x - h, exactly, in one mixed-precision operation each.
-__device__ __forceinline__ float2 minus_f16(float2 x, __half2 h) {
-  float2 d;
-  asm("{\n\t.reg .b16 p, q, m;\n\tmov.b32 {p, q}, %2;\n\tmov.b16 m, 0xBC00;\n\t"   // -1
-      "fma.rn.f32.f16 %0, p, m, %3;\n\tfma.rn.f32.f16 %1, q, m, %4;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "r"(*(const uint32_t*)&h), "f"(x.x), "f"(x.y));
   return d;
 }
 // x 2^by, where the factor alone may be out of range (a sum of weights beside values 2^126 as large).
