@@ -58,7 +58,7 @@ struct RowsCfg {
   static constexpr int kTiles = kR == 16 ? 2 : 1;   // tiles of 8 rows; warps w and w + kW / 2 share blocks, a tile each
   static constexpr int kTeams = kW / kTiles;        // warps, or pairs, that take blocks in turn
   static constexpr int kTileRows = kR < 8 ? kR : 8;
-  static constexpr int kSmem = kSt * (2 * kTileBytes + kCB * 4) + kW * kTileRows * kRowO * 4 + 1024;
+  static constexpr int kSmem = kSt * (2 * kTileBytes + kCB * 4) + kW * kTileRows * kRowO * 4 + 2 * kR * 256 + 1024;
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -183,8 +183,9 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   unsigned char* ringV = ringK + kSt * kTileBytes;
   float* sBias = (float*)(ringV + kSt * kTileBytes);
   float* sO = sBias + kSt * kCB;                                 // [warp][row of its tile][kRowO]
-  int* pre = (int*)(sO + kW * kTR * kRowO);                       // dense: [S + 1]
-  __shared__ __align__(8) uint64_t fullK[kSt], emptyK[kSt], fullV[kSt], emptyV[kSt];
+  bf16* sQ = (bf16*)(sO + kW * kTR * kRowO);                     // [parity of the run][row][128]
+  int* pre = (int*)(sQ + 2 * kR * 128);                       // dense: [S + 1]
+  __shared__ __align__(8) uint64_t fullK[kSt], emptyK[kSt], fullV[kSt], emptyV[kSt], fullQ[2], emptyQ[2];
   __shared__ float sKs[kSt], sVs[kSt];
   __shared__ int sBlk[kSt];
   __shared__ float sM[kW][kTR], sL[kW][kTR];
@@ -198,6 +199,10 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       tc::mbar_init(&emptyK[s], Cfg::kTiles);
       tc::mbar_init(&fullV[s], 1);
       tc::mbar_init(&emptyV[s], Cfg::kTiles);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&fullQ[i], 1);
+      tc::mbar_init(&emptyQ[i], kW);
     }
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -260,17 +265,30 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
 
   if (warp >= kW) {
-    // ------------------------------------- producers: keys (with scales and biases) and values
+    // ------------------------------------- producers: keys (with scales and biases); queries and values
     const bool keys = warp == kW;
     uint64_t *full = keys ? fullK : fullV, *empty = keys ? emptyK : emptyV;
     unsigned char* ring = keys ? ringK : ringV;
     const CUtensorMap* map = keys ? &mK : &mV;
     const float* scales = keys ? c.k_scale : c.v_scale;
     float* sScale = keys ? sKs : sVs;
-    int it = 0;   // blocks issued
+    int it = 0, run = 0;   // blocks and runs issued
     bool ok = true;
-    for (Run p; ok && walk.next(p);) {
+    for (Run p; ok && walk.next(p); ++run) {
       const int n = p.n, len = cache_len(c, p.s);
+      if (!keys && !walk.parts) {   // a run ahead, as far as the ring reaches
+        const int buf = run & 1, r = p.group * kR + lane, nrows = kSparse ? d.G : d.n_pos * d.G;
+        if (run >= 2) ok = __all_sync(0xffffffffu, tc::mbar_wait(&emptyQ[buf], ((run >> 1) - 1) & 1, abortp, stt));
+        if (!ok) {
+          ++it;   // (as where a block's wait gives up: `it` is one more than were issued)
+          break;
+        }
+        if (lane == 0) tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * min(kR, nrows - p.group * kR));
+        if (lane < kR && r < nrows) {
+          const int pos = kSparse ? p.pos : r / d.G, gq = kSparse ? r : r - pos * d.G;
+          tc::bulk_load(sQ + (buf * kR + lane) * 128, Q + p.s * qs.s + p.h * qs.h + pos * qs.i + gq * 128, 256, &fullQ[buf]);
+        }
+      }
       for (int k0 = 0; k0 < n && ok; k0 += 32) {
         const int k = k0 + lane;
         int b = -1;
@@ -319,6 +337,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     if (!ok) {   // let the copies in flight land before the CTA's memory goes
       volatile int never = 0;
       for (int q = max(0, it - 1 - kSt); q < it - 1; ++q) tc::mbar_wait(&full[q % kSt], (q / kSt) & 1, &never, stt);
+      if (!keys && !walk.parts)
+        for (int q = max(0, run - 2); q < run; ++q) tc::mbar_wait(&fullQ[q & 1], (q >> 1) & 1, &never, stt);
     }
     return;
   }
@@ -329,23 +349,27 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
   // this lane's row of a V tile (key lane & 15), and its 16-byte chunk (dims 32j + 16 (lane >> 4)) as stored for j = 0
   const uint32_t v_row = (lane & 15) * 128, v_chunk = ((lane >> 4) ^ (lane & 7)) << 4;
   constexpr float kGrow = 8.f, kLift = 7.f;   // weights reach 2^15: the range of f16
-  int base = 0;                  // blocks of earlier runs
+  int base = 0, run = 0;         // blocks of earlier runs, and their number
   bool ok = true;
-  for (Run p; walk.next(p);) {
+  for (Run p; walk.next(p); ++run) {
     const int n = p.n, len = cache_len(c, p.s), h = p.h, nrows = kSparse ? d.G : d.n_pos * d.G;
     // query rows: column n is row n of the tile (four rows: twice the same four)
     uint32_t qf[8][2];
     float fac[2];           // 2^e scale (log2 e) of rows 2t, 2t + 1
     int see[2], see_min;    // tokens that they see
     {
-      const int r = p.group * kR + tile0 + (kR == 4 ? (g & 3) : g);
-      const int pos = kSparse ? p.pos : r / d.G, gq = kSparse ? r : r - pos * d.G;
+      const int rt = tile0 + (kR == 4 ? (g & 3) : g), r = p.group * kR + rt, pos = kSparse ? p.pos : r / d.G;
       float x[32], amax = 0.f;
+      // Queries of a CTA's only run are read here, beside its first copies; of several runs, they have come to shared
+      // memory (64 x 8K decode 117 us; read from memory 120; a single 1K sequence 6.0 us by way of shared memory, 5.7)
+      const bf16* mine = sQ + ((run & 1) * kR + rt) * 128;
+      if (walk.parts) mine = Q + p.s * qs.s + h * qs.h + pos * qs.i + (kSparse ? r : r - pos * d.G) * 128;
+      else ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
       if (r < nrows) {
-        const uint4* src = (const uint4*)(Q + p.s * qs.s + h * qs.h + pos * qs.i + gq * 128 + 32 * t);
+        const uint4* src = (const uint4*)(mine + 32 * t);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint4 v = __ldg(src + e);
+          const uint4 v = src[e];
           const __nv_bfloat162* y = (const __nv_bfloat162*)&v;
 #pragma unroll
           for (int f = 0; f < 4; ++f) {
@@ -360,6 +384,8 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = 0.f;
       }
+      __syncwarp();
+      if (!walk.parts && lane == 0) tc::mbar_arrive(&emptyQ[run & 1]);
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       // exponent of the row's largest element, kept where 2^(14 - e) and 2^(e - 14) are normal
@@ -385,7 +411,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
     // block base + i of the CTA belongs to team (base + i) % kTeams
-    for (int i = (team - base % kTeams + kTeams) % kTeams; i < n; i += kTeams) {
+    for (int i = (team - base % kTeams + kTeams) % kTeams; i < n && ok; i += kTeams) {
       const int q = base + i, st = q % kSt;
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullK[st], (q / kSt) & 1, abortp, stt));
       if (!ok) break;
