@@ -89,7 +89,7 @@ struct Run {
 
 // Smallest number of blocks that are worth a CTA of their own: joining two CTAs' parts takes about as long as this
 // many blocks, which the warps of one CTA have at the same time.
-constexpr int kPartMin = 6;
+constexpr int kPartMin = 4;
 
 // The runs of a CTA, in order.  Items are numbered over sequences, then heads (sparse: positions, row groups); dense,
 // pre[s] are the blocks (or parts) before sequence s of one head.

@@ -529,11 +529,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     }
   } else {
     // --------------------------------------------------------------- softmax
-    // a warp has 16 rows of its tile: lane l rows l / 4 and l / 4 + 8 of them, two columns of eight
+    // a warp has 16 rows of its tile: lane l rows l / 4 and l / 4 + 8 of them, two columns of eight.  Warp w has the
+    // tile's rows 16 (w % 8) .. in the TMEM lanes that it can reach, so that few rows are spread over the SM's quarters;
+    // warps that are left without rows only keep the count of the barriers.
     regs_inc<Cfg::kRegsSoft>();
     const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;   // (a warp reaches the lanes of its quarter)
-    const int r_warp = quarter * 32 + half * 16, cl = 2 * (lane & 3);
-    const uint32_t Sb = tmem + 256 * t + ((uint32_t)r_warp << 16), Ot = Sb + 128;
+    const int r_warp = 16 * (warp & 7), cl = 2 * (lane & 3);
+    const uint32_t Sb = tmem + 256 * t + ((uint32_t)(quarter * 32 + half * 16) << 16), Ot = Sb + 128;
     const int nrows = d.n_pos * d.G;
     bool ok = true;
     // P V of block q is in O.  (The one before it, whose phase this could be taken for, is known to be: S of block
@@ -551,7 +553,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const int row0 = g.tile * kRows + t * 128, h = (int)(g.sh - (long long)g.s * d.H), len = cache_len(c, g.s);
       float row_fac;
       {   // the queries as f16, each row scaled by a power of two: here a lane is a row, and has 64 dims
-        const int r = quarter * 32 + lane, row = row0 + r, pos = row / d.G, gq = row - pos * d.G;
+        const int r = quarter * 32 + lane, row = row0 + 64 * (lane >> 4) + 16 * quarter + (lane & 15);   // (r: TMEM lane)
+        const int pos = row / d.G, gq = row - pos * d.G;
         uint4 x[8];
         float amax = 0.f;
 #pragma unroll
@@ -608,12 +611,17 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       float bref[2] = {-INFINITY, -INFINITY}, brefv[2] = {0.f, 0.f}, ref[2] = {-INFINITY, -INFINITY};
       float refv[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
       const float* bias = kBias ? c.bias + g.sh * c.cap : nullptr;
+      const bool any_row = row0 + r_warp < nrows;
       for (int i = 0; i < n; ++i) {
         const int q = it + i, j0 = (g.step + i) * kCB + cl;
         const uint32_t S = Sb + (q & 1) * 64;
         // S is in, and with it the block's scales (written before `full`, which the MMA warp waited for)
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q & 1], (q >> 1) & 1, abortp, stt));
         if (!ok) break;
+        if (kT == 1 && !any_row) {
+          if (lane == 0) tc::mbar_arrive(&pfull[t][q & 1]);
+          continue;
+        }
         tc::fence_after_sync();
         if (i > 0 && i % kFlush == 0) {
           if (!product_done(q - 1)) break;
@@ -789,7 +797,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       if (tid == 0) stop_flag = *abortp;   // one reading for all
       asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
       if (stop_flag) break;
-      const bool whole = g.step == 0 && n == g.count, flushed = n > kFlush, any_row = row0 + r_warp < nrows;
+      const bool whole = g.step == 0 && n == g.count, flushed = n > kFlush;
       float bw[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -877,7 +885,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
     const int first = s_item[x / Cfg::kSoft], warp = x % Cfg::kSoft;
     const int4 cut = cuts[first];
     const int n = cut.z - first + 1;
-    const int row0 = cut.y * Cfg::kRows + (warp >> 3) * 128 + (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
+    const int row0 = cut.y * Cfg::kRows + warp * 16;
     if (row0 >= nrows) continue;   // (uniform)
     auto part = [&](int p) { return parts + (2ll * (first + p) + (p == 0)) * Cfg::kSlot + warp * 128; };
     {   // weights of the parts for row tid / 16, sixteen parts at a time
