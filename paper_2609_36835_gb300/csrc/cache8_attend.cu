@@ -87,10 +87,6 @@ struct Run {
   int first, last;        // the CTAs that share the item
 };
 
-// Smallest number of blocks that are worth a CTA of their own: joining two CTAs' parts takes about as long as this
-// many blocks, which the warps of one CTA have at the same time.
-constexpr int kPartMin = 4;
-
 // The runs of a CTA, in order.  Items are numbered over sequences, then heads (sparse: positions, row groups); dense,
 // pre[s] are the blocks (or parts) before sequence s of one head.
 template <bool kSparse>
@@ -177,6 +173,10 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
                       const arckv_cache8 c, RowsShape d, const bf16* Q, RowStrides qs, float scale, const int* blocks,
                       float* O, RowStrides os, float* parts, int* tickets, DevStatus* stt) {
   using Cfg = RowsCfg<kR>;
+  // Fewest blocks that are worth a CTA of their own: joining parts takes over 1 us, in which the warps of one CTA, with a
+  // block each, get further (4 rows of 8 heads, 450 tokens: 6.0 us with 6, 7.1 with 4; 12 rows of 4 x 8 heads, 1000
+  // tokens: 10.9 with 6, 9.4 with 4).
+  constexpr int kPartMin = kR == 16 ? 4 : 6;
   constexpr int kTR = Cfg::kTileRows, kTeams = Cfg::kTeams, kW = Cfg::kW, kSt = Cfg::kSt;
   extern __shared__ __align__(1024) unsigned char smraw[];
   unsigned char* ringK = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         int run = 0;
         for (int s0 = 0; s0 < c.S; s0 += 32) {
           int x = s0 + lane < c.S ? max(1, (cache_len(c, s0 + lane) + kCB - 1) / kCB) : 0;
-          if (cut > 0) x = (x + cut - 1) / cut;
+          if (cut > 0 && x > 0) x = max(1, min((x + cut - 1) / cut, x / kPartMin));
 #pragma unroll
           for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       };
       int all = scan();
       if (c.S * d.H <= (int)gridDim.x) {   // the smallest parts that the CTAs suffice for
-        cut = max(kPartMin, (all * d.H + (int)gridDim.x - 1) / (int)gridDim.x);
+        cut = (all * d.H + (int)gridDim.x - 1) / (int)gridDim.x;
         for (all = scan(); all * d.H > (int)gridDim.x; all = scan())
           cut = max(cut + 1, (int)((long long)cut * all * d.H / (int)gridDim.x));
       }
@@ -469,28 +469,29 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(&emptyK[st]);   // the next block's keys may come
-        float alpha[2];
+        // each lane looks whether one of its own logits is past what the reference allows; the rows' maxima are taken
+        // where one is
+        float top[2];
         bool grows = false;
 #pragma unroll
         for (int e2 = 0; e2 < 2; ++e2) {   // rows 2t, 2t + 1
-          float top = max3(s[0][e2], s[0][2 + e2], s[1][e2]);
-          top = max3(top, s[1][2 + e2], s[2][e2]);
-          top = max3(top, s[2][2 + e2], s[3][e2]);
-          top = fmaxf(top, s[3][2 + e2]);
-#pragma unroll
-          for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-          alpha[e2] = 1.f;
-          const float old = mx[e2];
-          if (!kBias) top = fmaf(top, f[e2], -kLift);
-          if (top != -INFINITY && (old == -INFINITY || (kBias ? (top - old) * kLog2e : top - old) > kGrow)) {
-            mx[e2] = top;
-            alpha[e2] = ex2_approx(kBias ? (old - top) * kLog2e : old - top);   // (of -inf: zero)
-            grows = true;
-          }
+          top[e2] = max3(s[0][e2], s[0][2 + e2], s[1][e2]);
+          top[e2] = fmaxf(max3(top[e2], s[1][2 + e2], s[2][e2]), max3(s[2][2 + e2], s[3][e2], s[3][2 + e2]));
+          if (!kBias) top[e2] = fmaf(top[e2], f[e2], -kLift);
+          grows |= (kBias ? (top[e2] - mx[e2]) * kLog2e : top[e2] - mx[e2]) > kGrow;   // (mx = -inf: by any but -inf)
         }
         if (__any_sync(0xffffffffu, grows)) {
+          float alpha[2];
 #pragma unroll
-          for (int e2 = 0; e2 < 2; ++e2) l[e2] *= alpha[e2];
+          for (int e2 = 0; e2 < 2; ++e2) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) top[e2] = fmaxf(top[e2], __shfl_xor_sync(0xffffffffu, top[e2], w));
+            const float by = kBias ? (mx[e2] - top[e2]) * kLog2e : mx[e2] - top[e2];
+            const bool up = top[e2] != -INFINITY && (mx[e2] == -INFINITY || -by > kGrow);
+            alpha[e2] = up ? ex2_approx(by) : 1.f;   // (mx = -inf: zero)
+            if (up) mx[e2] = top[e2];
+            l[e2] *= alpha[e2];
+          }
 #pragma unroll
           for (int k = 0; k < 8; ++k)
 #pragma unroll

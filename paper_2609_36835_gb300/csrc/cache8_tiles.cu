@@ -693,52 +693,55 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             for (int k = 0; k < 4; ++k)
               if (j0 + 8 * j + (k & 1) >= see[k >> 1]) v[4 * j + k] = -INFINITY;
         }
-        float alpha[2];
+        // Each lane looks whether one of its own logits is past what the reference allows; the rows' maxima are taken
+        // where one is.  (f > 0: the largest product is the largest logit.)
+        float top[2];
         bool grows = false;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          float top = fmaxf(v[2 * k], v[2 * k + 1]), b = fmaxf(v[4 + 2 * k], v[4 + 2 * k + 1]);
+          float b = max3(v[4 + 2 * k], v[5 + 2 * k], v[8 + 2 * k]);
+          top[k] = max3(v[2 * k], v[2 * k + 1], v[9 + 2 * k]);
 #pragma unroll
-          for (int j = 2; j < 8; j += 2) {
-            top = max3(top, v[4 * j + 2 * k], v[4 * j + 2 * k + 1]);
-            b = max3(b, v[4 * j + 4 + 2 * k], v[4 * j + 4 + 2 * k + 1]);
+          for (int j = 3; j < 8; j += 2) {
+            top[k] = max3(top[k], v[4 * j + 2 * k], v[4 * j + 2 * k + 1]);
+            if (j < 7) b = max3(b, v[4 * j + 4 + 2 * k], v[4 * j + 5 + 2 * k]);
           }
-          top = fmaxf(top, b);
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          alpha[k] = 1.f;
-          if (kBias) {
-            // in units of log2: (x - ref) log2 e + lv - refv; differences of logits first, so that the type's lowest
-            // value cancels against itself
-            if (top != -INFINITY && (ref[k] == -INFINITY || fmaf(top - ref[k], kLog2e, m.lv - refv[k]) > kGrow)) {
-              const float by = ref[k] == -INFINITY ? -INFINITY : fmaf(ref[k] - top, kLog2e, refv[k] - m.lv);
-              alpha[k] = ex2_approx(by);
-              l[k] = scaled(l[k], by);
-              ref[k] = top;
-              refv[k] = m.lv;
-              grows = true;
-            }
-          } else {
-            top = fmaf(top, f[k], m.lv);   // f > 0: the largest product is the largest logit
-            if (top > ref[k] + kGrow || (ref[k] == -INFINITY && top != -INFINITY)) {
-              alpha[k] = ex2_approx(ref[k] - top);
-              l[k] = scaled(l[k], ref[k] - top);
-              ref[k] = top;
-              grows = true;
-            }
-          }
+          top[k] = fmaxf(top[k], b);
+          // in units of log2; with biases (x - ref) log2 e + lv - refv, differences of logits first, so that the type's
+          // lowest value cancels against itself.  (A reference of -inf is past by any logit but -inf.)
+          grows |= kBias ? fmaf(top[k] - ref[k], kLog2e, m.lv - refv[k]) > kGrow : fmaf(top[k], f[k], m.lv) > ref[k] + kGrow;
         }
-        if (i % kFlush != 0 && __any_sync(0xffffffffu, grows)) {   // scale O
-          if (!product_done(q - 1)) break;
-#pragma unroll 1
-          for (int ch = 0; ch < 4; ++ch) {
-            float o[16];
-            tmem_ld_rows32(Ot + ch * 32, o);
-            tmem_wait_ld();
-            settle(o);
+        if (__any_sync(0xffffffffu, grows)) {
+          float alpha[2];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] *= alpha[(e >> 1) & 1];
-            tmem_st_rows32(Ot + ch * 32, o);
+          for (int k = 0; k < 2; ++k) {
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+            top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+            const float to = kBias ? top[k] : fmaf(top[k], f[k], m.lv), tov = kBias ? m.lv : 0.f;
+            // what the sums shrink by, as a power of two
+            const float by = ref[k] == -INFINITY ? -INFINITY
+                             : kBias             ? fmaf(ref[k] - to, kLog2e, refv[k] - tov)
+                                                 : ref[k] - to;
+            const bool up = to != -INFINITY && -by > kGrow;
+            alpha[k] = up ? ex2_approx(by) : 1.f;
+            if (up) {
+              l[k] = scaled(l[k], by);
+              ref[k] = to;
+              refv[k] = tov;
+            }
+          }
+          if (i % kFlush != 0) {   // scale O
+            if (!product_done(q - 1)) break;
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
+              float o[16];
+              tmem_ld_rows32(Ot + ch * 32, o);
+              tmem_wait_ld();
+              settle(o);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] *= alpha[(e >> 1) & 1];
+              tmem_st_rows32(Ot + ch * 32, o);
+            }
           }
         }
         float2 base[2], add[2], sum[2];
