@@ -4,20 +4,29 @@
 // With n rows a head every code is used n times, so the call is bound by the
 // tensor pipe.  A CTA takes 128 or 256 rows of one head (one or two M = 128
 // tiles) and goes over the keys a block of 64 at a time:
-//   converters (4 warps)  read the codes of K and V and leave them in shared
-//                         memory as f16 operands, V transposed, four blocks
-//                         ahead; a code costs about one instruction for 256 rows
+//   codes (1 warp)        TMA of a block's codes (64 x 128 of K and of V) into a ring
+//   converters (4 warps)  codes to f16 operands in shared memory, V transposed by
+//                         matrix loads and stores, three blocks ahead; a code costs
+//                         about one instruction for 256 rows
 //   MMA warp              S = Q K^T (exact products, fp32 sums in TMEM), O += P V
 //   softmax (8 warps a tile, 16 rows each, four lanes a row)  turn S into weights
 //                         in place: the f16 pair hi + lo of 32 keys takes the 32
 //                         columns that their logits had; P is the MMA's operand
 //                         from TMEM
+//   scales, cuts (1 warp each)  the blocks' scales; which item other CTAs go on with
 // P V runs once for hi and once for lo, which keeps 22 bits of a weight: three
 // units of MMA work where f16 weights would do with two, so 2/3 of the pipe's
 // peak is the most that the fp32 output allows.  A tile has two buffers of S in
 // TMEM: the softmax of one block runs beside the products of its neighbours.  (With
 // one buffer and Q in TMEM too, S takes 256 instead of 392 cycles a block and tile,
-// but softmax and products wait for each other: 374 instead of XXX us.)
+// but softmax and products wait for each other: 374 us instead of 338 then.)
+//
+// Work is dealt out in equal shares of blocks; an item (head and row tile) that
+// several CTAs share is added up by cache_join_kernel behind this one.
+// Measured (8 heads): 512 positions of 4 rows over 32K 300 us, 0.91 PFLOP/s of the
+// 1.28 that two passes over V leave of the pipe's 1.91; softmax issue (61 %) and
+// tensor pipe (75 % busy) bound it.  128 rows over 16 x 8K 131 us, 32 rows 110: one
+// tile's chain of S, softmax and P V, 1700 cycles a block.
 //
 // The weight of key j of block b carries the block's scale of V:
 //   w_j = 2^{x_j + log2 vs_b - ref + 7},  O = sum_j w_j c_j / sum_b (sum_{j in b} w_j) / vs_b
@@ -45,7 +54,7 @@ constexpr float kTiny = -40.f;                // log2 of the scale of a block of
 constexpr float kVsUnit = 0x1p-20f;           // sums are in units of kVsUnit / vs: the least vs, 2^-107, stays in range
 
 struct TileShape {
-  int H, n_pos, G, nblk, cap, tiles;   // tiles: row tiles of a head
+  int H, n_pos, G, nblk, tiles;   // tiles: row tiles of a head
   bool causal;
 };
 
@@ -54,7 +63,7 @@ struct TileCfg {
   static constexpr int kRows = 128 * kT;
   static constexpr int kSoft = 8 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
   static constexpr int kSoftThreads = 32 * kSoft;
-  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: MMA, scales, two idle warps
+  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: MMA, scales, codes, cuts
   // registers at launch, and how the warpgroups share them: softmax (2 kT groups), converters, MMA
   static constexpr int kRegs = kT == 2 ? 80 : 128;
   static constexpr int kRegsSoft = kT == 2 ? 96 : 176, kRegsConv = kT == 2 ? 64 : 96, kRegsMma = kT == 2 ? 32 : 64;
@@ -967,7 +976,6 @@ int launch_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float*
   d.n_pos = q.n_pos;
   d.G = q.G;
   d.nblk = c.cap / kCB;
-  d.cap = c.cap;
   d.tiles = cdiv((long long)q.n_pos * q.G, Cfg::kRows);
   d.causal = q.causal;
   auto kern = cache_tiles_kernel<kT, kBias>;
@@ -995,6 +1003,7 @@ size_t cache_tiles_scratch(long long rows) {
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
                        cudaStream_t st) {
   const long long rows = (long long)q.n_pos * q.G;
+  // one tile where it holds all rows (128 over 16 x 8 heads of 8K: 131 us, with two 195)
   if (rows <= 128)
     return c.bias ? launch_tiles<1, true>(c, q, scale, O, os, ws, st) : launch_tiles<1, false>(c, q, scale, O, os, ws, st);
   return c.bias ? launch_tiles<2, true>(c, q, scale, O, os, ws, st) : launch_tiles<2, false>(c, q, scale, O, os, ws, st);
