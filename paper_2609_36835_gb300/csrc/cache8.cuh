@@ -33,16 +33,23 @@ constexpr int kCacheMaxCtas = 160;   // CTAs of the persistent kernels, at most 
 __host__ __device__ inline int* ws_tickets(void* ws) { return (int*)((char*)ws + sizeof(DevStatus)); }
 static_assert(sizeof(DevStatus) + kCacheMaxCtas * sizeof(int) <= ARCKV_CACHE_WS_HEADER, "tickets fit the header");
 
-// Equal shares of `total` units: CTA c has [start(c), start(c + 1)).
+// a / b for a >= 0, b > 0, in 32 bits where both fit.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return (long long)((unsigned int)a / (unsigned int)b);
+  return a / b;
+}
+// Equal shares of `total` units: CTA c has [start(c), start(c + 1)), one unit more for the first r.
 struct CacheShares {
-  long long total;
-  int ctas;
-  __device__ long long start(int c) const { return total * c / ctas; }
+  long long total, q;
+  int ctas, r;
+  __device__ CacheShares(long long units, int grid) : total(units), ctas((int)min((long long)grid, units)) {
+    q = quotient(total, ctas);
+    r = (int)(total - q * ctas);
+  }
+  __device__ long long start(int c) const { return q * c + min(c, r); }
   __device__ int owner(long long u) const {   // the CTA that has unit u
-    int c = (int)((u * ctas + ctas - 1) / total);
-    while (c > 0 && start(c) > u) --c;
-    while (c + 1 < ctas && start(c + 1) <= u) ++c;
-    return c;
+    const long long big = r * (q + 1);
+    return u < big ? (int)quotient(u, q + 1) : r + (int)quotient(u - big, q);
   }
 };
 

@@ -241,7 +241,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
     else hi = mid;
   }
   g.s = lo;
-  const long long per = pre[lo + 1] - pre[lo], rest = u - pre[lo] * d.H, h = rest / per;
+  const long long per = pre[lo + 1] - pre[lo], rest = u - pre[lo] * d.H, h = quotient(rest, per);
   g.sh = (long long)lo * d.H + h;
   const int len = cache_len(c, lo), lane = threadIdx.x & 31;
   int at = (int)(rest - h * per);
@@ -303,6 +303,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   __shared__ __align__(8) uint64_t raw_full[kRaw], raw_empty[kRaw];
   __shared__ Meta meta[2 * kStages];
   __shared__ uint32_t tmem_slot;
+  __shared__ long long s_share[2];
+  __shared__ Segment s_first;
   __shared__ int abort_flag, stop_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abortp = &abort_flag;
@@ -353,23 +355,32 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       run += __shfl_sync(0xffffffffu, x, 31);
     }
     if (lane == 0) pre[0] = 0;
+    __syncwarp();
+    // the CTA's share and its first item, found once: short calls take their code from memory, every copy of it
+    const CacheShares sh(run * d.H, gridDim.x);
+    const long long u0 = sh.start(min((int)blockIdx.x, sh.ctas)), u1 = sh.start(min((int)blockIdx.x + 1, sh.ctas));
+    Segment g = {};
+    if (u0 < u1) g = segment_of(u0, d, c, pre, kRows);
+    if (lane == 0) {
+      s_share[0] = u0;
+      s_share[1] = u1;
+      s_first = g;
+    }
   }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = tmem_slot;   // tile t: two buffers of S / P at columns 256 t, O at 256 t + 128
-  CacheShares sh;
-  sh.total = pre[c.S] * d.H;
-  sh.ctas = (int)min((long long)gridDim.x, sh.total);
-  const bool active = (int)blockIdx.x < sh.ctas;
-  const long long u0 = active ? sh.start(blockIdx.x) : 0, u1 = active ? sh.start(blockIdx.x + 1) : 0;
+  const long long u0 = s_share[0], u1 = s_share[1];
 
   if (warp == kSoft + 7) {
     // ------------------------ the item that begins here and goes on in other CTAs
     regs_dec<Cfg::kRegsMma>();
     int4 cut = make_int4(0, 0, -1, 0);
-    if (active) {
-      const Segment g = segment_of(u1 - 1, d, c, pre, kRows);
+    if (u0 < u1) {
+      const CacheShares sh(pre[c.S] * d.H, gridDim.x);
+      Segment g = s_first;
+      if (g.first + g.count < u1) g = segment_of(u1 - 1, d, c, pre, kRows);
       const long long end = g.first + g.count;
       if (end > u1 && g.first >= u0) cut = make_int4((int)g.sh, g.tile, sh.owner(end - 1), 0);
     }
@@ -379,8 +390,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     regs_dec<Cfg::kRegsMma>();
     bool ok = true;
     int q = 0;   // blocks issued
+    Segment g = s_first;
     for (long long u = u0; u < u1 && ok;) {
-      const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
       for (int i = 0; i < n; ++i, ++q) {   // (blocks lie within the capacity: `count` does)
         const int st = q % kRaw;
@@ -393,6 +404,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         }
       }
       u += n;
+      if (u < u1) g = segment_of(u, d, c, pre, kRows);
     }
     if (!ok) {   // let the copies in flight land before the CTA's memory goes
       volatile int never = 0;
@@ -403,8 +415,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     regs_dec<Cfg::kRegsMma>();
     bool ok = true;
     int it = 0;
+    Segment g = s_first;
     for (long long u = u0; u < u1 && ok;) {
-      const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u), len = cache_len(c, g.s);
       Meta m;
       for (int i = 0; i < n && ok; ++i) {
@@ -427,6 +439,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       }
       it += n;
       u += n;
+      if (u < u1) g = segment_of(u, d, c, pre, kRows);
     }
   } else if (warp == kSoft + 4) {
     // ------------------------------------------------------------ MMA issuer
@@ -436,10 +449,10 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     // warp-wide reductions leave their result in uniform registers
     const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
     const uint64_t q_desc = tc::sdesc_k128(tc::smem_u32(sQ)), kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
+    int steps = s_first.count - s_first.step;   // of this item
     int seg = 0, left = __reduce_max_sync(0xffffffffu, (int)(u1 - u0));   // blocks to come
     for (long long u = u0; left > 0 && ok; ++seg) {
-      const Segment g = segment_of(u, d, c, pre, kRows);
-      const int n = __reduce_max_sync(0xffffffffu, min(g.count - g.step, left));
+      const int n = __reduce_max_sync(0xffffffffu, min(steps, left));
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&qfull, seg & 1, abortp, stt));
       // S of block i, then P V of block i - 1
       for (int i = 0; i <= n && ok; ++i) {
@@ -479,6 +492,10 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       }
       left -= n;
       u += n;
+      if (left > 0) {
+        const Segment next = segment_of(u, d, c, pre, kRows);
+        steps = next.count - next.step;
+      }
     }
     __syncwarp();
     {   // every MMA done before TMEM and shared memory go
@@ -556,8 +573,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     };
     auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
     int it = 0;
+    Segment g = s_first;
     for (long long u = u0; u < u1;) {
-      const Segment g = segment_of(u, d, c, pre, kRows);
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
       const int row0 = g.tile * kRows + t * 128, h = (int)(g.sh - (long long)g.s * d.H), len = cache_len(c, g.s);
       float row_fac;
@@ -855,6 +872,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           __stcg((float4*)(slot + (long long)(16 + k) * Cfg::kSoftThreads * 4), make_float4(ref[k], refv[k], l[k], 0.f));
       }
       u += n;
+      if (u < u1) g = segment_of(u, d, c, pre, kRows);
     }
   }
   tc::fence_before_sync();
@@ -875,18 +893,25 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
                                                                   const float* parts, const int4* cuts, int n_cuts,
                                                                   DevStatus* stt) {
   using Cfg = TileCfg<kT>;
-  __shared__ int s_item[kCacheMaxCtas];
+  __shared__ int4 s_cut[kCacheMaxCtas];   // of the items, in order; w: the CTA in which it begins
   __shared__ int s_items;
   __shared__ float s_w[kCacheMaxCtas][16], s_inv[16];
   const int tid = threadIdx.x, lane = tid & 31, nrows = n_pos * G;
   pdl_trigger();
   pdl_wait();
-  if (tid < 32) {   // the items, in order
+  if (tid < 32) {
+    int4 cut[kCacheMaxCtas / 32];
+#pragma unroll
+    for (int i = 0; i < kCacheMaxCtas / 32; ++i) {
+      cut[i] = make_int4(0, 0, -1, 0);
+      if (32 * i + lane < n_cuts) cut[i] = __ldcg(cuts + 32 * i + lane);
+    }
     int n = 0;
-    for (int c0 = 0; c0 < n_cuts; c0 += 32) {
-      const bool cut = c0 + lane < n_cuts && cuts[c0 + lane].z >= 0;
-      const unsigned int all = __ballot_sync(0xffffffffu, cut);
-      if (cut) s_item[n + __popc(all & ((1u << lane) - 1u))] = c0 + lane;
+#pragma unroll
+    for (int i = 0; i < kCacheMaxCtas / 32; ++i) {
+      const unsigned int all = __ballot_sync(0xffffffffu, cut[i].z >= 0);
+      cut[i].w = 32 * i + lane;
+      if (cut[i].z >= 0) s_cut[n + __popc(all & ((1u << lane) - 1u))] = cut[i];
       n += __popc(all);
     }
     if (lane == 0) s_items = n;
@@ -894,12 +919,23 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
   __syncthreads();
   const int work = s_items * Cfg::kSoft;
   for (int x = blockIdx.x; x < work; x += gridDim.x) {
-    const int first = s_item[x / Cfg::kSoft], warp = x % Cfg::kSoft;
-    const int4 cut = cuts[first];
-    const int n = cut.z - first + 1;
+    const int4 cut = s_cut[x / Cfg::kSoft];
+    const int first = cut.w, warp = x % Cfg::kSoft, n = cut.z - first + 1;
     const int row0 = cut.y * Cfg::kRows + warp * 16;
     if (row0 >= nrows) continue;   // (uniform)
     auto part = [&](int p) { return parts + (2ll * (first + p) + (p == 0)) * Cfg::kSlot + warp * 128; };
+    // The sums' loads wait for nothing: the first eight parts' are under way while the weights are found.  Sixteen bytes
+    // of two units a thread: columns 8 j + 2 (lane % 4), + 1 of rows lane / 4 and lane / 4 + 8.
+    const int r8 = lane >> 2, j8 = tid >> 5;
+    float4 ahead[8][2];
+    auto load = [&](int p0) {
+#pragma unroll
+      for (int p = 0; p < 8; ++p)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (p0 + p < n) ahead[p][e] = __ldcg((const float4*)(part(p0 + p) + lane * 4 + (long long)(j8 + 8 * e) * Cfg::kSoftThreads * 4));
+    };
+    load(0);
     {   // weights of the parts for row tid / 16, sixteen parts at a time
       const int r = tid >> 4, l16 = tid & 15;
       const long long at = (long long)(16 + (r >> 3)) * Cfg::kSoftThreads * 4 + (r & 7) * 16;
@@ -912,7 +948,10 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
           topv = av;
         }
       };
-      for (int p = l16; p < n; p += 16) {
+      float4 mine = make_float4(-INFINITY, 0.f, 0.f, 0.f);   // of the first sixteen parts
+      if (l16 < n) mine = __ldcg((const float4*)(part(l16) + at));
+      raise(mine.x, mine.y);
+      for (int p = l16 + 16; p < n; p += 16) {
         const float2 y = __ldcg((const float2*)(part(p) + at));
         raise(y.x, y.y);
       }
@@ -923,7 +962,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
       }
       float z = 0.f;
       for (int p = l16; p < n; p += 16) {
-        const float4 y = __ldcg((const float4*)(part(p) + at));
+        const float4 y = p == l16 ? mine : __ldcg((const float4*)(part(p) + at));
         float w = 0.f;
         if (y.x != -INFINITY) {   // (else a part that saw nothing)
           const float by = beyond(y.x, y.y, top, topv);
@@ -937,26 +976,28 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(int H, int n_p
       if (l16 == 0) s_inv[r] = z == 0.f ? 0.f : kVsUnit / z;
     }
     __syncthreads();
-    {   // sixteen bytes of two units a thread: columns 8 j + 2 (lane % 4), + 1 of rows lane / 4 and lane / 4 + 8
-      const int r = lane >> 2, j = tid >> 5;
+    {
       float4 a[2];
       a[0] = a[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int p = 0; p < n; ++p) {
-        const float* src = part(p) + lane * 4;
-        const float w0 = s_w[p][r], w1 = s_w[p][r + 8];
+      for (int p0 = 0; p0 < n; p0 += 8) {
+        if (p0 > 0) load(p0);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float4 y = __ldcg((const float4*)(src + (long long)(j + 8 * e) * Cfg::kSoftThreads * 4));
-          a[e] = make_float4(fmaf(y.x, w0, a[e].x), fmaf(y.y, w0, a[e].y), fmaf(y.z, w1, a[e].z), fmaf(y.w, w1, a[e].w));
+        for (int p = 0; p < 8; ++p) {
+          if (p0 + p >= n) break;
+          const float w0 = s_w[p0 + p][r8], w1 = s_w[p0 + p][r8 + 8];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float4 y = ahead[p][e];
+            a[e] = make_float4(fmaf(y.x, w0, a[e].x), fmaf(y.y, w0, a[e].y), fmaf(y.z, w1, a[e].z), fmaf(y.w, w1, a[e].w));
+          }
         }
       }
-      const int s = cut.x / H, h = cut.x - s * H, q0 = row0 + r, q1 = q0 + 8;
+      const int s = cut.x / H, h = cut.x - s * H, q0 = row0 + r8, q1 = q0 + 8;
       const long long at0 = (q0 / G) * os.i + (q0 % G) * 128, at1 = (q1 / G) * os.i + (q1 % G) * 128;
-      const float i0 = s_inv[r], i1 = s_inv[r + 8];
+      const float i0 = s_inv[r8], i1 = s_inv[r8 + 8];
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        store_rows(O + s * os.s + h * os.h + 8 * (j + 8 * e) + 2 * (lane & 3), at0, at1, q0 < nrows, q1 < nrows,
+        store_rows(O + s * os.s + h * os.h + 8 * (j8 + 8 * e) + 2 * (lane & 3), at0, at1, q0 < nrows, q1 < nrows,
                    make_float4(a[e].x * i0, a[e].y * i0, a[e].z * i1, a[e].w * i1), stt);
     }
     __syncthreads();
