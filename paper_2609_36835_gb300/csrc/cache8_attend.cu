@@ -31,8 +31,8 @@
 //    weights go from one product to the other by an 8 x 8 transpose in registers;
 //    V's operand comes by transposed loads of 16-bit units, two dims of a key each.
 //
-// Measured: 64 ragged sequences x 8 heads, up to 8K, 4 rows: 117 us, 6.6 TB/s (97 % of
-// a copy's rate); one of 128K 47.8 us (5.6 TB/s: 6 us are start and join).  12 rows with
+// Measured: 64 ragged sequences x 8 heads, up to 8K, 4 rows: 118 us, 6.6 TB/s (97 % of
+// a copy's rate); one of 128K 48 us (5.6 TB/s: 6 us are start and join).  12 rows with
 // biases over 64 x 8 x 1641: 65 us, 3.4 TB/s, bound by two warps' dequantising and
 // products of a block (44 without arithmetic).  32 listed blocks for each of 128
 // positions x 8 heads: 76 us, 7.1 TB/s of codes from L2 (50 us without arithmetic).
@@ -42,7 +42,7 @@
 namespace arckv {
 namespace {
 
-// More rows of a head go to the tcgen05 kernel (32 x 8 heads of 8K: 16 rows take 117 us here and 244 there, as 17 do).
+// More rows of a head go to the tcgen05 kernel (32 x 8 heads of 8K: 16 rows take 117 us here, 17 there 215).
 constexpr int kRowsMax = 16;
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 

@@ -23,10 +23,10 @@
 //
 // Work is dealt out in equal shares of blocks; an item (head and row tile) that
 // several CTAs share is added up by cache_join_kernel behind this one.
-// Measured (8 heads): 512 positions of 4 rows over 32K 300 us, 0.91 PFLOP/s of the
+// Measured (8 heads): 512 positions of 4 rows over 32K 296 us, 0.92 PFLOP/s of the
 // 1.28 that two passes over V leave of the pipe's 1.91; softmax issue (61 %) and
-// tensor pipe (75 % busy) bound it.  128 rows over 16 x 8K 131 us, 32 rows 110: one
-// tile's chain of S, softmax and P V, 1700 cycles a block.
+// tensor pipe (75 % busy) bound it.  128 rows over 16 x 8K 129 us, 32 rows 109: one
+// tile's chain of S, softmax and P V, 1700 cycles a block; 32 rows over 1K 13 us.
 //
 // The weight of key j of block b carries the block's scale of V:
 //   w_j = 2^{x_j + log2 vs_b - ref + 7},  O = sum_j w_j c_j / sum_b (sum_{j in b} w_j) / vs_b
@@ -1044,7 +1044,7 @@ size_t cache_tiles_scratch(long long rows) {
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
                        cudaStream_t st) {
   const long long rows = (long long)q.n_pos * q.G;
-  // one tile where it holds all rows (128 over 16 x 8 heads of 8K: 131 us, with two 195)
+  // one tile where it holds all rows (128 over 16 x 8 heads of 8K: 129 us; 132 rows, with two, 178)
   if (rows <= 128)
     return c.bias ? launch_tiles<1, true>(c, q, scale, O, os, ws, st) : launch_tiles<1, false>(c, q, scale, O, os, ws, st);
   return c.bias ? launch_tiles<2, true>(c, q, scale, O, os, ws, st) : launch_tiles<2, false>(c, q, scale, O, os, ws, st);
