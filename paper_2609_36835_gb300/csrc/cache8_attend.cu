@@ -611,11 +611,12 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
     auto store = [&](int r, int dim, float4 v, float z) {
       const float inv = z == 0.f ? 0.f : 1.f / z;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      const int row = p.group * kR + r, pos = kSparse ? p.pos : row / d.G, gq = kSparse ? row : row - pos * d.G;
+      if (row >= nrows) return;   // (a tile without rows masks nothing: it may have met anything behind the end)
+      *(float4*)(O + p.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
       const float big = 3.402823466e38f;
       if (!(fabsf(v.x) <= big && fabsf(v.y) <= big && fabsf(v.z) <= big && fabsf(v.w) <= big))
         set_status(stt, ARCKV_ERR_NONFINITE);
-      const int row = p.group * kR + r, pos = kSparse ? p.pos : row / d.G, gq = kSparse ? row : row - pos * d.G;
-      if (row < nrows) *(float4*)(O + p.s * os.s + h * os.h + pos * os.i + gq * 128 + dim) = v;
     };
     // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
     constexpr int kSlot = kR * 132;   // 128 outputs, m, l (and two unused) for each row

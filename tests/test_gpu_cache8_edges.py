@@ -151,3 +151,17 @@ def test_rows_written_over_earlier_ones(n, dtype):
         for h in range(H):
             assert_holds(c, s, h, torch.cat([k[s, h, :at], k2[s, h], more[s, h]]),
                          torch.cat([v[s, h, :at], v2[s, h], more[s, h]]))
+
+
+# --------------------------------------------------------------- attention
+
+@pytest.mark.parametrize("G", [17, 20, 24, 33, 40])
+@pytest.mark.parametrize("behind", [float("nan"), float("inf")])
+def test_rows_that_do_not_exist_report_nothing(G, behind):
+    """Listed blocks, and query heads that leave a tile of 8 rows empty: what lies behind the end is nobody's."""
+    c = pk.cache_alloc(1, 2, 192, bias=True)
+    pk.cache_append(c, rows(21, 1, 2, 70), rows(22, 1, 2, 70, grow=0.0), bias=biases(23, 1, 2, 70))
+    c.bias[:, :, 70:] = behind
+    Q = queries(24, 1, 2, 1, G)
+    blocks = i32([0, 1, -1]).expand(1, 2, 1, 3).contiguous()
+    check_attend(c, Q, pk.cache_attend(c, Q, blocks=blocks), False, blocks)
