@@ -477,6 +477,10 @@ class Cache8:
         object.__setattr__(self, "_c", _Cache8(S, H, cap, d, *[_ptr(getattr(self, n)) for n, _ in _Cache8._fields_[4:]]))
         object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
+    def _tensors(self):
+        """All arrays that the calls read or write."""
+        return [getattr(self, n) for n, _ in _Cache8._fields_[4:]]
+
     @property
     def capacity(self) -> int:
         return self._c.cap
@@ -577,7 +581,7 @@ def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream
     if n == 0:
         return
     handle = (_current_handle(dev) if stream is None else
-              _side_stream(stream, dev, K, V, bias, at, counts, cache.K, cache.V).cuda_stream)
+              _side_stream(stream, dev, K, V, bias, at, counts, *cache._tensors()).cuda_stream)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
     st = load_library().arckv_cache_append(cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
                                            _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr, flags, handle)
@@ -594,7 +598,7 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
     c, dev = cache._c, cache.K.device
     if stream is not None:   # the outputs belong to the stream that fills them
-        stream = _side_stream(stream, dev, cache.K, cache.V)
+        stream = _side_stream(stream, dev, *cache._tensors())
         with torch.cuda.stream(stream):
             return cache_read(cache, start, count, dtype=dtype, check=check)
     K = torch.empty((c.S, c.H, max(count, 0), 128), dtype=dtype, device=dev)
@@ -630,7 +634,7 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     import torch
     n_pos, G = _check_queries(cache, Q)
     if stream is not None:   # a workspace and an output made here belong to the stream that fills them
-        stream = _side_stream(stream, Q.device, Q, blocks, out, ws, cache.K, cache.V)
+        stream = _side_stream(stream, Q.device, Q, blocks, out, ws, *cache._tensors())
         with torch.cuda.stream(stream):
             return cache_attend(cache, Q, logit_scale, blocks=blocks, causal=causal, out=out, ws=ws, check=check)
     m = 0
@@ -665,7 +669,7 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: in
     import torch
     n_pos, G = _check_queries(cache, Q)
     if stream is not None:
-        stream = _side_stream(stream, Q.device, Q, ws, cache.K, cache.V)
+        stream = _side_stream(stream, Q.device, Q, ws, *cache._tensors())
         with torch.cuda.stream(stream):
             return cache_select(cache, Q, m, keep_first=keep_first, keep_last=keep_last, causal=causal, ws=ws,
                                 check=check)

@@ -1,0 +1,108 @@
+"""What the 8-bit cache's Python calls do around the library call, on the host: the library is a stand-in that records
+its calls, and tensors that record the streams they are used on take the place of device memory."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+import paper_2609_36835_gb300 as pk
+
+S, H, CAP, G = 2, 3, 128, 4
+
+
+class Recorded(torch.Tensor):
+    """A host tensor that notes the streams it is recorded on."""
+    used = None
+
+    def record_stream(self, stream):
+        self.used.append((self.data_ptr(), stream))
+
+
+class Stream:
+    cuda_stream = 77
+
+
+@pytest.fixture
+def rig(monkeypatch):
+    """The cache calls over a stand-in library; `calls` are its calls, `used` the recorded (address, stream)."""
+    r = types.SimpleNamespace(calls=[], used=[], guards=[], device=0)
+    monkeypatch.setattr(Recorded, "used", r.used)
+
+    def entry(name, value=0):
+        def call(*args):
+            r.calls.append((name, args, list(r.guards)))
+            return value
+        return call
+
+    lib = types.SimpleNamespace(**{n: entry(n) for n in ("arckv_cache_append", "arckv_cache_read", "arckv_cache_attend",
+                                                         "arckv_cache_select")},
+                                arckv_cache_workspace_bytes=entry("arckv_cache_workspace_bytes", 8192))
+    monkeypatch.setattr(pk, "load_library", lambda: lib)
+    monkeypatch.setattr(pk, "_on_one_cuda_device", lambda **tensors: None)
+    monkeypatch.setattr(pk, "_current_handle", lambda device: 11)
+
+    @contextlib.contextmanager
+    def guard(what):
+        r.guards.append(what)
+        yield
+        r.guards.pop()
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: object())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: r.device)
+    monkeypatch.setattr(torch.cuda, "stream", guard)
+    monkeypatch.setattr(torch.cuda, "device", guard)
+    return r
+
+
+def z(*shape, dt=torch.float32):
+    return torch.zeros(*shape, dtype=dt).as_subclass(Recorded)
+
+
+def cache(bias=True):
+    nb = CAP // 64
+    return pk.Cache8(K=z(S, H, CAP, 128, dt=torch.uint8), V=z(S, H, CAP, 128, dt=torch.uint8), k_scale=z(S, H, nb),
+                     v_scale=z(S, H, nb), bounds=z(S, H, nb, 2, 128, dt=torch.int8), tail=z(S, H, 2, 64, 128),
+                     tail_amax=z(S, H, 2, 64), len=z(S, dt=torch.int32), bias=z(S, H, CAP) if bias else None,
+                     state=z(256, dt=torch.uint8))
+
+
+ARRAYS = ("K", "V", "k_scale", "v_scale", "bounds", "tail", "tail_amax", "len", "state")
+
+
+def arguments(n=5):
+    return dict(rows=z(S, H, n, 128, dt=torch.bfloat16), more=z(S, H, n, 128, dt=torch.bfloat16), bias=z(S, H, n),
+                at=z(S, dt=torch.int32), counts=z(S, dt=torch.int32), Q=z(S, H, 2, G, 128, dt=torch.bfloat16),
+                blocks=z(S, H, 2, 3, dt=torch.int32), out=z(S, H, 2, G, 128), ws=z(8192, dt=torch.uint8))
+
+
+CALLS = {
+    "append": (("rows", "more", "bias", "at", "counts"),
+               lambda c, a, **kw: pk.cache_append(c, a["rows"], a["more"], bias=a["bias"], at=a["at"], counts=a["counts"],
+                                                  **kw)),
+    "read": ((), lambda c, a, **kw: pk.cache_read(c, 0, 4, **kw)),
+    "attend": (("Q", "blocks", "out", "ws"),
+               lambda c, a, **kw: pk.cache_attend(c, a["Q"], blocks=a["blocks"], out=a["out"], ws=a["ws"], **kw)),
+    "select": (("Q", "ws"), lambda c, a, **kw: pk.cache_select(c, a["Q"], 3, ws=a["ws"], **kw)),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("bias", [True, False])
+def test_every_tensor_is_recorded_on_another_stream(rig, name, bias):
+    """All memory that a call reads or writes on a stream other than the current one: the cache's arrays too."""
+    c, a, stream = cache(bias=bias or name == "append"), arguments(), Stream()
+    given, call = CALLS[name]
+    call(c, a, stream=stream, check=False)
+    assert [n for n, _, _ in rig.calls] == ["arckv_cache_" + name]
+    want = {getattr(c, n).data_ptr() for n in ARRAYS} | {a[n].data_ptr() for n in given}
+    if c.bias is not None:
+        want.add(c.bias.data_ptr())
+    assert {address for address, _ in rig.used} == want
+    assert all(s is stream for _, s in rig.used)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_nothing_is_recorded_on_the_current_stream(rig, name):
+    CALLS[name][1](cache(), arguments(), check=False)
+    assert not rig.used
