@@ -281,6 +281,9 @@ def arckv_truncated_error(H: int, n: int, T: int, t: int, d: int, logit_scale: f
 
 
 def arckv_query_status(ws, stream=None) -> int:
+    dev = getattr(ws, "device", None)
+    if stream is None and dev is not None and dev.type == "cuda":   # the current stream of its device
+        return int(_on_device(dev, load_library().arckv_query_status, _ptr(ws), _current_handle(dev)))
     return int(load_library().arckv_query_status(_ptr(ws), _stream_handle(stream)))
 
 
@@ -547,6 +550,15 @@ def _current_handle(device) -> int:
     return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+def _on_device(device, call, *args):
+    """call(*args) with `device` as the current one: the library launches, and sizes its grids, for the current device."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
+
+
 def _counts_ptr(name: str, x, cache: "Cache8"):
     """Address of an int32 [S] argument on the cache's device, None for none."""
     import torch
@@ -583,8 +595,8 @@ def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream
     handle = (_current_handle(dev) if stream is None else
               _side_stream(stream, dev, K, V, bias, at, counts, *cache._tensors()).cuda_stream)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
-    st = load_library().arckv_cache_append(cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
-                                           _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr, flags, handle)
+    st = _on_device(dev, load_library().arckv_cache_append, cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
+                    _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr, flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_append")
 
@@ -607,7 +619,7 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
         return K, V
     handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
-    st = load_library().arckv_cache_read(cache._ref, start, count, K.data_ptr(), V.data_ptr(), flags, handle)
+    st = _on_device(dev, load_library().arckv_cache_read, cache._ref, start, count, K.data_ptr(), V.data_ptr(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_read")
     return K, V
@@ -653,9 +665,9 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
         raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = load_library().arckv_cache_attend(cache._ref, n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3),
-                                           _ptr(blocks), m, out.data_ptr(),
-                                           _strides3("out", out, 3), ws.data_ptr(), ws.numel(), flags, handle)
+    st = _on_device(Q.device, load_library().arckv_cache_attend, cache._ref, n_pos, G, logit_scale, Q.data_ptr(),
+                    _strides3("Q", Q, 3), _ptr(blocks), m, out.data_ptr(), _strides3("out", out, 3), ws.data_ptr(),
+                    ws.numel(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_attend")
     return out
@@ -678,9 +690,8 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: in
     blocks = torch.empty((Q.shape[0], Q.shape[1], n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = load_library().arckv_cache_select(cache._ref, n_pos, G, m, keep_first, keep_last, Q.data_ptr(),
-                                           _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags,
-                                           handle)
+    st = _on_device(Q.device, load_library().arckv_cache_select, cache._ref, n_pos, G, m, keep_first, keep_last,
+                    Q.data_ptr(), _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_select")
     return blocks

@@ -36,7 +36,7 @@ def rig(monkeypatch):
         return call
 
     lib = types.SimpleNamespace(**{n: entry(n) for n in ("arckv_cache_append", "arckv_cache_read", "arckv_cache_attend",
-                                                         "arckv_cache_select")},
+                                                         "arckv_cache_select", "arckv_query_status")},
                                 arckv_cache_workspace_bytes=entry("arckv_cache_workspace_bytes", 8192))
     monkeypatch.setattr(pk, "load_library", lambda: lib)
     monkeypatch.setattr(pk, "_on_one_cuda_device", lambda **tensors: None)
@@ -106,3 +106,32 @@ def test_every_tensor_is_recorded_on_another_stream(rig, name, bias):
 def test_nothing_is_recorded_on_the_current_stream(rig, name):
     CALLS[name][1](cache(), arguments(), check=False)
     assert not rig.used
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("check", [True, False])
+def test_the_library_runs_with_the_caches_device_current(rig, name, check):
+    """A cache on another device than the current one: the call is made inside a guard for the cache's device."""
+    c = cache()
+    rig.device = 1                       # (host tensors: a device without an index, which no current device equals)
+    CALLS[name][1](c, arguments(), check=check)
+    (entry, args, guards), = rig.calls
+    assert entry == "arckv_cache_" + name and guards == [c.K.device] and not rig.guards
+    assert args[-1] == 11                # the current stream of that device
+
+
+def test_no_guard_where_the_device_is_current(rig):
+    c = cache()
+    rig.device = c.K.device.index
+    for name in CALLS:
+        CALLS[name][1](c, arguments())
+    assert len(rig.calls) == len(CALLS) and not any(guards for _, _, guards in rig.calls)
+
+
+def test_the_status_is_read_on_the_words_device(rig):
+    word = types.SimpleNamespace(device=torch.device("cuda", 1), is_contiguous=lambda: True, data_ptr=lambda: 4096)
+    assert pk.arckv_query_status(word) == 0
+    assert rig.calls == [("arckv_query_status", (4096, 11), [word.device])]
+    rig.device = 1
+    assert pk.arckv_query_status(word) == 0 and rig.calls[1][2] == []
+    assert pk.arckv_query_status(4096, stream=Stream()) == 0 and rig.calls[2][1] == (4096, 77)
