@@ -625,6 +625,13 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
     return K, V
 
 
+def _check_workspace(cache: Cache8, ws):
+    """A workspace is bytes on the cache's device (the library checks size and alignment)."""
+    import torch
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or ws.device != cache.K.device or not ws.is_contiguous():
+        raise ValueError("arckv: ws must be a dense uint8 tensor on %s (cache_workspace makes one)" % cache.K.device)
+
+
 def _check_queries(cache: Cache8, Q):
     """Positions and query heads of Q, which must fit the cache."""
     import torch
@@ -659,6 +666,8 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
         m = shape[3]
     if ws is None:
         ws = cache_workspace(cache, n_pos, G)
+    else:
+        _check_workspace(cache, ws)
     if out is None:
         out = torch.empty_like(Q, dtype=torch.float32)
     elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
@@ -687,6 +696,8 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: in
                                 check=check)
     if ws is None:
         ws = cache_workspace(cache, n_pos, G)
+    else:
+        _check_workspace(cache, ws)
     blocks = torch.empty((Q.shape[0], Q.shape[1], n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)

@@ -135,3 +135,13 @@ def test_the_status_is_read_on_the_words_device(rig):
     rig.device = 1
     assert pk.arckv_query_status(word) == 0 and rig.calls[1][2] == []
     assert pk.arckv_query_status(4096, stream=Stream()) == 0 and rig.calls[2][1] == (4096, 77)
+
+
+@pytest.mark.parametrize("name", ["attend", "select"])
+@pytest.mark.parametrize("ws", [torch.zeros(8192, dtype=torch.uint8, device="meta"), torch.zeros(8192, dtype=torch.int8),
+                                torch.zeros(4096), torch.zeros(16384, dtype=torch.uint8)[::2], 4096])
+def test_workspaces_that_are_not_bytes_on_the_device_are_refused(rig, name, ws):
+    """Another device or type, gaps, or an address: the library would take the numbers as they are."""
+    with pytest.raises(ValueError, match="ws"):
+        CALLS[name][1](cache(), {**arguments(), "ws": ws})
+    assert not rig.calls
