@@ -659,9 +659,9 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     m = 0
     if blocks is not None:
         shape = blocks.shape
-        if (len(shape) != 4 or blocks.dtype != torch.int32 or shape[:3] != Q.shape[:3] or blocks.device != Q.device or
-                not blocks.is_contiguous()):
-            raise ValueError("arckv: blocks must be a dense int32 tensor of shape %s on %s, got %s %s on %s"
+        if (len(shape) != 4 or blocks.dtype != torch.int32 or shape[:3] != Q.shape[:3] or shape[3] == 0 or
+                blocks.device != Q.device or not blocks.is_contiguous()):   # (an empty one's address means no list)
+            raise ValueError("arckv: blocks must be a dense int32 tensor of shape %s, m >= 1, on %s, got %s %s on %s"
                              % (tuple(Q.shape[:3]) + ("m",), Q.device, blocks.dtype, tuple(shape), blocks.device))
         m = shape[3]
     if ws is None:

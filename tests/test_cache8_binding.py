@@ -145,3 +145,10 @@ def test_workspaces_that_are_not_bytes_on_the_device_are_refused(rig, name, ws):
     with pytest.raises(ValueError, match="ws"):
         CALLS[name][1](cache(), {**arguments(), "ws": ws})
     assert not rig.calls
+
+
+def test_a_list_without_entries_is_refused(rig):
+    """The address of an empty tensor is null, which stands for no list: every block would be read."""
+    with pytest.raises(ValueError, match="blocks"):
+        CALLS["attend"][1](cache(), {**arguments(), "blocks": z(S, H, 2, 0, dt=torch.int32)})
+    assert not rig.calls
