@@ -682,13 +682,15 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     return out
 
 
-def cache_select(cache: Cache8, Q, m: int, *, keep_first: int = 1, keep_last: int = 1, causal: bool = False, ws=None,
-                 stream=None, check: bool = True):
+def cache_select(cache: Cache8, Q, m: int, *, keep_first: Optional[int] = None, keep_last: int = 1, causal: bool = False,
+                 ws=None, stream=None, check: bool = True):
     """The m blocks of 64 tokens that each query position reads, [S, H, n_pos, m] int32 ascending, -1 for none: the
-    first keep_first, the newest keep_last and those whose logits can be largest.  Q, causal and ws as for
-    ``cache_attend``."""
+    first keep_first (one where m leaves room for it beside the newest, unless given), the newest keep_last and those
+    whose logits can be largest.  Q, causal and ws as for ``cache_attend``."""
     import torch
     n_pos, G = _check_queries(cache, Q)
+    if keep_first is None:
+        keep_first = 1 if m > keep_last else 0
     if stream is not None:
         stream = _side_stream(stream, Q.device, Q, ws, *cache._tensors())
         with torch.cuda.stream(stream):

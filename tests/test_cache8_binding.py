@@ -152,3 +152,11 @@ def test_a_list_without_entries_is_refused(rig):
     with pytest.raises(ValueError, match="blocks"):
         CALLS["attend"][1](cache(), {**arguments(), "blocks": z(S, H, 2, 0, dt=torch.int32)})
     assert not rig.calls
+
+
+@pytest.mark.parametrize("m,last,first", [(1, 1, 0), (1, 0, 1), (2, 1, 1), (2, 2, 0), (9, 1, 1)])
+def test_the_first_block_is_kept_where_there_is_room(rig, m, last, first):
+    c, a = cache(), arguments()
+    pk.cache_select(c, a["Q"], m, keep_last=last, ws=a["ws"])
+    pk.cache_select(c, a["Q"], m, keep_first=2, keep_last=last, ws=a["ws"])
+    assert [args[3:6] for _, args, _ in rig.calls] == [(m, first, last), (m, 2, last)]

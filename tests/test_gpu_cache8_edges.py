@@ -165,3 +165,19 @@ def test_rows_that_do_not_exist_report_nothing(G, behind):
     Q = queries(24, 1, 2, 1, G)
     blocks = i32([0, 1, -1]).expand(1, 2, 1, 3).contiguous()
     check_attend(c, Q, pk.cache_attend(c, Q, blocks=blocks), False, blocks)
+
+
+# --------------------------------------------------------------- selection
+
+@pytest.mark.parametrize("T", [0, 1, 64, 700])
+def test_one_block_is_the_newest(T):
+    """m = 1 leaves no room for the first block beside the newest one."""
+    c = pk.cache_alloc(1, 2, 704)
+    if T:
+        pk.cache_append(c, rows(44, 1, 2, T), rows(45, 1, 2, T))
+    Q = queries(46, 1, 2, 3, 4)
+    for causal in (False, True):
+        got = pk.cache_select(c, Q, 1, causal=causal).cpu().numpy()
+        for h in range(2):
+            _, ks, bounds, _, _ = held(c, 0, h)
+            assert np.array_equal(got[0, h], ref.select(host(Q[0, h]), bounds, ks, T, 1, 0, 1, causal))
