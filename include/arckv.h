@@ -395,7 +395,7 @@ size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d,
  *      begins q_strides[0] s + q_strides[1] h + q_strides[2] p + 128 g elements
  *      after the base (NULL: dense [S][H][n_pos][G][d]); base and strides are
  *      multiples of 16 bytes
- *   O  out fp32, addressed in the same way with o_strides
+ *   O  out fp32, addressed in the same way with o_strides; rows do not overlap
  *   blocks  NULL: all tokens; else int32 [S][H][n_pos][m] block indices, the
  *      only ones that position p of head h reads (arckv_cache_select writes
  *      them; distinct, in any order, -1 for none; an index past the cache

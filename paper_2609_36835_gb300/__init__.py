@@ -530,6 +530,16 @@ def _strides3(name: str, x, dense_from: int):
     return (ctypes.c_int64 * 3)(*[st[i] if x.shape[i] != 1 else 0 for i in range(3)])
 
 
+def _apart(x) -> bool:
+    """Whether no two elements of x share memory, for a view that slices and permutes a dense tensor."""
+    reach = 1
+    for st, n in sorted((st, n) for st, n in zip(x.stride(), x.shape) if n > 1):
+        if st < reach:
+            return False
+        reach = st * n
+    return True
+
+
 def _side_stream(stream, device, *tensors):
     """`stream` as a torch stream.  Tensors in use on a stream other than the current one are recorded there, so that
     their memory is not reused too early."""
@@ -672,6 +682,8 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
         out = torch.empty_like(Q, dtype=torch.float32)
     elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
         raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
+    elif not out.is_contiguous() and not _apart(out):
+        raise ValueError("arckv: rows of out share memory, strides %s" % (tuple(out.stride()),))
     handle = _current_handle(Q.device)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
     st = _on_device(Q.device, load_library().arckv_cache_attend, cache._ref, n_pos, G, logit_scale, Q.data_ptr(),

@@ -160,3 +160,17 @@ def test_the_first_block_is_kept_where_there_is_room(rig, m, last, first):
     pk.cache_select(c, a["Q"], m, keep_last=last, ws=a["ws"])
     pk.cache_select(c, a["Q"], m, keep_first=2, keep_last=last, ws=a["ws"])
     assert [args[3:6] for _, args, _ in rig.calls] == [(m, first, last), (m, 2, last)]
+
+
+def test_outputs_whose_rows_share_memory_are_refused(rig):
+    c, a = cache(), arguments()
+    whole = torch.zeros(S, 2, H, G, 128)
+    for out in (torch.zeros(S, 1, 2, G, 128).expand(S, H, 2, G, 128), torch.zeros(1, H, 2, G, 128).expand(S, H, 2, G, 128),
+                torch.zeros(9999).as_strided((S, H, 2, G, 128), (3 * H * 512, 2 * 512, 512 - 128, 128, 1))):
+        with pytest.raises(ValueError, match="out"):
+            CALLS["attend"][1](c, {**a, "out": out})
+    assert not rig.calls
+    for out in (whole.transpose(1, 2), torch.zeros(S, H, 5, G, 128)[:, :, 1:3], torch.zeros(2 * S, H, 4, G, 128)[::2, :, ::2],
+                torch.zeros(H, S, 2, G, 128).transpose(0, 1)):
+        CALLS["attend"][1](c, {**a, "out": out})
+    assert len(rig.calls) == 4
