@@ -530,6 +530,13 @@ def _strides3(name: str, x, dense_from: int):
     return (ctypes.c_int64 * 3)(*[st[i] if x.shape[i] != 1 else 0 for i in range(3)])
 
 
+def _expect_32_bits(**numbers):
+    """Numbers that are passed on as 32-bit integers, of which only the low bits would arrive."""
+    for name, x in numbers.items():
+        if not -(1 << 31) <= x < 1 << 31:
+            raise ValueError("arckv: %s is out of range: %d" % (name, x))
+
+
 def _apart(x) -> bool:
     """Whether no two elements of x share memory, for a view that slices and permutes a dense tensor."""
     reach = 1
@@ -618,6 +625,7 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
+    _expect_32_bits(start=start, count=count)
     c, dev = cache._c, cache.K.device
     if stream is not None:   # the outputs belong to the stream that fills them
         stream = _side_stream(stream, dev, *cache._tensors())
@@ -703,6 +711,7 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: Optional[int] = None, 
     n_pos, G = _check_queries(cache, Q)
     if keep_first is None:
         keep_first = 1 if m > keep_last else 0
+    _expect_32_bits(m=m, keep_first=keep_first, keep_last=keep_last)
     if stream is not None:
         stream = _side_stream(stream, Q.device, Q, ws, *cache._tensors())
         with torch.cuda.stream(stream):

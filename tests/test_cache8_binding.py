@@ -174,3 +174,14 @@ def test_outputs_whose_rows_share_memory_are_refused(rig):
                 torch.zeros(H, S, 2, G, 128).transpose(0, 1)):
         CALLS["attend"][1](c, {**a, "out": out})
     assert len(rig.calls) == 4
+
+
+@pytest.mark.parametrize("beyond", [1 << 32, -(1 << 32), 1 << 31])
+def test_numbers_past_32_bits_are_refused(rig, beyond):
+    """The library takes 32-bit integers: token 2^32 would be read as token 0."""
+    c, a = cache(), arguments()
+    for call in (lambda: pk.cache_read(c, beyond, 4), lambda: pk.cache_select(c, a["Q"], 3, keep_first=beyond, ws=a["ws"]),
+                 lambda: pk.cache_select(c, a["Q"], 3, keep_last=beyond, ws=a["ws"])):
+        with pytest.raises(ValueError, match="out of range"):
+            call()
+    assert not rig.calls
