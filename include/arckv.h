@@ -378,11 +378,14 @@ arckv_status arckv_cache_append(const arckv_cache8* c, int32_t n, const void* K,
 arckv_status arckv_cache_read(const arckv_cache8* c, int32_t start, int32_t count, void* K_out, void* V_out,
                               uint32_t flags, void* stream);
 
-/* Workspace bytes of arckv_cache_attend and arckv_cache_select (0 if the sizes
- * are invalid).  Host-only.  The first ARCKV_CACHE_WS_HEADER bytes of the
+/* Workspace bytes of arckv_cache_attend, of arckv_cache_select, and of one that
+ * serves both (0 if the sizes are invalid).  A selection holds a score of every
+ * block for each position, which attention does not need.  Host-only.  The first ARCKV_CACHE_WS_HEADER bytes of the
  * workspace must be zeroed once before its first use (and after
  * ARCKV_ERR_TIMEOUT); calls leave them zero (but for the status word). */
 #define ARCKV_CACHE_WS_HEADER 4096
+size_t arckv_cache_attend_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G);
+size_t arckv_cache_select_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G);
 size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G);
 
 /*

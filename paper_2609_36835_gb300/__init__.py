@@ -139,8 +139,10 @@ def load_library():
                                                                                               ctypes.c_uint32, P]
     lib.arckv_truncated_error.restype = ctypes.c_int
     I, L3, C = ctypes.c_int32, ctypes.POINTER(ctypes.c_int64 * 3), ctypes.POINTER(_Cache8)
-    lib.arckv_cache_workspace_bytes.argtypes = [I] * 6
-    lib.arckv_cache_workspace_bytes.restype = ctypes.c_size_t
+    for size in (lib.arckv_cache_workspace_bytes, lib.arckv_cache_attend_workspace_bytes,
+                 lib.arckv_cache_select_workspace_bytes):
+        size.argtypes = [I] * 6
+        size.restype = ctypes.c_size_t
     lib.arckv_cache_append.argtypes = [C, I, P, L3, P, L3, P, P, P, ctypes.c_uint32, P]
     lib.arckv_cache_append.restype = ctypes.c_int
     lib.arckv_cache_read.argtypes = [C, I, I, P, P, ctypes.c_uint32, P]
@@ -505,12 +507,16 @@ def cache_alloc(S: int, H: int, capacity: int, *, bias: bool = False, device="cu
 
 def cache_workspace(cache: Cache8, n_pos: int, G: int):
     """A workspace for ``cache_attend`` and ``cache_select`` with up to n_pos positions of G query heads.  Calls that
-    may run at the same time need one each."""
+    may run at the same time need one each.  (One of either call alone is smaller: the sizes are in the header.)"""
+    return _cache_workspace(cache, n_pos, G, "arckv_cache_workspace_bytes")
+
+
+def _cache_workspace(cache: Cache8, n_pos: int, G: int, size: str):
     import torch
     c = cache._c
-    need = int(load_library().arckv_cache_workspace_bytes(c.S, c.H, c.cap, c.d, n_pos, G))
+    need = int(getattr(load_library(), size)(c.S, c.H, c.cap, c.d, n_pos, G))
     if need == 0:
-        raise ArckvError(2, "arckv_cache_workspace_bytes")
+        raise ArckvError(2, size)
     ws = torch.empty(need, dtype=torch.uint8, device=cache.K.device)
     ws[:CACHE_WS_HEADER].zero_()
     return ws
@@ -683,7 +689,7 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
                              % (tuple(Q.shape[:3]) + ("m",), Q.device, blocks.dtype, tuple(shape), blocks.device))
         m = shape[3]
     if ws is None:
-        ws = cache_workspace(cache, n_pos, G)
+        ws = _cache_workspace(cache, n_pos, G, "arckv_cache_attend_workspace_bytes")
     else:
         _check_workspace(cache, ws)
     if out is None:
@@ -718,7 +724,7 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: Optional[int] = None, 
             return cache_select(cache, Q, m, keep_first=keep_first, keep_last=keep_last, causal=causal, ws=ws,
                                 check=check)
     if ws is None:
-        ws = cache_workspace(cache, n_pos, G)
+        ws = _cache_workspace(cache, n_pos, G, "arckv_cache_select_workspace_bytes")
     else:
         _check_workspace(cache, ws)
     blocks = torch.empty((Q.shape[0], Q.shape[1], n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)

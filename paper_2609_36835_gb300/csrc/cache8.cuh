@@ -125,7 +125,7 @@ int launch_cache_attend(const arckv_cache8& c, const CacheQuery& q, float scale,
 size_t cache_tiles_scratch(long long rows);
 int launch_cache_tiles(const arckv_cache8& c, const CacheQuery& q, float scale, float* O, RowStrides os, void* ws,
                        cudaStream_t st);
-size_t cache_select_scratch(int S, int H, int cap, int n_pos);
+size_t cache_select_scratch(int S, int H, int cap, int n_pos, int G);
 int launch_cache_select(const arckv_cache8& c, const CacheQuery& q, int m, int keep_first, int keep_last, int* blocks,
                         void* ws, cudaStream_t st);
 

@@ -48,13 +48,14 @@ arckv_status finish(void* status, uint32_t flags, void* stream) {
 }
 
 arckv_status check_query(const arckv_cache8* c, int32_t n_pos, int32_t G, const void* Q, const int64_t* q_strides,
-                         void* ws, size_t ws_bytes, uint32_t flags, CacheQuery* q) {
+                         void* ws, size_t ws_bytes, size_t scratch(int, int, int, int, int), uint32_t flags,
+                         CacheQuery* q) {
   if (flags & ~(ARCKV_FLAG_NONBLOCKING | ARCKV_FLAG_CAUSAL)) return ARCKV_ERR_INVALID_ARG;
   const arckv_status e = check_cache(c);
   if (e != ARCKV_OK) return e;
   if (!rows_ok(c->S, c->H, n_pos, G)) return ARCKV_ERR_SHAPE;
   if (!Q || !row_strides(Q, q_strides, c->H, n_pos, (int64_t)G * 128, 2, &q->qs)) return ARCKV_ERR_INVALID_ARG;
-  if (!ws || misaligned(ws, 256) || ws_bytes < arckv_cache_workspace_bytes(c->S, c->H, c->cap, c->d, n_pos, G))
+  if (!ws || misaligned(ws, 256) || ws_bytes < ARCKV_CACHE_WS_HEADER + scratch(c->S, c->H, c->cap, n_pos, G))
     return ARCKV_ERR_WORKSPACE;
   q->n_pos = n_pos;
   q->G = G;
@@ -67,10 +68,19 @@ arckv_status check_query(const arckv_cache8* c, int32_t n_pos, int32_t G, const 
 
 extern "C" {
 
-size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G) {
+size_t arckv_cache_attend_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G) {
   if (d != 128 || !sizes_ok(S, H, cap) || !rows_ok(S, H, n_pos, G)) return 0;
-  return ARCKV_CACHE_WS_HEADER +
-         std::max(cache_attend_scratch(S, H, cap, n_pos, G), cache_select_scratch(S, H, cap, n_pos));
+  return ARCKV_CACHE_WS_HEADER + cache_attend_scratch(S, H, cap, n_pos, G);
+}
+
+size_t arckv_cache_select_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G) {
+  if (d != 128 || !sizes_ok(S, H, cap) || !rows_ok(S, H, n_pos, G)) return 0;
+  return ARCKV_CACHE_WS_HEADER + cache_select_scratch(S, H, cap, n_pos, G);
+}
+
+size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d, int32_t n_pos, int32_t G) {
+  return std::max(arckv_cache_attend_workspace_bytes(S, H, cap, d, n_pos, G),
+                  arckv_cache_select_workspace_bytes(S, H, cap, d, n_pos, G));
 }
 
 arckv_status arckv_cache_append(const arckv_cache8* c, int32_t n, const void* K, const int64_t* k_strides,
@@ -108,7 +118,7 @@ arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G,
                                 const int64_t* q_strides, const int32_t* blocks, int32_t m, float* O,
                                 const int64_t* o_strides, void* ws, size_t ws_bytes, uint32_t flags, void* stream) {
   CacheQuery q;
-  const arckv_status e = check_query(c, n_pos, G, Q, q_strides, ws, ws_bytes, flags, &q);
+  const arckv_status e = check_query(c, n_pos, G, Q, q_strides, ws, ws_bytes, cache_attend_scratch, flags, &q);
   if (e != ARCKV_OK) return e;
   RowStrides os;
   if (!O || !row_strides(O, o_strides, c->H, n_pos, (int64_t)G * 128, 4, &os)) return ARCKV_ERR_INVALID_ARG;
@@ -126,7 +136,7 @@ arckv_status arckv_cache_select(const arckv_cache8* c, int32_t n_pos, int32_t G,
                                 int32_t keep_last, const void* Q, const int64_t* q_strides, int32_t* blocks, void* ws,
                                 size_t ws_bytes, uint32_t flags, void* stream) {
   CacheQuery q;
-  const arckv_status e = check_query(c, n_pos, G, Q, q_strides, ws, ws_bytes, flags, &q);
+  const arckv_status e = check_query(c, n_pos, G, Q, q_strides, ws, ws_bytes, cache_select_scratch, flags, &q);
   if (e != ARCKV_OK) return e;
   if (m < 1 || m > 8192 || keep_first < 0 || keep_last < 0 || (long long)keep_first + keep_last > m)
     return ARCKV_ERR_SHAPE;

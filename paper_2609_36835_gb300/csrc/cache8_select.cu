@@ -248,7 +248,7 @@ cudaError_t launch_pick(const arckv_cache8& c, const CacheQuery& q, const float*
 
 }  // namespace
 
-size_t cache_select_scratch(int S, int H, int cap, int n_pos) {
+size_t cache_select_scratch(int S, int H, int cap, int n_pos, int) {
   return (size_t)S * H * n_pos * (cap / kCB) * sizeof(float);
 }
 
