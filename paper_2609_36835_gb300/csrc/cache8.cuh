@@ -88,7 +88,9 @@ __device__ __forceinline__ float2 minus_f16(float2 x, __half2 h) {
 // The kernels of this file's callers start while the kernel before them on the
 // stream is still ending: pdl_wait() comes before their first access to memory
 // that another kernel may write or read, and pdl_trigger() lets the next one in
-// as soon as all CTAs have started.
+// as soon as all CTAs have started.  What the kernel before may still write is not
+// read-only for this one's whole life: loads are plain ones, never those of the
+// read-only path, which the compiler may also move above the wait.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

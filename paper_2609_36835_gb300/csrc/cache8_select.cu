@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(kScoreThreads) cache_score_kernel(const arckv_
   if (b < cand) {
     const int4* src = (const int4*)(c.bounds + (sh * nblk + b) * 256);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = __ldg(src + e);
+    for (int e = 0; e < 16; ++e) w[e] = src[e];
     ks = c.k_scale[sh * nblk + b];
   }
   const int rows = (p1 - p0) * q.G;
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kScoreThreads) cache_score_kernel(const arckv_
     __syncthreads();
     for (int r = warp; r < nr; r += kScoreThreads / 32) {
       const int pos = p0 + (r0 + r) / q.G, g = (r0 + r) % q.G;
-      const uint2 raw = __ldg((const uint2*)(q.Q + s * q.qs.s + h * q.qs.h + pos * q.qs.i + g * 128 + lane * 4));
+      const uint2 raw = *(const uint2*)(q.Q + s * q.qs.s + h * q.qs.h + pos * q.qs.i + g * 128 + lane * 4);
       const float2 a01 = __bfloat1622float2(*(const __nv_bfloat162*)&raw.x);
       const float2 a23 = __bfloat1622float2(*(const __nv_bfloat162*)&raw.y);
       const float x[4] = {a01.x, a01.y, a23.x, a23.y};

@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         for (int e = 0; e < 8; ++e) {
           x[e] = make_uint4(0u, 0u, 0u, 0u);
           if (row < nrows)
-            x[e] = __ldg((const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128 + half * 64) + e);
+            x[e] = *((const uint4*)(Q + g.s * qs.s + h * qs.h + pos * qs.i + gq * 128 + half * 64) + e);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float2 x = make_float2(0.f, 0.f);
-            if (j0 + 8 * j < max(see[0], see[1])) x = __ldg((const float2*)(bias + j0 + 8 * j));
+            if (j0 + 8 * j < max(see[0], see[1])) x = *(const float2*)(bias + j0 + 8 * j);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               v[4 * j + 2 * k] = fmaf(v[4 * j + 2 * k], f[k], x.x);

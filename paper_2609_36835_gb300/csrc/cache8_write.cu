@@ -38,7 +38,7 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466
 struct Eight16 {
   uint4 v;
   __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ void load(const bf16* p) { v = __ldg((const uint4*)p); }
+  __device__ __forceinline__ void load(const bf16* p) { v = *(const uint4*)p; }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     const unsigned int w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -52,8 +52,8 @@ struct Eight32 {
   float4 a, b;
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void load(const float* p) {
-    a = __ldg((const float4*)p);
-    b = __ldg((const float4*)p + 1);
+    a = *(const float4*)p;
+    b = *((const float4*)p + 1);
   }
   __device__ __forceinline__ void get(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
@@ -364,9 +364,9 @@ __global__ void __launch_bounds__(kWT, 4) cache_append_kernel(const arckv_cache8
   }
 }
 
-__device__ __forceinline__ float4 load4(const float* p) { return __ldg((const float4*)p); }
+__device__ __forceinline__ float4 load4(const float* p) { return *(const float4*)p; }
 __device__ __forceinline__ float4 load4(const bf16* p) {
-  const uint2 v = __ldg((const uint2*)p);
+  const uint2 v = *(const uint2*)p;
   return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
                      __uint_as_float(v.y & 0xffff0000u));
 }
