@@ -50,8 +50,9 @@ constexpr int kRawBytes = 2 * kTileBytes;                      // of a block as 
 constexpr int kFlush = 32;                    // blocks that O is summed up over in TMEM
 constexpr float kFar = 60.f;                  // growth of ref (log2) past which the flushed sums are scaled down
 constexpr float kGrow = 8.f, kLift = 7.f;     // see above
-constexpr float kTiny = -40.f;                // log2 of the scale of a block of tiny values (see below)
-constexpr float kVsUnit = 0x1p-20f;           // sums are in units of kVsUnit / vs: the least vs, 2^-107, stays in range
+// Sums of weights are in units of kVsUnit / vs, for scales vs of V between 2^-107 (a block of zeros) and 2^121.  The weight
+// of a row's reference is 2^7 to 2^15, so its sum is at least 2^-128 (22 bits), and that of 2^20 zeros of 2^7 is 2^120.
+constexpr float kVsUnit = 0x1p-14f;
 
 struct TileShape {
   int H, n_pos, G, nblk, tiles;   // tiles: row tiles of a head
@@ -283,9 +284,18 @@ __device__ __forceinline__ void store_rows(float* o, long long at0, long long at
     set_status(stt, ARCKV_ERR_NONFINITE);
 }
 
-struct Meta {   // of a block
-  float ks, lv, iv;   // scale of K, log2 and inverse (in units of kVsUnit) of V's
+// Of a block: the scale of K, log2 of V's, and what the sum of weights is multiplied by, kVsUnit / vs.  Where that leaves
+// the normal range, or the weights may, the sum is taken of weights 2^lift as large (see lift_of).
+struct __align__(16) Meta {
+  float ks, lv, iv, lift;
 };
+// Beside large values the weights of a block of tiny ones may all be below fp32's range, and their sum with them: they are
+// lifted, by as much as keeps both sums of 2^15 and iv in range.  A row's reference lies at most `top`, the largest lv
+// so far, above a logit, so weights of equal logits are otherwise 2^-93 at least.
+__device__ __forceinline__ float lift_of(float lv, float top) {
+  if (lv < top - 100.f) return lv < -30.f ? 106.f : 60.f;
+  return lv >= 100.f ? -40.f : 0.f;
+}
 
 template <int kT, bool kBias>
 __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
@@ -418,6 +428,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     Segment g = s_first;
     for (long long u = u0; u < u1 && ok;) {
       const int n = (int)min((long long)(g.count - g.step), u1 - u), len = cache_len(c, g.s);
+      float top = -INFINITY;   // largest log2 of V's scales so far
       Meta m;
       for (int i = 0; i < n && ok; ++i) {
         const int q = it + i, st = q % kStages;
@@ -428,7 +439,17 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             ks = c.k_scale[g.sh * d.nblk + b];
             vs = c.v_scale[g.sh * d.nblk + b];
           }
-          m = Meta{ks, log2f(vs), kVsUnit / vs};
+          const float lv = log2f(vs);
+          float upto = lv;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const float y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto = fmaxf(upto, y);
+          }
+          upto = fmaxf(upto, top);
+          top = __shfl_sync(0xffffffffu, upto, 31);
+          const float lift = lift_of(lv, upto);
+          m = Meta{ks, lv, kVsUnit * __uint_as_float((unsigned)(127 - (int)lift) << 23) / vs, lift};
         }
         if (q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
         ok = __all_sync(0xffffffffu, ok);
@@ -778,16 +799,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           add[k] = make_float2(a, a);
           sum[k] = make_float2(0.f, 0.f);
         }
-        // Beside large values the weights of a block of tiny ones may all be below fp32's range, and their sum with them:
-        // it is then taken with weights 2^64 as large.
-        const bool tiny = m.lv < kTiny;
         float lifted[2] = {0.f, 0.f};
-        if (tiny) {
+        if (m.lift != 0.f) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const int k = (e >> 1) & 1;
             const float x = kBias ? fmaf(v[e] + base[k].x, kLog2e, add[k].x) : fmaf(v[e], f[k], add[k].x);
-            lifted[k] += ex2_approx(x + 64.f);
+            lifted[k] += ex2_approx(x + m.lift);
           }
         }
 #pragma unroll
@@ -815,7 +833,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           tmem_st_pairs16(S + ch * 32 + 16, lr);
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) l[k] = tiny ? fmaf(lifted[k], m.iv * 0x1p-64f, l[k]) : fmaf(sum[k].x + sum[k].y, m.iv, l[k]);
+        for (int k = 0; k < 2; ++k) l[k] = fmaf(m.lift != 0.f ? lifted[k] : sum[k].x + sum[k].y, m.iv, l[k]);
         tmem_wait_st();
         tc::fence_before_sync();
         __syncwarp();

@@ -167,6 +167,54 @@ def test_rows_that_do_not_exist_report_nothing(G, behind):
     check_attend(c, Q, pk.cache_attend(c, Q, blocks=blocks), False, blocks)
 
 
+def large(seed, n, exponent, most=4.0):
+    """Positive values up to 2^(exponent + 2): sums of them do not cancel."""
+    x = torch.randn(1, 1, n, 128, generator=torch.Generator().manual_seed(seed)).abs().clamp(0.25, most)
+    return (x * 2.0 ** exponent).cuda()
+
+
+@pytest.mark.parametrize("n_pos", [16, 70])
+@pytest.mark.parametrize("exponent", [100, 110, 118, 125])
+@pytest.mark.parametrize("bias", [False, True])
+def test_large_values_in_many_rows(n_pos, exponent, bias):
+    n = 320
+    c = pk.cache_alloc(1, 1, n, bias=bias)
+    pk.cache_append(c, rows(25, 1, 1, n, grow=0.0).float(), large(26, n, exponent), bias=biases(27, 1, 1, n) if bias else None)
+    Q = queries(28, 1, 1, n_pos, 4)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=True), True)
+
+
+@pytest.mark.parametrize("n_pos", [16, 70])
+@pytest.mark.parametrize("n", [320, 6400])
+@pytest.mark.parametrize("order", [[0, 1, 2, 3, 4], [4, 3, 2, 1, 0], [2, 0, 4, 1, 3]])
+@pytest.mark.parametrize("bias", [False, True])
+def test_magnitudes_from_end_to_end_in_many_rows(n_pos, n, order, bias):
+    """Zeros, ordinary values and the largest ones in one sequence, equal logits but for biases: each takes its share."""
+    v = large(29, n, 0)
+    for b in range(n // 64):
+        v[:, :, 64 * b:64 * (b + 1)] *= [0.0, 2.0 ** -60, 1.0, 2.0 ** 60, 2.0 ** 123][order[b * 5 * 64 // n]]
+    c = pk.cache_alloc(1, 1, n, bias=bias)
+    pk.cache_append(c, torch.zeros_like(v), v, bias=biases(36, 1, 1, n) * 4 / 3 if bias else None)
+    Q = queries(30, 1, 1, n_pos, 4)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=False))
+
+
+@pytest.mark.parametrize("n_pos", [16, 33])
+@pytest.mark.parametrize("order", [[0, 4, 1, 3, 2], [4, 2, 0, 3, 1]])
+@pytest.mark.parametrize("bias", [False, True])
+def test_magnitudes_side_by_side_in_many_rows(n_pos, order, bias):
+    """As above with several blocks of one sequence for each SM, so that one follows the other in the same sums."""
+    n = 64 * 5 * torch.cuda.get_device_properties(0).multi_processor_count
+    v = large(37, n, 0).view(1, 1, n // 64, 64, 128)
+    for i, k in enumerate(order):
+        v[:, :, i::5] *= [0.0, 2.0 ** -60, 1.0, 2.0 ** 60, 2.0 ** 123][k]
+    v = v.view(1, 1, n, 128)
+    c = pk.cache_alloc(1, 1, n, bias=bias)
+    pk.cache_append(c, torch.zeros_like(v), v, bias=biases(38, 1, 1, n) * 4 / 3 if bias else None)
+    Q = queries(39, 1, 1, n_pos, 4)
+    check_attend(c, Q, pk.cache_attend(c, Q, causal=False))
+
+
 # --------------------------------------------------------------- selection
 
 @pytest.mark.parametrize("T", [0, 1, 64, 700])
