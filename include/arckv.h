@@ -393,7 +393,10 @@ size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d,
  *   O[s,h,p,g] = softmax_j(logit_scale q . k_j + bias_j) v_j  over the visible tokens j,
  * j < len[s], or with ARCKV_FLAG_CAUSAL j <= len[s] - n_pos + p (the query
  * positions are the newest n_pos tokens).  A row that sees no token, or only
- * biases of -inf, is zero.
+ * biases of -inf, is zero.  Sums are in fp32 and outputs that are not finite
+ * record ARCKV_ERR_NONFINITE: with up to 16 rows a head, and with listed
+ * blocks, that may happen where the values' magnitude times the tokens that a
+ * row sees passes 2^127.
  *   Q  bf16, n_pos positions of the G query heads of each KV head: row (p, g)
  *      begins q_strides[0] s + q_strides[1] h + q_strides[2] p + 128 g elements
  *      after the base (NULL: dense [S][H][n_pos][G][d]); base and strides are

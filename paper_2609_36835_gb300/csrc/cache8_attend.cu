@@ -30,6 +30,8 @@
 //  - S^T and O^T are what the instructions give (keys x rows, dims x rows), so
 //    weights go from one product to the other by an 8 x 8 transpose in registers;
 //    V's operand comes by transposed loads of 16-bit units, two dims of a key each.
+//  - V's scales enter 2^-15 as large (kValues): a token then adds at most its value to O, which overflows only where the
+//    values' magnitude times the tokens does.
 //
 // Measured: 64 ragged sequences x 8 heads, up to 8K, 4 rows: 118 us, 6.6 TB/s (97 % of
 // a copy's rate); one of 128K 48 us (5.6 TB/s: 6 us are start and join).  12 rows with
@@ -44,6 +46,7 @@ namespace {
 
 // More rows of a head go to the tcgen05 kernel (32 x 8 heads of 8K: 16 rows take 117 us here, 17 there 215).
 constexpr int kRowsMax = 16;
+constexpr float kValues = 0x1p-15f;          // O's unit: 1 / the largest weight
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 
 struct RowsShape {
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
           }
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullV[st], (q / kSt) & 1, abortp, stt));
         if (!ok) break;
-        const float vs = sVs[st];
+        const float vs = sVs[st] * kValues;   // (2^-122 at least; by the producer it would hold up the first copies)
         const uint32_t vt = tc::smem_u32(ringV) + st * kTileBytes + v_row;
         // ---- O^T += V^T P^T, 16 dims and 16 keys a product: a transposed 16-bit load gives lane (g, t) dims 2g, 2g + 1
         // of keys 2t, 2t + 1 in one word; even dims are the product's rows 0 .. 7, odd ones 8 .. 15
@@ -609,7 +612,7 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
       return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
     };
     auto store = [&](int r, int dim, float4 v, float z) {
-      const float inv = z == 0.f ? 0.f : 1.f / z;
+      const float inv = z == 0.f ? 0.f : 1.f / kValues / z;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       const int row = p.group * kR + r, pos = kSparse ? p.pos : row / d.G, gq = kSparse ? row : row - pos * d.G;
       if (row >= nrows) return;   // (a tile without rows masks nothing: it may have met anything behind the end)

@@ -215,6 +215,28 @@ def test_magnitudes_side_by_side_in_many_rows(n_pos, order, bias):
     check_attend(c, Q, pk.cache_attend(c, Q, causal=False))
 
 
+@pytest.mark.parametrize("G,n_pos", [(4, 1), (8, 1), (4, 4)])
+@pytest.mark.parametrize("n,exponent", [(320, 118), (6400, 112), (131072, 105)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_large_values_in_few_rows(G, n_pos, n, exponent, bias):
+    """Equal logits: every token weighs the same, and their sum is below 2^126."""
+    v = large(31, n, exponent, most=3.0)
+    c = pk.cache_alloc(1, 1, n, bias=bias)
+    pk.cache_append(c, torch.zeros_like(v), v)
+    Q = queries(32, 1, 1, n_pos, G)
+    check_attend(c, Q, pk.cache_attend(c, Q))
+
+
+@pytest.mark.parametrize("G,n_pos", [(4, 1), (8, 1), (4, 4)])
+def test_large_values_in_listed_blocks(G, n_pos):
+    v = large(33, 640, 116)
+    c = pk.cache_alloc(1, 1, 640)
+    pk.cache_append(c, rows(34, 1, 1, 640, grow=0.0).float(), v)
+    Q = queries(35, 1, 1, n_pos, G)
+    blocks = i32([0, 3, 4, 9]).expand(1, 1, n_pos, 4).contiguous()
+    check_attend(c, Q, pk.cache_attend(c, Q, blocks=blocks), False, blocks)
+
+
 # --------------------------------------------------------------- selection
 
 @pytest.mark.parametrize("T", [0, 1, 64, 700])
