@@ -285,7 +285,7 @@ def arckv_truncated_error(H: int, n: int, T: int, t: int, d: int, logit_scale: f
 def arckv_query_status(ws, stream=None) -> int:
     dev = getattr(ws, "device", None)
     if stream is None and dev is not None and dev.type == "cuda":   # the current stream of its device
-        return int(_on_device(dev, load_library().arckv_query_status, _ptr(ws), _current_handle(dev)))
+        return int(_on_device(dev, load_library().arckv_query_status)(_ptr(ws), _current_handle(dev)))
     return int(load_library().arckv_query_status(_ptr(ws), _stream_handle(stream)))
 
 
@@ -481,10 +481,16 @@ class Cache8:
                             tail=self.tail, tail_amax=self.tail_amax, len=self.len, bias=self.bias, state=self.state)
         object.__setattr__(self, "_c", _Cache8(S, H, cap, d, *[_ptr(getattr(self, n)) for n, _ in _Cache8._fields_[4:]]))
         object.__setattr__(self, "_ref", ctypes.byref(self._c))
+        object.__setattr__(self, "_alone", torch.cuda.device_count() == 1)   # no other device can be the current one
 
     def _tensors(self):
         """All arrays that the calls read or write."""
         return [getattr(self, n) for n, _ in _Cache8._fields_[4:]]
+
+    def _entry(self, name):
+        """The library's entry `name`, to be called with this cache's device current."""
+        call = getattr(load_library(), name)
+        return call if self._alone else _on_device(self.K.device, call)
 
     @property
     def capacity(self) -> int:
@@ -536,11 +542,7 @@ def _strides3(name: str, x, dense_from: int):
     return (ctypes.c_int64 * 3)(*[st[i] if x.shape[i] != 1 else 0 for i in range(3)])
 
 
-def _expect_32_bits(**numbers):
-    """Numbers that are passed on as 32-bit integers, of which only the low bits would arrive."""
-    for name, x in numbers.items():
-        if not -(1 << 31) <= x < 1 << 31:
-            raise ValueError("arckv: %s is out of range: %d" % (name, x))
+_LEAST, _MOST = -0x80000000, 0x7fffffff   # 32-bit integers: of others only the low bits would reach the library
 
 
 def _apart(x) -> bool:
@@ -566,20 +568,29 @@ def _side_stream(stream, device, *tensors):
     return stream
 
 
+_raw_stream = None
+
+
 def _current_handle(device) -> int:
     """The raw handle of the device's current stream, without making a stream object where torch has a call for that."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(device.index)
 
 
-def _on_device(device, call, *args):
-    """call(*args) with `device` as the current one: the library launches, and sizes its grids, for the current device."""
+def _on_device(device, call):
+    """`call` made with `device` as the current one: the library launches, and sizes its grids, for the current device."""
     import torch
     if torch.cuda.current_device() == device.index:
-        return call(*args)
-    with torch.cuda.device(device):
-        return call(*args)
+        return call
+
+    def guarded(*args):
+        with torch.cuda.device(device):
+            return call(*args)
+    return guarded
 
 
 def _counts_ptr(name: str, x, cache: "Cache8"):
@@ -618,8 +629,9 @@ def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream
     handle = (_current_handle(dev) if stream is None else
               _side_stream(stream, dev, K, V, bias, at, counts, *cache._tensors()).cuda_stream)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
-    st = _on_device(dev, load_library().arckv_cache_append, cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(),
-                    _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr, flags, handle)
+    st = cache._entry("arckv_cache_append")(
+        cache._ref, n, K.data_ptr(), _strides3("K", K, 3), V.data_ptr(), _strides3("V", V, 3), _ptr(bias), at_ptr, counts_ptr,
+        flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_append")
 
@@ -631,7 +643,8 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
     dtype = torch.bfloat16 if dtype is None else dtype
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
-    _expect_32_bits(start=start, count=count)
+    if not (_LEAST <= start <= _MOST and _LEAST <= count <= _MOST):
+        raise ValueError("arckv: start, count out of range: %s" % ((start, count),))
     c, dev = cache._c, cache.K.device
     if stream is not None:   # the outputs belong to the stream that fills them
         stream = _side_stream(stream, dev, *cache._tensors())
@@ -643,29 +656,22 @@ def cache_read(cache: Cache8, start: int, count: int, *, dtype=None, stream=None
         return K, V
     handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_F32 if dtype == torch.float32 else 0)
-    st = _on_device(dev, load_library().arckv_cache_read, cache._ref, start, count, K.data_ptr(), V.data_ptr(), flags, handle)
+    st = cache._entry("arckv_cache_read")(cache._ref, start, count, K.data_ptr(), V.data_ptr(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_read")
     return K, V
 
 
-def _check_workspace(cache: Cache8, ws):
-    """A workspace is bytes on the cache's device (the library checks size and alignment)."""
-    import torch
-    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or ws.device != cache.K.device or not ws.is_contiguous():
-        raise ValueError("arckv: ws must be a dense uint8 tensor on %s (cache_workspace makes one)" % cache.K.device)
-
-
-def _check_queries(cache: Cache8, Q):
-    """Positions and query heads of Q, which must fit the cache."""
-    import torch
+def _check_queries(torch, cache: Cache8, Q):
+    """Positions, query heads and device of Q, which must fit the cache."""
     c, shape = cache._c, Q.shape
     if len(shape) != 5 or Q.dtype != torch.bfloat16 or shape[0] != c.S or shape[1] != c.H or shape[4] != 128:
         raise ValueError("arckv: Q must be bfloat16 of shape %s, got %s %s"
                          % ((c.S, c.H, "n_pos", "G", 128), Q.dtype, tuple(shape)))
-    if Q.device != cache.K.device:
-        raise ValueError("arckv: Q is on %s but the cache on %s" % (Q.device, cache.K.device))
-    return shape[2], shape[3]
+    dev = cache.K.device
+    if Q.device != dev:
+        raise ValueError("arckv: Q is on %s but the cache on %s" % (Q.device, dev))
+    return shape[2], shape[3], dev
 
 
 def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, causal: bool = False, out=None, ws=None,
@@ -675,34 +681,34 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     each sees the tokens up to itself.  blocks [S, H, n_pos, m] int32: the only blocks that each position reads
     (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often."""
     import torch
-    n_pos, G = _check_queries(cache, Q)
+    n_pos, G, dev = _check_queries(torch, cache, Q)
     if stream is not None:   # a workspace and an output made here belong to the stream that fills them
-        stream = _side_stream(stream, Q.device, Q, blocks, out, ws, *cache._tensors())
+        stream = _side_stream(stream, dev, Q, blocks, out, ws, *cache._tensors())
         with torch.cuda.stream(stream):
             return cache_attend(cache, Q, logit_scale, blocks=blocks, causal=causal, out=out, ws=ws, check=check)
-    m = 0
+    m, listed = 0, None
     if blocks is not None:
         shape = blocks.shape
         if (len(shape) != 4 or blocks.dtype != torch.int32 or shape[:3] != Q.shape[:3] or shape[3] == 0 or
-                blocks.device != Q.device or not blocks.is_contiguous()):   # (an empty one's address means no list)
+                blocks.device != dev or not blocks.is_contiguous()):   # (an empty one's address means no list)
             raise ValueError("arckv: blocks must be a dense int32 tensor of shape %s, m >= 1, on %s, got %s %s on %s"
-                             % (tuple(Q.shape[:3]) + ("m",), Q.device, blocks.dtype, tuple(shape), blocks.device))
-        m = shape[3]
+                             % (tuple(Q.shape[:3]) + ("m",), dev, blocks.dtype, tuple(shape), blocks.device))
+        m, listed = shape[3], blocks.data_ptr()
     if ws is None:
         ws = _cache_workspace(cache, n_pos, G, "arckv_cache_attend_workspace_bytes")
-    else:
-        _check_workspace(cache, ws)
+    elif not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError("arckv: ws must be a dense uint8 tensor on %s (cache_workspace makes one)" % dev)
     if out is None:
         out = torch.empty_like(Q, dtype=torch.float32)
-    elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != Q.device:
-        raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), Q.device))
+    elif out.dtype != torch.float32 or out.shape != Q.shape or out.device != dev:
+        raise ValueError("arckv: out must be float32 of shape %s on %s" % (tuple(Q.shape), dev))
     elif not out.is_contiguous() and not _apart(out):
         raise ValueError("arckv: rows of out share memory, strides %s" % (tuple(out.stride()),))
-    handle = _current_handle(Q.device)
+    handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = _on_device(Q.device, load_library().arckv_cache_attend, cache._ref, n_pos, G, logit_scale, Q.data_ptr(),
-                    _strides3("Q", Q, 3), _ptr(blocks), m, out.data_ptr(), _strides3("out", out, 3), ws.data_ptr(),
-                    ws.numel(), flags, handle)
+    st = cache._entry("arckv_cache_attend")(
+        cache._ref, n_pos, G, logit_scale, Q.data_ptr(), _strides3("Q", Q, 3), listed, m, out.data_ptr(),
+        _strides3("out", out, 3), ws.data_ptr(), ws.numel(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_attend")
     return out
@@ -714,24 +720,26 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: Optional[int] = None, 
     first keep_first (one where m leaves room for it beside the newest, unless given), the newest keep_last and those
     whose logits can be largest.  Q, causal and ws as for ``cache_attend``."""
     import torch
-    n_pos, G = _check_queries(cache, Q)
+    n_pos, G, dev = _check_queries(torch, cache, Q)
     if keep_first is None:
         keep_first = 1 if m > keep_last else 0
-    _expect_32_bits(m=m, keep_first=keep_first, keep_last=keep_last)
+    if not (_LEAST <= m <= _MOST and _LEAST <= keep_first <= _MOST and _LEAST <= keep_last <= _MOST):
+        raise ValueError("arckv: m, keep_first, keep_last out of range: %s" % ((m, keep_first, keep_last),))
     if stream is not None:
-        stream = _side_stream(stream, Q.device, Q, ws, *cache._tensors())
+        stream = _side_stream(stream, dev, Q, ws, *cache._tensors())
         with torch.cuda.stream(stream):
             return cache_select(cache, Q, m, keep_first=keep_first, keep_last=keep_last, causal=causal, ws=ws,
                                 check=check)
     if ws is None:
         ws = _cache_workspace(cache, n_pos, G, "arckv_cache_select_workspace_bytes")
-    else:
-        _check_workspace(cache, ws)
-    blocks = torch.empty((Q.shape[0], Q.shape[1], n_pos, max(m, 0)), dtype=torch.int32, device=Q.device)
-    handle = _current_handle(Q.device)
+    elif not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError("arckv: ws must be a dense uint8 tensor on %s (cache_workspace makes one)" % dev)
+    blocks = torch.empty((cache._c.S, cache._c.H, n_pos, max(m, 0)), dtype=torch.int32, device=dev)
+    handle = _current_handle(dev)
     flags = (0 if check else FLAG_NONBLOCKING) | (FLAG_CAUSAL if causal else 0)
-    st = _on_device(Q.device, load_library().arckv_cache_select, cache._ref, n_pos, G, m, keep_first, keep_last,
-                    Q.data_ptr(), _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(), ws.numel(), flags, handle)
+    st = cache._entry("arckv_cache_select")(
+        cache._ref, n_pos, G, m, keep_first, keep_last, Q.data_ptr(), _strides3("Q", Q, 3), blocks.data_ptr(), ws.data_ptr(),
+        ws.numel(), flags, handle)
     if st != 0:
         raise ArckvError(st, "arckv_cache_select")
     return blocks

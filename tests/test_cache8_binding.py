@@ -26,7 +26,7 @@ class Stream:
 @pytest.fixture
 def rig(monkeypatch):
     """The cache calls over a stand-in library; `calls` are its calls, `used` the recorded (address, stream)."""
-    r = types.SimpleNamespace(calls=[], used=[], guards=[], device=0)
+    r = types.SimpleNamespace(calls=[], used=[], guards=[], device=0, devices=2)
     monkeypatch.setattr(Recorded, "used", r.used)
 
     def entry(name, value=0):
@@ -50,6 +50,7 @@ def rig(monkeypatch):
 
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: object())
     monkeypatch.setattr(torch.cuda, "current_device", lambda: r.device)
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: r.devices)
     monkeypatch.setattr(torch.cuda, "stream", guard)
     monkeypatch.setattr(torch.cuda, "device", guard)
     return r
@@ -123,6 +124,14 @@ def test_the_library_runs_with_the_caches_device_current(rig, name, check):
 def test_no_guard_where_the_device_is_current(rig):
     c = cache()
     rig.device = c.K.device.index
+    for name in CALLS:
+        CALLS[name][1](c, arguments())
+    assert len(rig.calls) == len(CALLS) and not any(guards for _, _, guards in rig.calls)
+
+
+def test_no_guard_where_there_is_one_device(rig):
+    rig.devices, rig.device = 1, 1
+    c = cache()
     for name in CALLS:
         CALLS[name][1](c, arguments())
     assert len(rig.calls) == len(CALLS) and not any(guards for _, _, guards in rig.calls)
