@@ -358,7 +358,11 @@ typedef struct {
  *   bias      fp32 [S][H][n] or NULL (zeros); NULL when the cache has none
  *   at        int32 [S] device or NULL: first token written instead of len[s],
  *             which writes over rejected tokens.  It must be a multiple of 64
- *             or in the newest block, and at most len[s].
+ *             or in the newest block, and at most len[s]: only the newest
+ *             block's rows are staged.  Where a draft has gone on into a new
+ *             block, tokens of the one before are rejected by writing that
+ *             block again from its first row, which takes up to 63 rows that
+ *             the caller has kept.
  *   counts    int32 [S] device or NULL (n): rows of sequence s that are written,
  *             the first counts[s] of its n (0 leaves the sequence as it is)
  * A sequence whose at, count or end (above cap) is out of range is left as it

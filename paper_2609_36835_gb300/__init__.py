@@ -607,7 +607,9 @@ def _counts_ptr(name: str, x, cache: "Cache8"):
 def cache_append(cache: Cache8, K, V, *, bias=None, at=None, counts=None, stream=None, check: bool = True) -> None:
     """Write the rows K, V [S, H, n, 128] (bf16 or fp32, dense in the last dimension) at the end of every sequence.
     bias [S, H, n]: their logit biases (zeros when not given).  at [S] int32: first token written instead of the end,
-    over rejected tokens of the newest block.  counts [S] int32: how many of the n rows each sequence takes.
+    over rejected tokens; it lies in the newest block or is a multiple of 64 (a draft that went on into a new block is
+    taken back further by writing the block before again from its first row).  counts [S] int32: how many of the n rows
+    each sequence takes.
     With check=False the call only enqueues, and ``arckv_query_status(cache.state)`` reports errors."""
     import torch
     c, dev, shape, dtype = cache._c, cache.K.device, K.shape, K.dtype
@@ -679,7 +681,8 @@ def cache_attend(cache: Cache8, Q, logit_scale: float = 0.0, *, blocks=None, cau
     """O = softmax(scale Q K^T + bias) V over the cache for Q [S, H, n_pos, G, 128] bf16 (the last two dimensions
     dense); returns fp32 of Q's shape and layout, or fills `out`.  causal: the positions are the newest n_pos tokens, and
     each sees the tokens up to itself.  blocks [S, H, n_pos, m] int32: the only blocks that each position reads
-    (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often."""
+    (``cache_select``).  ws: a ``cache_workspace``, kept by programs that call often.  With check=False the call only
+    enqueues, and ``arckv_query_status(ws)`` reports errors: of a workspace made here they are lost."""
     import torch
     n_pos, G, dev = _check_queries(torch, cache, Q)
     if stream is not None:   # a workspace and an output made here belong to the stream that fills them

@@ -185,8 +185,9 @@ __global__ void __launch_bounds__(RowsCfg<kR>::kThreads, 1)
                       float* O, RowStrides os, float* parts, int* tickets, DevStatus* stt) {
   using Cfg = RowsCfg<kR>;
   // Fewest blocks that are worth a CTA of their own: joining parts takes over 1 us, in which the warps of one CTA, with a
-  // block each, get further (4 rows of 8 heads, 450 tokens: 6.0 us with 6, 7.1 with 4; 12 rows of 4 x 8 heads, 1000
-  // tokens: 10.9 with 6, 9.4 with 4).
+  // block each, get further.  4 rows of 8 heads with 6 and with 4: 450 tokens 5.9 us and 7.1, 4 x 500 6.2 and 7.7, 4000
+  // 8.9 and 9.7, but 1000 7.5 and 7.1, 4 x 1000 8.1 and 7.9 (8 rows alike).  12 rows of 4 x 8 heads, 1000 tokens: 10.9
+  // with 6, 9.4 with 4.
   constexpr int kPartMin = kR == 16 ? 4 : 6;
   constexpr int kTR = Cfg::kTileRows, kTeams = Cfg::kTeams, kW = Cfg::kW, kSt = Cfg::kSt;
   extern __shared__ __align__(1024) unsigned char smraw[];

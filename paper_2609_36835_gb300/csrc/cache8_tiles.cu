@@ -23,9 +23,9 @@
 //
 // Work is dealt out in equal shares of blocks; an item (head and row tile) that
 // several CTAs share is added up by cache_join_kernel behind this one.
-// Measured (8 heads): 512 positions of 4 rows over 32K 296 us, 0.92 PFLOP/s of the
+// Measured (8 heads): 512 positions of 4 rows over 32K 294 us, 0.93 PFLOP/s of the
 // 1.28 that two passes over V leave of the pipe's 1.91; softmax issue (61 %) and
-// tensor pipe (75 % busy) bound it.  128 rows over 16 x 8K 129 us, 32 rows 109: one
+// tensor pipe (77 % busy) bound it.  128 rows over 16 x 8K 130 us, 32 rows 109: one
 // tile's chain of S, softmax and P V, 1700 cycles a block; 32 rows over 1K 13 us.
 //
 // The weight of key j of block b carries the block's scale of V:
