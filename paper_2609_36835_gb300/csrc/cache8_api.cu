@@ -92,7 +92,8 @@ arckv_status arckv_cache_append(const arckv_cache8* c, int32_t n, const void* K,
   if (n < 1 || n > c->cap) return ARCKV_ERR_SHAPE;
   const bool f32 = (flags & ARCKV_FLAG_F32) != 0;
   RowStrides ks, vs;
-  if (!K || !V || (bias && !c->bias) || !row_strides(K, k_strides, c->H, n, 128, f32 ? 4 : 2, &ks) ||
+  if (!K || !V || (bias && !c->bias) || misaligned(bias, 4) || misaligned(at, 4) || misaligned(counts, 4) ||
+      !row_strides(K, k_strides, c->H, n, 128, f32 ? 4 : 2, &ks) ||
       !row_strides(V, v_strides, c->H, n, 128, f32 ? 4 : 2, &vs))
     return ARCKV_ERR_INVALID_ARG;
   cudaGetLastError();
@@ -121,7 +122,8 @@ arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G,
   const arckv_status e = check_query(c, n_pos, G, Q, q_strides, ws, ws_bytes, cache_attend_scratch, flags, &q);
   if (e != ARCKV_OK) return e;
   RowStrides os;
-  if (!O || !row_strides(O, o_strides, c->H, n_pos, (int64_t)G * 128, 4, &os)) return ARCKV_ERR_INVALID_ARG;
+  if (!O || misaligned(blocks, 4) || !row_strides(O, o_strides, c->H, n_pos, (int64_t)G * 128, 4, &os))
+    return ARCKV_ERR_INVALID_ARG;
   // blocks read in all are counted in 32 bits
   if (blocks && (m < 1 || m > c->cap / kCB + 8192 || (long long)c->S * c->H * n_pos * ((G + 3) / 4) * m >= (1LL << 31)))
     return ARCKV_ERR_SHAPE;
