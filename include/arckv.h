@@ -431,6 +431,151 @@ arckv_status arckv_cache_select(const arckv_cache8* c, int32_t n_pos, int32_t G,
                                 int32_t keep_last, const void* Q, const int64_t* q_strides, int32_t* blocks, void* ws,
                                 size_t ws_bytes, uint32_t flags, void* stream);
 
+/*
+ * Paged caches held in 4 bits.  The paper has no counterpart: these calls serve
+ * batches of requests whose lengths differ and grow, from one pool of pages.
+ *
+ * A page has ARCKV_PAGE_TOKENS = 64 tokens of all H KV heads.  Each row of a
+ * token and head is held by itself: K in 4 groups of 32 dimensions, V as one of
+ * 128.  A group with elements x_e holds, in fp32 arithmetic,
+ *     m   = bf16(min x_e)
+ *     s   = max(bf16(fl(fl(max x_e - m) fl(1/15))), 2^-100)
+ *     c_e = min(max(rint(fl(fl(x_e - m) fl(1/s))), 0), 15)
+ * and stands for the values m + c_e s (rounded to fp32).  Elements past +-2^96
+ * are held as +-2^96.  A token and head take 148 bytes.  How a page's bytes
+ * are laid out is the library's own affair: arckv_pages_read gives values back.
+ *
+ * All arrays are device memory of the caller, dense; data and bias are 16-byte,
+ * state 256-byte and the others 4-byte aligned:
+ *   S requests, H KV heads, P pages in the pool, M pages of a request at most,
+ *   d = 128
+ *   data    uint8 [P][H][ARCKV_PAGE_BYTES]
+ *   bias    fp32 [P][H][64] or NULL   added to the logits of a token (beta of a compact cache)
+ *   table   int32 [S][M]   pages of each request; -1 where it has none
+ *   len     int32 [S]      tokens of each request
+ *   free    int32 [P]      the pages that no request has are its first n_free
+ *   n_free  int32 [1]
+ *   state   256 bytes: the status word of all calls but attend, and a counter
+ * To begin with, len and state are zero, table is -1 and free lists all pages.
+ * Lengths live on the device only: a serving step can be captured in a CUDA
+ * graph and replayed while the requests grow.
+ *
+ * Rows of a call are packed: those of request s are starts[s] .. starts[s+1] - 1
+ * of N, and rows from starts[S] on belong to no request.
+ *
+ * Status words are sticky, as those of the 8-bit cache.
+ */
+#define ARCKV_PAGE_TOKENS 64
+#define ARCKV_PAGE_BYTES 9472
+typedef struct {
+  int32_t S, H, P, M, d;
+  uint8_t* data;
+  float* bias;
+  int32_t *table, *len, *free, *n_free;
+  void* state;
+} arckv_pages4;
+
+/*
+ * Make room for counts[s] new tokens of every request: takes pages from the end
+ * of the free list, in the order of the requests and of the tokens, enters them
+ * into the table and advances len.
+ *   counts     int32 [S]
+ *   starts     out int32 [S + 1]: sums of the counts before each request
+ *   slots      out int32 [N]: page * 64 + offset of each row's token, -1 for
+ *              rows of no request
+ *   positions  out int32 [N]: its position in the request, -1 likewise
+ * 0 <= N < 2^30.  A request whose new length passes 64 M, whose rows pass N, or
+ * that the free pages do not suffice for (then every later one that needs a page
+ * too) is left as it is: its rows have slots and positions of -1, and
+ * ARCKV_ERR_SHAPE is recorded.  A negative count is taken as zero and records
+ * ARCKV_ERR_INVALID_ARG.
+ */
+arckv_status arckv_pages_extend(const arckv_pages4* p, const int32_t* counts, int32_t N, int32_t* starts, int32_t* slots,
+                                int32_t* positions, uint32_t flags, void* stream);
+
+/*
+ * Shorten every request to lens[s] tokens (int32 [S]; zero ends it) and give the
+ * pages behind them back, such that an extension and this call that takes it
+ * back leave the free list as it was.  A request with lens[s] < 0 or past its
+ * length is left as it is and records ARCKV_ERR_INVALID_ARG.
+ */
+arckv_status arckv_pages_truncate(const arckv_pages4* p, const int32_t* lens, uint32_t flags, void* stream);
+
+/*
+ * Write N rows at their slots (int32 [N], distinct; those below zero are passed
+ * over, those past the pool too and record ARCKV_ERR_INVALID_ARG).
+ *   K, V   bf16 (fp32 with ARCKV_FLAG_F32); row i of head h begins strides[0] i +
+ *          strides[1] h elements after the base (NULL: dense [N][H][d]).  Base
+ *          and strides are multiples of 16 bytes.
+ *   bias   fp32 [N][H] or NULL (zeros); NULL when the pages have none
+ * Non-finite elements are written as zero and record ARCKV_ERR_NONFINITE.
+ */
+arckv_status arckv_pages_append(const arckv_pages4* p, int32_t N, const void* K, const int64_t* k_strides, const void* V,
+                                const int64_t* v_strides, const int32_t* slots, const float* bias, uint32_t flags,
+                                void* stream);
+
+/*
+ * Read N rows back from their slots, as the values that they stand for:
+ *   K_out, V_out  bf16 (fp32 with ARCKV_FLAG_F32) [N][H][d]; either may be NULL.
+ * Slots below zero read as zero, those past the pool too and record
+ * ARCKV_ERR_INVALID_ARG.
+ */
+arckv_status arckv_pages_read(const arckv_pages4* p, int32_t N, const int32_t* slots, void* K_out, void* V_out,
+                              uint32_t flags, void* stream);
+
+/* Workspace bytes of arckv_pages_attend for up to max_count rows of a request
+ * (0 if the sizes are invalid).  Host-only.  As for the 8-bit cache, the first
+ * ARCKV_CACHE_WS_HEADER bytes must be zeroed once before the first use. */
+size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32_t d, int32_t max_count, int32_t G);
+
+/*
+ * Attention of packed queries over the pages of their requests:
+ *   O[i,h,g] = softmax_j(logit_scale q . k_j + bias_j) v_j
+ * over the tokens j < len[s] of row i's request s, or with ARCKV_FLAG_CAUSAL over
+ * j <= len[s] - (starts[s+1] - i): the rows are the request's newest tokens.  A
+ * row that sees no token, or only biases of -inf, is zero.
+ *   Q  bf16, rows (i, h, g) of the G query heads of each KV head begin
+ *      q_strides[0] i + q_strides[1] h + 128 g elements after the base (NULL:
+ *      dense [N][H][G][d]); base and strides are multiples of 16 bytes
+ *   starts  int32 [S + 1], ascending from zero or more to N at most
+ *   max_count  no request has more rows; one that does is left out and
+ *      records ARCKV_ERR_SHAPE
+ *   O  out bf16, addressed as Q with o_strides; rows do not overlap.  Rows of no
+ *      request are left as they are.
+ * Softmax weights and sums are fp32; weights enter the value products as f16
+ * (2^-12 of each), beside 2^-9 that an output's rounding to bf16 takes.  Pages that
+ * the table names past the pool record ARCKV_ERR_INVALID_ARG and are passed over,
+ * as are missing ones.  Outputs that are not finite record ARCKV_ERR_NONFINITE.
+ */
+arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int32_t max_count, float logit_scale,
+                                const void* Q, const int64_t* q_strides, const int32_t* starts, void* O,
+                                const int64_t* o_strides, void* ws, size_t ws_bytes, uint32_t flags, void* stream);
+
+/*
+ * Rotary positions.  Of each row's first r of d elements, pair i is turned by
+ * a = 2 pi positions[n] turns[i] / 2^64:
+ *   y1 = f (x1 cos a - x2 sin a),  y2 = f (x2 cos a + x1 sin a)
+ * (products in fp32, rounded once at the end); the other d - r are copied.
+ * Angles are reduced exactly, so they are as good at any position as at zero.
+ *   turns      uint64 [r/2] device: turns a position, in units of 2^-64
+ *   positions  int32 [N] device; rows with one below zero are copied
+ *   X, Y       two tensors (the second may be NULL) of rows (n, head), bf16 or
+ *              fp32 with ARCKV_FLAG_F32; row (n, h) of X[k] begins x_strides[2k] n +
+ *              x_strides[2k+1] h elements after the base.  Y[k] is X[k] (in place,
+ *              with the same strides) or does not overlap any X.  Bases and strides
+ *              are multiples of 16 bytes.
+ *   heads      heads of the two tensors
+ * Pairs are (i, i + r/2), or with ARCKV_FLAG_INTERLEAVED (2i, 2i + 1).  With
+ * ARCKV_FLAG_TRANSPOSE the transposed map, which turns by -a: what gradients
+ * take.  d a multiple of 16 up to 512, r a multiple of 16 up to d.  The call only
+ * enqueues.
+ */
+#define ARCKV_FLAG_INTERLEAVED 0x10u
+#define ARCKV_FLAG_TRANSPOSE 0x20u
+arckv_status arckv_rotate(int32_t N, int32_t d, int32_t r, float f, const uint64_t* turns, const int32_t* positions,
+                          const void* const* X, const int64_t* x_strides, void* const* Y, const int64_t* y_strides,
+                          const int32_t* heads, uint32_t flags, void* stream);
+
 /* Read (and clear) the device status word of a workspace after a
  * non-blocking call; synchronises `stream`. */
 arckv_status arckv_query_status(void* ws, void* stream);

@@ -19,7 +19,9 @@ __all__ = [
     "compact_layer", "attend", "INDEXER_FIELDS", "attend_joint", "arckv_attend_joint",
     "attend_joint_workspace_bytes", "FLAG_COMPACT_BF16", "truncated_error", "arckv_truncated_error", "SELECTOR_INDEXER", "SELECTOR_HA", "SELECTOR_VI",
     "arckv_wait_probe", "Cache8", "cache_alloc", "cache_workspace", "cache_append", "cache_read", "cache_attend",
-    "cache_select", "CACHE_BLOCK", "FLAG_F32", "FLAG_CAUSAL",
+    "cache_select", "CACHE_BLOCK", "FLAG_F32", "FLAG_CAUSAL", "Pages4", "pages_alloc", "pages_workspace", "pages_extend",
+    "pages_truncate", "pages_append", "pages_read", "pages_attend", "PAGE_TOKENS", "PAGE_BYTES", "Rotary", "rotary",
+    "rotary_frequencies", "rotate",
 ]
 
 _LIB_PATH = Path(__file__).resolve().parent / "libarckv.so"
@@ -152,6 +154,7 @@ def load_library():
     lib.arckv_cache_attend.restype = ctypes.c_int
     lib.arckv_cache_select.argtypes = [C, I, I, I, I, I, P, L3, P, P, ctypes.c_size_t, ctypes.c_uint32, P]
     lib.arckv_cache_select.restype = ctypes.c_int
+    _declare_pages(lib)
     lib.arckv_query_status.argtypes = [P, P]
     lib.arckv_query_status.restype = ctypes.c_int
     lib.arckv_wait_probe.argtypes = [P, ctypes.c_size_t, ctypes.c_uint32, P]
@@ -746,3 +749,9 @@ def cache_select(cache: Cache8, Q, m: int, *, keep_first: Optional[int] = None, 
     if st != 0:
         raise ArckvError(st, "arckv_cache_select")
     return blocks
+
+
+# paged 4-bit caches and rotary positions (the helpers above are what they share with the calls of this file)
+from .pages import (PAGE_BYTES, PAGE_TOKENS, Pages4, Rotary, pages_alloc, pages_append, pages_attend, pages_extend,  # noqa: E402
+                    pages_read, pages_truncate, pages_workspace, rotary, rotary_frequencies, rotate)
+from .pages import _declare as _declare_pages  # noqa: E402
