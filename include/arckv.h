@@ -441,8 +441,8 @@ arckv_status arckv_cache_select(const arckv_cache8* c, int32_t n_pos, int32_t G,
  *     m   = bf16(min x_e)
  *     s   = max(bf16(fl(fl(max x_e - m) fl(1/15))), 2^-100)
  *     c_e = min(max(rint(fl(fl(x_e - m) fl(1/s))), 0), 15)
- * and stands for the values m + c_e s (rounded to fp32).  Elements past +-2^96
- * are held as +-2^96.  A token and head take 148 bytes.  How a page's bytes
+ * and stands for the values m + c_e s (rounded to fp32).  Elements past +-2^64
+ * are held as +-2^64.  A token and head take 148 bytes.  How a page's bytes
  * are laid out is the library's own affair: arckv_pages_read gives values back.
  *
  * All arrays are device memory of the caller, dense; data and bias are 16-byte,

@@ -10,7 +10,7 @@ from __future__ import annotations
 import numpy as np
 
 PAGE = 64
-MOST = np.float32(2.0 ** 96)
+MOST = np.float32(2.0 ** 64)
 
 
 def as_bf16(x: np.ndarray) -> np.ndarray:

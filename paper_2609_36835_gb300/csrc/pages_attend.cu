@@ -1,19 +1,634 @@
-// Attention of packed queries over paged 4-bit caches:
+// Attention of packed queries over paged 4-bit caches, for requests of few rows
+// (decode and draft steps):
 //
 //   O_r = sum_j e^{x_rj} v_j / sum_j e^{x_rj},  x_rj = scale q_r . k_j + bias_j
 //
-// A warp takes one query row of one head and goes over the request's pages: a
-// lane has two tokens of a page for the logits, four dims for the output.
+// 148 bytes a token and head are read once.  That is 9472 bytes for 16384 codes: HBM gives an SM a page every 430 cycles or
+// so, in which it can issue 1700 warp instructions, so the work on a code has to stay near one tenth of an instruction
+// of a warp.  So:
+//  - A page of one head is one contiguous piece, and comes by one bulk copy into a ring of stages in shared memory.  The
+//    pages lie in the order in which the lanes take them, 16 bytes at a time and free of bank conflicts.
+//  - Products run on mma.sync m16n8k16: tokens (dims for V) are the 16 rows, query rows the 8 columns.  A nibble becomes
+//    an f16 by one mask: 1024 + c in the lowest four bits of the significand, 64 + c in the next four, two at a time;
+//    a word of eight codes costs a shift and four masks.  Nothing is subtracted from a code: what the 1024s and 64s add
+//    is known from the queries (for V: the weights) alone, and the sums begin at minus that.
+//  - Scales stay out of the products.  The four groups of a key are four sums, exact but for fp32 roundings, that are
+//    scaled and added up afterwards; the least values multiply the sum of the query's elements.  A value's scale goes into
+//    its weight, its least value times the weight into a sum of its own that all dims share.
+//  - Work is the list of (request, head, page): with more items than SMs each CTA takes an equal share of it; with fewer,
+//    items are cut into equal parts, a CTA each.  An item in several CTAs is finished by the one that comes last (a
+//    ticket), which adds the parts up in CTA order.  Consumer warps take whole pages in turn, each with its own
+//    running maximum, sum and output.
+//  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
+//    by up to 2^8): half a step is 2^-12 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
+//    without limit from page to page: the output is then scaled down, as for a maximum that grows.
 #include "pages.cuh"
+#include "tc.cuh"
 
 namespace arckv {
 namespace {
 
+constexpr int kRowsMax = 16;                 // rows of a head in this kernel
+constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
+constexpr float kGrow = 8.f, kLift = 7.f;    // weights reach 2^15: the range of f16
+
+struct RowsShape {
+  int G, N, limit, max_count;   // limit: rows of a head that a request may have here
+  bool causal;
+};
+
+// One producer warp.  Registers are dealt out to the SM's quarters: up to 12 warps may have 168 each, up to 8 all 255.
+// Every consumer warp has two stages, so that a page comes in while it works on another.
+template <int kR, bool kBias>
+struct RowsCfg {
+  static constexpr int kW = kR == 16 ? 7 : kBias ? 8 : 9, kSt = 2 * kW, kThreads = 32 * (kW + 1);
+  static constexpr int kT = kR / 8;          // tiles of 8 rows, both of a warp
+  static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kW * kR * kRowO * 4 + 2 * kR * 256;
+  // the rest of it beside 4097 sums and 2 KB of fixed arrays
+  static_assert(kSmem + 4097 * 4 + 2048 <= 227 * 1024, "shared memory");
+};
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *(const uint32_t*)&h;
+}
+// Two codes as f16: the lowest nibbles of w's halves, 1024 + c; the ones above them, 64 + c.
+__device__ __forceinline__ uint32_t pair_low(uint32_t w) { return (w & 0x000f000fu) | 0x64006400u; }
+__device__ __forceinline__ uint32_t pair_high(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
+constexpr float kLow = 1024.f, kHigh = 64.f;
+__device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+// A CTA's run of pages of one item.
+struct Run {
+  int s, h;
+  int blk, n;             // pages blk .. blk + n - 1 of the request
+  int first, last;        // the CTAs that share the item
+};
+
+// The runs of a CTA, in order.  Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request
+// s of one head.
+struct Walk {
+  const arckv_pages4& c;
+  const int* pre;
+  int cta;
+  bool parts;             // items are cut into equal parts
+  int u, u1;              // parts: this CTA's part of all; else units (pages) of its share
+  int q, r;               // shares: q units each, one more for the first r CTAs
+
+  __device__ int owner(int unit) const {
+    const int big = r * (q + 1);
+    return unit < big ? unit / (q + 1) : r + (unit - big) / q;
+  }
+  __device__ bool next(Run& p) {
+    if (u >= u1) return false;
+    int lo = 0, hi = c.S;   // last s with pre[s] H <= u: the one with unit u, as those without rows have none
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] * c.H <= u) lo = mid;
+      else hi = mid;
+    }
+    p.s = lo;
+    const int cut = pre[lo + 1] - pre[lo], rest = u - pre[lo] * c.H;
+    p.h = rest / cut;
+    const int k = rest - p.h * cut;
+    if (parts) {
+      const int nb = max(1, pages_of(pages_len(c, p.s)));
+      p.blk = (int)((long long)nb * k / cut);
+      p.n = (int)((long long)nb * (k + 1) / cut) - p.blk;
+      p.first = u - k;
+      p.last = p.first + cut - 1;
+      ++u;
+      return true;
+    }
+    p.blk = k;
+    p.n = min(cut - k, u1 - u);
+    p.first = p.last = cta;
+    if (p.n < cut) {
+      p.first = owner(u - k);
+      p.last = owner(u - k + cut - 1);
+    }
+    u += p.n;
+    return true;
+  }
+};
+
+template <int kR, bool kBias>
+__global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
+    pages_rows_kernel(const arckv_pages4 c, RowsShape d, const bf16* Q, PackedStrides qs, float scale, const int* starts, bf16* O,
+                      PackedStrides os, float* parts, int* tickets, DevStatus* stt) {
+  using Cfg = RowsCfg<kR, kBias>;
+  // Fewest pages that are worth a CTA of their own (joining parts takes over 1 us).
+  constexpr int kPartMin = 6;
+  constexpr int kW = Cfg::kW, kSt = Cfg::kSt, kT = Cfg::kT;
+  extern __shared__ __align__(128) unsigned char smraw[];
+  unsigned char* ring = smraw;                                   // [stage][page]
+  float* sBias = (float*)(ring + kSt * ARCKV_PAGE_BYTES);        // [stage][64]
+  float* sO = sBias + (kBias ? kSt * kPT : 0);                                 // [warp][row][kRowO]
+  bf16* sQ = (bf16*)(sO + kW * kR * kRowO);                      // [parity of the run][row][128]
+  int* pre = (int*)(sQ + 2 * kR * 128);                          // [S + 1]
+  __shared__ __align__(8) uint64_t full[kSt], empty[kSt], fullQ[2], emptyQ[2];
+  __shared__ int sHeld[kSt];                                     // whether the stage has a page
+  __shared__ float sM[kW][kR], sL[kW][kR];
+  __shared__ int abort_flag, last_flag, stop_flag, s_cut;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile int* abortp = &abort_flag;
+
+  if (tid == 0) {
+    for (int s = 0; s < kSt; ++s) {
+      tc::mbar_init(&full[s], 1);
+      tc::mbar_init(&empty[s], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(&fullQ[i], 1);
+      tc::mbar_init(&emptyQ[i], kW);
+    }
+    abort_flag = 0;
+    tc::mbar_fence_init();
+  }
+  pdl_trigger();
+  pdl_wait();
+  // First row and number of rows of request s; none where it has more than the launch was made for.
+  auto rows_of = [&](int s, int& first) {
+    first = min(max(starts[s], 0), d.N);
+    const int n = min(max(starts[s + 1], first), d.N) - first;
+    if (n > d.max_count) set_status(stt, ARCKV_ERR_SHAPE);
+    return (long long)n * d.G <= d.limit ? n : 0;
+  };
+  if (warp == kW) {   // pages, or parts, before each request, by warp scan
+    int cut = 0, items = 0;
+    auto scan = [&] {
+      int run = 0;
+      for (int s0 = 0; s0 < c.S; s0 += 32) {
+        int x = 0, first;
+        if (s0 + lane < c.S && rows_of(s0 + lane, first) > 0) x = max(1, pages_of(pages_len(c, s0 + lane)));
+        if (cut == 0) items += __popc(__ballot_sync(0xffffffffu, x > 0));
+        if (cut > 0 && x > 0) x = max(1, min((x + cut - 1) / cut, x / kPartMin));
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        if (s0 + lane < c.S) pre[s0 + lane + 1] = run + x;
+        run += __shfl_sync(0xffffffffu, x, 31);
+      }
+      return run;
+    };
+    int all = scan();
+    if (all > 0 && items * c.H <= (int)gridDim.x) {   // the smallest parts that the CTAs suffice for
+      cut = (all * c.H + (int)gridDim.x - 1) / (int)gridDim.x;
+      for (all = scan(); all * c.H > (int)gridDim.x; all = scan())
+        cut = max(cut + 1, (int)((long long)cut * all * c.H / (int)gridDim.x));
+    }
+    if (lane == 0) {
+      pre[0] = 0;
+      s_cut = cut;
+    }
+  }
+  __syncthreads();
+  const int total = pre[c.S] * c.H, ctas = min((int)gridDim.x, total), me = blockIdx.x;
+  if (me >= ctas) return;
+  Walk walk{c, pre, me, s_cut > 0};
+  walk.q = total / ctas;
+  walk.r = total - walk.q * ctas;
+  walk.u = walk.q * me + min(me, walk.r);
+  walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
+
+  if (warp == kW) {
+    // ------------------------------------------------------------- producer: queries and pages
+    int it = 0, run = 0;   // pages and runs issued
+    bool ok = true;
+    for (Run p; ok && walk.next(p); ++run) {
+      const int n = p.n, held = pages_of(pages_len(c, p.s));
+      if (!walk.parts) {   // a run ahead, as far as the ring reaches
+        int first;
+        const int buf = run & 1, nrows = rows_of(p.s, first) * d.G;
+        if (run >= 2) ok = __all_sync(0xffffffffu, tc::mbar_wait(&emptyQ[buf], ((run >> 1) - 1) & 1, abortp, stt));
+        if (!ok) {
+          ++it;   // (as where a page's wait gives up: `it` is one more than were issued)
+          break;
+        }
+        if (lane == 0) tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
+        __syncwarp();
+        if (lane < nrows) {
+          const int i = lane / d.G, g = lane - i * d.G;
+          tc::bulk_load(sQ + (buf * kR + lane) * 128, Q + (first + i) * qs.i + p.h * qs.h + g * 128, 256, &fullQ[buf]);
+        }
+      }
+      for (int k0 = 0; k0 < n && ok; k0 += 32) {
+        const int b = p.blk + k0 + lane;
+        int page = -1;
+        if (k0 + lane < n && b < held) {
+          page = c.table[(long long)p.s * c.M + b];
+          if (page >= c.P) {
+            set_status(stt, ARCKV_ERR_INVALID_ARG);
+            page = -1;
+          }
+        }
+        const int cnt = min(32, n - k0);
+        auto load = [&](int st) {   // this lane's page into stage st
+          sHeld[st] = page >= 0;
+          if (page < 0) {
+            tc::mbar_arrive(&full[st]);
+            return;
+          }
+          const long long at = (long long)page * c.H + p.h;
+          tc::mbar_arrive_expect_tx(&full[st], ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
+          tc::bulk_load(ring + st * ARCKV_PAGE_BYTES, c.data + at * ARCKV_PAGE_BYTES, ARCKV_PAGE_BYTES, &full[st]);
+          if (kBias) tc::bulk_load(sBias + st * kPT, c.bias + at * kPT, kPT * 4, &full[st]);
+        };
+        int j = 0;
+        if (it < kSt) {   // the ring's first round
+          j = min(cnt, kSt - it);
+          if (lane < j) load(it + lane);
+          __syncwarp();
+        }
+        for (; j < cnt && ok; ++j) {
+          const int q = it + j, st = q % kSt;
+          ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[st], ((q / kSt) - 1) & 1, abortp, stt));
+          if (ok && lane == j) load(st);
+        }
+        it += j;
+      }
+    }
+    if (!ok) {   // let the copies in flight land before the CTA's memory goes
+      volatile int never = 0;
+      for (int q = max(0, it - 1 - kSt); q < it - 1; ++q) tc::mbar_wait(&full[q % kSt], (q / kSt) & 1, &never, stt);
+      if (!walk.parts)
+        for (int q = max(0, run - 2); q < run; ++q) tc::mbar_wait(&fullQ[q & 1], (q >> 1) & 1, &never, stt);
+    }
+    return;
+  }
+
+  // --------------------------------------------------------------- consumers
+  const int g = lane >> 2, t = lane & 3;
+  int base = 0, run = 0;         // pages of earlier runs, and their number
+  bool ok = true;
+  for (Run p; walk.next(p); ++run) {
+    int first;
+    const int n = p.n, len = pages_len(c, p.s), h = p.h, count = rows_of(p.s, first), nrows = count * d.G;
+    // query rows: column n of tile e is row 8 e + n
+    uint32_t qf[kT][8][2];
+    float q_off[kT][4][2], q_sum[kT][4][2];   // minus what the codes' offsets add, and the sums of a group's elements, rows 2t, 2t + 1
+    float fac[kT][2];                         // 2^e scale (log2 e) of them
+    int see[kT][2], see_min = 0x7fffffff;     // tokens that they see
+    if (!walk.parts) ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
+#pragma unroll
+    for (int e = 0; e < kT; ++e) {
+      const int r = 8 * e + g, i = r / d.G;
+      // Queries of a CTA's only run are read here, beside its first copies; of several runs, they have come to shared memory
+      const bf16* mine = walk.parts ? Q + (first + i) * qs.i + h * qs.h + (r - i * d.G) * 128 : sQ + ((run & 1) * kR + r) * 128;
+      uint4 x[4];
+      float amax = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        x[w] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < nrows) x[w] = *(const uint4*)(mine + 32 * w + 8 * t);
+        const uint32_t y[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(y[f])), fabsf(bf16_hi(y[f]))));
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      // exponent of the row's largest element, kept where 2^(14 - ex) and 2^(ex - 14) are normal
+      const int ex = min(max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100), 127);
+      const float up = __uint_as_float((unsigned)(14 - ex + 127) << 23), down = __uint_as_float((unsigned)(ex - 14 + 127) << 23);
+      float off[4], sum[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t y[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+        off[w] = sum[w] = 0.f;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {   // pair f of the word: dims 32 w + 8 t + 2 f, + 1
+          qf[e][2 * w + (f >> 1)][f & 1] = pack_f16(bf16_lo(y[f]) * up, bf16_hi(y[f]) * up);
+          const float2 z = __half22float2(*(const __half2*)&qf[e][2 * w + (f >> 1)][f & 1]);
+          sum[w] += z.x + z.y;
+          off[w] = fmaf(f & 1 ? -kHigh : -kLow, z.x + z.y, off[w]);
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+          sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], o);
+          off[w] += __shfl_xor_sync(0xffffffffu, off[w], o);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          q_sum[e][w][k] = __shfl_sync(0xffffffffu, sum[w], (2 * t + k) * 4);
+          q_off[e][w][k] = __shfl_sync(0xffffffffu, off[w], (2 * t + k) * 4);
+        }
+      }
+      const float f = down * scale * (kBias ? 1.f : kLog2e);
+      const int sees = r < nrows ? (d.causal ? max(0, min(len, len - count + i + 1)) : len) : 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {   // (a factor is never zero: a masked product is -inf)
+        fac[e][k] = fmaxf(__shfl_sync(0xffffffffu, f, (2 * t + k) * 4), 0x1p-126f);
+        see[e][k] = __shfl_sync(0xffffffffu, sees, (2 * t + k) * 4);
+      }
+      see_min = min(see_min, __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff));
+    }
+    __syncwarp();
+    if (!walk.parts && lane == 0) tc::mbar_arrive(&emptyQ[run & 1]);
+    float o[kT][8][4], mx[kT][2], l[kT][2], low[kT][2];   // low: sums of weights times least values
+    float v_ref = 0.f;                                     // unit of o: a power of two
+#pragma unroll
+    for (int e = 0; e < kT; ++e) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) o[e][k][f] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        mx[e][k] = -INFINITY;
+        l[e][k] = low[e][k] = 0.f;
+      }
+    }
+    // page base + i of the CTA belongs to warp (base + i) % kW
+    for (int i = (warp - base % kW + kW) % kW; i < n && ok; i += kW) {
+      const int q = base + i, st = q % kSt, j0 = (p.blk + i) * kPT;   // first token of the page
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[st], (q / kSt) & 1, abortp, stt));
+      if (!ok) break;
+      if (sHeld[st]) {
+        const unsigned char* page = ring + st * ARCKV_PAGE_BYTES;
+        // ---- S^T = K Q^T: lane (g, t) has tokens g, g + 8 of 16, and eight dims of each group
+        float s[kT][4][4];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+          const uint4 a = *(const uint4*)(page + (mt * 16 + g) * 64 + t * 16);
+          const uint4 b = *(const uint4*)(page + (mt * 16 + g + 8) * 64 + t * 16);
+          const uint4 pa = *(const uint4*)(page + kPageKp + (mt * 16 + g) * 16);
+          const uint4 pb = *(const uint4*)(page + kPageKp + (mt * 16 + g + 8) * 16);
+          const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+          const uint32_t pw[4] = {pa.x, pa.y, pa.z, pa.w}, pv[4] = {pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t a8 = aw[w] >> 8, b8 = bw[w] >> 8;
+            const uint32_t f0 = pair_low(aw[w]), f1 = pair_low(bw[w]), f2 = pair_high(aw[w]), f3 = pair_high(bw[w]);
+            const uint32_t f4 = pair_low(a8), f5 = pair_low(b8), f6 = pair_high(a8), f7 = pair_high(b8);
+#pragma unroll
+            for (int e = 0; e < kT; ++e) {
+              float acc[4] = {q_off[e][w][0], q_off[e][w][1], q_off[e][w][0], q_off[e][w][1]};
+              mma_f16(acc, f0, f1, f2, f3, qf[e][2 * w][0], qf[e][2 * w][1]);
+              mma_f16(acc, f4, f5, f6, f7, qf[e][2 * w + 1][0], qf[e][2 * w + 1][1]);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float x = fmaf(bf16_hi(pw[w]), q_sum[e][w][k], w ? s[e][mt][k] : 0.f);
+                const float y = fmaf(bf16_hi(pv[w]), q_sum[e][w][k], w ? s[e][mt][2 + k] : 0.f);
+                s[e][mt][k] = fmaf(bf16_lo(pw[w]), acc[k], x);
+                s[e][mt][2 + k] = fmaf(bf16_lo(pv[w]), acc[2 + k], y);
+              }
+            }
+          }
+        }
+        // ---- softmax of the page.  References follow the maximum only when it has grown by more than 2^8 (kGrow), so
+        // that sums are scaled on few pages.  Without biases the maximum is that of the products, whose factor is
+        // positive, and a weight is 2^{product factor - mx}.
+        if (kBias) {
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const float bias = sBias[st * kPT + mt * 16 + hf * 8 + g];
+#pragma unroll
+              for (int e = 0; e < kT; ++e)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) s[e][mt][2 * hf + k] = fmaf(s[e][mt][2 * hf + k], fac[e][k], bias);
+            }
+        }
+        if (j0 + kPT > see_min) {   // (also where no row has been: anything may be there)
+#pragma unroll
+          for (int e = 0; e < kT; ++e)
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+              for (int f = 0; f < 4; ++f)
+                if (j0 + mt * 16 + (f >> 1) * 8 + g >= see[e][f & 1]) s[e][mt][f] = -INFINITY;
+        }
+        float top[kT][2];
+        bool grows = false;
+#pragma unroll
+        for (int e = 0; e < kT; ++e)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {   // rows 2t, 2t + 1
+            float& x = top[e][k];
+            x = max3(s[e][0][k], s[e][0][2 + k], s[e][1][k]);
+            x = fmaxf(max3(x, s[e][1][2 + k], s[e][2][k]), max3(s[e][2][2 + k], s[e][3][k], s[e][3][2 + k]));
+            if (!kBias) x = fmaf(x, fac[e][k], -kLift);
+            grows |= (kBias ? (x - mx[e][k]) * kLog2e : x - mx[e][k]) > kGrow;   // (mx = -inf: by any but -inf)
+          }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int e = 0; e < kT; ++e) {
+            float alpha[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float& x = top[e][k];
+#pragma unroll
+              for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+              const float by = kBias ? (mx[e][k] - x) * kLog2e : mx[e][k] - x;
+              const bool up = x != -INFINITY && (mx[e][k] == -INFINITY || -by > kGrow);
+              alpha[k] = up ? ex2_approx(by) : 1.f;   // (mx = -inf: zero)
+              if (up) mx[e][k] = x;
+              l[e][k] *= alpha[k];
+              low[e][k] *= alpha[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+              for (int f = 0; f < 4; ++f) o[e][k][f] *= alpha[f & 1];
+          }
+        }
+        // the values' scales and least values; of tokens that are not held, zero
+        float vs[8], vm[8], most = 0.f;
+        {
+          const bool edge = j0 + kPT > len;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            uint32_t w = *(const uint32_t*)(page + kPageVp + (x * 8 + g) * 4);
+            if (edge && j0 + x * 8 + g >= len) w = 0u;
+            vs[x] = bf16_lo(w);
+            vm[x] = bf16_hi(w);
+            most = fmaxf(most, vs[x]);
+          }
+        }
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+        if (most > v_ref) {   // (uniform) a larger unit: between two and four times the scale, so that few pages raise it
+          const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23)), by = v_ref / to;
+#pragma unroll
+          for (int e = 0; e < kT; ++e)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+              for (int f = 0; f < 4; ++f) o[e][k][f] *= by;
+          v_ref = to;
+        }
+        const float inv_ref = v_ref > 0.f ? 1.f / v_ref : 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) vs[x] *= inv_ref;
+        uint32_t ph[kT][4][2];
+#pragma unroll
+        for (int e = 0; e < kT; ++e) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float ref = mx[e][k] == -INFINITY ? 0.f : mx[e][k];   // nothing visible yet: weights 2^{-inf} = 0
+            float sum = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                float& x = s[e][mt][2 * hf + k];
+                // a bias of the type's lowest value cancels against itself before the factor log2 e
+                x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kLift) : fmaf(x, fac[e][k], -ref));
+                sum += x;
+                low[e][k] = fmaf(x, vm[2 * mt + hf], low[e][k]);
+                x *= vs[2 * mt + hf];
+              }
+            l[e][k] += sum;
+          }
+          // as f16, transposed to (tokens, row) operands; their sums times the codes' offsets leave the output
+          float one[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) ph[e][mt][hf] = transpose8x8(pack_f16(s[e][mt][2 * hf], s[e][mt][2 * hf + 1]));
+            mma_f16(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][mt][0], ph[e][mt][1]);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) o[e][k][f] = fmaf(f < 2 ? -kLow : -kHigh, one[f & 1], o[e][k][f]);
+        }
+        // ---- O^T += V^T P^T, 16 dims and 16 tokens a product: lane (g, t) has tokens 2t, 2t + 1 and 8 on, dims g + 8 x
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+          const uint4 a = *(const uint4*)(page + kPageV + (mt * 8 + t) * 128 + ((g ^ (t << 1)) << 4));
+          const uint4 b = *(const uint4*)(page + kPageV + (mt * 8 + t + 4) * 128 + ((g ^ (t << 1)) << 4));
+          const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t a8 = aw[x] >> 8, b8 = bw[x] >> 8;
+            const uint32_t f0 = pair_low(aw[x]), f1 = pair_high(aw[x]), f2 = pair_low(bw[x]), f3 = pair_high(bw[x]);
+            const uint32_t f4 = pair_low(a8), f5 = pair_high(a8), f6 = pair_low(b8), f7 = pair_high(b8);
+#pragma unroll
+            for (int e = 0; e < kT; ++e) {
+              mma_f16(o[e][2 * x], f0, f1, f2, f3, ph[e][mt][0], ph[e][mt][1]);
+              mma_f16(o[e][2 * x + 1], f4, f5, f6, f7, ph[e][mt][0], ph[e][mt][1]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&empty[st]);
+    }
+    base += n;
+    // ---- the item's end (or this CTA's part of it): add the warps up
+#pragma unroll
+    for (int e = 0; e < kT; ++e)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) {
+          l[e][k] += __shfl_xor_sync(0xffffffffu, l[e][k], w);
+          low[e][k] += __shfl_xor_sync(0xffffffffu, low[e][k], w);
+        }
+        const int r = 8 * e + 2 * t + k;
+        if (g == 0) {
+          sM[warp][r] = mx[e][k];
+          sL[warp][r] = l[e][k];
+        }
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+            sO[(warp * kR + r) * kRowO + 16 * x + 8 * z + g] = fmaf(o[e][x][2 * z + k], v_ref, low[e][k]);
+      }
+    if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
+    bar_consumers(kW * 32);
+    if (stop_flag) break;   // a wait gave up: write nothing
+    const bool whole = p.first == p.last;
+    auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
+      return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
+    };
+    auto store = [&](int r, int dim, float4 v, float z) {
+      const float inv = z == 0.f ? 0.f : 1.f / z;
+      v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+      if (r >= nrows) return;   // (a tile without rows masks nothing: it may have met anything behind the end)
+      const int i = r / d.G;
+      __nv_bfloat162 y[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+      *(uint2*)(O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + dim) = *(const uint2*)&y[0];
+      const float big = 3.3895313892515355e38f;   // (the largest bf16)
+      if (!(fabsf(v.x) <= big && fabsf(v.y) <= big && fabsf(v.z) <= big && fabsf(v.w) <= big))
+        set_status(stt, ARCKV_ERR_NONFINITE);
+    };
+    // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
+    constexpr int kSlot = kR * 132;   // 128 outputs, m, l (and two unused) for each row
+    for (int x = tid; x < kR * 32; x += kW * 32) {
+      const int r = x >> 5, dim = (x & 31) * 4;
+      float up = -INFINITY, z = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) up = fmaxf(up, sM[w][r]);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float f = weight(sM[w][r], up);
+        const float4 y = *(const float4*)(sO + (w * kR + r) * kRowO + dim);
+        z = fmaf(sL[w][r], f, z);
+        v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
+      }
+      if (whole) store(r, dim, v, z);
+      else {
+        float* slot = parts + (2ll * blockIdx.x + (p.blk == 0 ? 1 : 0)) * kSlot + r * 132;
+        __stcg((float4*)(slot + dim), v);
+        if (dim == 0) __stcg((float2*)(slot + 128), make_float2(up, z));
+      }
+    }
+    if (!whole) {
+      bar_consumers(kW * 32);
+      if (tid == 0) {
+        // the CTA's results before the ticket, the others' after it
+        int ticket;
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(&tickets[p.first]) : "memory");
+        last_flag = ticket == p.last - p.first;
+        if (last_flag) tickets[p.first] = 0;
+      }
+      bar_consumers(kW * 32);
+      if (last_flag) {
+        for (int x = tid; x < kR * 32; x += kW * 32) {
+          const int r = x >> 5, dim = (x & 31) * 4;
+          // with a running maximum, so that a part's loads wait for nothing
+          float up0 = -INFINITY, z = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int cc = p.first; cc <= p.last; ++cc) {
+            const float* slot = parts + (2ll * cc + (cc == p.first)) * kSlot + r * 132;
+            const float2 ml = __ldcg((const float2*)(slot + 128));
+            const float4 y = __ldcg((const float4*)(slot + dim));
+            const float up = fmaxf(up0, ml.x), f = weight(ml.x, up), f0 = weight(up0, up);
+            up0 = up;
+            z = fmaf(z, f0, ml.y * f);
+            v = make_float4(fmaf(v.x, f0, y.x * f), fmaf(v.y, f0, y.y * f), fmaf(v.z, f0, y.z * f), fmaf(v.w, f0, y.w * f));
+          }
+          store(r, dim, v, z);
+        }
+      }
+    }
+    bar_consumers(kW * 32);   // sO, sM, sL are free
+  }
+}
+
 constexpr int kAW = 4;   // warps of a CTA
 
 template <bool kBias>
-__global__ void __launch_bounds__(32 * kAW) pages_attend_kernel(const arckv_pages4 p, PagesQuery a, float scale,
-                                                                DevStatus* stt) {
+__global__ void __launch_bounds__(32 * kAW) pages_wide_kernel(const arckv_pages4 p, PagesQuery a, float scale,
+                                                              int above, DevStatus* stt) {
   __shared__ float sq[kAW][128];
   __shared__ float sp[kAW][kPT];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -36,6 +651,7 @@ __global__ void __launch_bounds__(32 * kAW) pages_attend_kernel(const arckv_page
       set_status(stt, ARCKV_ERR_SHAPE);
       continue;
     }
+    if ((long long)(end - a.starts[s]) * a.G <= above) continue;
     const int sees = a.causal ? max(0, min(len, len - (end - i) + 1)) : len;
     const bf16* q = a.Q + i * a.qs.i + h * a.qs.h + g * 128;
     __syncwarp();
@@ -109,15 +725,37 @@ __global__ void __launch_bounds__(32 * kAW) pages_attend_kernel(const arckv_page
   }
 }
 
+template <int kR, bool kBias>
+int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int limit, void* ws, cudaStream_t st) {
+  RowsShape d;
+  d.G = q.G;
+  d.N = q.N;
+  d.limit = limit;
+  d.max_count = q.max_count;
+  d.causal = q.causal;
+  auto kern = pages_rows_kernel<kR, kBias>;
+  const int smem = RowsCfg<kR, kBias>::kSmem + (p.S + 1) * (int)sizeof(int);
+  if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
+  const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
+  const cudaError_t e = launch_pdl(kern, dim3(ctas), RowsCfg<kR, kBias>::kThreads, smem, st, p, d, q.Q, q.qs, scale, q.starts, q.O, q.os,
+                                   (float*)((char*)ws + ARCKV_CACHE_WS_HEADER), ws_tickets(ws), (DevStatus*)ws);
+  return e == cudaSuccess ? 1 : -1;
+}
+
 }  // namespace
 
-size_t pages_attend_scratch(int, int, int, int, int) { return 0; }
+size_t pages_attend_scratch(int, int, int, int, int) { return (size_t)2 * kCacheMaxCtas * kRowsMax * 132 * sizeof(float); }
 
 int launch_pages_attend(const arckv_pages4& p, const PagesQuery& q, float scale, void* ws, cudaStream_t st) {
+  const long long rows = (long long)q.max_count * q.G;
+  const int limit = (int)std::min<long long>(rows, kRowsMax);
+  int n = rows <= 8 ? (p.bias ? launch_rows<8, true>(p, q, scale, limit, ws, st) : launch_rows<8, false>(p, q, scale, limit, ws, st))
+                    : (p.bias ? launch_rows<16, true>(p, q, scale, limit, ws, st) : launch_rows<16, false>(p, q, scale, limit, ws, st));
+  if (n < 0 || rows <= kRowsMax) return n;
   const int ctas = stride_grid((long long)q.N * p.H * q.G, kAW, 16);
-  const cudaError_t e = p.bias ? launch_pdl(pages_attend_kernel<true>, dim3(ctas), 32 * kAW, 0, st, p, q, scale, (DevStatus*)ws)
-                               : launch_pdl(pages_attend_kernel<false>, dim3(ctas), 32 * kAW, 0, st, p, q, scale, (DevStatus*)ws);
-  return e == cudaSuccess ? 1 : -1;
+  const cudaError_t e = p.bias ? launch_pdl(pages_wide_kernel<true>, dim3(ctas), 32 * kAW, 0, st, p, q, scale, kRowsMax, (DevStatus*)ws)
+                               : launch_pdl(pages_wide_kernel<false>, dim3(ctas), 32 * kAW, 0, st, p, q, scale, kRowsMax, (DevStatus*)ws);
+  return e == cudaSuccess ? n + 1 : -1;
 }
 
 }  // namespace arckv

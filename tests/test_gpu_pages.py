@@ -2,11 +2,14 @@
 calls.
 
 Tables, slots and what the rows are held as are compared exactly.  An output of attention is a bf16: it is off by at most
-2^-8 of itself, half a step.  Before that, each weight is rounded to f16 (2^-11 of it, and 2^-32 of a weight of one where that
-is below f16's normal range); keys and values may be rounded to f16 too (2^-11 of each element, 2^-25 of the page's largest
-below the normal range), which moves a logit by up to 2^-11 scale sum |q_e k_e| and its weight by as much, relatively, and the
-sum of weights likewise.  fp32 logits and sums add less than 2^-15 of a weight.  So, with A = sum p |v|:
-    |O - ref| <= 2^-8 |ref| + (2^-10 + 2^-13 + 2 (2^-11 + 2^-22) scale max_j sum |q_e k_je|) A + T 2^-24 max |v|
+2^-8 of itself, half a step.  Before that, each weight p is rounded to f16 (2^-11 of it, and 2^-32 of a weight of one where
+that is below f16's normal range).  It may multiply a value's code times scale alone, c s = v - m, where m is the row's least
+value and enters with the weight as it was: with |m| <= (1 + 2^-8) max |v| that is 2^-11 p (|v| + 1.01 max |v|), and sums that
+begin 1024 codes off add 6 roundings of 2^-24 * 1024 s p, s <= 2.02 max |v| / 15, which is 2^-14 p max |v|.  Or it multiplies a
+value rounded to f16: 2^-10 p |v|.  Keys may be rounded to f16 too (2^-11 of each element, 2^-25 of the page's largest below the
+normal range), which moves a logit by up to 2^-11 scale sum |q_e k_e| and its weight by as much, relatively, and the sum of
+weights likewise.  fp32 logits and sums add less than 2^-14 of a weight.  So, with A = sum p |v| and B = sum p max |v|:
+    |O - ref| <= 2^-8 |ref| + (2^-10 + 2^-13 + 2 (2^-11 + 2^-22) scale max_j sum |q_e k_je|) A + 2^-10 B + T 2^-24 max |v|
 """
 import numpy as np
 import pytest
@@ -72,11 +75,12 @@ def check_rows(O, q, k, v, bias, sees, scale=SC):
     """Rows O [n, 128] of one head against the plain form over what the pages hold of k, v [T, 128]."""
     k, v = ref.held_rows(host(k), host(v))
     want, size = ref.attend(host(q), k, v, scale, sees, None if bias is None else host(bias))
+    _, large = ref.attend(host(q), k, np.abs(v).max(1, keepdims=True), scale, sees, None if bias is None else host(bias))
     got = host(O).astype(np.float64)
     T = max(max(sees, default=0), 1)
     moved = scale * (np.abs(host(q)).astype(np.float64) @ np.abs(k[:T]).T).max(1, initial=0.0)[:, None]
     most = np.abs(v[:T]).max(initial=0.0)
-    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -13 + 2 * (2.0 ** -11 + 2.0 ** -22) * moved) * size + T * 2.0 ** -24 * most
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -13 + 2 * (2.0 ** -11 + 2.0 ** -22) * moved) * size + 2.0 ** -10 * large + T * 2.0 ** -24 * most
     empty = ~size.any(-1)
     assert not got[empty].any()
     assert np.all(np.abs(got - want) <= bound), float(np.max(np.abs(got - want) / np.maximum(bound, 1e-300)))
@@ -185,7 +189,7 @@ def test_rows_are_held_as_defined(n, dtype, H):
 
 def test_rows_of_every_magnitude():
     x = torch.randn(40, 2, 128, generator=gen(3))
-    scale = torch.tensor([0.0, 1e-38, 2.0 ** -101, 1e-20, 1.0, 3e4, 1e20, 2.0 ** 95]).repeat(5).view(40, 1, 1)
+    scale = torch.tensor([0.0, 1e-38, 2.0 ** -101, 1e-20, 1.0, 3e4, 1e12, 2.0 ** 66]).repeat(5).view(40, 1, 1)
     x = x * scale
     x[8] = 7.0                                               # constant rows, negative ones, one that an element dominates
     x[9], x[10, :, 3] = -x[9].abs() - 1, 1e9
