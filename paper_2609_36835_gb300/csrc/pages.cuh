@@ -55,6 +55,9 @@ int launch_pages_append(const arckv_pages4& p, int N, bool f32, const void* K, P
 int launch_pages_read(const arckv_pages4& p, int N, bool f32, const int* slots, void* K, void* V, cudaStream_t st);
 size_t pages_attend_scratch(int S, int H, int M, int max_count, int G);
 int launch_pages_attend(const arckv_pages4& p, const PagesQuery& q, float scale, void* ws, cudaStream_t st);
+// the same for requests of more than `above` rows of a head
+size_t pages_tiles_scratch(long long rows);
+int launch_pages_tiles(const arckv_pages4& p, const PagesQuery& q, float scale, int above, void* ws, cudaStream_t st);
 
 struct RotateTensor {
   const void* x;
