@@ -41,17 +41,57 @@ struct RowsShape {
 // Every consumer warp has two stages, so that a page comes in while it works on another.
 template <int kR, bool kBias>
 struct RowsCfg {
-  static constexpr int kW = kR == 16 ? 7 : kBias ? 8 : 9, kSt = 2 * kW, kThreads = 32 * (kW + 1);
+  static constexpr int kW = kR == 16 ? 7 : 8, kSt = 2 * kW, kThreads = 32 * (kW + 1);
   static constexpr int kT = kR / 8;          // tiles of 8 rows, both of a warp
   static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kW * kR * kRowO * 4 + 2 * kR * 256;
   // the rest of it beside 4097 sums and 2 KB of fixed arrays
   static_assert(kSmem + 4097 * 4 + 2048 <= 227 * 1024, "shared memory");
 };
 
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                        float c0, float c1, float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// bf16 operands, sums that begin at zero.
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -62,10 +102,36 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *(const uint32_t*)&h;
 }
-// Two codes as f16: the lowest nibbles of w's halves, 1024 + c; the ones above them, 64 + c.
-__device__ __forceinline__ uint32_t pair_low(uint32_t w) { return (w & 0x000f000fu) | 0x64006400u; }
-__device__ __forceinline__ uint32_t pair_high(uint32_t w) { return (w & 0x00f000f0u) | 0x54005400u; }
+// Codes as f16: the lowest nibbles of w's halves, 1024 + c; the ones above them, 64 + c.  The exponents stay in registers
+// (as constants they would be made anew for most masks).
+struct Masks {
+  uint32_t low, high;
+  __device__ Masks() {
+    asm volatile("mov.u32 %0, 0x64006400;" : "=r"(low));
+    asm volatile("mov.u32 %0, 0x54005400;" : "=r"(high));
+  }
+  // (w & mask) | exponent
+  static __device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask, uint32_t exponent) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "r"(mask), "r"(exponent));
+    return d;
+  }
+  __device__ __forceinline__ uint32_t pair_low(uint32_t w) const { return pick(w, 0x000f000fu, low); }
+  __device__ __forceinline__ uint32_t pair_high(uint32_t w) const { return pick(w, 0x00f000f0u, high); }
+};
 constexpr float kLow = 1024.f, kHigh = 64.f;
+// Whether the phase of `parity` has ended, without waiting.
+__device__ __forceinline__ bool mbar_ended(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok)
+      : "r"(tc::smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
 // A CTA's run of pages of one item.
@@ -204,73 +270,102 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
 
   if (warp == kW) {
-    // ------------------------------------------------------------- producer: queries and pages
-    int it = 0, run = 0;   // pages and runs issued
-    bool ok = true;
-    for (Run p; ok && walk.next(p); ++run) {
-      const int n = p.n, held = pages_of(pages_len(c, p.s));
-      if (!walk.parts) {   // a run ahead, as far as the ring reaches
-        int first;
-        const int buf = run & 1, nrows = rows_of(p.s, first) * d.G;
-        if (run >= 2) ok = __all_sync(0xffffffffu, tc::mbar_wait(&emptyQ[buf], ((run >> 1) - 1) & 1, abortp, stt));
-        if (!ok) {
-          ++it;   // (as where a page's wait gives up: `it` is one more than were issued)
-          break;
-        }
-        if (lane == 0) tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
-        __syncwarp();
-        if (lane < nrows) {
-          const int i = lane / d.G, g = lane - i * d.G;
-          tc::bulk_load(sQ + (buf * kR + lane) * 128, Q + (first + i) * qs.i + p.h * qs.h + g * 128, 256, &fullQ[buf]);
+    // ------------------------------------------------------------- producer
+    // Lane w fills the stages of consumer warp w as that gives them back, each lane at its own pace (in one order for all, the
+    // slowest warp held up the others' pages: 104 us instead of 97 for 64 x 8K); lane 31 brings the queries of the runs, two
+    // ahead.
+    const bool feeds = lane < kW, asks = lane == 31 && !walk.parts;
+    constexpr int kOwn = kSt / kW;   // stages of a warp
+    Run p;
+    int i = 0, base0 = 0, run = 0, issued = 0, entry = -1, held = 0;
+    bool left = (feeds || asks) && walk.next(p);
+    if (left) held = pages_of(pages_len(c, p.s));
+    auto look = [&] {   // the table's entry of page i of the run, on its way while the one before it is waited for
+      entry = p.blk + i < held ? c.table[(long long)p.s * c.M + p.blk + i] : -1;
+    };
+    auto settle = [&] {   // from page i on, the next one of this lane's warp
+      while (left && i >= p.n) {
+        base0 += p.n;
+        left = walk.next(p);
+        if (left) held = pages_of(pages_len(c, p.s));
+        i = (lane + kW - base0 % kW) % kW;
+      }
+      if (left) look();
+    };
+    if (feeds && left) {
+      i = lane;
+      settle();
+    }
+    unsigned long long since = tc::globaltimer();
+    uint32_t spins = 0;
+    while (__any_sync(0xffffffffu, left)) {
+      bool moved = false;
+      if (left) {
+        if (feeds) {
+          const int q = base0 + i, st = q % kSt;
+          if (issued < kOwn || mbar_ended(&empty[st], ((q / kSt) - 1) & 1)) {
+            if (entry >= c.P) {
+              set_status(stt, ARCKV_ERR_INVALID_ARG);
+              entry = -1;
+            }
+            sHeld[st] = entry >= 0;
+            if (entry >= 0) {
+              const long long at = (long long)entry * c.H + p.h;
+              tc::mbar_arrive_expect_tx(&full[st], ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
+              tc::bulk_load(ring + st * ARCKV_PAGE_BYTES, c.data + at * ARCKV_PAGE_BYTES, ARCKV_PAGE_BYTES, &full[st]);
+              if (kBias) tc::bulk_load(sBias + st * kPT, c.bias + at * kPT, kPT * 4, &full[st]);
+            } else {
+              tc::mbar_arrive(&full[st]);
+            }
+            moved = true;
+            ++issued;
+            i += kW;
+            settle();
+          }
+        } else if (run < 2 || mbar_ended(&emptyQ[run & 1], ((run >> 1) - 1) & 1)) {
+          int first;
+          const int buf = run & 1, nrows = rows_of(p.s, first) * d.G;
+          tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
+          for (int r = 0; r < nrows; ++r) {
+            const int k = r / d.G;
+            tc::bulk_load(sQ + (buf * kR + r) * 128, Q + (first + k) * qs.i + p.h * qs.h + (r - k * d.G) * 128, 256, &fullQ[buf]);
+          }
+          moved = true;
+          ++run;
+          left = walk.next(p);
         }
       }
-      for (int k0 = 0; k0 < n && ok; k0 += 32) {
-        const int b = p.blk + k0 + lane;
-        int page = -1;
-        if (k0 + lane < n && b < held) {
-          page = c.table[(long long)p.s * c.M + b];
-          if (page >= c.P) {
-            set_status(stt, ARCKV_ERR_INVALID_ARG);
-            page = -1;
-          }
+      if (__any_sync(0xffffffffu, moved)) {
+        since = tc::globaltimer();
+      } else if ((++spins & 63u) == 0) {
+        bool stop = *abortp != 0;
+        if (!stop && tc::globaltimer() - since > tc::kWaitLimitNs) {
+          *abortp = 1;
+          set_status(stt, ARCKV_ERR_TIMEOUT);
+          stop = true;
         }
-        const int cnt = min(32, n - k0);
-        auto load = [&](int st) {   // this lane's page into stage st
-          sHeld[st] = page >= 0;
-          if (page < 0) {
-            tc::mbar_arrive(&full[st]);
-            return;
-          }
-          const long long at = (long long)page * c.H + p.h;
-          tc::mbar_arrive_expect_tx(&full[st], ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
-          tc::bulk_load(ring + st * ARCKV_PAGE_BYTES, c.data + at * ARCKV_PAGE_BYTES, ARCKV_PAGE_BYTES, &full[st]);
-          if (kBias) tc::bulk_load(sBias + st * kPT, c.bias + at * kPT, kPT * 4, &full[st]);
-        };
-        int j = 0;
-        if (it < kSt) {   // the ring's first round
-          j = min(cnt, kSt - it);
-          if (lane < j) load(it + lane);
-          __syncwarp();
-        }
-        for (; j < cnt && ok; ++j) {
-          const int q = it + j, st = q % kSt;
-          ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[st], ((q / kSt) - 1) & 1, abortp, stt));
-          if (ok && lane == j) load(st);
-        }
-        it += j;
+        if (__any_sync(0xffffffffu, stop)) break;
       }
     }
-    if (!ok) {   // let the copies in flight land before the CTA's memory goes
+    if (*abortp) {   // let the copies in flight land before the CTA's memory goes: a barrier's last phase is complete, or will be
       volatile int never = 0;
-      for (int q = max(0, it - 1 - kSt); q < it - 1; ++q) tc::mbar_wait(&full[q % kSt], (q / kSt) & 1, &never, stt);
-      if (!walk.parts)
-        for (int q = max(0, run - 2); q < run; ++q) tc::mbar_wait(&fullQ[q & 1], (q >> 1) & 1, &never, stt);
+      if (feeds)   // (the n-th page of a stage completes its phase n - 1)
+        for (int k = 0; k < kOwn; ++k) {
+          const int n = (issued + kOwn - 1 - k) / kOwn;   // pages that stage k of this warp's got
+          if (n > 0) tc::mbar_wait(&full[lane + k * kW], (n - 1) & 1, &never, stt);
+        }
+      if (asks)
+        for (int k = 0; k < 2; ++k) {
+          const int n = (run + 1 - k) / 2;
+          if (n > 0) tc::mbar_wait(&fullQ[k], (n - 1) & 1, &never, stt);
+        }
     }
     return;
   }
 
   // --------------------------------------------------------------- consumers
   const int g = lane >> 2, t = lane & 3;
+  const Masks as;
   int base = 0, run = 0;         // pages of earlier runs, and their number
   bool ok = true;
   for (Run p; walk.next(p); ++run) {
@@ -278,7 +373,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     const int n = p.n, len = pages_len(c, p.s), h = p.h, count = rows_of(p.s, first), nrows = count * d.G;
     // query rows: column n of tile e is row 8 e + n
     uint32_t qf[kT][8][2];
-    float q_off[kT][4][2], q_sum[kT][4][2];   // minus what the codes' offsets add, and the sums of a group's elements, rows 2t, 2t + 1
+    float q_off[kT][4][2];                    // minus what the codes' offsets add to a group, rows 2t, 2t + 1
+    uint32_t q_sum[kT][2];                    // the sums of the groups' elements as three bf16 each, an operand of 16 such: row g, group t
     float fac[kT][2];                         // 2^e scale (log2 e) of them
     int see[kT][2], see_min = 0x7fffffff;     // tokens that they see
     if (!walk.parts) ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
@@ -320,10 +416,14 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           off[w] += __shfl_xor_sync(0xffffffffu, off[w], o);
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          q_sum[e][w][k] = __shfl_sync(0xffffffffu, sum[w], (2 * t + k) * 4);
-          q_off[e][w][k] = __shfl_sync(0xffffffffu, off[w], (2 * t + k) * 4);
-        }
+        for (int k = 0; k < 2; ++k) q_off[e][w][k] = __shfl_sync(0xffffffffu, off[w], (2 * t + k) * 4);
+      }
+      {
+        bf16 hi, mid, lo;
+        split3_bf16(t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3], hi, mid, lo);
+        const __nv_bfloat162 a = __halves2bfloat162(hi, mid), b = __halves2bfloat162(lo, __float2bfloat16_rn(0.f));
+        q_sum[e][0] = *(const uint32_t*)&a;
+        q_sum[e][1] = *(const uint32_t*)&b;
       }
       const float f = down * scale * (kBias ? 1.f : kLog2e);
       const int sees = r < nrows ? (d.causal ? max(0, min(len, len - count + i + 1)) : len) : 0;
@@ -337,7 +437,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     __syncwarp();
     if (!walk.parts && lane == 0) tc::mbar_arrive(&emptyQ[run & 1]);
     float o[kT][8][4], mx[kT][2], l[kT][2], low[kT][2];   // low: sums of weights times least values
-    float v_ref = 0.f;                                     // unit of o: a power of two
+    float wide[kT][2];                                     // what the higher nibbles' offsets have added to o, over 64
+    float v_ref = 0.f;                                     // unit of o and wide: a power of two
 #pragma unroll
     for (int e = 0; e < kT; ++e) {
 #pragma unroll
@@ -347,7 +448,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         mx[e][k] = -INFINITY;
-        l[e][k] = low[e][k] = 0.f;
+        l[e][k] = low[e][k] = wide[e][k] = 0.f;
       }
     }
     // page base + i of the CTA belongs to warp (base + i) % kW
@@ -367,22 +468,27 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           const uint4 pb = *(const uint4*)(page + kPageKp + (mt * 16 + g + 8) * 16);
           const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
           const uint32_t pw[4] = {pa.x, pa.y, pa.z, pa.w}, pv[4] = {pb.x, pb.y, pb.z, pb.w};
+          {   // least values times the sums of the queries' elements: here lane (g, t) has group t of its tokens
+            const uint32_t ma = *(const uint32_t*)(page + kPageKp + (mt * 16 + g) * 16 + 4 * t);
+            const uint32_t mb = *(const uint32_t*)(page + kPageKp + (mt * 16 + g + 8) * 16 + 4 * t);
+#pragma unroll
+            for (int e = 0; e < kT; ++e)
+              mma_bf16(s[e][mt], __byte_perm(ma, 0u, 0x3232), __byte_perm(mb, 0u, 0x3232), ma >> 16, mb >> 16, q_sum[e][0], q_sum[e][1]);
+          }
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const uint32_t a8 = aw[w] >> 8, b8 = bw[w] >> 8;
-            const uint32_t f0 = pair_low(aw[w]), f1 = pair_low(bw[w]), f2 = pair_high(aw[w]), f3 = pair_high(bw[w]);
-            const uint32_t f4 = pair_low(a8), f5 = pair_low(b8), f6 = pair_high(a8), f7 = pair_high(b8);
+            const uint32_t f0 = as.pair_low(aw[w]), f1 = as.pair_low(bw[w]), f2 = as.pair_high(aw[w]), f3 = as.pair_high(bw[w]);
+            const uint32_t f4 = as.pair_low(a8), f5 = as.pair_low(b8), f6 = as.pair_high(a8), f7 = as.pair_high(b8);
 #pragma unroll
             for (int e = 0; e < kT; ++e) {
-              float acc[4] = {q_off[e][w][0], q_off[e][w][1], q_off[e][w][0], q_off[e][w][1]};
-              mma_f16(acc, f0, f1, f2, f3, qf[e][2 * w][0], qf[e][2 * w][1]);
+              float acc[4];
+              mma_f16(acc, f0, f1, f2, f3, qf[e][2 * w][0], qf[e][2 * w][1], q_off[e][w][0], q_off[e][w][1], q_off[e][w][0], q_off[e][w][1]);
               mma_f16(acc, f4, f5, f6, f7, qf[e][2 * w + 1][0], qf[e][2 * w + 1][1]);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                const float x = fmaf(bf16_hi(pw[w]), q_sum[e][w][k], w ? s[e][mt][k] : 0.f);
-                const float y = fmaf(bf16_hi(pv[w]), q_sum[e][w][k], w ? s[e][mt][2 + k] : 0.f);
-                s[e][mt][k] = fmaf(bf16_lo(pw[w]), acc[k], x);
-                s[e][mt][2 + k] = fmaf(bf16_lo(pv[w]), acc[2 + k], y);
+                s[e][mt][k] = fmaf(bf16_lo(pw[w]), acc[k], s[e][mt][k]);
+                s[e][mt][2 + k] = fmaf(bf16_lo(pv[w]), acc[2 + k], s[e][mt][2 + k]);
               }
             }
           }
@@ -438,6 +544,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
               if (up) mx[e][k] = x;
               l[e][k] *= alpha[k];
               low[e][k] *= alpha[k];
+              wide[e][k] *= alpha[k];
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -448,26 +555,34 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         // the values' scales and least values; of tokens that are not held, zero
         float vs[8], vm[8], most = 0.f;
         {
-          const bool edge = j0 + kPT > len;
+          uint32_t par[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) par[x] = *(const uint32_t*)(page + kPageVp + (x * 8 + g) * 4);
+          if (j0 + kPT > len) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (j0 + x * 8 + g >= len) par[x] = 0u;
+          }
 #pragma unroll
           for (int x = 0; x < 8; ++x) {
-            uint32_t w = *(const uint32_t*)(page + kPageVp + (x * 8 + g) * 4);
-            if (edge && j0 + x * 8 + g >= len) w = 0u;
-            vs[x] = bf16_lo(w);
-            vm[x] = bf16_hi(w);
-            most = fmaxf(most, vs[x]);
+            vs[x] = bf16_lo(par[x]);
+            vm[x] = bf16_hi(par[x]);
           }
+          most = fmaxf(max3(max3(vs[0], vs[1], vs[2]), vs[3], vs[4]), max3(vs[5], vs[6], vs[7]));
         }
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
         if (most > v_ref) {   // (uniform) a larger unit: between two and four times the scale, so that few pages raise it
           const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23)), by = v_ref / to;
 #pragma unroll
-          for (int e = 0; e < kT; ++e)
+          for (int e = 0; e < kT; ++e) {
+            wide[e][0] *= by;
+            wide[e][1] *= by;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
 #pragma unroll
               for (int f = 0; f < 4; ++f) o[e][k][f] *= by;
+          }
           v_ref = to;
         }
         const float inv_ref = v_ref > 0.f ? 1.f / v_ref : 0.f;
@@ -476,35 +591,40 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         uint32_t ph[kT][4][2];
 #pragma unroll
         for (int e = 0; e < kT; ++e) {
+          // (nothing visible yet: weights 2^{-inf} = 0)
+          const float2 ref = make_float2(mx[e][0] == -INFINITY ? 0.f : -mx[e][0], mx[e][1] == -INFINITY ? 0.f : -mx[e][1]);
+          const float2 fac2 = make_float2(fac[e][0], fac[e][1]);
+          float2 sum = make_float2(0.f, 0.f), lows = make_float2(low[e][0], low[e][1]);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float ref = mx[e][k] == -INFINITY ? 0.f : mx[e][k];   // nothing visible yet: weights 2^{-inf} = 0
-            float sum = 0.f;
+          for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
-            for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-              for (int hf = 0; hf < 2; ++hf) {
-                float& x = s[e][mt][2 * hf + k];
-                // a bias of the type's lowest value cancels against itself before the factor log2 e
-                x = ex2_approx(kBias ? fmaf(x - ref, kLog2e, kLift) : fmaf(x, fac[e][k], -ref));
-                sum += x;
-                low[e][k] = fmaf(x, vm[2 * mt + hf], low[e][k]);
-                x *= vs[2 * mt + hf];
-              }
-            l[e][k] += sum;
-          }
-          // as f16, transposed to (tokens, row) operands; their sums times the codes' offsets leave the output
+            for (int hf = 0; hf < 2; ++hf) {
+              float2 x = make_float2(s[e][mt][2 * hf], s[e][mt][2 * hf + 1]);
+              // a bias of the type's lowest value cancels against itself before the factor log2 e
+              if (kBias) x = fma2(add2(x, ref), make_float2(kLog2e, kLog2e), make_float2(kLift, kLift));
+              else x = fma2(x, fac2, ref);
+              x.x = ex2_approx(x.x);
+              x.y = ex2_approx(x.y);
+              sum = add2(sum, x);
+              lows = fma2(x, make_float2(vm[2 * mt + hf], vm[2 * mt + hf]), lows);
+              x = mul2(x, make_float2(vs[2 * mt + hf], vs[2 * mt + hf]));
+              ph[e][mt][hf] = transpose8x8(pack_f16(x.x, x.y));   // as f16, transposed to (tokens, row) operands
+            }
+          l[e][0] += sum.x;
+          l[e][1] += sum.y;
+          low[e][0] = lows.x;
+          low[e][1] = lows.y;
+          // Their sums times the codes' offsets leave the output: at once where that is 1024 (the output would be lost in it),
+          // and at the end where it is 64.
           float one[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int mt = 0; mt < 4; ++mt) {
+          for (int mt = 0; mt < 4; ++mt) mma_f16(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][mt][0], ph[e][mt][1]);
+          wide[e][0] += one[0];
+          wide[e][1] += one[1];
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) ph[e][mt][hf] = transpose8x8(pack_f16(s[e][mt][2 * hf], s[e][mt][2 * hf + 1]));
-            mma_f16(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][mt][0], ph[e][mt][1]);
-          }
+          for (int x = 0; x < 8; ++x)
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int f = 0; f < 4; ++f) o[e][k][f] = fmaf(f < 2 ? -kLow : -kHigh, one[f & 1], o[e][k][f]);
+            for (int k = 0; k < 2; ++k) o[e][x][k] = fmaf(-kLow, one[k], o[e][x][k]);
         }
         // ---- O^T += V^T P^T, 16 dims and 16 tokens a product: lane (g, t) has tokens 2t, 2t + 1 and 8 on, dims g + 8 x
 #pragma unroll
@@ -515,8 +635,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const uint32_t a8 = aw[x] >> 8, b8 = bw[x] >> 8;
-            const uint32_t f0 = pair_low(aw[x]), f1 = pair_high(aw[x]), f2 = pair_low(bw[x]), f3 = pair_high(bw[x]);
-            const uint32_t f4 = pair_low(a8), f5 = pair_high(a8), f6 = pair_low(b8), f7 = pair_high(b8);
+            const uint32_t f0 = as.pair_low(aw[x]), f1 = as.pair_high(aw[x]), f2 = as.pair_low(bw[x]), f3 = as.pair_high(bw[x]);
+            const uint32_t f4 = as.pair_low(a8), f5 = as.pair_high(a8), f6 = as.pair_low(b8), f7 = as.pair_high(b8);
 #pragma unroll
             for (int e = 0; e < kT; ++e) {
               mma_f16(o[e][2 * x], f0, f1, f2, f3, ph[e][mt][0], ph[e][mt][1]);
@@ -548,7 +668,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         for (int x = 0; x < 8; ++x)
 #pragma unroll
           for (int z = 0; z < 2; ++z)
-            sO[(warp * kR + r) * kRowO + 16 * x + 8 * z + g] = fmaf(o[e][x][2 * z + k], v_ref, low[e][k]);
+            sO[(warp * kR + r) * kRowO + 16 * x + 8 * z + g] = fmaf(z ? fmaf(-kHigh, wide[e][k], o[e][x][2 + k]) : o[e][x][k], v_ref, low[e][k]);
       }
     if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
     bar_consumers(kW * 32);
