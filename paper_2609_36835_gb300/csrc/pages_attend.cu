@@ -48,22 +48,27 @@ struct RowsCfg {
   static_assert(kSmem + 4097 * 4 + 2048 <= 227 * 1024, "shared memory");
 };
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
-                                        float c0, float c1, float c2, float c3) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// bf16 operands, sums that begin at zero.
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+// Sums that begin at zero.
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// bf16 operands: the same word for both halves of a row's elements.
+__device__ __forceinline__ void mma_bf16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %4, %5}, {%6, %7}, {%8, %8, %8, %8};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %4, %5}, {%6, %7}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
 }
 // Two fp32 operations an instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -373,8 +378,9 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     const int n = p.n, len = pages_len(c, p.s), h = p.h, count = rows_of(p.s, first), nrows = count * d.G;
     // query rows: column n of tile e is row 8 e + n
     uint32_t qf[kT][8][2];
-    float q_off[kT][4][2];                    // minus what the codes' offsets add to a group, rows 2t, 2t + 1
-    uint32_t q_sum[kT][2];                    // the sums of the groups' elements as three bf16 each, an operand of 16 such: row g, group t
+    // What a token's scales and least values multiply beside the codes' sums, row g, group t: minus what the codes' offsets add
+    // to the group, and the sum of its elements, each as three bf16
+    uint32_t q_sum[kT][3];
     float fac[kT][2];                         // 2^e scale (log2 e) of them
     int see[kT][2], see_min = 0x7fffffff;     // tokens that they see
     if (!walk.parts) ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
@@ -415,15 +421,13 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           sum[w] += __shfl_xor_sync(0xffffffffu, sum[w], o);
           off[w] += __shfl_xor_sync(0xffffffffu, off[w], o);
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) q_off[e][w][k] = __shfl_sync(0xffffffffu, off[w], (2 * t + k) * 4);
       }
       {
-        bf16 hi, mid, lo;
-        split3_bf16(t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3], hi, mid, lo);
-        const __nv_bfloat162 a = __halves2bfloat162(hi, mid), b = __halves2bfloat162(lo, __float2bfloat16_rn(0.f));
-        q_sum[e][0] = *(const uint32_t*)&a;
-        q_sum[e][1] = *(const uint32_t*)&b;
+        bf16 a[3], b[3];
+        split3_bf16(t == 0 ? off[0] : t == 1 ? off[1] : t == 2 ? off[2] : off[3], a[0], a[1], a[2]);
+        split3_bf16(t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3], b[0], b[1], b[2]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) q_sum[e][k] = __bfloat16_as_ushort(a[k]) | (uint32_t)__bfloat16_as_ushort(b[k]) << 16;
       }
       const float f = down * scale * (kBias ? 1.f : kLog2e);
       const int sees = r < nrows ? (d.causal ? max(0, min(len, len - count + i + 1)) : len) : 0;
@@ -468,12 +472,14 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           const uint4 pb = *(const uint4*)(page + kPageKp + (mt * 16 + g + 8) * 16);
           const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
           const uint32_t pw[4] = {pa.x, pa.y, pa.z, pa.w}, pv[4] = {pb.x, pb.y, pb.z, pb.w};
-          {   // least values times the sums of the queries' elements: here lane (g, t) has group t of its tokens
+          {   // here lane (g, t) has scale and least value of group t of its tokens
             const uint32_t ma = *(const uint32_t*)(page + kPageKp + (mt * 16 + g) * 16 + 4 * t);
             const uint32_t mb = *(const uint32_t*)(page + kPageKp + (mt * 16 + g + 8) * 16 + 4 * t);
 #pragma unroll
-            for (int e = 0; e < kT; ++e)
-              mma_bf16(s[e][mt], __byte_perm(ma, 0u, 0x3232), __byte_perm(mb, 0u, 0x3232), ma >> 16, mb >> 16, q_sum[e][0], q_sum[e][1]);
+            for (int e = 0; e < kT; ++e) {
+              mma_bf16_zero(s[e][mt], ma, mb, q_sum[e][2], 0u);
+              mma_bf16(s[e][mt], ma, mb, q_sum[e][0], q_sum[e][1]);
+            }
           }
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
@@ -483,7 +489,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 #pragma unroll
             for (int e = 0; e < kT; ++e) {
               float acc[4];
-              mma_f16(acc, f0, f1, f2, f3, qf[e][2 * w][0], qf[e][2 * w][1], q_off[e][w][0], q_off[e][w][1], q_off[e][w][0], q_off[e][w][1]);
+              mma_f16_zero(acc, f0, f1, f2, f3, qf[e][2 * w][0], qf[e][2 * w][1]);
               mma_f16(acc, f4, f5, f6, f7, qf[e][2 * w + 1][0], qf[e][2 * w + 1][1]);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
@@ -616,9 +622,10 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           low[e][1] = lows.y;
           // Their sums times the codes' offsets leave the output: at once where that is 1024 (the output would be lost in it),
           // and at the end where it is 64.
-          float one[4] = {0.f, 0.f, 0.f, 0.f};
+          float one[4];
+          mma_f16_zero(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][0][0], ph[e][0][1]);
 #pragma unroll
-          for (int mt = 0; mt < 4; ++mt) mma_f16(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][mt][0], ph[e][mt][1]);
+          for (int mt = 1; mt < 4; ++mt) mma_f16(one, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, ph[e][mt][0], ph[e][mt][1]);
           wide[e][0] += one[0];
           wide[e][1] += one[1];
 #pragma unroll
