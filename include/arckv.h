@@ -559,12 +559,11 @@ arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int
  * Angles are reduced exactly, so they are as good at any position as at zero.
  *   turns      uint64 [r/2] device: turns a position, in units of 2^-64
  *   positions  int32 [N] device; rows with one below zero are copied
- *   X, Y       two tensors (the second may be NULL) of rows (n, head), bf16 or
- *              fp32 with ARCKV_FLAG_F32; row (n, h) of X[k] begins x_strides[2k] n +
- *              x_strides[2k+1] h elements after the base.  Y[k] is X[k] (in place,
- *              with the same strides) or does not overlap any X.  Bases and strides
- *              are multiples of 16 bytes.
- *   heads      heads of the two tensors
+ *   X, Y       rows (n, head) of the given number of heads, bf16 or fp32 with ARCKV_FLAG_F32; row (n, h)
+ *              begins strides[0] n + strides[1] h elements after the base (NULL: dense [N][heads][d]).  Y is X
+ *              (in place, with the same strides) or does not overlap any input.  Bases and strides are
+ *              multiples of 16 bytes.
+ *   X2, Y2     a second tensor of the same type, turned in the same launch (keys beside queries); NULL: none
  * Pairs are (i, i + r/2), or with ARCKV_FLAG_INTERLEAVED (2i, 2i + 1).  With
  * ARCKV_FLAG_TRANSPOSE the transposed map, which turns by -a: what gradients
  * take.  d a multiple of 16 up to 512, r a multiple of 16 up to d.  The call only
@@ -573,8 +572,9 @@ arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int
 #define ARCKV_FLAG_INTERLEAVED 0x10u
 #define ARCKV_FLAG_TRANSPOSE 0x20u
 arckv_status arckv_rotate(int32_t N, int32_t d, int32_t r, float f, const uint64_t* turns, const int32_t* positions,
-                          const void* const* X, const int64_t* x_strides, void* const* Y, const int64_t* y_strides,
-                          const int32_t* heads, uint32_t flags, void* stream);
+                          const void* X, const int64_t* x_strides, void* Y, const int64_t* y_strides, int32_t heads,
+                          const void* X2, const int64_t* x2_strides, void* Y2, const int64_t* y2_strides, int32_t heads2,
+                          uint32_t flags, void* stream);
 
 /* Read (and clear) the device status word of a workspace after a
  * non-blocking call; synchronises `stream`. */

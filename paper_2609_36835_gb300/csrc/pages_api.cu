@@ -142,28 +142,28 @@ arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int
 }
 
 arckv_status arckv_rotate(int32_t N, int32_t d, int32_t r, float f, const uint64_t* turns, const int32_t* positions,
-                          const void* const* X, const int64_t* x_strides, void* const* Y, const int64_t* y_strides,
-                          const int32_t* heads, uint32_t flags, void* stream) {
+                          const void* X, const int64_t* x_strides, void* Y, const int64_t* y_strides, int32_t heads,
+                          const void* X2, const int64_t* x2_strides, void* Y2, const int64_t* y2_strides, int32_t heads2,
+                          uint32_t flags, void* stream) {
   if (flags & ~(ARCKV_FLAG_NONBLOCKING | ARCKV_FLAG_F32 | ARCKV_FLAG_INTERLEAVED | ARCKV_FLAG_TRANSPOSE))
     return ARCKV_ERR_INVALID_ARG;
   if (d < 16 || d > 512 || d % 16 || r < 16 || r > d || r % 16) return ARCKV_ERR_UNSUPPORTED;
   if (N < 1 || N >= (1 << 30)) return ARCKV_ERR_SHAPE;
-  if (!turns || misaligned(turns, 8) || !positions || misaligned(positions, 4) || !X || !x_strides || !Y || !y_strides || !heads ||
+  if (!turns || misaligned(turns, 8) || !positions || misaligned(positions, 4) || !X || !Y || (!X2 && Y2) || (X2 && !Y2) ||
       !isfinite(f))
     return ARCKV_ERR_INVALID_ARG;
+  if (heads < 1 || heads > 65535 || (X2 && (heads2 < 1 || heads2 > 65535))) return ARCKV_ERR_SHAPE;
   const int size = flags & ARCKV_FLAG_F32 ? 4 : 2;
   RotateTensor t[2] = {};
-  for (int k = 0; k < 2; ++k) {
-    if (k == 1 && !X[1]) break;
-    if (!X[k] || !Y[k]) return ARCKV_ERR_INVALID_ARG;
-    if (heads[k] < 1 || heads[k] > 65535) return ARCKV_ERR_SHAPE;
-    t[k].x = X[k];
-    t[k].y = Y[k];
-    t[k].heads = heads[k];
-    if (!packed_strides(X[k], x_strides + 2 * k, 0, 0, size, &t[k].xs) || !packed_strides(Y[k], y_strides + 2 * k, 0, 0, size, &t[k].ys))
-      return ARCKV_ERR_INVALID_ARG;
-    if (X[k] == Y[k] && (t[k].xs.i != t[k].ys.i || t[k].xs.h != t[k].ys.h)) return ARCKV_ERR_INVALID_ARG;
-  }
+  auto take = [&](RotateTensor& to, const void* x, const int64_t* xs, void* y, const int64_t* ys, int32_t n) {
+    to.x = x;
+    to.y = y;
+    to.heads = n;
+    return packed_strides(x, xs, (int64_t)n * d, d, size, &to.xs) && packed_strides(y, ys, (int64_t)n * d, d, size, &to.ys) &&
+           !(x == y && (to.xs.i != to.ys.i || to.xs.h != to.ys.h));
+  };
+  if (!take(t[0], X, x_strides, Y, y_strides, heads) || (X2 && !take(t[1], X2, x2_strides, Y2, y2_strides, heads2)))
+    return ARCKV_ERR_INVALID_ARG;
   cudaGetLastError();
   if (launch_rotate(N, d, r, f, (const unsigned long long*)turns, positions, t, size == 4,
                     (flags & ARCKV_FLAG_INTERLEAVED) != 0, (flags & ARCKV_FLAG_TRANSPOSE) != 0, (cudaStream_t)stream) < 0)

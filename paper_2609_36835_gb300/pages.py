@@ -28,7 +28,7 @@ def _declare(lib) -> None:
     for name, args in (("arckv_pages_extend", [C, P, I, P, P, P, U, P]), ("arckv_pages_truncate", [C, P, U, P]),
                        ("arckv_pages_append", [C, I, P, L2, P, L2, P, P, U, P]), ("arckv_pages_read", [C, I, P, P, P, U, P]),
                        ("arckv_pages_attend", [C, I, I, I, ctypes.c_float, P, L2, P, P, L2, P, ctypes.c_size_t, U, P]),
-                       ("arckv_rotate", [I, I, I, ctypes.c_float, P, P, P, P, P, P, P, U, P])):
+                       ("arckv_rotate", [I, I, I, ctypes.c_float, P, P, P, L2, P, L2, I, P, L2, P, L2, I, U, P])):
         entry = getattr(lib, name)
         entry.argtypes, entry.restype = args, ctypes.c_int
     lib.arckv_pages_attend_workspace_bytes.argtypes = [I] * 6
@@ -111,14 +111,13 @@ def _int32(name: str, x: int) -> int:
 
 
 def _index(name: str, x, shape, device):
-    """Address of a dense int32 tensor of `shape` (None: any extent) on `device`."""
+    """Address of a dense int32 tensor of one dimension, of `shape` (None: any), on `device`."""
     import torch
-    if (not isinstance(x, torch.Tensor) or x.dtype != torch.int32 or x.dim() != len(shape)
-            or any(w is not None and g != w for g, w in zip(x.shape, shape)) or x.device != device or not x.is_contiguous()):
-        got = "%s %s on %s" % (x.dtype, tuple(x.shape), x.device) if isinstance(x, torch.Tensor) else type(x).__name__
-        raise ValueError("arckv: %s must be a dense int32 tensor of shape %s on %s, got %s"
-                         % (name, tuple("*" if w is None else w for w in shape), device, got))
-    return x.data_ptr()
+    if (isinstance(x, torch.Tensor) and x.dtype == torch.int32 and (x.shape == shape if shape is not None else x.dim() == 1)
+            and x.device == device and x.is_contiguous()):
+        return x.data_ptr()
+    got = "%s %s on %s" % (x.dtype, tuple(x.shape), x.device) if isinstance(x, torch.Tensor) else type(x).__name__
+    raise ValueError("arckv: %s must be a dense int32 tensor of shape %s on %s, got %s" % (name, shape or ("*",), device, got))
 
 
 def _strides2(name: str, x, dense_from: int):
@@ -152,12 +151,11 @@ def pages_extend(pages: Pages4, counts, n_rows: int, *, stream=None, check: bool
         stream = _pk._side_stream(stream, dev, counts, *pages._tensors())
         with torch.cuda.stream(stream):
             return pages_extend(pages, counts, n_rows, check=check)
-    out = torch.empty(c.S + 1 + 2 * n_rows, dtype=torch.int32, device=dev)
-    at = out.data_ptr()
+    starts, slots, positions = counts.new_empty(c.S + 1), counts.new_empty(n_rows), counts.new_empty(n_rows)
     _raise_for(pages._entry("arckv_pages_extend")(
-        pages._ref, counts_ptr, n_rows, at, at + 4 * (c.S + 1), at + 4 * (c.S + 1 + n_rows),
+        pages._ref, counts_ptr, n_rows, starts.data_ptr(), slots.data_ptr(), positions.data_ptr(),
         0 if check else _pk.FLAG_NONBLOCKING, _pk._current_handle(dev)), "arckv_pages_extend")
-    return out[:c.S + 1], out[c.S + 1:c.S + 1 + n_rows], out[c.S + 1 + n_rows:]
+    return starts, slots, positions
 
 
 def pages_truncate(pages: Pages4, lens, *, stream=None, check: bool = True) -> None:
@@ -207,7 +205,7 @@ def pages_read(pages: Pages4, slots, *, dtype=None, stream=None, check: bool = T
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("arckv: dtype must be torch.bfloat16 or torch.float32, got %s" % dtype)
     c, dev = pages._c, pages.data.device
-    slots_ptr = _index("slots", slots, (None,), dev)
+    slots_ptr = _index("slots", slots, None, dev)
     if stream is not None:
         stream = _pk._side_stream(stream, dev, slots, *pages._tensors())
         with torch.cuda.stream(stream):
@@ -362,53 +360,66 @@ def rotate(how: Rotary, positions, X, X2=None, *, out=None, transpose: bool = Fa
     Returns new tensors (a pair when X2 is given), or fills `out` (a tensor or a pair), which may be X and X2 themselves.
     transpose: the transposed map, which takes gradients of the outputs to those of X and X2."""
     import torch
-    dev = X.device
-    given = [X] if X2 is None else [X, X2]
-    for name, x in zip(("X", "X2"), given):
-        if x.dim() != 3 or x.dtype not in (torch.bfloat16, torch.float32) or x.dtype != X.dtype or x.shape[0] != X.shape[0] \
-                or x.shape[2] != X.shape[2] or x.device != dev:
-            raise ValueError("arckv: %s must be bfloat16 or float32 of shape ('n', 'heads', 'd'), as X is, got %s %s on %s"
-                             % (name, x.dtype, tuple(x.shape), x.device))
+    dev, dtype = X.device, X.dtype
+    if X.dim() != 3 or (dtype != torch.bfloat16 and dtype != torch.float32):
+        raise ValueError("arckv: X must be bfloat16 or float32 of shape ('n', 'heads', 'd'), got %s %s" % (dtype, tuple(X.shape)))
+    N, heads, d = X.shape
+    heads2 = 0
+    if X2 is not None:
+        if X2.dim() != 3 or X2.dtype != dtype or X2.shape[0] != N or X2.shape[2] != d or X2.device != dev:
+            raise ValueError("arckv: X2 must be %s of shape %s on %s, got %s %s on %s"
+                             % (dtype, (N, "heads", d), dev, X2.dtype, tuple(X2.shape), X2.device))
+        heads2 = X2.shape[1]
     if dev.type != "cuda":
         raise ValueError("arckv: X must be on a CUDA device, got %s (there is no CPU path)" % dev)
-    N, _, d = X.shape
-    if d % 16 or d > 512 or how.width > d:
-        raise ValueError("arckv: d must be a multiple of 16 up to 512 and at least the width %d, got %d" % (how.width, d))
-    if how.turns.device != dev:
-        raise ValueError("arckv: the rotary's turns are on %s but X on %s" % (how.turns.device, dev))
+    turns = how.turns
+    width = 2 * turns.shape[0]
+    if d % 16 or d > 512 or width > d:
+        raise ValueError("arckv: d must be a multiple of 16 up to 512 and at least the width %d, got %d" % (width, d))
+    if turns.device != dev:
+        raise ValueError("arckv: the rotary's turns are on %s but X on %s" % (turns.device, dev))
     positions_ptr = _index("positions", positions, (N,), dev)
-    outs = [] if out is None else list(out) if isinstance(out, (tuple, list)) else [out]
-    if out is not None and len(outs) != len(given):
-        raise ValueError("arckv: out must have %d tensors, got %d" % (len(given), len(outs)))
-    if stream is not None:
-        stream = _pk._side_stream(stream, dev, how.turns, positions, *given, *outs)
+    if stream is not None:   # outputs made here belong to the stream that fills them
+        given = out if isinstance(out, (tuple, list)) else (out,)
+        stream = _pk._side_stream(stream, dev, turns, positions, X, X2, *given)
         with torch.cuda.stream(stream):
             return rotate(how, positions, X, X2, out=out, transpose=transpose)
     if out is None:
-        outs = [torch.empty(x.shape, dtype=x.dtype, device=dev) for x in given]
-    for x, y in zip(given, outs):
-        if y.dtype != x.dtype or y.shape != x.shape or y.device != dev or not (y.is_contiguous() or _pk._apart(y)):
-            raise ValueError("arckv: out must be as X and X2 are, rows apart, got %s %s on %s" % (y.dtype, tuple(y.shape), y.device))
-        if y.data_ptr() == x.data_ptr() and y.stride() != x.stride() and N > 0:
-            raise ValueError("arckv: out in place must have its input's strides, got %s and %s" % (y.stride(), x.stride()))
-    result = outs[0] if X2 is None else tuple(outs)
-    heads = [x.shape[1] for x in given]
-    if N == 0 or sum(heads) == 0:
+        Y = torch.empty((N, heads, d), dtype=dtype, device=dev)
+        Y2 = None if X2 is None else torch.empty((N, heads2, d), dtype=dtype, device=dev)
+        ys = ys2 = None
+    else:
+        if X2 is None:
+            Y, Y2 = out[0] if isinstance(out, (tuple, list)) and len(out) == 1 else out, None
+        elif isinstance(out, (tuple, list)) and len(out) == 2:
+            Y, Y2 = out
+        else:
+            raise ValueError("arckv: out must be a pair of tensors")
+        ys, ys2 = _rotated("out", X, Y), None if X2 is None else _rotated("out's second", X2, Y2)
+    result = Y if X2 is None else (Y, Y2)
+    xs, xs2 = _strides2("X", X, 2), None if X2 is None else _strides2("X2", X2, 2)
+    if heads2 == 0:
+        X2 = None
+    if heads == 0:   # the second tensor alone
+        X, xs, Y, ys, heads, X2 = X2, xs2, Y2, ys2, heads2, None
+    if N == 0 or X is None:
         return result
-    keep = [k for k, h in enumerate(heads) if h > 0]
-    def strides(tensors):
-        flat = []
-        for k in keep:
-            x = tensors[k]
-            if x.stride(2) != 1:
-                raise ValueError("arckv: the last dimension must be dense, got strides %s" % (x.stride(),))
-            flat += [x.stride(i) if x.shape[i] != 1 else 0 for i in range(2)]
-        return (ctypes.c_int64 * 4)(*flat)
-    def pointers(tensors):
-        return (ctypes.c_void_p * 2)(*[tensors[k].data_ptr() for k in keep])
-    flags = ((_pk.FLAG_F32 if X.dtype == torch.float32 else 0) | (FLAG_INTERLEAVED if how.interleaved else 0)
+    flags = ((_pk.FLAG_F32 if dtype == torch.float32 else 0) | (FLAG_INTERLEAVED if how.interleaved else 0)
              | (FLAG_TRANSPOSE if transpose else 0))
+    second = (None, None, None, None, 0) if X2 is None else (X2.data_ptr(), xs2, Y2.data_ptr(), ys2, heads2)
     entry = _pk._on_device(dev, _pk.load_library().arckv_rotate)
-    _raise_for(entry(N, d, how.width, how.factor, how.turns.data_ptr(), positions_ptr, pointers(given), strides(given), pointers(outs),
-                     strides(outs), (ctypes.c_int32 * 2)(*[heads[k] for k in keep]), flags, _pk._current_handle(dev)), "arckv_rotate")
+    _raise_for(entry(N, d, width, how.factor, turns.data_ptr(), positions_ptr, X.data_ptr(), xs, Y.data_ptr(), ys, heads, *second,
+                     flags, _pk._current_handle(dev)), "arckv_rotate")
     return result
+
+
+def _rotated(name: str, x, y):
+    """Strides of an output y of ``rotate`` for x, which it must match."""
+    import torch
+    if not isinstance(y, torch.Tensor) or y.dtype != x.dtype or y.shape != x.shape or y.device != x.device:
+        raise ValueError("arckv: %s must be %s of shape %s on %s" % (name, x.dtype, tuple(x.shape), x.device))
+    if not y.is_contiguous() and not _pk._apart(y):
+        raise ValueError("arckv: rows of %s share memory, strides %s" % (name, tuple(y.stride())))
+    if y.data_ptr() == x.data_ptr() and y.stride() != x.stride() and y.numel() > 0:
+        raise ValueError("arckv: %s in place must have its input's strides, got %s and %s" % (name, y.stride(), x.stride()))
+    return _strides2(name, y, 2)

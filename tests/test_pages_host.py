@@ -182,18 +182,18 @@ def test_bad_arguments_are_refused(lib, name, kw, code):
     assert CALLS[name](lib, _struct(), **kw) == code
 
 
-def _rotate(lib, N=4, d=128, r=128, f=1.0, turns=8, positions=4, X=(16, None), xs=(128, 128) * 2, Y=(16, None), ys=(128, 128) * 2, heads=(1, 1),
-            flags=0):
-    return lib.arckv_rotate(N, d, r, f, turns, positions, (ctypes.c_void_p * 2)(*X), (ctypes.c_int64 * 4)(*xs), (ctypes.c_void_p * 2)(*Y),
-                            (ctypes.c_int64 * 4)(*ys), (ctypes.c_int32 * 2)(*heads), flags, None)
+def _rotate(lib, N=4, d=128, r=128, f=1.0, turns=8, positions=4, X=16, xs=None, Y=16, ys=None, heads=1, X2=None, xs2=None, Y2=None, ys2=None,
+            heads2=0, flags=0):
+    return lib.arckv_rotate(N, d, r, f, turns, positions, X, l2(xs), Y, l2(ys), heads, X2, l2(xs2), Y2, l2(ys2), heads2, flags, None)
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(d=120), UNSUPPORTED), (dict(d=528), UNSUPPORTED), (dict(r=0), UNSUPPORTED), (dict(r=24), UNSUPPORTED), (dict(d=64), UNSUPPORTED),
     (dict(N=0), SHAPE), (dict(N=1 << 30), SHAPE), (dict(turns=None), BAD), (dict(turns=4), BAD), (dict(positions=None), BAD),
-    (dict(positions=2), BAD), (dict(f=math.inf), BAD), (dict(X=(None, None)), BAD), (dict(X=(24, None)), BAD), (dict(Y=(None, None)), BAD),
-    (dict(Y=(8, None)), BAD), (dict(heads=(0, 1)), SHAPE), (dict(xs=(4, 128, 0, 0)), BAD), (dict(ys=(128, 4, 0, 0)), BAD),
-    (dict(ys=(256, 128, 0, 0)), BAD), (dict(X=(16, 32)), BAD), (dict(X=(16, 32), Y=(16, 32), heads=(1, 0)), SHAPE), (dict(flags=8), BAD)])
+    (dict(positions=2), BAD), (dict(f=math.inf), BAD), (dict(X=None), BAD), (dict(X=24), BAD), (dict(Y=None), BAD),
+    (dict(Y=8), BAD), (dict(heads=0), SHAPE), (dict(heads=65536), SHAPE), (dict(xs=(4, 128)), BAD), (dict(ys=(128, 4)), BAD),
+    (dict(xs=(128, 128), ys=(256, 128)), BAD), (dict(ys=(256, 128)), BAD), (dict(X2=32), BAD), (dict(Y2=32), BAD),
+    (dict(X2=32, Y2=32), SHAPE), (dict(X2=32, Y2=40, heads2=1), BAD), (dict(X2=32, Y2=64, heads2=1, xs2=(2, 128)), BAD), (dict(flags=8), BAD)])
 def test_bad_rotations_are_refused(lib, kw, code):
     assert _rotate(lib, **kw) == code
 
