@@ -542,8 +542,9 @@ size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32
  *      records ARCKV_ERR_SHAPE
  *   O  out bf16, addressed as Q with o_strides; rows do not overlap.  Rows of no
  *      request are left as they are.
- * Softmax weights and sums are fp32; weights enter the value products as f16
- * (2^-12 of each), beside 2^-9 that an output's rounding to bf16 takes.  Pages that
+ * Softmax weights and sums are fp32; weights, and with many rows keys and values,
+ * enter the products as f16 (2^-11 of each), where an output's rounding to bf16
+ * takes 2^-8.  Pages that
  * the table names past the pool record ARCKV_ERR_INVALID_ARG and are passed over,
  * as are missing ones.  Outputs that are not finite record ARCKV_ERR_NONFINITE.
  */

@@ -20,7 +20,7 @@
 //    ticket), which adds the parts up in CTA order.  Consumer warps take whole pages in turn, each with its own
 //    running maximum, sum and output.
 //  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
-//    by up to 2^8): half a step is 2^-12 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
+//    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
 //    without limit from page to page: the output is then scaled down, as for a maximum that grows.
 #include "pages.cuh"
 #include "tc.cuh"

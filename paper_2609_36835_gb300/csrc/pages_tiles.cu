@@ -17,13 +17,15 @@
 // added up by pages_join_kernel behind this one.
 //
 // A key or value m + c s enters the products as f16, in units of a power of two near its page's largest: half a step is
-// 2^-12 of an element, an eighth of what the bf16 outputs round to, and elements below 2^-14 of the largest lose bits.  K's
-// unit goes into the factor of its page's logits.  V's goes into the exponent of the weights:
-//   w_j = 2^{x_j - ref + 7 + ev - eref},  O = 2^eref sum_j w_j v_j 2^-ev / sum_b 2^{eref - ev} sum_{j in b} w_j
+// 2^-11 of an element, an eighth of what the bf16 outputs round to, and elements below 2^-8 of the largest lose bits below 2^-19
+// of it.  K's unit goes into the factor of its page's logits.  V's goes into the exponent of the weights:
+//   w_j = 2^{x_j - ref + ev - eref},  O = 2^eref sum_j w_j v_j 2^-ev / sum_b 2^{eref - ev} sum_{j in b} w_j
 // where eref is at least every ev so far (when it grows, O is scaled down, as for a maximum that grows) and ev at least
-// eref - 20: a page of smaller values has them as f16 below the normal range, off by 2^-45 of the largest at most.  ref
-// follows the running maximum only when that has grown by more than 8: weights then stay below 2^15, in the range of f16.
-// Weights enter as one f16, 2^-12 of each.  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
+// eref - 20: a page of smaller values has them as f16 below the normal range, off by 2^-38 of the largest at most.
+// Weights enter as one f16, 2^-11 of each, and ref follows the running maximum only when that has grown by more than 15: to
+// scale O is to wait for its products, and with 8 some warp of a tile did on most pages (512 positions over 8K 97 us, 91 now;
+// one jump a row, of its own token, is common).  Weights then reach 2^15, and lose bits where they are below 2^-12 of the
+// page's largest.  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -33,7 +35,7 @@ namespace {
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
 constexpr int kStages = 3, kStageBytes = 2 * kKTile + kHalf;   // pages (K, V) as operands
-constexpr float kGrow = 8.f, kLift = 7.f;     // see above
+constexpr float kGrow = 15.f;                // see above
 
 struct TileShape {
   int G, N, above, max_count;   // requests of more than `above` rows of a head
@@ -54,8 +56,8 @@ struct TileCfg {
   static constexpr int kRaw = kT == 2 ? 3 : 6;           // pages on their way as codes
   static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + kRaw * ARCKV_PAGE_BYTES + 1024;
   static_assert(kSmem + 4097 * 8 + 2048 <= 227 * 1024, "shared memory");
-  // floats of a partial result: 64 outputs and twice (ref, sum) of each softmax thread
-  static constexpr int kSlot = 68 * kSoftThreads;
+  // 32-bit words of a partial result: 64 outputs as f16, twice (ref, sum), and the unit, of each softmax thread
+  static constexpr int kSlot = 40 * kSoftThreads;
 };
 
 // The products of one block and row tile, issued by one elected lane of a converged warp with warp-uniform operands
@@ -280,14 +282,26 @@ struct __align__(16) Units {   // for the converters: 1 / unit of K, of V, and t
   float k, v;
   int held;
 };
-// The pairs of codes in a word as f16, less the offsets.
-__device__ __forceinline__ __half2 code_pair(uint32_t w, bool high) {
-  const uint32_t y = high ? (w & 0x00f000f0u) | 0x54005400u : (w & 0x000f000fu) | 0x64006400u;
-  const __half_raw off = high ? __half_raw{0x5400} : __half_raw{0x6400};   // 64, 1024
-  return __hsub2(*(const __half2*)&y, __half2{off, off});
+// Codes as f16: a nibble c is the number c 2^-24 by itself, c 2^-20 four bits up.  Both are below the normal range, exact, and
+// ordinary operands: one operation makes c s + m of two, with s 2^24 or s 2^20 for the scale.  The latter must stay below
+// 2^16, so elements are taken in units that leave them below 2^-6 (kDown): then s < 2^-8.9.
+constexpr int kDown = 7;
+struct Scale {
+  __half2 low, high, m;   // s 2^24, s 2^20, m
+  __device__ __forceinline__ Scale(float s0, float s1, float m0, float m1) {
+    high = __floats2half2_rn(s0 * 1048576.f, s1 * 1048576.f);
+    low = __hmul2(high, __half2{__half_raw{0x4c00}, __half_raw{0x4c00}});   // 16
+    m = __floats2half2_rn(m0, m1);
+  }
+};
+__device__ __forceinline__ uint32_t low_pair(uint32_t w, const Scale& s) {
+  const uint32_t c = w & 0x000f000fu;
+  const __half2 z = __hfma2(*(const __half2*)&c, s.low, s.m);
+  return *(const uint32_t*)&z;
 }
-__device__ __forceinline__ uint32_t value_pair(uint32_t w, bool high, __half2 s, __half2 m) {
-  const __half2 z = __hfma2(code_pair(w, high), s, m);
+__device__ __forceinline__ uint32_t high_pair(uint32_t w, const Scale& s) {
+  const uint32_t c = w & 0x00f000f0u;
+  const __half2 z = __hfma2(*(const __half2*)&c, s.high, s.m);
   return *(const uint32_t*)&z;
 }
 
@@ -475,13 +489,13 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           eref = own + 2;
         }
         const int ev = max(own, eref - 20);
-        m.ks = pow2(ek);
+        m.ks = pow2(ek + kDown);
         m.dv = (float)(ev - eref);
         m.undo = pow2(eref - ev);
-        m.unit = pow2(eref);
+        m.unit = pow2(eref + kDown);
         m.page = page;
         if (lane == 0) {
-          units[rs] = Units{pow2(-ek), pow2(-ev), held};
+          units[rs] = Units{pow2(-ek - kDown), pow2(-ev - kDown), held};
           tc::mbar_arrive(&scaled[rs]);
           tc::mbar_arrive(&raw_empty[rs]);
         }
@@ -595,33 +609,30 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const uint32_t cws[4] = {cw4.x, cw4.y, cw4.z, cw4.w}, pws[4] = {pw4.x, pw4.y, pw4.z, pw4.w};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const __half2 s = __float2half2_rn(bf16_lo(pws[w]) * un.k), m = __float2half2_rn(bf16_hi(pws[w]) * un.k);
+          const float sc = bf16_lo(pws[w]) * un.k, least = bf16_hi(pws[w]) * un.k;
+          const Scale z(sc, sc, least, least);
           const uint32_t a = cws[w], b = a >> 8;
           *(uint4*)(Ks + (w >> 1) * kKTile + r * 128 + ((((w & 1) * 4 + t) ^ (r & 7)) << 4)) =
-              make_uint4(value_pair(a, false, s, m), value_pair(a, true, s, m), value_pair(b, false, s, m), value_pair(b, true, s, m));
+              make_uint4(low_pair(a, z), high_pair(a, z), low_pair(b, z), high_pair(b, z));
         }
       }
-      uint4 vc[2];
-      __half2 vs[2], vm[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int pair = cw * 8 + t + 4 * x;
-        vc[x] = *(const uint4*)(raw + kPageV + pair * 128 + ((g ^ (t << 1)) << 4));
+      auto pair_scale = [&](int pair) {
         uint2 p = *(const uint2*)(raw + kPageVp + pair * 8);
         if (2 * pair >= un.held) p.x = 0u;
         if (2 * pair + 1 >= un.held) p.y = 0u;
-        vs[x] = __floats2half2_rn(bf16_lo(p.x) * un.v, bf16_lo(p.y) * un.v);
-        vm[x] = __floats2half2_rn(bf16_hi(p.x) * un.v, bf16_hi(p.y) * un.v);
-      }
+        return Scale(bf16_lo(p.x) * un.v, bf16_lo(p.y) * un.v, bf16_hi(p.x) * un.v, bf16_hi(p.y) * un.v);
+      };
+      const int pair = cw * 8 + t;
+      const Scale z0 = pair_scale(pair), z1 = pair_scale(pair + 4);
+      const uint4 va = *(const uint4*)(raw + kPageV + pair * 128 + ((g ^ (t << 1)) << 4));
+      const uint4 vb = *(const uint4*)(raw + kPageV + (pair + 4) * 128 + ((g ^ (t << 1)) << 4));
+      const uint32_t aw[4] = {va.x, va.y, va.z, va.w}, bw[4] = {vb.x, vb.y, vb.z, vb.w};
       const uint32_t vd = kv0 + st * kStageBytes + 2 * kKTile + v_row;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t a = w == 0 ? vc[0].x : w == 1 ? vc[0].y : w == 2 ? vc[0].z : vc[0].w;
-        const uint32_t b = w == 0 ? vc[1].x : w == 1 ? vc[1].y : w == 2 ? vc[1].z : vc[1].w;
-#pragma unroll
-        for (int z = 0; z < 2; ++z)   // dims 32 w + 16 z .. + 15
-          store_matrices(vd + (w * 32 + z * 16) * 128, value_pair(a >> 8 * z, false, vs[0], vm[0]), value_pair(b >> 8 * z, false, vs[1], vm[1]),
-                         value_pair(a >> 8 * z, true, vs[0], vm[0]), value_pair(b >> 8 * z, true, vs[1], vm[1]));
+      for (int w = 0; w < 4; ++w) {   // dims 32 w .. + 31, 16 at a time
+        const uint32_t a8 = aw[w] >> 8, b8 = bw[w] >> 8;
+        store_matrices(vd + w * (32 * 128), low_pair(aw[w], z0), low_pair(bw[w], z1), high_pair(aw[w], z0), high_pair(bw[w], z1));
+        store_matrices(vd + w * (32 * 128) + 16 * 128, low_pair(a8, z0), low_pair(b8, z1), high_pair(a8, z0), high_pair(b8, z1));
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
@@ -798,7 +809,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         float2 base[2], add[2], sum[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float b = ref[k] == -INFINITY ? 0.f : ref[k], a = (kBias ? 0.f : -b) + kLift + m.dv;
+          const float b = ref[k] == -INFINITY ? 0.f : ref[k], a = (kBias ? 0.f : -b) + m.dv;
           base[k] = make_float2(-b, -b);
           add[k] = make_float2(a, a);
           sum[k] = make_float2(0.f, 0.f);
@@ -848,7 +859,9 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         asm volatile("" : "+r"(q0));
         const int q1 = q0 + 8;
         const long long at0 = (g.row + q0 / d.G) * os.i + (q0 % d.G) * 128, at1 = (g.row + q1 / d.G) * os.i + (q1 % d.G) * 128;
-        const float inv0 = whole ? (l[0] == 0.f ? 0.f : 1.f / l[0]) : 1.f, inv1 = whole ? (l[1] == 0.f ? 0.f : 1.f / l[1]) : 1.f;
+        const float inv0 = l[0] == 0.f ? 0.f : 1.f / l[0], inv1 = l[1] == 0.f ? 0.f : 1.f / l[1];
+        // A part goes to memory divided by its sum, as f16 in O's units, in which it is 2^-6 at most: half a step is 2^-11 of a
+        // part, and parts as fp32 took twice the time to write and read (half of them 13.8 us to join)
         float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + tid * 4;
         if (any_row) {
 #pragma unroll 1
@@ -857,17 +870,29 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             tmem_ld_rows32(Ot + ch * 32, v);
             tmem_wait_ld();
             settle(v);
+            if (whole) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // (the unit first: it may be far from one, and the sum as far from it as the values are)
-              const float4 x = make_float4(v[4 * e] * unit * inv0, v[4 * e + 1] * unit * inv0, v[4 * e + 2] * unit * inv1,
-                                           v[4 * e + 3] * unit * inv1);
-              if (whole) store_rows(O + g.h * os.h + 8 * (ch * 4 + e) + cl, at0, at1, q0 < nrows, q1 < nrows, x, stt);
-              else __stcg((float4*)(slot + (long long)(ch * 4 + e) * Cfg::kSoftThreads * 4), x);
+              for (int e = 0; e < 4; ++e)   // (the unit first: it may be far from one, and the sum as far from it as the values are)
+                store_rows(O + g.h * os.h + 8 * (ch * 4 + e) + cl, at0, at1, q0 < nrows, q1 < nrows,
+                           make_float4(v[4 * e] * unit * inv0, v[4 * e + 1] * unit * inv0, v[4 * e + 2] * unit * inv1,
+                                       v[4 * e + 3] * unit * inv1), stt);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                __half2 y[4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                  const float inv = f & 1 ? inv1 : inv0;
+                  y[f] = __floats2half2_rn(v[8 * e + 2 * f] * inv, v[8 * e + 2 * f + 1] * inv);
+                }
+                __stcg((uint4*)(slot + (long long)(ch * 2 + e) * Cfg::kSoftThreads * 4), *(const uint4*)&y[0]);
+              }
             }
           }
-          if (!whole)   // joined by the kernel behind this one
-            __stcg((float4*)(slot + 16ll * Cfg::kSoftThreads * 4), make_float4(ref[0], l[0], ref[1], l[1]));
+          if (!whole) {   // joined by the kernel behind this one
+            __stcg((float4*)(slot + 8ll * Cfg::kSoftThreads * 4), make_float4(ref[0], l[0], ref[1], l[1]));
+            __stcg(slot + 9ll * Cfg::kSoftThreads * 4, unit);
+          }
         }
       }
       tc::fence_before_sync();
@@ -925,21 +950,19 @@ __global__ void __launch_bounds__(kJoinThreads) pages_join_kernel(int H, TileSha
     const int nrows = tile_rows(d, starts, s, row, stt) * d.G;
     if (row0 >= nrows) continue;   // (uniform)
     auto part = [&](int p) { return parts + (2ll * (first + p) + (p == 0)) * Cfg::kSlot + warp * 128; };
-    // The sums' loads wait for nothing: the first eight parts' are under way while the weights are found.  Sixteen bytes
-    // of two units a thread: columns 8 j + 2 (lane % 4), + 1 of rows lane / 4 and lane / 4 + 8.
+    // The parts' loads wait for nothing: the first eight parts' are under way while the weights are found.  A thread has 16
+    // bytes of each: columns 8 j + 2 (lane % 4), + 1 of rows lane / 4 and lane / 4 + 8, for two j.
     const int r8 = lane >> 2, j8 = tid >> 5;
-    float4 ahead[8][2];
+    uint4 ahead[8];
     auto load = [&](int p0) {
 #pragma unroll
       for (int p = 0; p < 8; ++p)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (p0 + p < n) ahead[p][e] = __ldcg((const float4*)(part(p0 + p) + lane * 4 + (long long)(j8 + 8 * e) * Cfg::kSoftThreads * 4));
+        if (p0 + p < n) ahead[p] = __ldcg((const uint4*)(part(p0 + p) + lane * 4 + (long long)j8 * Cfg::kSoftThreads * 4));
     };
     load(0);
     {   // weights of the parts for row tid / 16, sixteen parts at a time
       const int r = tid >> 4, l16 = tid & 15;
-      const long long at = 16ll * Cfg::kSoftThreads * 4 + (r & 7) * 16 + (r >> 3) * 2;
+      const long long at = 8ll * Cfg::kSoftThreads * 4 + (r & 7) * 16 + (r >> 3) * 2, unit = 9ll * Cfg::kSoftThreads * 4 + (r & 7) * 16;
       float top = -INFINITY;
       float2 mine = make_float2(-INFINITY, 0.f);   // of the first sixteen parts
       if (l16 < n) mine = __ldcg((const float2*)(part(l16) + at));
@@ -953,7 +976,7 @@ __global__ void __launch_bounds__(kJoinThreads) pages_join_kernel(int H, TileSha
         // log2 of what separates two references; of a part that saw nothing no weight
         const float w = y.x == -INFINITY ? 0.f : ex2_approx(kBias ? (y.x - top) * kLog2e : y.x - top);
         z = fmaf(y.y, w, z);
-        s_w[p][r] = w;
+        s_w[p][r] = y.y * w * __ldcg(part(p) + unit);
       }
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
@@ -969,10 +992,11 @@ __global__ void __launch_bounds__(kJoinThreads) pages_join_kernel(int H, TileSha
         for (int p = 0; p < 8; ++p) {
           if (p0 + p >= n) break;
           const float w0 = s_w[p0 + p][r8], w1 = s_w[p0 + p][r8 + 8];
+          const uint32_t y[4] = {ahead[p].x, ahead[p].y, ahead[p].z, ahead[p].w};
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float4 y = ahead[p][e];
-            a[e] = make_float4(fmaf(y.x, w0, a[e].x), fmaf(y.y, w0, a[e].y), fmaf(y.z, w1, a[e].z), fmaf(y.w, w1, a[e].w));
+            const float2 y0 = __half22float2(*(const __half2*)&y[2 * e]), y1 = __half22float2(*(const __half2*)&y[2 * e + 1]);
+            a[e] = make_float4(fmaf(y0.x, w0, a[e].x), fmaf(y0.y, w0, a[e].y), fmaf(y1.x, w1, a[e].z), fmaf(y1.y, w1, a[e].w));
           }
         }
       }
@@ -981,7 +1005,7 @@ __global__ void __launch_bounds__(kJoinThreads) pages_join_kernel(int H, TileSha
       const float i0 = s_inv[r8], i1 = s_inv[r8 + 8];
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        store_rows(O + h * os.h + 8 * (j8 + 8 * e) + 2 * (lane & 3), at0, at1, q0 < nrows, q1 < nrows,
+        store_rows(O + h * os.h + 8 * (2 * j8 + e) + 2 * (lane & 3), at0, at1, q0 < nrows, q1 < nrows,
                    make_float4(a[e].x * i0, a[e].y * i0, a[e].z * i1, a[e].w * i1), stt);
     }
     __syncthreads();
