@@ -263,10 +263,23 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   return g;
 }
 
+constexpr float kLargestBf16 = 3.3895313892515355e38f;
+
+// Of four lanes with four words each, lane c ends with word c of all, in the order of the lanes.
+__device__ __forceinline__ void transpose4(uint32_t (&y)[4], int lane) {
+  const bool b0 = lane & 1, b1 = lane & 2;
+  uint32_t a = __shfl_xor_sync(0xffffffffu, b0 ? y[0] : y[1], 1), b = __shfl_xor_sync(0xffffffffu, b0 ? y[2] : y[3], 1);
+  if (b0) y[0] = a, y[2] = b;
+  else y[1] = a, y[3] = b;
+  a = __shfl_xor_sync(0xffffffffu, b1 ? y[0] : y[2], 2), b = __shfl_xor_sync(0xffffffffu, b1 ? y[1] : y[3], 2);
+  if (b1) y[0] = a, y[1] = b;
+  else y[2] = a, y[3] = b;
+}
+
 // Two columns of two rows of the output, at o + at0 and o + at1.
 __device__ __forceinline__ void store_rows(bf16* o, long long at0, long long at1, bool row0, bool row1, float4 x,
                                            DevStatus* stt) {
-  const float big = 3.3895313892515355e38f;   // (the largest bf16)
+  const float big = kLargestBf16;
   if (row0) *(__nv_bfloat162*)(o + at0) = __floats2bfloat162_rn(x.x, x.y);
   if (row1) *(__nv_bfloat162*)(o + at1) = __floats2bfloat162_rn(x.z, x.w);
   if ((row0 && !(fabsf(x.x) <= big && fabsf(x.y) <= big)) || (row1 && !(fabsf(x.z) <= big && fabsf(x.w) <= big)))
@@ -658,7 +671,6 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       tc::fence_after_sync();
       return ok;
     };
-    auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + t) : "memory"); };
     int it = 0, all = 0;   // pages of this tile, of the CTA, in earlier items
     Segment g = s_first;
     for (long long u = u0; u < u1;) {
@@ -666,50 +678,54 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const int row0 = g.tile * kRows + t * 128, len = pages_len(c, g.s), nrows = g.rows * d.G;
       const bool idle = t == 1 && !both(g);
       const bf16* Qh = Q + g.row * qs.i + g.h * qs.h;
-      float row_fac = 0.f;
-      if (!idle) {   // the queries as f16, each row scaled by a power of two: here a lane is a row, and has 64 dims
-        const int r = quarter * 32 + lane, row = row0 + 64 * (lane >> 4) + 16 * quarter + (lane & 15);   // (r: TMEM lane)
-        const int i = row / d.G, gq = row - i * d.G;
+      // the products' factor (for powers of two without biases, of e with them) and sight of this thread's two rows
+      float fac = 0.f;
+      int see[2];
+      if (!idle) {
+        // This warp's 16 queries as f16, scaled by a power of two that leaves the largest element of all in [2^14, 2^15): a bf16
+        // is exact down to 2^-31 of it, and next to nothing below 2^-39.  16 lanes have a row, two rows at a time.
         uint4 x[8];
-        float amax = 0.f;
+        int row = row0 + r_warp + (lane >> 4), i = row / d.G, gq = row - i * d.G;
+        uint32_t amax = 0u;   // magnitudes of two elements, as integers
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = make_uint4(0u, 0u, 0u, 0u);
-          if (row < nrows) x[e] = *((const uint4*)(Qh + i * qs.i + gq * 128 + half * 64) + e);
+          if (row < nrows) x[e] = *((const uint4*)(Qh + i * qs.i + gq * 128) + (lane & 15));
+          row += 2;
+          gq += 2;
+          while (gq >= d.G) {
+            gq -= d.G;
+            ++i;
+          }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t y[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(y[k])), fabsf(bf16_hi(y[k]))));
+          for (int k = 0; k < 4; ++k) amax = __vmaxu2(amax, y[k] & 0x7fff7fffu);
         }
-        float* half_max = (float*)(sQ + t * 2 * kHalf);   // (the products of the item before have been waited for)
-        half_max[half * 128 + r] = amax;
-        tile_sync();
-        amax = fmaxf(amax, half_max[(half ^ 1) * 128 + r]);
-        tile_sync();
-        const int ex = min(max((int)((__float_as_uint(amax) >> 23) & 0xff) - 127, -100), 127);
+        amax = __reduce_max_sync(0xffffffffu, max(amax & 0xffffu, amax >> 16));
+        const int ex = min(max((int)(amax >> 7) - 127, -100), 127);
         const float up = pow2(14 - ex);
-        row_fac = pow2(ex - 14) * scale * (kBias ? 1.f : kLog2e);
+        fac = pow2(ex - 14) * scale * (kBias ? 1.f : kLog2e);
+        const int c16 = lane & 15;   // chunk of 8 dims
+        unsigned char* to = sQ + (t * 2 + (c16 >> 3)) * kHalf;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t y[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
           __half2 z[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) z[k] = __floats2half2_rn(bf16_lo(y[k]) * up, bf16_hi(y[k]) * up);
-          *(uint4*)(sQ + (t * 2 + half) * kHalf + r * 128 + ((e ^ (r & 7)) << 4)) = *(const uint4*)&z[0];
+          const int r = quarter * 32 + half * 16 + 2 * e + (lane >> 4);   // TMEM lane
+          *(uint4*)(to + r * 128 + (((c16 & 7) ^ (r & 7)) << 4)) = *(const uint4*)&z[0];
         }
         tc::fence_proxy_async_smem();
       }
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&qfull);
-      // products' factors (powers of two without biases, of e with them) and sight of this thread's two rows
-      float fac[2];
-      int see[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = r_warp + (lane >> 2) + 8 * i, row = row0 + r;
-        fac[i] = __shfl_sync(0xffffffffu, row_fac, half * 16 + (lane >> 2) + 8 * i);   // (r is a row of this warp's lanes)
+        const int row = row0 + r_warp + (lane >> 2) + 8 * i;
         see[i] = row < nrows ? row_sees(d.causal, len, g.rows, row / d.G) : 0;
       }
       const int see_min = __reduce_min_sync(0xffffffffu, min(see[0], see[1]));
@@ -731,7 +747,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tmem_ld_rows64(S, v);
         const Meta m = meta[(all + i) % (2 * kStages)];
         // (never zero: a masked product is -inf)
-        const float f[2] = {fmaxf(fac[0] * m.ks, 0x1p-126f), fmaxf(fac[1] * m.ks, 0x1p-126f)};
+        const float f = fmaxf(fac * m.ks, 0x1p-126f);
         unit = m.unit;
         tmem_wait_ld();
         settle(v);
@@ -743,8 +759,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             const float2 x = *(const float2*)(bias + 8 * j);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              v[4 * j + 2 * k] = fmaf(v[4 * j + 2 * k], f[k], x.x);
-              v[4 * j + 2 * k + 1] = fmaf(v[4 * j + 2 * k + 1], f[k], x.y);
+              v[4 * j + 2 * k] = fmaf(v[4 * j + 2 * k], f, x.x);
+              v[4 * j + 2 * k + 1] = fmaf(v[4 * j + 2 * k + 1], f, x.y);
             }
           }
         }
@@ -771,7 +787,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           top[k] = fmaxf(top[k], b);
           // in units of log2; with biases differences of logits first, so that the type's lowest value cancels against
           // itself.  (A reference of -inf is past by any logit but -inf.)
-          grows |= kBias ? (top[k] - ref[k]) * kLog2e > kGrow : top[k] * f[k] > ref[k] + kGrow;
+          grows |= kBias ? (top[k] - ref[k]) * kLog2e > kGrow : top[k] * f > ref[k] + kGrow;
         }
         grows = __any_sync(0xffffffffu, grows);
         if (grows || m.shrink != 1.f) {
@@ -781,7 +797,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             for (int k = 0; k < 2; ++k) {
               top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
               top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
-              const float to = kBias ? top[k] : top[k] * f[k];
+              const float to = kBias ? top[k] : top[k] * f;
               // what the sums shrink by, as a power of two
               const float by = ref[k] == -INFINITY ? -INFINITY : kBias ? (ref[k] - to) * kLog2e : ref[k] - to;
               if (to != -INFINITY && -by > kGrow) {
@@ -824,7 +840,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             if (kBias)
               x = fma2(add2(x, base[k]), make_float2(kLog2e, kLog2e), add[k]);
             else
-              x = fma2(x, make_float2(f[k], f[k]), add[k]);
+              x = fma2(x, make_float2(f, f), add[k]);
             x.x = ex2_approx(x.x);
             x.y = ex2_approx(x.y);
             sum[k] = add2(sum[k], x);
@@ -870,12 +886,25 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             tmem_ld_rows32(Ot + ch * 32, v);
             tmem_wait_ld();
             settle(v);
-            if (whole) {
+            if (whole) {   // four lanes have a row's 32 columns, two of each eight: each takes eight of its own
 #pragma unroll
-              for (int e = 0; e < 4; ++e)   // (the unit first: it may be far from one, and the sum as far from it as the values are)
-                store_rows(O + g.h * os.h + 8 * (ch * 4 + e) + cl, at0, at1, q0 < nrows, q1 < nrows,
-                           make_float4(v[4 * e] * unit * inv0, v[4 * e + 1] * unit * inv0, v[4 * e + 2] * unit * inv1,
-                                       v[4 * e + 3] * unit * inv1), stt);
+              for (int k = 0; k < 2; ++k) {
+                const float inv = k ? inv1 : inv0;
+                uint32_t y[4];
+                bool bad = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {   // (the unit first: it may be far from one, and the sum as far from it as the values are)
+                  const float2 z = make_float2(v[4 * e + 2 * k] * unit * inv, v[4 * e + 2 * k + 1] * unit * inv);
+                  bad |= !(fabsf(z.x) <= kLargestBf16 && fabsf(z.y) <= kLargestBf16);
+                  const __nv_bfloat162 w = __floats2bfloat162_rn(z.x, z.y);
+                  y[e] = *(const uint32_t*)&w;
+                }
+                transpose4(y, lane);
+                if ((k ? q1 : q0) < nrows) {
+                  *(uint4*)(O + g.h * os.h + (k ? at1 : at0) + ch * 32 + 8 * (lane & 3)) = make_uint4(y[0], y[1], y[2], y[3]);
+                  if (bad) set_status(stt, ARCKV_ERR_NONFINITE);
+                }
+              }
             } else {
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
