@@ -574,3 +574,57 @@ def test_two_graphs_with_a_workspace_each_run_side_by_side():
     torch.cuda.synchronize()
     for _, want, got, ws, _, _ in graphs:
         assert torch.equal(want, got) and pk.arckv_query_status(ws) == 0
+
+
+def test_single_tokens_without_an_announced_maximum():
+    """N rows that could be one request's: the heavier path is there and finds nothing."""
+    lens = [70, 3, 300, 1000, 64, 9]
+    p, k, v, b = filled(160, lens, 2)
+    Q = queries(161, 6, 2, 4)
+    check_attend(p, k, v, b, lens, [1] * 6, Q, pk.pages_attend(p, Q, starts_of([1] * 6)))
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    p, k, v, b = filled(170, [70], 2)
+    ws = pk.pages_workspace(p, 1, 4)
+    with pytest.raises(pk.ArckvError):
+        pk.pages_attend(p, queries(1, 64, 2, 4), starts_of([64]), max_count=64, ws=ws)
+
+
+def test_pages_past_four_gigabytes():
+    """Offsets of pages and of queries' and outputs' rows past 32 bits."""
+    P, H, T = 60000, 8, 200
+    p = pk.pages_alloc(2, H, P, 256)                                 # 4.5 GB
+    p.free[:8] = torch.arange(P - 1, P - 9, -1, dtype=torch.int32, device="cuda")
+    p.n_free.fill_(8)
+    starts, slots, _ = pk.pages_extend(p, i32([T, T]), 2 * T)
+    assert int(p.table.max()) == P - 1 and int(slots.min()) > (P - 9) * 64
+    k, v = rows(180, 2 * T, H), rows(181, 2 * T, H, outliers=False)
+    pk.pages_append(p, k, v, slots)
+    K, V = pk.pages_read(p, slots, dtype=torch.float32)
+    wk, wv = ref.held_rows(host(k), host(v))
+    assert np.array_equal(host(K), wk.astype(np.float32)) and np.array_equal(host(V), wv.astype(np.float32))
+    del K, V
+    for n in (1, 30):
+        step = (1 << 31) // (2 * n)                                  # elements between rows: the last is past 2^31 bytes, and 2^32
+        base = torch.zeros(step * (2 * n - 1) + H * 4 * 128, dtype=torch.bfloat16, device="cuda")
+        Q = base.as_strided((2 * n, H, 4, 128), (step // 8 * 8, 512, 128, 1))
+        Q.copy_(queries(182, 2 * n, H, 4))
+        room = torch.zeros_like(base)
+        out = room.as_strided((2 * n, H, 4, 128), (step // 8 * 8, 512, 128, 1))
+        pk.pages_attend(p, Q, starts_of([n, n]), max_count=n, out=out)
+        check_attend(p, k, v, None, [T, T], [n, n], Q.contiguous(), out.contiguous(), heads=[0, 7])
+        del base, room, Q, out
+
+
+def test_the_serving_example():
+    import sys
+    from pathlib import Path
+    sys.path.insert(0, str(Path(__file__).resolve().parent.parent / "examples"))
+    import serve_4bit
+    f = serve_4bit.main(["--requests", "5", "--longest", "700", "--chunk", "128", "--steps", "24"])
+    assert f["pages_free_after"] == f["pages"] and 0 < f["pages_used"] <= f["pages"] and f["tokens"] > f["length"] > 0
+    # values of a standard deviation of one in steps of their range / 15, about 5.4 / 15, are off by 5.4 / 15 / sqrt(12) = 0.10;
+    # keys, in groups of 32, by 4.1 / 15 / sqrt(12) = 0.08, which moves logits of that size by 0.08 and weights alike: with
+    # independent errors 0.13 of the outputs' size; twice that is never reached
+    assert f["error"] < 0.26
