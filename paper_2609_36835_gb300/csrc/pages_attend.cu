@@ -69,11 +69,6 @@ __device__ __forceinline__ void mma_bf16_zero(float (&d)[4], uint32_t a0, uint32
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %4, %5}, {%6, %7}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
-}
 // Two fp32 operations an instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;
@@ -133,6 +128,11 @@ struct Run {
   int s, h;
   int blk, n;             // pages blk .. blk + n - 1 of the request
   int first, last;        // the CTAs that share the item
+};
+// A run with what its request is, as the producer hands it to the consumers; n < 0 behind the last one.
+struct RunInfo {
+  Run p;
+  int row, count, len;    // first row in the packed call, rows, tokens
 };
 
 // The runs of a CTA, in order.  Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request
@@ -198,6 +198,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   int* pre = (int*)(sQ + 2 * kR * 128);                          // [S + 1]
   __shared__ __align__(8) uint64_t full[kSt], empty[kSt], fullQ[2], emptyQ[2];
   __shared__ int sHeld[kSt];                                     // whether the stage has a page
+  __shared__ RunInfo sRun[2];                                    // by parity of the run, with its queries
   __shared__ float sM[kW][8], sL[kW][8];
   __shared__ int abort_flag, last_flag, stop_flag, s_cut;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -317,16 +318,27 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
             settle();
           }
         } else if (run < 2 || mbar_ended(&emptyQ[run & 1], ((run >> 1) - 1) & 1)) {
-          int first;
-          const int buf = run & 1, nrows = rows_of(p.s, first) * d.G;
-          tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
-          for (int r = 0; r < nrows; ++r) {
-            const int k = r / d.G;
-            tc::bulk_load(sQ + (buf * kR + r) * 128, Q + (first + k) * qs.i + p.h * qs.h + (r - k * d.G) * 128, 256, &fullQ[buf]);
+          const int buf = run & 1;
+          RunInfo info;
+          info.p = p;
+          if (p.n >= 0) {
+            info.count = rows_of(p.s, info.row);
+            info.len = pages_len(c, p.s);
+            const int nrows = info.count * d.G;
+            sRun[buf] = info;
+            tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
+            for (int r = 0; r < nrows; ++r) {
+              const int k = r / d.G;
+              tc::bulk_load(sQ + (buf * kR + r) * 128, Q + (info.row + k) * qs.i + p.h * qs.h + (r - k * d.G) * 128, 256, &fullQ[buf]);
+            }
+            if (!walk.next(p)) p.n = -1;
+          } else {   // no more runs
+            sRun[buf].p.n = -1;
+            tc::mbar_arrive(&fullQ[buf]);
+            left = false;
           }
           moved = true;
           ++run;
-          left = walk.next(p);
         }
       }
       if (__any_sync(0xffffffffu, moved)) {
@@ -362,9 +374,19 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
   int base = 0, run = 0;         // pages of earlier runs, and their number
   bool ok = true;
-  for (Run p; walk.next(p); ++run) {
-    int first;
-    const int n = p.n, len = pages_len(c, p.s), h = p.h, count = rows_of(p.s, first), nrows = count * d.G;
+  for (;; ++run) {
+    RunInfo info = {};
+    if (walk.parts) {   // a CTA's only run
+      if (!walk.next(info.p)) break;
+      info.len = pages_len(c, info.p.s);
+      info.count = rows_of(info.p.s, info.row);
+    } else {
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
+      if (ok) info = sRun[run & 1];   // (else nothing, up to the barrier at which all warps learn of it)
+      if (info.p.n < 0) break;
+    }
+    const Run& p = info.p;
+    const int n = p.n, len = info.len, h = p.h, first = info.row, count = info.count, nrows = count * d.G;
     // query rows: column n is row n of the tile
     uint32_t qf[8][2];
     // what a token's least values multiply beside the codes' sums: the sum of a group's elements as two bf16, row g, group t, and
@@ -372,7 +394,6 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     uint32_t q_sum[2];
     float fac[2];                         // 2^e scale (log2 e) of rows 2t, 2t + 1
     int see[2], see_min;                  // tokens that they see
-    if (!walk.parts) ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
     {
       const int r = tile0 + g, i = r / d.G;
       // Queries of a CTA's only run are read here, beside its first copies; of several runs, they have come to shared memory
