@@ -33,6 +33,8 @@ constexpr int kRowsMax = 16;                 // rows of a head in this kernel
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 constexpr float kGrow = 8.f, kLift = 7.f;    // weights reach 2^15: the range of f16
 
+constexpr int kKnown = 1024;                 // requests whose rows and lengths every CTA keeps in shared memory
+
 struct RowsShape {
   int G, N, limit, max_count;   // limit: rows of a head that a request may have here
   bool causal;
@@ -48,8 +50,8 @@ struct RowsCfg {
   static constexpr int kTiles = kR / 8, kTeams = kW / kTiles;   // warps w and w + kTeams share pages, a tile each
   static constexpr int kSt = 16, kOwn = kSt / kTeams;           // stages of the ring, and of a team: each is consumed by one team
   static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kW * 8 * kRowO * 4 + 2 * kR * 256;
-  // the rest of it beside 4097 sums and 2 KB of fixed arrays
-  static_assert(kSmem + 4097 * 4 + 2048 <= 227 * 1024, "shared memory");
+  // the rest of it beside 4097 sums, what kKnown requests are, and 2 KB of fixed arrays
+  static_assert(kSmem + 4097 * 4 + kKnown * 12 + 2048 <= 227 * 1024, "shared memory");
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -140,6 +142,7 @@ struct RunInfo {
 struct Walk {
   const arckv_pages4& c;
   const int* pre;
+  const int* known;       // [kKnown] first row, rows, tokens
   int cta;
   bool parts;             // items are cut into equal parts
   int u, u1;              // parts: this CTA's part of all; else units (pages) of its share
@@ -162,7 +165,7 @@ struct Walk {
     p.h = rest / cut;
     const int k = rest - p.h * cut;
     if (parts) {
-      const int nb = max(1, pages_of(pages_len(c, p.s)));
+      const int nb = max(1, pages_of(p.s < kKnown ? known[3 * p.s + 2] : pages_len(c, p.s)));
       p.blk = (int)((long long)nb * k / cut);
       p.n = (int)((long long)nb * (k + 1) / cut) - p.blk;
       p.first = u - k;
@@ -195,7 +198,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   float* sBias = (float*)(ring + kSt * ARCKV_PAGE_BYTES);        // [stage][64]
   float* sO = sBias + (kBias ? kSt * kPT : 0);                                 // [warp][row of its tile][kRowO]
   bf16* sQ = (bf16*)(sO + kW * 8 * kRowO);                      // [parity of the run][row][128]
-  int* pre = (int*)(sQ + 2 * kR * 128);                          // [S + 1]
+  int* known = (int*)(sQ + 2 * kR * 128);                        // [kKnown] first row, rows, tokens of a request
+  int* pre = known + 3 * min(c.S, kKnown);                       // [S + 1]
   __shared__ __align__(8) uint64_t full[kSt], empty[kSt], fullQ[2], emptyQ[2];
   __shared__ int sHeld[kSt];                                     // whether the stage has a page
   __shared__ RunInfo sRun[2];                                    // by parity of the run, with its queries
@@ -218,20 +222,37 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   }
   pdl_trigger();
   pdl_wait();
-  // First row and number of rows of request s; none where it has more than the launch was made for.
-  auto rows_of = [&](int s, int& first) {
-    first = min(max(starts[s], 0), d.N);
-    const int n = min(max(starts[s + 1], first), d.N) - first;
+  // First row, number of rows and tokens of request s, from memory; no rows where it has more than the launch was made for.
+  auto look_up = [&](int s, int& first, int& n, int& len) {
+    const int a = starts[s], b = starts[s + 1], l = c.len[s];
+    first = min(max(a, 0), d.N);
+    n = min(max(b, first), d.N) - first;
+    len = min(max(l, 0), c.M * kPT);
     if (n > d.max_count) set_status(stt, ARCKV_ERR_SHAPE);
-    return (long long)n * d.G <= d.limit ? n : 0;
+    if ((long long)n * d.G > d.limit) n = 0;
   };
   if (warp == kW) {   // pages, or parts, before each request, by warp scan
     int cut = 0, items = 0;
     auto scan = [&] {
       int run = 0;
       for (int s0 = 0; s0 < c.S; s0 += 32) {
-        int x = 0, first;
-        if (s0 + lane < c.S && rows_of(s0 + lane, first) > 0) x = max(1, pages_of(pages_len(c, s0 + lane)));
+        const int s = s0 + lane;
+        int x = 0;
+        if (s < c.S) {
+          int first, n, len;
+          if (cut > 0 && s < kKnown) {
+            n = known[3 * s + 1];
+            len = known[3 * s + 2];
+          } else {
+            look_up(s, first, n, len);
+          }
+          if (cut == 0 && s < kKnown) {
+            known[3 * s] = first;
+            known[3 * s + 1] = n;
+            known[3 * s + 2] = len;
+          }
+          if (n > 0) x = max(1, pages_of(len));
+        }
         if (cut == 0) items += __popc(__ballot_sync(0xffffffffu, x > 0));
         if (cut > 0 && x > 0) x = max(1, min((x + cut - 1) / cut, x / kPartMin));
 #pragma unroll
@@ -256,9 +277,15 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     }
   }
   __syncthreads();
+  auto request = [&](int s, int& first, int& n, int& len) {
+    if (s >= kKnown) return look_up(s, first, n, len);
+    first = known[3 * s];
+    n = known[3 * s + 1];
+    len = known[3 * s + 2];
+  };
   const int total = pre[c.S] * c.H, ctas = min((int)gridDim.x, total), me = blockIdx.x;
   if (me >= ctas) return;
-  Walk walk{c, pre, me, s_cut > 0};
+  Walk walk{c, pre, known, me, s_cut > 0};
   walk.q = total / ctas;
   walk.r = total - walk.q * ctas;
   walk.u = walk.q * me + min(me, walk.r);
@@ -274,7 +301,12 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     Run p;
     int i = 0, base0 = 0, run = 0, issued = 0, entry = -1, held = 0;
     bool left = (feeds || asks) && walk.next(p);
-    if (left) held = pages_of(pages_len(c, p.s));
+    auto held_by = [&](int s) {
+      int first, n, len;
+      request(s, first, n, len);
+      return pages_of(len);
+    };
+    if (left) held = held_by(p.s);
     auto look = [&] {   // the table's entry of page i of the run, on its way while the one before it is waited for
       entry = p.blk + i < held ? c.table[(long long)p.s * c.M + p.blk + i] : -1;
     };
@@ -282,7 +314,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       while (left && i >= p.n) {
         base0 += p.n;
         left = walk.next(p);
-        if (left) held = pages_of(pages_len(c, p.s));
+        if (left) held = held_by(p.s);
         i = (lane + kTeams - base0 % kTeams) % kTeams;
       }
       if (left) look();
@@ -322,8 +354,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           RunInfo info;
           info.p = p;
           if (p.n >= 0) {
-            info.count = rows_of(p.s, info.row);
-            info.len = pages_len(c, p.s);
+            request(p.s, info.row, info.count, info.len);
             const int nrows = info.count * d.G;
             sRun[buf] = info;
             tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
@@ -378,8 +409,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     RunInfo info = {};
     if (walk.parts) {   // a CTA's only run
       if (!walk.next(info.p)) break;
-      info.len = pages_len(c, info.p.s);
-      info.count = rows_of(info.p.s, info.row);
+      request(info.p.s, info.row, info.count, info.len);
     } else {
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
       if (ok) info = sRun[run & 1];   // (else nothing, up to the barrier at which all warps learn of it)
@@ -720,7 +750,7 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
   d.max_count = q.max_count;
   d.causal = q.causal;
   auto kern = pages_rows_kernel<kR, kBias>;
-  const int smem = RowsCfg<kR, kBias>::kSmem + (p.S + 1) * (int)sizeof(int);
+  const int smem = RowsCfg<kR, kBias>::kSmem + (3 * std::min(p.S, kKnown) + p.S + 1) * (int)sizeof(int);
   if (set_dyn_smem((const void*)kern, smem) != cudaSuccess) return -1;
   const int ctas = std::min(tc_gemm_sm_count(), kCacheMaxCtas);
   const cudaError_t e = launch_pdl(kern, dim3(ctas), RowsCfg<kR, kBias>::kThreads, smem, st, p, d, q.Q, q.qs, scale, q.starts, q.O, q.os,
