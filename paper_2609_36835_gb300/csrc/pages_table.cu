@@ -13,7 +13,7 @@ namespace arckv {
 namespace {
 
 constexpr int kTT = 512;       // threads
-constexpr int kTRows = 2048;   // rows of a CTA
+constexpr int kTRows = 512;    // rows of a CTA, one a thread (250 requests, 16,000 rows: 4.4 us, 6.5 with 2048)
 
 // Exclusive prefix sums of x[0 .. n) in place over the block, at most `most` (sums stay below 2^62); returns the total.
 // kTT threads take n / kTT consecutive entries each.

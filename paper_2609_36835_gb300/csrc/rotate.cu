@@ -4,8 +4,8 @@
 //
 // The angle is a whole number of 2^-64 turns: pos * turns_i mod 2^64 is exact, and what is left is within half a turn
 // whatever the position, so cos and sin take no reduction and lose nothing far out.  A CTA takes a few tokens: it finds
-// their cosines and sines once, in shared memory, and turns all heads with them.  A thread's unit is 16 elements
-// (eight pairs): bound by HBM for prompts, by latency for a decode step.
+// their cosines and sines once, in shared memory, and turns all heads with them.  A thread's unit is twice 16 bytes (of the
+// layout in halves, two places of the head): bound by HBM for prompts, by latency for a decode step.
 #include "pages.cuh"
 
 namespace arckv {
@@ -21,8 +21,8 @@ struct RotateArgs {
   int N, d, r, tokens, split;   // tokens of a CTA, CTAs that share a token's heads
 };
 
-// Eight elements as fp32.
-__device__ __forceinline__ void load8(const bf16* p, float (&x)[8]) {
+// Sixteen bytes as fp32.
+__device__ __forceinline__ void load16(const bf16* p, float (&x)[8]) {
   const uint4 v = *(const uint4*)p;
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -31,25 +31,24 @@ __device__ __forceinline__ void load8(const bf16* p, float (&x)[8]) {
     x[2 * e + 1] = bf16_hi(w[e]);
   }
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = *(const float4*)p, b = *((const float4*)p + 1);
+__device__ __forceinline__ void load16(const float* p, float (&x)[4]) {
+  const float4 a = *(const float4*)p;
   x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-  x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
 }
-__device__ __forceinline__ void store8(bf16* p, const float (&x)[8]) {
+__device__ __forceinline__ void store16(bf16* p, const float (&x)[8]) {
   __nv_bfloat162 h[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
   *(uint4*)p = *(const uint4*)&h[0];
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+__device__ __forceinline__ void store16(float* p, const float (&x)[4]) {
   *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-  *((float4*)p + 1) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
 template <typename T, bool kInter>
 __global__ void __launch_bounds__(kRT) pages_rotate_kernel(const RotateArgs a, bool transpose) {
-  extern __shared__ float2 cs[];   // [token][pair] f cos, f sin
+  constexpr int kE = 16 / sizeof(T);   // elements of 16 bytes: a thread's unit is two of them, kE pairs
+  extern __shared__ float2 cs[];       // [token][pair] f cos, f sin
   const int tid = threadIdx.x, half = a.r >> 1, n0 = blockIdx.x * a.tokens, tokens = min(a.tokens, a.N - n0);
   pdl_trigger();
   pdl_wait();
@@ -62,7 +61,7 @@ __global__ void __launch_bounds__(kRT) pages_rotate_kernel(const RotateArgs a, b
     cs[x] = make_float2(a.f * c, transpose ? -a.f * s : a.f * s);
   }
   __syncthreads();
-  const int units = a.d >> 4, turned = a.r >> 4, heads = a.t[0].heads + a.t[1].heads;
+  const int units = a.d / (2 * kE), turned = a.r / (2 * kE), heads = a.t[0].heads + a.t[1].heads;
   const int h0 = (int)((long long)heads * blockIdx.y / a.split), hn = (int)((long long)heads * (blockIdx.y + 1) / a.split) - h0;
   for (int x = tid; x < tokens * hn * units; x += kRT) {
     const int u = x % units, hx = x / units, n = hx / hn;
@@ -74,24 +73,26 @@ __global__ void __launch_bounds__(kRT) pages_rotate_kernel(const RotateArgs a, b
     T* dst = (T*)t.y + (n0 + n) * t.ys.i + h * t.ys.h;
     const bool turns = u < turned && a.positions[n0 + n] >= 0;
     if (!turns && (const void*)src == (const void*)dst) continue;
-    const int at1 = !kInter && u < turned ? 8 * u : 16 * u, at2 = !kInter && u < turned ? half + 8 * u : 16 * u + 8;
-    float p[8], q[8];
-    load8(src + at1, p);
-    load8(src + at2, q);
+    const bool apart = !kInter && u < turned;
+    const int at1 = apart ? kE * u : 2 * kE * u, at2 = apart ? half + kE * u : 2 * kE * u + kE;
+    float p[kE], q[kE];
+    load16(src + at1, p);
+    load16(src + at2, q);
     if (turns) {
-      const float2* w = cs + n * half + 8 * u;
+      const float2* w = cs + n * half + kE * u;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kE; ++e) {
         const float2 z = w[e];
-        float& x1 = kInter ? (e < 4 ? p[2 * (e & 3)] : q[2 * (e & 3)]) : p[e];
-        float& x2 = kInter ? (e < 4 ? p[2 * (e & 3) + 1] : q[2 * (e & 3) + 1]) : q[e];
+        constexpr int kH = kE / 2;
+        float& x1 = kInter ? (e < kH ? p[2 * (e % kH)] : q[2 * (e % kH)]) : p[e];
+        float& x2 = kInter ? (e < kH ? p[2 * (e % kH) + 1] : q[2 * (e % kH) + 1]) : q[e];
         const float y1 = x1 * z.x - x2 * z.y, y2 = x2 * z.x + x1 * z.y;
         x1 = y1;
         x2 = y2;
       }
     }
-    store8(dst + at1, p);
-    store8(dst + at2, q);
+    store16(dst + at1, p);
+    store16(dst + at2, q);
   }
 }
 
@@ -109,9 +110,12 @@ int launch_rotate(int N, int d, int r, float f, const unsigned long long* turns,
   a.d = d;
   a.r = r;
   const int heads = t[0].heads + t[1].heads, sms = tc_gemm_sm_count();
-  a.tokens = std::max(1, std::min(4, N / (8 * sms)));
+  // Two rounds of a CTA's threads or more, while there are CTAs for every SM (8191 tokens of 40 fp32 heads: one token a CTA
+  // 51 us, two 52.5, four 55); few tokens are shared by several
+  const int units = heads * (f32 ? d >> 3 : d >> 4);
+  a.tokens = std::max(1, std::min({16, 2 * kRT / units, N / (4 * sms)}));
   const int ctas = cdiv(N, a.tokens);
-  a.split = std::max(1, std::min(cdiv((long long)a.tokens * heads * (d >> 4), kRT), 4 * sms / ctas));
+  a.split = std::max(1, std::min(cdiv((long long)a.tokens * units, kRT), 4 * sms / ctas));
   auto kern = f32 ? (interleaved ? pages_rotate_kernel<float, true> : pages_rotate_kernel<float, false>)
                   : (interleaved ? pages_rotate_kernel<bf16, true> : pages_rotate_kernel<bf16, false>);
   const int smem = a.tokens * (r / 2) * (int)sizeof(float2);
