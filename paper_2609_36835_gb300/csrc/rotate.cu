@@ -63,9 +63,11 @@ __global__ void __launch_bounds__(kRT) pages_rotate_kernel(const RotateArgs a, b
   __syncthreads();
   const int units = a.d / (2 * kE), turned = a.r / (2 * kE), heads = a.t[0].heads + a.t[1].heads;
   const int h0 = (int)((long long)heads * blockIdx.y / a.split), hn = (int)((long long)heads * (blockIdx.y + 1) / a.split) - h0;
-  for (int x = tid; x < tokens * hn * units; x += kRT) {
-    const int u = x % units, hx = x / units, n = hx / hn;
-    int h = h0 + hx - n * hn;
+  const int u = tid % units, rows = kRT / units;   // rows of heads at a time
+  for (int x = tid / units; x < tokens * hn; x += rows) {
+    if (tid >= rows * units) break;
+    const int n = tokens > 1 ? x / hn : 0;
+    int h = h0 + x - n * hn;
     const bool second = h >= a.t[0].heads;
     const RotateTensor& t = a.t[second];
     if (second) h -= a.t[0].heads;
@@ -110,10 +112,10 @@ int launch_rotate(int N, int d, int r, float f, const unsigned long long* turns,
   a.d = d;
   a.r = r;
   const int heads = t[0].heads + t[1].heads, sms = tc_gemm_sm_count();
-  // Two rounds of a CTA's threads or more, while there are CTAs for every SM (8191 tokens of 40 fp32 heads: one token a CTA
-  // 51 us, two 52.5, four 55); few tokens are shared by several
+  // Five rounds of a CTA's threads or so, while there are CTAs for every SM (8191 tokens of 40 heads: 52 us in fp32, 32 in bf16;
+  // half as many rounds 51 and 35, twice as many 55 and 35); few tokens are shared by several CTAs
   const int units = heads * (f32 ? d >> 3 : d >> 4);
-  a.tokens = std::max(1, std::min({16, 2 * kRT / units, N / (4 * sms)}));
+  a.tokens = std::max(1, std::min({16, 5 * kRT / units, N / (4 * sms)}));
   const int ctas = cdiv(N, a.tokens);
   a.split = std::max(1, std::min(cdiv((long long)a.tokens * units, kRT), 4 * sms / ctas));
   auto kern = f32 ? (interleaved ? pages_rotate_kernel<float, true> : pages_rotate_kernel<float, false>)
