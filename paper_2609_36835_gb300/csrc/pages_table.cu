@@ -6,7 +6,9 @@
 // every row.  A few hundred bytes decide everything, so each CTA does the sums
 // by itself in shared memory and fills its share of the rows from the state
 // before the call; the CTA that comes last (a ticket) then writes the new state.
-// One launch, bound by its chain of dependent loads.
+// One launch, bound by its chain of dependent loads.  Measured (CUDA graph): with
+// the truncation behind it 5.3 us for 64 requests of a token each, 8.5 for 250
+// requests and 16,000 rows.
 #include "pages.cuh"
 
 namespace arckv {

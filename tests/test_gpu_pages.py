@@ -2,14 +2,19 @@
 calls.
 
 Tables, slots and what the rows are held as are compared exactly.  An output of attention is a bf16: it is off by at most
-2^-8 of itself, half a step.  Before that, each weight p is rounded to f16 (2^-11 of it, and 2^-32 of a weight of one where
-that is below f16's normal range).  It may multiply a value's code times scale alone, c s = v - m, where m is the row's least
-value and enters with the weight as it was: with |m| <= (1 + 2^-8) max |v| that is 2^-11 p (|v| + 1.01 max |v|), and sums that
-begin 1024 codes off add 6 roundings of 2^-24 * 1024 s p, s <= 2.02 max |v| / 15, which is 2^-14 p max |v|.  Or it multiplies a
-value rounded to f16: 2^-10 p |v|.  Keys may be rounded to f16 too (2^-11 of each element, 2^-25 of the page's largest below the
-normal range), which moves a logit by up to 2^-11 scale sum |q_e k_e| and its weight by as much, relatively, and the sum of
-weights likewise.  fp32 logits and sums add less than 2^-14 of a weight.  So, with A = sum p |v| and B = sum p max |v|:
-    |O - ref| <= 2^-8 |ref| + (2^-10 + 2^-13 + 2 (2^-11 + 2^-22) scale max_j sum |q_e k_je|) A + 2^-10 B + T 2^-24 max |v|
+2^-8 of itself, half a step.  What comes before that, with M the largest magnitude of the values:
+ - Each weight p is rounded to f16: 2^-11 of it, and below f16's normal range 2^-25 of the weights' unit.  The values' unit is at
+   most 4 M, and one where their codes count 15 at most: a weight costs 2^-22 M there.
+ - It may multiply a value's code times scale alone, c s = v - m, where m is the row's least value and enters with the weight as it
+   was: with |m| <= (1 + 2^-8) max |v| that is 2^-11 p (|v| + 1.01 max |v|).  Or it multiplies a value rounded to f16: 2^-10 p |v|.
+ - Values and keys may be rounded to f16, in units that leave a page's largest below 2^-6: 2^-11 of each element, and twice 2^-25 of
+   the unit below the normal range, m's rounding and the sum's, which is 2^-17 of the page's largest.  For keys that moves a logit
+   by up to 2^-11 scale sum |q_e k_e| + 2^-17 scale sum |q_e| max |k|, its weight by as much, relatively, and the sum of weights
+   likewise.
+ - A query's sums over groups of its elements, which the keys' least values multiply, are two bf16: 2^-17 scale sum |q_e| max |k| too.
+ - fp32 logits and sums add less than 2^-14 of a weight.
+With A = sum p |v|, B = sum p max |v| and d the largest move of a logit,
+    |O - ref| <= 2^-8 |ref| + (2^-10 + 2^-13 + 2 d) A + 2^-10 B + (2^-17 + T 2^-22) M
 """
 import numpy as np
 import pytest
@@ -78,9 +83,11 @@ def check_rows(O, q, k, v, bias, sees, scale=SC):
     _, large = ref.attend(host(q), k, np.abs(v).max(1, keepdims=True), scale, sees, None if bias is None else host(bias))
     got = host(O).astype(np.float64)
     T = max(max(sees, default=0), 1)
-    moved = scale * (np.abs(host(q)).astype(np.float64) @ np.abs(k[:T]).T).max(1, initial=0.0)[:, None]
+    q, most_k = np.abs(host(q)).astype(np.float64), np.abs(k[:T]).max(initial=0.0)
+    moved = scale * (2.0 ** -11 * (q @ np.abs(k[:T]).T).max(1, initial=0.0) + 2.0 ** -16 * q.sum(1) * most_k)[:, None]
     most = np.abs(v[:T]).max(initial=0.0)
-    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -13 + 2 * (2.0 ** -11 + 2.0 ** -22) * moved) * size + 2.0 ** -10 * large + T * 2.0 ** -24 * most
+    bound = (2.0 ** -8 * np.abs(want) + (2.0 ** -10 + 2.0 ** -13 + 2 * moved) * size + 2.0 ** -10 * large
+             + (2.0 ** -17 + T * 2.0 ** -22) * most)
     empty = ~size.any(-1)
     assert not got[empty].any()
     assert np.all(np.abs(got - want) <= bound), float(np.max(np.abs(got - want) / np.maximum(bound, 1e-300)))
@@ -404,6 +411,18 @@ def test_many_requests(n):
     Q = queries(102, sum(counts), 1, 2)
     O = pk.pages_attend(p, Q, starts_of(counts), max_count=n)
     check_attend(p, k, v, b, lens, counts, Q, O, requests=[0, 1, 57, 300, 698, 699])
+
+
+def test_more_requests_than_a_block_keeps_in_shared_memory():
+    S = 1300
+    lens = torch.randint(1, 150, (S,), generator=gen(105)).tolist()
+    counts = [20 if s % 400 == 399 and lens[s] >= 20 else 1 for s in range(S)]
+    p, k, v, b = filled(106, lens, 1)
+    Q = queries(107, sum(counts), 1, 4)
+    listed = [0, 399, 799, 1023, 1024, 1025, 1199, 1299]
+    check_attend(p, k, v, b, lens, counts, Q, pk.pages_attend(p, Q, starts_of(counts), max_count=20), requests=listed)
+    Q = queries(108, S, 1, 4)
+    check_attend(p, k, v, b, lens, [1] * S, Q, pk.pages_attend(p, Q, starts_of([1] * S), max_count=1), requests=listed)
 
 
 @pytest.mark.parametrize("n", [1, 3, 64])
