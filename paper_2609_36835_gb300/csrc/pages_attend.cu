@@ -16,18 +16,18 @@
 //    scaled and added up afterwards; the least values multiply the sums of the query's elements (one more product, of the
 //    words as they are).  A value's scale goes into its weight, its least value times the weight into a sum of its own that
 //    all dims share.
-//  - Work is the list of (request, head, page): with more items than SMs each CTA takes an equal share of it; with fewer,
-//    items are cut into equal parts, a CTA each.  An item in several CTAs is finished by the one that comes last (a
-//    ticket), which adds the parts up in CTA order.  Consumer warps take whole pages in turn, each with its own
-//    running maximum, sum and output.
+//  - Work is the list of (request, head, page).  With more items than SMs each warp (or pair of warps) of the launch takes an
+//    equal share of it, and waits for no other: what it has of an item at the ends of its share goes to memory as it lies in
+//    registers.  (Shares for CTAs, whose warps then add up every item: 94 us instead of 81 for 64 x 8K, 102 instead of 55 for 250
+//    requests of up to 1000 tokens.)  With fewer items they are cut into equal parts, a CTA each, whose warps take pages in
+//    turn.  An item in several places is finished by the one that comes last (a ticket), which adds the parts up in order.
 //  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
 //    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
 //    without limit from page to page: the output is then scaled down, as for a maximum that grows.
 //
-// Bound by the warps: a page is 863 instructions a tile of 8 rows, 320 of them the shifts and masks, and two warps a quarter do
-// not hide all of each other's latencies (38 % of the issue slots, ALU 30 %).  Measured (CUDA graph), 4 rows: 64 ragged requests
-// x 8 heads of up to 8192 tokens 94 us, 5.0 TB/s (copies alone 74, with every page in L2 89); one of 131,072 tokens 35 us,
-// 4.4 TB/s.  12 rows with biases, 64 x 8 x 1641: 64 us.
+// Bound by HBM and by the warps at once: a page is 860 instructions a tile of 8 rows, 320 of them the shifts and masks.
+// Measured (CUDA graph), 4 rows: 64 ragged requests x 8 heads of up to 8192 tokens 81 us, 5.8 TB/s (copies alone 74); one
+// of 131,072 tokens 35 us, 4.4 TB/s.  12 rows with biases, 64 x 8 x 1641: 49 us.
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -38,23 +38,29 @@ constexpr int kRowsMax = 16;                 // rows of a head in this kernel
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 constexpr float kGrow = 8.f, kLift = 7.f;    // weights reach 2^15: the range of f16
 
-constexpr int kKnown = 1024;                 // requests whose rows and lengths every CTA keeps in shared memory
+constexpr int kWarpsMost = 11;               // consumer warps of a CTA
+constexpr int kKnown = 256;                  // requests whose rows and lengths every CTA keeps in shared memory
+constexpr int kTeamSlot = 9 * 32 * 4;        // floats of a tile's partial result in registers' order: 32 outputs a lane, two (m, l)
 
 struct RowsShape {
   int G, N, limit, max_count;   // limit: rows of a head that a request may have here
   bool causal;
 };
 
-// Eight consumer warps, two on each quarter of the SM, and a producer: up to 12 warps may have 168 registers each.  (Measured
-// with 4, 7, 9 and 11 consumers for 64 x 8K decode: 114, 104, 104 and 112 us, 100 with 8.)
-// A warp has a tile of 8 rows; with up to 16, pairs of warps share pages.  (One warp with both tiles: 72 us for 12 rows with
-// biases over 64 x 8 x 1641.)
+// Ten or eleven consumer warps and a producer, three to each quarter of the SM: up to 12 warps may have 168 registers each, and
+// shared memory is full.  (With 8, 9 and 10 consumers, 250 requests of up to 1000 tokens: 57.5, 57.6 and 55.5 us, 54.8 with 11;
+// 16 rows, 64 x 8K: 145 us with 8, 136 with 10.)
+// A warp has a tile of 8 rows; with up to 16, pairs of warps share pages.
 template <int kR, bool kBias>
 struct RowsCfg {
-  static constexpr int kW = 8, kThreads = 32 * (kW + 1);
+  static constexpr int kW = kR == 8 && !kBias ? kWarpsMost : 10, kThreads = 32 * (kW + 1);
   static constexpr int kTiles = kR / 8, kTeams = kW / kTiles;   // warps w and w + kTeams share pages, a tile each
-  static constexpr int kSt = 16, kOwn = kSt / kTeams;           // stages of the ring, and of a team: each is consumed by one team
-  static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kW * 8 * kRowO * 4 + 2 * kR * 256;
+  static constexpr int kOwn = kTiles == 1 ? 2 : 3, kSt = kTeams * kOwn;   // stages of a team, each consumed by it alone, and of the ring
+  // a warp's part of a CTA's item goes to shared memory where its pages were, if they were its alone
+  static constexpr int kSmemO = kTiles == 1 ? 0 : kW * 8 * kRowO * 4;
+  static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kSmemO;
+  static_assert(kTiles > 1 || 8 * kRowO * 4 <= ARCKV_PAGE_BYTES, "a part of an item fits a stage");
+  static_assert(sizeof(DevStatus) + kCacheMaxCtas * kW * 2 <= ARCKV_CACHE_WS_HEADER && kW <= kWarpsMost, "a ticket for each warp");
   // the rest of it beside 4097 sums, what kKnown requests are, and 2 KB of fixed arrays
   static_assert(kSmem + 4097 * 4 + kKnown * 12 + 2048 <= 227 * 1024, "shared memory");
 };
@@ -130,29 +136,34 @@ __device__ __forceinline__ bool mbar_ended(uint64_t* bar, uint32_t parity) {
 }
 __device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
-// A CTA's run of pages of one item.
+// A run of pages of one item.
 struct Run {
   int s, h;
   int blk, n;             // pages blk .. blk + n - 1 of the request
-  int first, last;        // the CTAs that share the item
-};
-// A run with what its request is, as the producer hands it to the consumers; n < 0 behind the last one.
-struct RunInfo {
-  Run p;
-  int row, count, len;    // first row in the packed call, rows, tokens
+  int first, last;        // the takers that share the item
 };
 
-// The runs of a CTA, in order.  Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request
-// s of one head.
+// The runs of a taker, in order: a CTA, which has one part of an item, or a team of a CTA, which has a share of all pages.
+// Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request s of one head.
 struct Walk {
   const arckv_pages4& c;
   const int* pre;
   const int* known;       // [kKnown] first row, rows, tokens
-  int cta;
   bool parts;             // items are cut into equal parts
+  int id;                 // of the taker
   int u, u1;              // parts: this CTA's part of all; else units (pages) of its share
-  int q, r;               // shares: q units each, one more for the first r CTAs
+  int q, r;               // shares: q units each, one more for the first r takers
 
+  __device__ Walk(const arckv_pages4& c, const int* pre, const int* known, bool parts, int id, int takers)
+      : c(c), pre(pre), known(known), parts(parts), id(id) {
+    const int total = pre[c.S] * c.H;
+    // a page a taker, or shares of two at least (64 x 300 tokens: 13.5 us, 14.6 with shares of one and two)
+    const int n = max(1, total <= takers ? total : min(takers, total - total / 2));
+    q = total / n;
+    r = total - q * n;
+    u = id < n ? q * id + min(id, r) : total;
+    u1 = id < n ? q * (id + 1) + min(id + 1, r) : total;
+  }
   __device__ int owner(int unit) const {
     const int big = r * (q + 1);
     return unit < big ? unit / (q + 1) : r + (unit - big) / q;
@@ -180,7 +191,7 @@ struct Walk {
     }
     p.blk = k;
     p.n = min(cut - k, u1 - u);
-    p.first = p.last = cta;
+    p.first = p.last = id;
     if (p.n < cut) {
       p.first = owner(u - k);
       p.last = owner(u - k + cut - 1);
@@ -201,13 +212,11 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   extern __shared__ __align__(128) unsigned char smraw[];
   unsigned char* ring = smraw;                                   // [stage][page]
   float* sBias = (float*)(ring + kSt * ARCKV_PAGE_BYTES);        // [stage][64]
-  float* sO = sBias + (kBias ? kSt * kPT : 0);                                 // [warp][row of its tile][kRowO]
-  bf16* sQ = (bf16*)(sO + kW * 8 * kRowO);                      // [parity of the run][row][128]
-  int* known = (int*)(sQ + 2 * kR * 128);                        // [kKnown] first row, rows, tokens of a request
+  float* sO = sBias + (kBias ? kSt * kPT : 0);                   // where warps do not have stages of their own: their parts of an item
+  int* known = (int*)((char*)sO + Cfg::kSmemO);                  // [kKnown] first row, rows, tokens of a request
   int* pre = known + 3 * min(c.S, kKnown);                       // [S + 1]
-  __shared__ __align__(8) uint64_t full[kSt], empty[kSt], fullQ[2], emptyQ[2];
+  __shared__ __align__(8) uint64_t full[kSt], empty[kSt];
   __shared__ int sHeld[kSt];                                     // whether the stage has a page
-  __shared__ RunInfo sRun[2];                                    // by parity of the run, with its queries
   __shared__ float sM[kW][8], sL[kW][8];
   __shared__ int abort_flag, last_flag, stop_flag, s_cut;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -217,10 +226,6 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     for (int s = 0; s < kSt; ++s) {
       tc::mbar_init(&full[s], 1);
       tc::mbar_init(&empty[s], Cfg::kTiles);
-    }
-    for (int i = 0; i < 2; ++i) {
-      tc::mbar_init(&fullQ[i], 1);
-      tc::mbar_init(&emptyQ[i], kW);
     }
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -288,93 +293,65 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     n = known[3 * s + 1];
     len = known[3 * s + 2];
   };
-  const int total = pre[c.S] * c.H, ctas = min((int)gridDim.x, total), me = blockIdx.x;
-  if (me >= ctas) return;
-  Walk walk{c, pre, known, me, s_cut > 0};
-  walk.q = total / ctas;
-  walk.r = total - walk.q * ctas;
-  walk.u = walk.q * me + min(me, walk.r);
-  walk.u1 = walk.q * (me + 1) + min(me + 1, walk.r);
+  const bool parts_mode = s_cut > 0;
+  // Teams of the launch are numbered over CTAs first, so that few of them are spread over the SMs.
+  auto walk_of = [&](int team) {
+    return Walk(c, pre, known, parts_mode, parts_mode ? (int)blockIdx.x : team * (int)gridDim.x + (int)blockIdx.x,
+                (int)gridDim.x * (parts_mode ? 1 : kTeams));
+  };
 
   if (warp == kW) {
     // ------------------------------------------------------------- producer
     // Lane w fills the stages of team w as that gives them back, each lane at its own pace (in one order for all, the
-    // slowest warp held up the others' pages: 104 us instead of 97 for 64 x 8K); lane 31 brings the queries of the runs, two
-    // ahead.
-    const bool feeds = lane < kTeams, asks = lane == 31 && !walk.parts;
+    // slowest warp held up the others' pages: 104 us instead of 97 for 64 x 8K).
+    const bool feeds = lane < kTeams;
     constexpr int kOwn = Cfg::kOwn;
+    Walk walk = walk_of(min(lane, kTeams - 1));
     Run p;
-    int i = 0, base0 = 0, run = 0, issued = 0, entry = -1, held = 0;
-    bool left = (feeds || asks) && walk.next(p);
-    auto held_by = [&](int s) {
+    int i = 0, issued = 0, entry = -1, held = 0;
+    const int step = parts_mode ? kTeams : 1;   // the teams of a CTA with a part take its pages in turn
+    auto begin = [&] {
+      if (!walk.next(p)) return false;
       int first, n, len;
-      request(s, first, n, len);
-      return pages_of(len);
+      request(p.s, first, n, len);
+      held = pages_of(len);
+      return true;
     };
-    if (left) held = held_by(p.s);
-    auto look = [&] {   // the table's entry of page i of the run, on its way while the one before it is waited for
-      entry = p.blk + i < held ? c.table[(long long)p.s * c.M + p.blk + i] : -1;
-    };
+    bool left = feeds && begin();
     auto settle = [&] {   // from page i on, the next one of this lane's team
       while (left && i >= p.n) {
-        base0 += p.n;
-        left = walk.next(p);
-        if (left) held = held_by(p.s);
-        i = (lane + kTeams - base0 % kTeams) % kTeams;
+        left = begin();
+        i = 0;
       }
-      if (left) look();
+      // the table's entry, on its way while the page before it is waited for
+      if (left) entry = p.blk + i < held ? c.table[(long long)p.s * c.M + p.blk + i] : -1;
     };
-    if (feeds && left) {
-      i = lane;
-      settle();
-    }
+    if (parts_mode) i = lane;
+    settle();
     unsigned long long since = tc::globaltimer();
     uint32_t spins = 0;
     while (__any_sync(0xffffffffu, left)) {
       bool moved = false;
       if (left) {
-        if (feeds) {
-          const int q = base0 + i, st = q % kSt;
-          if (issued < kOwn || mbar_ended(&empty[st], ((q / kSt) - 1) & 1)) {
-            if (entry >= c.P) {
-              set_status(stt, ARCKV_ERR_INVALID_ARG);
-              entry = -1;
-            }
-            sHeld[st] = entry >= 0;
-            if (entry >= 0) {
-              const long long at = (long long)entry * c.H + p.h;
-              tc::mbar_arrive_expect_tx(&full[st], ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
-              tc::bulk_load(ring + st * ARCKV_PAGE_BYTES, c.data + at * ARCKV_PAGE_BYTES, ARCKV_PAGE_BYTES, &full[st]);
-              if (kBias) tc::bulk_load(sBias + st * kPT, c.bias + at * kPT, kPT * 4, &full[st]);
-            } else {
-              tc::mbar_arrive(&full[st]);
-            }
-            moved = true;
-            ++issued;
-            i += kTeams;
-            settle();
+        const int st = lane + kTeams * (issued % kOwn);
+        if (issued < kOwn || mbar_ended(&empty[st], (issued / kOwn - 1) & 1)) {
+          if (entry >= c.P) {
+            set_status(stt, ARCKV_ERR_INVALID_ARG);
+            entry = -1;
           }
-        } else if (run < 2 || mbar_ended(&emptyQ[run & 1], ((run >> 1) - 1) & 1)) {
-          const int buf = run & 1;
-          RunInfo info;
-          info.p = p;
-          if (p.n >= 0) {
-            request(p.s, info.row, info.count, info.len);
-            const int nrows = info.count * d.G;
-            sRun[buf] = info;
-            tc::mbar_arrive_expect_tx(&fullQ[buf], 256 * nrows);
-            for (int r = 0; r < nrows; ++r) {
-              const int k = r / d.G;
-              tc::bulk_load(sQ + (buf * kR + r) * 128, Q + (info.row + k) * qs.i + p.h * qs.h + (r - k * d.G) * 128, 256, &fullQ[buf]);
-            }
-            if (!walk.next(p)) p.n = -1;
-          } else {   // no more runs
-            sRun[buf].p.n = -1;
-            tc::mbar_arrive(&fullQ[buf]);
-            left = false;
+          sHeld[st] = entry >= 0;
+          if (entry >= 0) {
+            const long long at = (long long)entry * c.H + p.h;
+            tc::mbar_arrive_expect_tx(&full[st], ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
+            tc::bulk_load(ring + st * ARCKV_PAGE_BYTES, c.data + at * ARCKV_PAGE_BYTES, ARCKV_PAGE_BYTES, &full[st]);
+            if (kBias) tc::bulk_load(sBias + st * kPT, c.bias + at * kPT, kPT * 4, &full[st]);
+          } else {
+            tc::mbar_arrive(&full[st]);
           }
           moved = true;
-          ++run;
+          ++issued;
+          i += step;
+          settle();
         }
       }
       if (__any_sync(0xffffffffu, moved)) {
@@ -396,11 +373,6 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           const int n = (issued + kOwn - 1 - k) / kOwn;   // pages that stage k of this team's got
           if (n > 0) tc::mbar_wait(&full[lane + k * kTeams], (n - 1) & 1, &never, stt);
         }
-      if (asks)
-        for (int k = 0; k < 2; ++k) {
-          const int n = (run + 1 - k) / 2;
-          if (n > 0) tc::mbar_wait(&fullQ[k], (n - 1) & 1, &never, stt);
-        }
     }
     return;
   }
@@ -408,20 +380,15 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   // --------------------------------------------------------------- consumers
   const int g = lane >> 2, t = lane & 3;
   const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
-  int base = 0, run = 0;         // pages of earlier runs, and their number
+  const int step = parts_mode ? kTeams : 1;
+  Walk walk = walk_of(team);
+  int taken = 0;                 // pages so far
   bool ok = true;
-  for (;; ++run) {
-    RunInfo info = {};
-    if (walk.parts) {   // a CTA's only run
-      if (!walk.next(info.p)) break;
-      request(info.p.s, info.row, info.count, info.len);
-    } else {
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(&fullQ[run & 1], (run >> 1) & 1, abortp, stt));
-      if (ok) info = sRun[run & 1];   // (else nothing, up to the barrier at which all warps learn of it)
-      if (info.p.n < 0) break;
-    }
-    const Run& p = info.p;
-    const int n = p.n, len = info.len, h = p.h, first = info.row, count = info.count, nrows = count * d.G;
+  Run p;
+  while (ok && walk.next(p)) {
+    int first, count, len;
+    request(p.s, first, count, len);
+    const int n = p.n, h = p.h, nrows = count * d.G;
     // query rows: column n is row n of the tile
     uint32_t qf[8][2];
     // what a token's least values multiply beside the codes' sums: the sum of a group's elements as two bf16, row g, group t, and
@@ -431,8 +398,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     int see[2], see_min;                  // tokens that they see
     {
       const int r = tile0 + g, i = r / d.G;
-      // Queries of a CTA's only run are read here, beside its first copies; of several runs, they have come to shared memory
-      const bf16* mine = walk.parts ? Q + (first + i) * qs.i + h * qs.h + (r - i * d.G) * 128 : sQ + ((run & 1) * kR + r) * 128;
+      const bf16* mine = Q + (first + i) * qs.i + h * qs.h + (r - i * d.G) * 128;
       uint4 x[4];
       float amax = 0.f;
 #pragma unroll
@@ -477,8 +443,6 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       }
       see_min = __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff);
     }
-    __syncwarp();
-    if (!walk.parts && lane == 0) tc::mbar_arrive(&emptyQ[run & 1]);
     float o[8][4], mx[2], l[2], low[2];   // low: sums of weights times least values
     float v_ref = 0.f;                         // unit of o: a power of two
 #pragma unroll
@@ -490,12 +454,11 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       mx[k] = -INFINITY;
       l[k] = low[k] = 0.f;
     }
-    // page base + i of the CTA belongs to team (base + i) % kTeams
-    for (int i = (team - base % kTeams + kTeams) % kTeams; i < n && ok; i += kTeams) {
-      const int q = base + i, st = q % kSt, j0 = (p.blk + i) * kPT;   // first token of the page
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[st], (q / kSt) & 1, abortp, stt));
+    for (int i = parts_mode ? team : 0; i < n && ok; i += step, ++taken) {
+      const int st = team + kTeams * (taken % Cfg::kOwn), j0 = (p.blk + i) * kPT;   // first token of the page
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[st], (taken / Cfg::kOwn) & 1, abortp, stt));
       if (!ok) break;
-      if (sHeld[st]) {
+      if (sHeld[st] && tile0 < nrows) {
         const unsigned char* page = ring + st * ARCKV_PAGE_BYTES;
         // ---- S^T = K Q^T: lane (g, t) has tokens g, g + 8 of 16, and eight dims of each group
         float s[4][4];
@@ -652,15 +615,108 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&empty[st]);
     }
-    base += n;
-    // ---- the item's end (or this CTA's part of it): add the warps up
+    // ---- the run's end
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int w = 4; w < 32; w <<= 1) {
         l[k] += __shfl_xor_sync(0xffffffffu, l[k], w);
         low[k] += __shfl_xor_sync(0xffffffffu, low[k], w);
       }
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int f = 0; f < 4; ++f)   // dims 16 x + g are of low nibbles, those 8 on of high ones
+        o[x][f] = fmaf(o[x][f] * (f >> 1 ? 0x1p20f : 0x1p24f), v_ref, low[f & 1]);
+    const bool whole = p.first == p.last;
+    auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
+      return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
+    };
+    constexpr float kBig = 3.3895313892515355e38f;   // (the largest bf16)
+    if (!parts_mode) {   // a share's run: the warp's own affair
+      if (!ok) break;    // a wait gave up: write nothing
+      const int tile = tile0 / 8;
+      const bool mine = tile0 + 2 * t < nrows;   // (rows 2t, 2t + 1 of the tile)
+      if (!whole) {
+        // slot 2c holds the item that team c went on with, 2c + 1 the one it began
+        auto slot_of = [&](int team, bool began) {
+          return (float4*)(parts + ((2ll * team + began) * Cfg::kTiles + tile) * kTeamSlot) + lane;
+        };
+        float4* slot = slot_of(walk.id, p.blk == 0);
+        if (mine) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x) __stcg(slot + 32 * x, make_float4(o[x][0], o[x][1], o[x][2], o[x][3]));
+          __stcg(slot + 32 * 8, make_float4(mx[0], mx[1], l[0], l[1]));
+        }
+        __syncwarp();
+        int last = 0;
+        if (lane == 0) {   // the warp's results before the ticket, the others' after it; tickets are halves of words
+          const int at = p.first * Cfg::kTiles + tile, shift = 16 * (at & 1);
+          unsigned int* word = (unsigned int*)tickets + (at >> 1);
+          unsigned int old;
+          asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(old) : "l"(word), "r"(1u << shift) : "memory");
+          last = (int)((old >> shift) & 0xffffu) == p.last - p.first;
+          if (last) atomicSub(word, (unsigned int)(p.last - p.first + 1) << shift);
+        }
+        if (!__shfl_sync(0xffffffffu, last, 0)) continue;
+        __syncwarp();
+        if (mine) {
+          float up[2] = {-INFINITY, -INFINITY};   // with a running maximum, so that a part's loads wait for nothing
+          l[0] = l[1] = 0.f;
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) o[x][f] = 0.f;
+#pragma unroll 1
+          for (int cc = p.first; cc <= p.last; ++cc) {
+            const float4* from = slot_of(cc, cc == p.first);
+            float4 y[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) y[x] = __ldcg(from + 32 * x);
+            const float4 ml = __ldcg(from + 32 * 8);
+            const float m0 = fmaxf(up[0], ml.x), m1 = fmaxf(up[1], ml.y);
+            const float f0 = weight(up[0], m0), f1 = weight(up[1], m1), b0 = weight(ml.x, m0), b1 = weight(ml.y, m1);
+            up[0] = m0;
+            up[1] = m1;
+            l[0] = fmaf(l[0], f0, ml.z * b0);
+            l[1] = fmaf(l[1], f1, ml.w * b1);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              o[x][0] = fmaf(o[x][0], f0, y[x].x * b0);
+              o[x][1] = fmaf(o[x][1], f1, y[x].y * b1);
+              o[x][2] = fmaf(o[x][2], f0, y[x].z * b0);
+              o[x][3] = fmaf(o[x][3], f1, y[x].w * b1);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int r = tile0 + 2 * t + k;
+        if (r >= nrows) continue;
+        const int i = r / d.G;
+        bf16* to = O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + g;
+        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
+        bool fine = true;
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const float v = o[x][2 * z + k] * inv;
+            to[16 * x + 8 * z] = __float2bfloat16_rn(v);
+            fine &= fabsf(v) <= kBig;
+          }
+        if (!fine) set_status(stt, ARCKV_ERR_NONFINITE);
+      }
+      continue;
+    }
+    // a part of an item: add the CTA's warps up
+    auto out_of = [&](int w, int r) {   // row r of warp w's tile
+      return (Cfg::kTiles == 1 ? (float*)(ring + w * ARCKV_PAGE_BYTES) : sO + w * 8 * kRowO) + r * kRowO;
+    };
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
       const int r = 2 * t + k;
       if (g == 0) {
         sM[warp][r] = mx[k];
@@ -669,16 +725,11 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 #pragma unroll
       for (int x = 0; x < 8; ++x)
 #pragma unroll
-        for (int z = 0; z < 2; ++z)   // dims 16 x + g are of low nibbles, those 8 on of high ones
-          sO[(warp * 8 + r) * kRowO + 16 * x + 8 * z + g] = fmaf(o[x][2 * z + k] * (z ? 0x1p20f : 0x1p24f), v_ref, low[k]);
+        for (int z = 0; z < 2; ++z) out_of(warp, r)[16 * x + 8 * z + g] = o[x][2 * z + k];
     }
     if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
     bar_consumers(kW * 32);
     if (stop_flag) break;   // a wait gave up: write nothing
-    const bool whole = p.first == p.last;
-    auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
-      return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
-    };
     auto store = [&](int r, int dim, float4 v, float z) {
       const float inv = z == 0.f ? 0.f : 1.f / z;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
@@ -686,8 +737,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       const int i = r / d.G;
       __nv_bfloat162 y[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
       *(uint2*)(O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + dim) = *(const uint2*)&y[0];
-      const float big = 3.3895313892515355e38f;   // (the largest bf16)
-      if (!(fabsf(v.x) <= big && fabsf(v.y) <= big && fabsf(v.z) <= big && fabsf(v.w) <= big))
+      if (!(fabsf(v.x) <= kBig && fabsf(v.y) <= kBig && fabsf(v.z) <= kBig && fabsf(v.w) <= kBig))
         set_status(stt, ARCKV_ERR_NONFINITE);
     };
     // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
@@ -696,12 +746,14 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       const int r = x >> 5, dim = (x & 31) * 4, w0 = r / 8 * kTeams, rr = r & 7;
       float up = -INFINITY, z = 0.f;
 #pragma unroll
-      for (int w = 0; w < kTeams; ++w) up = fmaxf(up, sM[w0 + w][rr]);
+      for (int w = 0; w < kTeams; ++w)
+        if (w < n) up = fmaxf(up, sM[w0 + w][rr]);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kTeams; ++w) {
+        if (w >= n) break;   // (these warps had no page)
         const float f = weight(sM[w0 + w][rr], up);
-        const float4 y = *(const float4*)(sO + ((w0 + w) * 8 + rr) * kRowO + dim);
+        const float4 y = *(const float4*)(out_of(w0 + w, rr) + dim);
         z = fmaf(sL[w0 + w][rr], f, z);
         v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
       }
@@ -742,7 +794,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         }
       }
     }
-    bar_consumers(kW * 32);   // sO, sM, sL are free
+    break;   // (the only one)
   }
 }
 
@@ -766,7 +818,8 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
 }  // namespace
 
 size_t pages_attend_scratch(int, int, int, int max_count, int G) {
-  const size_t rows = (size_t)2 * kCacheMaxCtas * kRowsMax * 132 * sizeof(float);
+  // partial results of CTAs, or of eight warps of each
+  const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(kRowsMax * 132, kWarpsMost * kTeamSlot) * sizeof(float);
   return (long long)max_count * G > kRowsMax ? std::max(rows, pages_tiles_scratch((long long)max_count * G)) : rows;
 }
 

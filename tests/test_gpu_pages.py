@@ -434,6 +434,41 @@ def test_a_long_request(n):
     check_attend(p, k, v, b, [T, 5], [n, 1], Q, O, heads=[1])
 
 
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("G", [2, 3, 5])
+def test_a_long_request_among_many_short_ones(G, bias):
+    """Shares of all pages: a request's end, the next ones' whole and another's beginning; rows of both tiles or of one."""
+    S, H = 60, 4
+    lens = torch.randint(0, 200, (S,), generator=gen(112)).tolist()
+    lens[0], lens[20], lens[21], lens[59] = 65, 30000, 6000, 4097
+    counts = [min(T, 1 + s % 3) if s % 7 else 1 for s, T in enumerate(lens)]
+    p, k, v, b = filled(113, lens, H, bias)
+    Q = queries(114, sum(counts), H, G)
+    ws = pk.pages_workspace(p, 3, G)
+    for causal in (True, False):
+        O = pk.pages_attend(p, Q, starts_of(counts), max_count=3, causal=causal, ws=ws)
+        check_attend(p, k, v, b, lens, counts, Q, O, causal, heads=[0, 3])
+    again = [pk.pages_attend(p, Q, starts_of(counts), max_count=3, ws=ws) for _ in range(8)]
+    assert all(torch.equal(x, again[0]) for x in again)
+
+
+def test_missing_pages_of_many_requests():
+    S, H, T = 50, 4, 700
+    p, k, v, b = filled(115, [T] * S, H)
+    Q = queries(116, S, H, 4)
+    gone = torch.arange(S, device="cuda") % 2 == 0
+    p.table[gone, 2:5] = -1
+    p.table[1, 3] = p.data.shape[0]
+    starts, ws = starts_of([1] * S), pk.pages_workspace(p, 1, 4)
+    O = pk.pages_attend(p, Q, starts, max_count=1, ws=ws, check=False)
+    assert pk.arckv_query_status(ws) == 1
+    for s in (0, 1, 2, 49):
+        out = range(2, 5) if s % 2 == 0 else [3] if s == 1 else []
+        held = [j for j in range(T) if j // 64 not in out]
+        kk, vv = k[s * T:(s + 1) * T, 3][held], v[s * T:(s + 1) * T, 3][held]
+        check_rows(O[s, 3], Q[s, 3], kk, vv, None, [len(held)] * 4)
+
+
 def test_another_scale():
     p, k, v, b = filled(120, [90], 1)
     Q = queries(121, 1, 1, 4)
