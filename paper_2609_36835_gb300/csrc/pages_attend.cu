@@ -16,18 +16,19 @@
 //    scaled and added up afterwards; the least values multiply the sums of the query's elements (one more product, of the
 //    words as they are).  A value's scale goes into its weight, its least value times the weight into a sum of its own that
 //    all dims share.
-//  - Work is the list of (request, head, page).  With more items than SMs each warp (or pair of warps) of the launch takes an
-//    equal share of it, and waits for no other: what it has of an item at the ends of its share goes to memory as it lies in
-//    registers.  (Shares for CTAs, whose warps then add up every item: 94 us instead of 81 for 64 x 8K, 102 instead of 55 for 250
+//  - Work is the list of (request, head, page).  With more items than SMs each warp of the launch takes an equal share of it,
+//    and waits for no other: what it has of an item at the ends of its share goes to memory as it lies in
+//    registers.  (Shares for CTAs, whose warps then add up every item: 94 us instead of 80 for 64 x 8K, 102 instead of 54 for 250
 //    requests of up to 1000 tokens.)  With fewer items they are cut into equal parts, a CTA each, whose warps take pages in
 //    turn.  An item in several places is finished by the one that comes last (a ticket), which adds the parts up in order.
 //  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
 //    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
 //    without limit from page to page: the output is then scaled down, as for a maximum that grows.
 //
-// Bound by HBM and by the warps at once: a page is 860 instructions a tile of 8 rows, 320 of them the shifts and masks.
-// Measured (CUDA graph), 4 rows: 64 ragged requests x 8 heads of up to 8192 tokens 81 us, 5.8 TB/s (copies alone 74); one
-// of 131,072 tokens 35 us, 4.4 TB/s.  12 rows with biases, 64 x 8 x 1641: 49 us.
+// Bound by HBM and by the warps at once: a page is 860 instructions with one tile of 8 rows, 320 of
+// them the shifts and masks, and some 1330 with two.
+// Measured (CUDA graph), 4 rows: 64 ragged requests x 8 heads of up to 8192 tokens 80 us, 5.8 TB/s (copies alone 74); one
+// of 131,072 tokens 35 us, 4.4 TB/s.  16 rows 126 us, of which HBM needs 69; 12 with biases, 64 x 8 x 1641: 47 us.
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -40,26 +41,24 @@ constexpr float kGrow = 8.f, kLift = 7.f;    // weights reach 2^15: the range of
 
 constexpr int kWarpsMost = 11;               // consumer warps of a CTA
 constexpr int kKnown = 256;                  // requests whose rows and lengths every CTA keeps in shared memory
-constexpr int kTeamSlot = 9 * 32 * 4;        // floats of a tile's partial result in registers' order: 32 outputs a lane, two (m, l)
+constexpr int kTileSlot = 9 * 32 * 4;        // floats of a tile's partial result in registers' order: 32 outputs a lane, two (m, l)
 
 struct RowsShape {
   int G, N, limit, max_count;   // limit: rows of a head that a request may have here
   bool causal;
 };
 
-// Ten or eleven consumer warps and a producer, three to each quarter of the SM: up to 12 warps may have 168 registers each, and
-// shared memory is full.  (With 8, 9 and 10 consumers, 250 requests of up to 1000 tokens: 57.5, 57.6 and 55.5 us, 54.8 with 11;
-// 16 rows, 64 x 8K: 145 us with 8, 136 with 10.)
-// A warp has a tile of 8 rows; with up to 16, pairs of warps share pages.
+// Rows of a tile are eight.  With one tile, ten or eleven consumer warps and a producer, three to each quarter of the SM: up to
+// 12 warps may have 168 registers each, and shared memory is full.  (With 8, 9 and 10 consumers, 250 requests of up to 1000
+// tokens: 57.5, 57.6 and 55.5 us, 54 with 11.)  With two tiles seven, which may have 255 each: a warp unpacks for both (two warps a
+// page, a tile each, ten in all: 135 us instead of 126 for 16 rows, 64 x 8K; ten that unpack for both and spill: 131).
 template <int kR, bool kBias>
 struct RowsCfg {
-  static constexpr int kW = kR == 8 && !kBias ? kWarpsMost : 10, kThreads = 32 * (kW + 1);
-  static constexpr int kTiles = kR / 8, kTeams = kW / kTiles;   // warps w and w + kTeams share pages, a tile each
-  static constexpr int kOwn = kTiles == 1 ? 2 : 3, kSt = kTeams * kOwn;   // stages of a team, each consumed by it alone, and of the ring
-  // a warp's part of a CTA's item goes to shared memory where its pages were, if they were its alone
-  static constexpr int kSmemO = kTiles == 1 ? 0 : kW * 8 * kRowO * 4;
-  static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0)) + kSmemO;
-  static_assert(kTiles > 1 || 8 * kRowO * 4 <= ARCKV_PAGE_BYTES, "a part of an item fits a stage");
+  static constexpr int kW = kR == 16 ? 7 : kBias ? 10 : kWarpsMost, kThreads = 32 * (kW + 1);
+  static constexpr int kTiles = kR / 8;
+  static constexpr int kOwn = kTiles == 1 ? 2 : 3, kSt = kW * kOwn;   // stages of a warp, and of the ring
+  static constexpr int kSmem = kSt * (ARCKV_PAGE_BYTES + (kBias ? kPT * 4 : 0));
+  static_assert(kR * kRowO * 4 <= ARCKV_PAGE_BYTES, "a warp's part of an item fits a stage");
   static_assert(sizeof(DevStatus) + kCacheMaxCtas * kW * 2 <= ARCKV_CACHE_WS_HEADER && kW <= kWarpsMost, "a ticket for each warp");
   // the rest of it beside 4097 sums, what kKnown requests are, and 2 KB of fixed arrays
   static_assert(kSmem + 4097 * 4 + kKnown * 12 + 2048 <= 227 * 1024, "shared memory");
@@ -143,7 +142,7 @@ struct Run {
   int first, last;        // the takers that share the item
 };
 
-// The runs of a taker, in order: a CTA, which has one part of an item, or a team of a CTA, which has a share of all pages.
+// The runs of a taker, in order: a CTA, which has one part of an item, or a warp, which has a share of all pages.
 // Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request s of one head.
 struct Walk {
   const arckv_pages4& c;
@@ -208,16 +207,15 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   using Cfg = RowsCfg<kR, kBias>;
   // Fewest pages that are worth a CTA of their own (joining parts takes over 1 us).
   constexpr int kPartMin = 6;
-  constexpr int kW = Cfg::kW, kSt = Cfg::kSt, kTeams = Cfg::kTeams;
+  constexpr int kW = Cfg::kW, kSt = Cfg::kSt;
   extern __shared__ __align__(128) unsigned char smraw[];
   unsigned char* ring = smraw;                                   // [stage][page]
   float* sBias = (float*)(ring + kSt * ARCKV_PAGE_BYTES);        // [stage][64]
-  float* sO = sBias + (kBias ? kSt * kPT : 0);                   // where warps do not have stages of their own: their parts of an item
-  int* known = (int*)((char*)sO + Cfg::kSmemO);                  // [kKnown] first row, rows, tokens of a request
+  int* known = (int*)(sBias + (kBias ? kSt * kPT : 0));          // [kKnown] first row, rows, tokens of a request
   int* pre = known + 3 * min(c.S, kKnown);                       // [S + 1]
   __shared__ __align__(8) uint64_t full[kSt], empty[kSt];
   __shared__ int sHeld[kSt];                                     // whether the stage has a page
-  __shared__ float sM[kW][8], sL[kW][8];
+  __shared__ float sM[kW][kR], sL[kW][kR];
   __shared__ int abort_flag, last_flag, stop_flag, s_cut;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   volatile int* abortp = &abort_flag;
@@ -225,7 +223,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < kSt; ++s) {
       tc::mbar_init(&full[s], 1);
-      tc::mbar_init(&empty[s], Cfg::kTiles);
+      tc::mbar_init(&empty[s], 1);
     }
     abort_flag = 0;
     tc::mbar_fence_init();
@@ -294,22 +292,22 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     len = known[3 * s + 2];
   };
   const bool parts_mode = s_cut > 0;
-  // Teams of the launch are numbered over CTAs first, so that few of them are spread over the SMs.
-  auto walk_of = [&](int team) {
-    return Walk(c, pre, known, parts_mode, parts_mode ? (int)blockIdx.x : team * (int)gridDim.x + (int)blockIdx.x,
-                (int)gridDim.x * (parts_mode ? 1 : kTeams));
+  // Warps of the launch are numbered over CTAs first, so that few of them are spread over the SMs.
+  auto walk_of = [&](int w) {
+    return Walk(c, pre, known, parts_mode, parts_mode ? (int)blockIdx.x : w * (int)gridDim.x + (int)blockIdx.x,
+                (int)gridDim.x * (parts_mode ? 1 : kW));
   };
 
   if (warp == kW) {
     // ------------------------------------------------------------- producer
-    // Lane w fills the stages of team w as that gives them back, each lane at its own pace (in one order for all, the
+    // Lane w fills the stages of warp w as that gives them back, each lane at its own pace (in one order for all, the
     // slowest warp held up the others' pages: 104 us instead of 97 for 64 x 8K).
-    const bool feeds = lane < kTeams;
+    const bool feeds = lane < kW;
     constexpr int kOwn = Cfg::kOwn;
-    Walk walk = walk_of(min(lane, kTeams - 1));
+    Walk walk = walk_of(min(lane, kW - 1));
     Run p;
     int i = 0, issued = 0, entry = -1, held = 0;
-    const int step = parts_mode ? kTeams : 1;   // the teams of a CTA with a part take its pages in turn
+    const int step = parts_mode ? kW : 1;   // the warps of a CTA with a part take its pages in turn
     auto begin = [&] {
       if (!walk.next(p)) return false;
       int first, n, len;
@@ -318,7 +316,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       return true;
     };
     bool left = feeds && begin();
-    auto settle = [&] {   // from page i on, the next one of this lane's team
+    auto settle = [&] {   // from page i on, the next one of this lane's warp
       while (left && i >= p.n) {
         left = begin();
         i = 0;
@@ -333,7 +331,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     while (__any_sync(0xffffffffu, left)) {
       bool moved = false;
       if (left) {
-        const int st = lane + kTeams * (issued % kOwn);
+        const int st = lane + kW * (issued % kOwn);
         if (issued < kOwn || mbar_ended(&empty[st], (issued / kOwn - 1) & 1)) {
           if (entry >= c.P) {
             set_status(stt, ARCKV_ERR_INVALID_ARG);
@@ -370,8 +368,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       volatile int never = 0;
       if (feeds)   // (the n-th page of a stage completes its phase n - 1)
         for (int k = 0; k < kOwn; ++k) {
-          const int n = (issued + kOwn - 1 - k) / kOwn;   // pages that stage k of this team's got
-          if (n > 0) tc::mbar_wait(&full[lane + k * kTeams], (n - 1) & 1, &never, stt);
+          const int n = (issued + kOwn - 1 - k) / kOwn;   // pages that stage k of this warp's got
+          if (n > 0) tc::mbar_wait(&full[lane + k * kW], (n - 1) & 1, &never, stt);
         }
     }
     return;
@@ -379,9 +377,9 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 
   // --------------------------------------------------------------- consumers
   const int g = lane >> 2, t = lane & 3;
-  const int team = warp % kTeams, tile0 = warp / kTeams * 8;   // first row of this warp's tile
-  const int step = parts_mode ? kTeams : 1;
-  Walk walk = walk_of(team);
+  constexpr int kT = Cfg::kTiles, kMt = 4 / kT;   // tiles, and 16s of tokens of a pass
+  const int step = parts_mode ? kW : 1;
+  Walk walk = walk_of(warp);
   int taken = 0;                 // pages so far
   bool ok = true;
   Run p;
@@ -390,14 +388,15 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     request(p.s, first, count, len);
     const int n = p.n, h = p.h, nrows = count * d.G;
     // query rows: column n is row n of the tile
-    uint32_t qf[8][2];
+    uint32_t qf[kT][8][2];
     // what a token's least values multiply beside the codes' sums: the sum of a group's elements as two bf16, row g, group t, and
     // zeros for the scales that are in the same words
-    uint32_t q_sum[2];
-    float fac[2];                         // 2^e scale (log2 e) of rows 2t, 2t + 1
-    int see[2], see_min;                  // tokens that they see
-    {
-      const int r = tile0 + g, i = r / d.G;
+    uint32_t q_sum[kT][2];
+    float fac[kT][2];                     // 2^e scale (log2 e) of rows 2t, 2t + 1
+    int see[kT][2], see_min = 0x7fffffff; // tokens that they see
+#pragma unroll
+    for (int tt = 0; tt < kT; ++tt) {
+      const int r = 8 * tt + g, i = r / d.G;
       const bf16* mine = Q + (first + i) * qs.i + h * qs.h + (r - i * d.G) * 128;
       uint4 x[4];
       float amax = 0.f;
@@ -422,7 +421,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
 #pragma unroll
         for (int f = 0; f < 4; ++f) {   // pair f of the word: dims 32 w + 8 t + 2 f, + 1
           const float by = f & 1 ? up * 0.0625f : up;   // (its codes are 16 times the others')
-          qf[2 * w + (f >> 1)][f & 1] = pack_f16(bf16_lo(y[f]) * by, bf16_hi(y[f]) * by);
+          qf[tt][2 * w + (f >> 1)][f & 1] = pack_f16(bf16_lo(y[f]) * by, bf16_hi(y[f]) * by);
           sum[w] += bf16_lo(y[f]) * up + bf16_hi(y[f]) * up;
         }
 #pragma unroll
@@ -431,184 +430,215 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       {   // in units of a code, which is 2^-24
         bf16 a, b;
         split_bf16((t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3]) * 0x1p-24f, a, b);
-        q_sum[0] = (uint32_t)__bfloat16_as_ushort(a) << 16;
-        q_sum[1] = (uint32_t)__bfloat16_as_ushort(b) << 16;
+        q_sum[tt][0] = (uint32_t)__bfloat16_as_ushort(a) << 16;
+        q_sum[tt][1] = (uint32_t)__bfloat16_as_ushort(b) << 16;
       }
       const float f = down * 0x1p24f * scale * (kBias ? 1.f : kLog2e);
       const int sees = r < nrows ? (d.causal ? max(0, min(len, len - count + i + 1)) : len) : 0;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {   // (a factor is never zero: a masked product is -inf)
-        fac[k] = fmaxf(__shfl_sync(0xffffffffu, f, (2 * t + k) * 4), 0x1p-126f);
-        see[k] = __shfl_sync(0xffffffffu, sees, (2 * t + k) * 4);
+        fac[tt][k] = fmaxf(__shfl_sync(0xffffffffu, f, (2 * t + k) * 4), 0x1p-126f);
+        see[tt][k] = __shfl_sync(0xffffffffu, sees, (2 * t + k) * 4);
       }
-      see_min = __reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff);
+      see_min = min(see_min, (int)__reduce_min_sync(0xffffffffu, r < nrows ? sees : 0x7fffffff));
     }
-    float o[8][4], mx[2], l[2], low[2];   // low: sums of weights times least values
+    float o[kT][8][4], mx[kT][2], l[kT][2], low[kT][2];   // low: sums of weights times least values
     float v_ref = 0.f;                         // unit of o: a power of two
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int tt = 0; tt < kT; ++tt) {
 #pragma unroll
-      for (int f = 0; f < 4; ++f) o[k][f] = 0.f;
+      for (int k = 0; k < 8; ++k)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      mx[k] = -INFINITY;
-      l[k] = low[k] = 0.f;
+        for (int f = 0; f < 4; ++f) o[tt][k][f] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        mx[tt][k] = -INFINITY;
+        l[tt][k] = low[tt][k] = 0.f;
+      }
     }
-    for (int i = parts_mode ? team : 0; i < n && ok; i += step, ++taken) {
-      const int st = team + kTeams * (taken % Cfg::kOwn), j0 = (p.blk + i) * kPT;   // first token of the page
+    for (int i = parts_mode ? warp : 0; i < n && ok; i += step, ++taken) {
+      const int st = warp + kW * (taken % Cfg::kOwn);
       ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[st], (taken / Cfg::kOwn) & 1, abortp, stt));
       if (!ok) break;
-      if (sHeld[st] && tile0 < nrows) {
-        const unsigned char* page = ring + st * ARCKV_PAGE_BYTES;
-        // ---- S^T = K Q^T: lane (g, t) has tokens g, g + 8 of 16, and eight dims of each group
-        float s[4][4];
+      if (sHeld[st]) {
+        // with two tiles a page is taken in two passes of 32 tokens, as far as registers go
+#pragma unroll 1
+        for (int pass = 0; pass < kT; ++pass) {
+          const unsigned char* page = ring + st * ARCKV_PAGE_BYTES;
+          const int m0 = pass * kMt, j0 = (p.blk + i) * kPT + 16 * m0;   // first token of the pass
+          // ---- S^T = K Q^T: lane (g, t) has tokens g, g + 8 of 16, and eight dims of each group
+          float s[kT][kMt][4];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
-          const uint4 a = *(const uint4*)(page + (mt * 16 + g) * 64 + t * 16);
-          const uint4 b = *(const uint4*)(page + (mt * 16 + g + 8) * 64 + t * 16);
-          const uint4 pa = *(const uint4*)(page + kPageKp + (mt * 16 + g) * 16);
-          const uint4 pb = *(const uint4*)(page + kPageKp + (mt * 16 + g + 8) * 16);
-          const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-          const uint32_t pw[4] = {pa.x, pa.y, pa.z, pa.w}, pv[4] = {pb.x, pb.y, pb.z, pb.w};
-          {   // here lane (g, t) has scale and least value of group t of its tokens
-            const uint32_t ma = *(const uint32_t*)(page + kPageKp + (mt * 16 + g) * 16 + 4 * t);
-            const uint32_t mb = *(const uint32_t*)(page + kPageKp + (mt * 16 + g + 8) * 16 + 4 * t);
-            mma_bf16_zero(s[mt], ma, mb, q_sum[0], q_sum[1]);
-          }
+          for (int mt = 0; mt < kMt; ++mt) {
+            const int row = (m0 + mt) * 16 + g;
+            const uint4 a = *(const uint4*)(page + row * 64 + t * 16);
+            const uint4 b = *(const uint4*)(page + (row + 8) * 64 + t * 16);
+            const uint4 pa = *(const uint4*)(page + kPageKp + row * 16);
+            const uint4 pb = *(const uint4*)(page + kPageKp + (row + 8) * 16);
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+            const uint32_t pw[4] = {pa.x, pa.y, pa.z, pa.w}, pv[4] = {pb.x, pb.y, pb.z, pb.w};
+            {   // here lane (g, t) has scale and least value of group t of its tokens
+              const uint32_t ma = *(const uint32_t*)(page + kPageKp + row * 16 + 4 * t);
+              const uint32_t mb = *(const uint32_t*)(page + kPageKp + (row + 8) * 16 + 4 * t);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t a8 = aw[w] >> 8, b8 = bw[w] >> 8;
-            const uint32_t f0 = pair_low(aw[w]), f1 = pair_low(bw[w]), f2 = pair_high(aw[w]), f3 = pair_high(bw[w]);
-            const uint32_t f4 = pair_low(a8), f5 = pair_low(b8), f6 = pair_high(a8), f7 = pair_high(b8);
-            float acc[4];
-            mma_f16_zero(acc, f0, f1, f2, f3, qf[2 * w][0], qf[2 * w][1]);
-            mma_f16(acc, f4, f5, f6, f7, qf[2 * w + 1][0], qf[2 * w + 1][1]);
+              for (int tt = 0; tt < kT; ++tt) mma_bf16_zero(s[tt][mt], ma, mb, q_sum[tt][0], q_sum[tt][1]);
+            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              s[mt][k] = fmaf(bf16_lo(pw[w]), acc[k], s[mt][k]);
-              s[mt][2 + k] = fmaf(bf16_lo(pv[w]), acc[2 + k], s[mt][2 + k]);
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t a8 = aw[w] >> 8, b8 = bw[w] >> 8;
+              const uint32_t f0 = pair_low(aw[w]), f1 = pair_low(bw[w]), f2 = pair_high(aw[w]), f3 = pair_high(bw[w]);
+              const uint32_t f4 = pair_low(a8), f5 = pair_low(b8), f6 = pair_high(a8), f7 = pair_high(b8);
+#pragma unroll
+              for (int tt = 0; tt < kT; ++tt) {
+                float acc[4];
+                mma_f16_zero(acc, f0, f1, f2, f3, qf[tt][2 * w][0], qf[tt][2 * w][1]);
+                mma_f16(acc, f4, f5, f6, f7, qf[tt][2 * w + 1][0], qf[tt][2 * w + 1][1]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  s[tt][mt][k] = fmaf(bf16_lo(pw[w]), acc[k], s[tt][mt][k]);
+                  s[tt][mt][2 + k] = fmaf(bf16_lo(pv[w]), acc[2 + k], s[tt][mt][2 + k]);
+                }
+              }
             }
           }
-        }
-        // ---- softmax of the page.  References follow the maximum only when it has grown by more than 2^8 (kGrow), so
-        // that sums are scaled on few pages.  Without biases the maximum is that of the products, whose factor is
-        // positive, and a weight is 2^{product factor - mx}.
-        if (kBias) {
+          // ---- softmax of the pass.  References follow the maximum only when it has grown by more than 2^8 (kGrow), so
+          // that sums are scaled on few pages.  Without biases the maximum is that of the products, whose factor is
+          // positive, and a weight is 2^{product factor - mx}.
+          if (kBias) {
 #pragma unroll
-          for (int mt = 0; mt < 4; ++mt)
+            for (int mt = 0; mt < kMt; ++mt)
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              const float bias = sBias[st * kPT + mt * 16 + hf * 8 + g];
+              for (int hf = 0; hf < 2; ++hf) {
+                const float bias = sBias[st * kPT + (m0 + mt) * 16 + hf * 8 + g];
 #pragma unroll
-              for (int k = 0; k < 2; ++k) s[mt][2 * hf + k] = fmaf(s[mt][2 * hf + k], fac[k], bias);
+                for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+                  for (int k = 0; k < 2; ++k) s[tt][mt][2 * hf + k] = fmaf(s[tt][mt][2 * hf + k], fac[tt][k], bias);
+              }
+          }
+          if (j0 + 16 * kMt > see_min) {   // (also where no row has been: anything may be there)
+#pragma unroll
+            for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+              for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                  if (j0 + mt * 16 + (f >> 1) * 8 + g >= see[tt][f & 1]) s[tt][mt][f] = -INFINITY;
+          }
+          float top[kT][2];
+          bool grows = false;
+#pragma unroll
+          for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {   // rows 2t, 2t + 1
+              float& x = top[tt][k];
+              x = fmaxf(s[tt][0][k], s[tt][0][2 + k]);
+#pragma unroll
+              for (int mt = 1; mt < kMt; ++mt) x = max3(x, s[tt][mt][k], s[tt][mt][2 + k]);
+              if (!kBias) x = fmaf(x, fac[tt][k], -kLift);
+              grows |= (kBias ? (x - mx[tt][k]) * kLog2e : x - mx[tt][k]) > kGrow;   // (mx = -inf: by any but -inf)
             }
-        }
-        if (j0 + kPT > see_min) {   // (also where no row has been: anything may be there)
+          if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
-          for (int mt = 0; mt < 4; ++mt)
+            for (int tt = 0; tt < kT; ++tt) {
+              float alpha[2];
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
-              if (j0 + mt * 16 + (f >> 1) * 8 + g >= see[f & 1]) s[mt][f] = -INFINITY;
-        }
-        float top[2];
-        bool grows = false;
+              for (int k = 0; k < 2; ++k) {
+                float& x = top[tt][k];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {   // rows 2t, 2t + 1
-          float& x = top[k];
-          x = max3(s[0][k], s[0][2 + k], s[1][k]);
-          x = fmaxf(max3(x, s[1][2 + k], s[2][k]), max3(s[2][2 + k], s[3][k], s[3][2 + k]));
-          if (!kBias) x = fmaf(x, fac[k], -kLift);
-          grows |= (kBias ? (x - mx[k]) * kLog2e : x - mx[k]) > kGrow;   // (mx = -inf: by any but -inf)
-        }
-        if (__any_sync(0xffffffffu, grows)) {
-          float alpha[2];
+                for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+                const float by = kBias ? (mx[tt][k] - x) * kLog2e : mx[tt][k] - x;
+                const bool up = x != -INFINITY && (mx[tt][k] == -INFINITY || -by > kGrow);
+                alpha[k] = up ? ex2_approx(by) : 1.f;   // (mx = -inf: zero)
+                if (up) mx[tt][k] = x;
+                l[tt][k] *= alpha[k];
+                low[tt][k] *= alpha[k];
+              }
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float& x = top[k];
+              for (int k = 0; k < 8; ++k)
 #pragma unroll
-            for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
-            const float by = kBias ? (mx[k] - x) * kLog2e : mx[k] - x;
-            const bool up = x != -INFINITY && (mx[k] == -INFINITY || -by > kGrow);
-            alpha[k] = up ? ex2_approx(by) : 1.f;   // (mx = -inf: zero)
-            if (up) mx[k] = x;
-            l[k] *= alpha[k];
-            low[k] *= alpha[k];
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int f = 0; f < 4; ++f) o[k][f] *= alpha[f & 1];
-        }
-        // the values' scales and least values; of tokens that are not held, zero
-        float vs[8], vm[8], most = 0.f;
-        {
-          uint32_t par[8];
-#pragma unroll
-          for (int x = 0; x < 8; ++x) par[x] = *(const uint32_t*)(page + kPageVp + (x * 8 + g) * 4);
-          if (j0 + kPT > len) {
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              if (j0 + x * 8 + g >= len) par[x] = 0u;
-          }
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            vs[x] = bf16_lo(par[x]);
-            vm[x] = bf16_hi(par[x]);
-          }
-          most = fmaxf(max3(max3(vs[0], vs[1], vs[2]), vs[3], vs[4]), max3(vs[5], vs[6], vs[7]));
-        }
-#pragma unroll
-        for (int w = 4; w < 32; w <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
-        if (most > v_ref) {   // (uniform) a larger unit: between two and four times the scale, so that few pages raise it
-          const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23)), by = v_ref / to;
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int f = 0; f < 4; ++f) o[k][f] *= by;
-          v_ref = to;
-        }
-        const float inv_ref = v_ref > 0.f ? 1.f / v_ref : 0.f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) vs[x] *= inv_ref;
-        uint32_t ph[4][2];
-        {
-          // (nothing visible yet: weights 2^{-inf} = 0)
-          const float2 ref = make_float2(mx[0] == -INFINITY ? 0.f : -mx[0], mx[1] == -INFINITY ? 0.f : -mx[1]);
-          const float2 fac2 = make_float2(fac[0], fac[1]);
-          float2 sum = make_float2(0.f, 0.f), lows = make_float2(low[0], low[1]);
-#pragma unroll
-          for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              float2 x = make_float2(s[mt][2 * hf], s[mt][2 * hf + 1]);
-              // a bias of the type's lowest value cancels against itself before the factor log2 e
-              if (kBias) x = fma2(add2(x, ref), make_float2(kLog2e, kLog2e), make_float2(kLift, kLift));
-              else x = fma2(x, fac2, ref);
-              x.x = ex2_approx(x.x);
-              x.y = ex2_approx(x.y);
-              sum = add2(sum, x);
-              lows = fma2(x, make_float2(vm[2 * mt + hf], vm[2 * mt + hf]), lows);
-              x = mul2(x, make_float2(vs[2 * mt + hf], vs[2 * mt + hf]));
-              ph[mt][hf] = transpose8x8(pack_f16(x.x, x.y));   // as f16, transposed to (tokens, row) operands
+                for (int f = 0; f < 4; ++f) o[tt][k][f] *= alpha[f & 1];
             }
-          l[0] += sum.x;
-          l[1] += sum.y;
-          low[0] = lows.x;
-          low[1] = lows.y;
-        }
-        // ---- O^T += V^T P^T, 16 dims and 16 tokens a product: lane (g, t) has tokens 2t, 2t + 1 and 8 on, dims g + 8 x
+          }
+          // the values' scales and least values; of tokens that are not held, zero
+          float vs[2 * kMt], vm[2 * kMt], most = 0.f;
+          {
+            uint32_t par[2 * kMt];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
-          const uint4 a = *(const uint4*)(page + kPageV + (mt * 8 + t) * 128 + ((g ^ (t << 1)) << 4));
-          const uint4 b = *(const uint4*)(page + kPageV + (mt * 8 + t + 4) * 128 + ((g ^ (t << 1)) << 4));
-          const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+            for (int x = 0; x < 2 * kMt; ++x) par[x] = *(const uint32_t*)(page + kPageVp + (16 * m0 + x * 8 + g) * 4);
+            if (j0 + 16 * kMt > len) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t a8 = aw[x] >> 8, b8 = bw[x] >> 8;
-            const uint32_t f0 = pair_low(aw[x]), f1 = pair_high(aw[x]), f2 = pair_low(bw[x]), f3 = pair_high(bw[x]);
-            const uint32_t f4 = pair_low(a8), f5 = pair_high(a8), f6 = pair_low(b8), f7 = pair_high(b8);
-            mma_f16(o[2 * x], f0, f1, f2, f3, ph[mt][0], ph[mt][1]);
-            mma_f16(o[2 * x + 1], f4, f5, f6, f7, ph[mt][0], ph[mt][1]);
+              for (int x = 0; x < 2 * kMt; ++x)
+                if (j0 + x * 8 + g >= len) par[x] = 0u;
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * kMt; ++x) {
+              vs[x] = bf16_lo(par[x]);
+              vm[x] = bf16_hi(par[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < 2 * kMt; x += 2) most = max3(most, vs[x], vs[x + 1]);
+          }
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+          if (most > v_ref) {   // (uniform) a larger unit: between two and four times the scale, so that few pages raise it
+            const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23)), by = v_ref / to;
+#pragma unroll
+            for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) o[tt][k][f] *= by;
+            v_ref = to;
+          }
+          const float inv_ref = v_ref > 0.f ? 1.f / v_ref : 0.f;
+#pragma unroll
+          for (int x = 0; x < 2 * kMt; ++x) vs[x] *= inv_ref;
+          uint32_t ph[kT][kMt][2];
+#pragma unroll
+          for (int tt = 0; tt < kT; ++tt) {
+            // (nothing visible yet: weights 2^{-inf} = 0)
+            const float2 ref = make_float2(mx[tt][0] == -INFINITY ? 0.f : -mx[tt][0], mx[tt][1] == -INFINITY ? 0.f : -mx[tt][1]);
+            const float2 fac2 = make_float2(fac[tt][0], fac[tt][1]);
+            float2 sum = make_float2(0.f, 0.f), lows = make_float2(low[tt][0], low[tt][1]);
+#pragma unroll
+            for (int mt = 0; mt < kMt; ++mt)
+#pragma unroll
+              for (int hf = 0; hf < 2; ++hf) {
+                float2 x = make_float2(s[tt][mt][2 * hf], s[tt][mt][2 * hf + 1]);
+                // a bias of the type's lowest value cancels against itself before the factor log2 e
+                if (kBias) x = fma2(add2(x, ref), make_float2(kLog2e, kLog2e), make_float2(kLift, kLift));
+                else x = fma2(x, fac2, ref);
+                x.x = ex2_approx(x.x);
+                x.y = ex2_approx(x.y);
+                sum = add2(sum, x);
+                lows = fma2(x, make_float2(vm[2 * mt + hf], vm[2 * mt + hf]), lows);
+                x = mul2(x, make_float2(vs[2 * mt + hf], vs[2 * mt + hf]));
+                ph[tt][mt][hf] = transpose8x8(pack_f16(x.x, x.y));   // as f16, transposed to (tokens, row) operands
+              }
+            l[tt][0] += sum.x;
+            l[tt][1] += sum.y;
+            low[tt][0] = lows.x;
+            low[tt][1] = lows.y;
+          }
+          // ---- O^T += V^T P^T, 16 dims and 16 tokens a product: lane (g, t) has tokens 2t, 2t + 1 and 8 on, dims g + 8 x
+#pragma unroll
+          for (int mt = 0; mt < kMt; ++mt) {
+            const unsigned char* pairs = page + kPageV + ((m0 + mt) * 8 + t) * 128 + ((g ^ (t << 1)) << 4);
+            const uint4 a = *(const uint4*)pairs;
+            const uint4 b = *(const uint4*)(pairs + 4 * 128);
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t a8 = aw[x] >> 8, b8 = bw[x] >> 8;
+              const uint32_t f0 = pair_low(aw[x]), f1 = pair_high(aw[x]), f2 = pair_low(bw[x]), f3 = pair_high(bw[x]);
+              const uint32_t f4 = pair_low(a8), f5 = pair_high(a8), f6 = pair_low(b8), f7 = pair_high(b8);
+#pragma unroll
+              for (int tt = 0; tt < kT; ++tt) {
+                mma_f16(o[tt][2 * x], f0, f1, f2, f3, ph[tt][mt][0], ph[tt][mt][1]);
+                mma_f16(o[tt][2 * x + 1], f4, f5, f6, f7, ph[tt][mt][0], ph[tt][mt][1]);
+              }
+            }
           }
         }
       }
@@ -617,17 +647,20 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     }
     // ---- the run's end
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int tt = 0; tt < kT; ++tt) {
 #pragma unroll
-      for (int w = 4; w < 32; w <<= 1) {
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], w);
-        low[k] += __shfl_xor_sync(0xffffffffu, low[k], w);
-      }
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int x = 0; x < 8; ++x)
+        for (int w = 4; w < 32; w <<= 1) {
+          l[tt][k] += __shfl_xor_sync(0xffffffffu, l[tt][k], w);
+          low[tt][k] += __shfl_xor_sync(0xffffffffu, low[tt][k], w);
+        }
 #pragma unroll
-      for (int f = 0; f < 4; ++f)   // dims 16 x + g are of low nibbles, those 8 on of high ones
-        o[x][f] = fmaf(o[x][f] * (f >> 1 ? 0x1p20f : 0x1p24f), v_ref, low[f & 1]);
+      for (int x = 0; x < 8; ++x)
+#pragma unroll
+        for (int f = 0; f < 4; ++f)   // dims 16 x + g are of low nibbles, those 8 on of high ones
+          o[tt][x][f] = fmaf(o[tt][x][f] * (f >> 1 ? 0x1p20f : 0x1p24f), v_ref, low[tt][f & 1]);
+    }
     const bool whole = p.first == p.last;
     auto weight = [](float m, float top) {   // e^{m - top}; 0 for a part that saw nothing
       return m == -INFINITY ? 0.f : ex2_approx(kBias ? (m - top) * kLog2e : m - top);
@@ -635,24 +668,23 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     constexpr float kBig = 3.3895313892515355e38f;   // (the largest bf16)
     if (!parts_mode) {   // a share's run: the warp's own affair
       if (!ok) break;    // a wait gave up: write nothing
-      const int tile = tile0 / 8;
-      const bool mine = tile0 + 2 * t < nrows;   // (rows 2t, 2t + 1 of the tile)
       if (!whole) {
-        // slot 2c holds the item that team c went on with, 2c + 1 the one it began
-        auto slot_of = [&](int team, bool began) {
-          return (float4*)(parts + ((2ll * team + began) * Cfg::kTiles + tile) * kTeamSlot) + lane;
-        };
+        // slot 2c holds the item that warp c went on with, 2c + 1 the one it began
+        auto slot_of = [&](int w, bool began) { return (float4*)(parts + (2ll * w + began) * kT * kTileSlot) + lane; };
         float4* slot = slot_of(walk.id, p.blk == 0);
-        if (mine) {
 #pragma unroll
-          for (int x = 0; x < 8; ++x) __stcg(slot + 32 * x, make_float4(o[x][0], o[x][1], o[x][2], o[x][3]));
-          __stcg(slot + 32 * 8, make_float4(mx[0], mx[1], l[0], l[1]));
-        }
+        for (int tt = 0; tt < kT; ++tt)
+          if (8 * tt + 2 * t < nrows) {   // (rows 2t, 2t + 1 of the tile)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              __stcg(slot + (9 * tt + x) * 32, make_float4(o[tt][x][0], o[tt][x][1], o[tt][x][2], o[tt][x][3]));
+            __stcg(slot + (9 * tt + 8) * 32, make_float4(mx[tt][0], mx[tt][1], l[tt][0], l[tt][1]));
+          }
         __syncwarp();
         int last = 0;
         if (lane == 0) {   // the warp's results before the ticket, the others' after it; tickets are halves of words
-          const int at = p.first * Cfg::kTiles + tile, shift = 16 * (at & 1);
-          unsigned int* word = (unsigned int*)tickets + (at >> 1);
+          const int shift = 16 * (p.first & 1);
+          unsigned int* word = (unsigned int*)tickets + (p.first >> 1);
           unsigned int old;
           asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(old) : "l"(word), "r"(1u << shift) : "memory");
           last = (int)((old >> shift) & 0xffffu) == p.last - p.first;
@@ -660,16 +692,18 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         }
         if (!__shfl_sync(0xffffffffu, last, 0)) continue;
         __syncwarp();
-        if (mine) {
+#pragma unroll
+        for (int tt = 0; tt < kT; ++tt) {
+          if (8 * tt + 2 * t >= nrows) continue;
           float up[2] = {-INFINITY, -INFINITY};   // with a running maximum, so that a part's loads wait for nothing
-          l[0] = l[1] = 0.f;
+          l[tt][0] = l[tt][1] = 0.f;
 #pragma unroll
           for (int x = 0; x < 8; ++x)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) o[x][f] = 0.f;
+            for (int f = 0; f < 4; ++f) o[tt][x][f] = 0.f;
 #pragma unroll 1
           for (int cc = p.first; cc <= p.last; ++cc) {
-            const float4* from = slot_of(cc, cc == p.first);
+            const float4* from = slot_of(cc, cc == p.first) + 9 * tt * 32;
             float4 y[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) y[x] = __ldcg(from + 32 * x);
@@ -678,62 +712,64 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
             const float f0 = weight(up[0], m0), f1 = weight(up[1], m1), b0 = weight(ml.x, m0), b1 = weight(ml.y, m1);
             up[0] = m0;
             up[1] = m1;
-            l[0] = fmaf(l[0], f0, ml.z * b0);
-            l[1] = fmaf(l[1], f1, ml.w * b1);
+            l[tt][0] = fmaf(l[tt][0], f0, ml.z * b0);
+            l[tt][1] = fmaf(l[tt][1], f1, ml.w * b1);
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-              o[x][0] = fmaf(o[x][0], f0, y[x].x * b0);
-              o[x][1] = fmaf(o[x][1], f1, y[x].y * b1);
-              o[x][2] = fmaf(o[x][2], f0, y[x].z * b0);
-              o[x][3] = fmaf(o[x][3], f1, y[x].w * b1);
+              o[tt][x][0] = fmaf(o[tt][x][0], f0, y[x].x * b0);
+              o[tt][x][1] = fmaf(o[tt][x][1], f1, y[x].y * b1);
+              o[tt][x][2] = fmaf(o[tt][x][2], f0, y[x].z * b0);
+              o[tt][x][3] = fmaf(o[tt][x][3], f1, y[x].w * b1);
             }
           }
         }
       }
 #pragma unroll
+      for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int r = 8 * tt + 2 * t + k;
+          if (r >= nrows) continue;   // (a tile without rows masks nothing: it may have met anything behind the end)
+          const int i = r / d.G;
+          bf16* to = O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + g;
+          const float inv = l[tt][k] == 0.f ? 0.f : 1.f / l[tt][k];
+          bool fine = true;
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const float v = o[tt][x][2 * z + k] * inv;
+              to[16 * x + 8 * z] = __float2bfloat16_rn(v);
+              fine &= fabsf(v) <= kBig;
+            }
+          if (!fine) set_status(stt, ARCKV_ERR_NONFINITE);
+        }
+      continue;
+    }
+    // a part of an item: add the CTA's warps up.  A warp's part lies where its pages were, all of which it has taken
+    auto out_of = [&](int w, int r) { return (float*)(ring + w * ARCKV_PAGE_BYTES) + r * kRowO; };
+    __syncwarp();
+#pragma unroll
+    for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int r = tile0 + 2 * t + k;
-        if (r >= nrows) continue;
-        const int i = r / d.G;
-        bf16* to = O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + g;
-        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
-        bool fine = true;
+        const int r = 8 * tt + 2 * t + k;
+        if (g == 0) {
+          sM[warp][r] = mx[tt][k];
+          sL[warp][r] = l[tt][k];
+        }
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float v = o[x][2 * z + k] * inv;
-            to[16 * x + 8 * z] = __float2bfloat16_rn(v);
-            fine &= fabsf(v) <= kBig;
-          }
-        if (!fine) set_status(stt, ARCKV_ERR_NONFINITE);
+          for (int z = 0; z < 2; ++z) out_of(warp, r)[16 * x + 8 * z + g] = o[tt][x][2 * z + k];
       }
-      continue;
-    }
-    // a part of an item: add the CTA's warps up
-    auto out_of = [&](int w, int r) {   // row r of warp w's tile
-      return (Cfg::kTiles == 1 ? (float*)(ring + w * ARCKV_PAGE_BYTES) : sO + w * 8 * kRowO) + r * kRowO;
-    };
-    __syncwarp();
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int r = 2 * t + k;
-      if (g == 0) {
-        sM[warp][r] = mx[k];
-        sL[warp][r] = l[k];
-      }
-#pragma unroll
-      for (int x = 0; x < 8; ++x)
-#pragma unroll
-        for (int z = 0; z < 2; ++z) out_of(warp, r)[16 * x + 8 * z + g] = o[x][2 * z + k];
-    }
     if (tid == 0) stop_flag = *abortp;   // one reading for all: the producer may raise the flag at any time
     bar_consumers(kW * 32);
     if (stop_flag) break;   // a wait gave up: write nothing
     auto store = [&](int r, int dim, float4 v, float z) {
       const float inv = z == 0.f ? 0.f : 1.f / z;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-      if (r >= nrows) return;   // (a tile without rows masks nothing: it may have met anything behind the end)
+      if (r >= nrows) return;
       const int i = r / d.G;
       __nv_bfloat162 y[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
       *(uint2*)(O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + dim) = *(const uint2*)&y[0];
@@ -743,18 +779,18 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     // partial results: slot 2c holds the item that CTA c went on with, 2c + 1 the one it began
     constexpr int kSlot = kR * 132;   // 128 outputs, m, l (and two unused) for each row
     for (int x = tid; x < kR * 32; x += kW * 32) {
-      const int r = x >> 5, dim = (x & 31) * 4, w0 = r / 8 * kTeams, rr = r & 7;
+      const int r = x >> 5, dim = (x & 31) * 4;
       float up = -INFINITY, z = 0.f;
 #pragma unroll
-      for (int w = 0; w < kTeams; ++w)
-        if (w < n) up = fmaxf(up, sM[w0 + w][rr]);
+      for (int w = 0; w < kW; ++w)
+        if (w < n) up = fmaxf(up, sM[w][r]);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kTeams; ++w) {
+      for (int w = 0; w < kW; ++w) {
         if (w >= n) break;   // (these warps had no page)
-        const float f = weight(sM[w0 + w][rr], up);
-        const float4 y = *(const float4*)(out_of(w0 + w, rr) + dim);
-        z = fmaf(sL[w0 + w][rr], f, z);
+        const float f = weight(sM[w][r], up);
+        const float4 y = *(const float4*)(out_of(w, r) + dim);
+        z = fmaf(sL[w][r], f, z);
         v = make_float4(fmaf(y.x, f, v.x), fmaf(y.y, f, v.y), fmaf(y.z, f, v.z), fmaf(y.w, f, v.w));
       }
       if (whole) store(r, dim, v, z);
@@ -818,8 +854,10 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
 }  // namespace
 
 size_t pages_attend_scratch(int, int, int, int max_count, int G) {
-  // partial results of CTAs, or of eight warps of each
-  const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(kRowsMax * 132, kWarpsMost * kTeamSlot) * sizeof(float);
+  // partial results of CTAs, or of the warps of each
+  const long long all = (long long)max_count * G;
+  const int slots = all > 8 && all <= kRowsMax ? 2 * RowsCfg<16, false>::kW : kWarpsMost;
+  const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(kRowsMax * 132, slots * kTileSlot) * sizeof(float);
   return (long long)max_count * G > kRowsMax ? std::max(rows, pages_tiles_scratch((long long)max_count * G)) : rows;
 }
 
