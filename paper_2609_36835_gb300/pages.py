@@ -360,7 +360,8 @@ def rotate(how: Rotary, positions, X, X2=None, *, out=None, transpose: bool = Fa
     """X, and X2 if given, with each row's head turned by its position (int32 [N]; rows with one below zero are copied):
     [N, heads, d] bf16 or fp32, dense in the last dimension, d a multiple of 16 up to 512, both of one type and d.
     Returns new tensors (a pair when X2 is given), or fills `out` (a tensor or a pair), which may be X and X2 themselves.
-    transpose: the transposed map, which takes gradients of the outputs to those of X and X2."""
+    transpose: the transposed map, which takes gradients of the outputs to those of X and X2 (autograd does not record the
+    call, as none of this package)."""
     import torch
     dev, dtype = X.device, X.dtype
     if X.dim() != 3 or (dtype != torch.bfloat16 and dtype != torch.float32):
