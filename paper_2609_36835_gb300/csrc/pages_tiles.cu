@@ -11,8 +11,9 @@
 //   MMA warp              S = Q K^T, O += P V, fp32 sums in TMEM
 //   softmax (8 warps a tile, 16 rows each, four lanes a row)  turn S into weights
 //                         in place; P is the MMA's operand from TMEM
-//   cuts (1 warp)         which item other CTAs go on with
-// A tile has two buffers of S in TMEM: the softmax of one page runs beside the products of its neighbours.  A tile without
+//   items (1 warp)        the CTA's items ahead of the other warps, and the one that
+//                         other CTAs go on with
+// A tile has two buffers of S in TMEM (four if it is alone): the softmax of one page runs beside the products of its neighbours.  A tile without
 // rows is left out.  Work is dealt out in equal shares of pages; an item (request, head, row tile) that several CTAs share is
 // added up by pages_join_kernel behind this one.
 //
@@ -28,8 +29,11 @@
 // page's largest.  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
 //
 // Bound by shared memory, which the N = 64 products of S read Q from once a page, and by the softmax's issue (a page and 256
-// rows take 0.94 us, of which the pipe needs 0.54; steps of two pages with one buffer of S took longer, 295 us against 237).
-// Measured (CUDA graph): 2048 rows of 8 heads over 32,768 tokens 237 us, 1.15 PFLOP/s; 256 rows over 8192 33 us with the join.
+// rows take 0.93 us, of which the pipe needs 0.54; steps of two pages with one buffer of S took longer, 295 us against 237;
+// a warp for S and one for P V 265).  With one tile a page takes 0.8 us: a chain of waits, whatever the rows.
+// Measured (CUDA graph): 2048 rows of 8 heads over 32,768 tokens 234 us, 1.16 PFLOP/s; 256 rows over 8192 34 us with the join;
+// 20 rows, 64 x 8 x up to 8192: 266 us; 32 rows, 250 x 8 x up to 500: 177 us, most of it changes of items (207 where each warp
+// looked up its next item itself).
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -38,7 +42,8 @@ namespace {
 
 constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand tile
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
-constexpr int kStages = 3, kStageBytes = 2 * kKTile + kHalf;   // pages (K, V) as operands
+constexpr int kSegments = 4;                  // items that are found ahead
+constexpr int kStageBytes = 2 * kKTile + kHalf;   // a page (K, V) as operands
 constexpr float kGrow = 15.f;                // see above
 
 struct TileShape {
@@ -51,13 +56,19 @@ struct TileCfg {
   static constexpr int kRows = 128 * kT;
   static constexpr int kSoft = 8 * kT;                   // softmax warps 0 .. kSoft - 1, then 4 converters, then MMA
   static constexpr int kSoftThreads = 32 * kSoft;
-  static constexpr int kThreads = 32 * (kSoft + 8);      // whole warpgroups: MMA, scales, pages, cuts
+  static constexpr int kMma = kSoft + 4;                 // first warp behind them
+  static constexpr int kThreads = 32 * (kMma + 4);       // whole warpgroups: MMA, scales, pages, items
   // registers at launch, and how the warpgroups share them: softmax (2 kT groups), converters, MMA
   static constexpr int kRegs = kT == 2 ? 80 : 128;
   static constexpr int kRegsSoft = kT == 2 ? 88 : 152, kRegsConv = kT == 2 ? 80 : 128, kRegsMma = kT == 2 ? 48 : 80;
   static_assert(2 * kT * kRegsSoft + kRegsConv + kRegsMma <= (2 * kT + 2) * kRegs && kRegs * kThreads <= 65536,
                 "the shares are within what the block was launched with");
-  static constexpr int kRaw = kT == 2 ? 3 : 6;           // pages on their way as codes
+  // pages as operands, and on their way as codes (two tiles: a third way ahead is in the others' way, 239 us instead of 234 for
+  // 2048 rows over 32K)
+  static constexpr int kStages = kT == 2 ? 3 : 4, kRaw = kT == 2 ? 2 : 3;
+  static constexpr int kBuf = kT == 2 ? 2 : 4;           // buffers of S in TMEM
+  static constexpr int kO = kBuf * 64;                   // first column of O
+  static_assert(kT == 2 || kBuf == kStages, "see the converters");
   static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + kRaw * ARCKV_PAGE_BYTES + 1024;
   static_assert(kSmem + 4097 * 8 + 2048 <= 227 * 1024, "shared memory");
   // 32-bit words of a partial result: 64 outputs as f16, twice (ref, sum), and the unit, of each softmax thread
@@ -220,7 +231,7 @@ __device__ __forceinline__ int tile_steps(const TileShape& d, int len, int count
 struct Segment {
   long long first;         // unit at which the item begins
   int s, h, tile, step, count;   // from step `step` of `count`
-  int rows, row;           // rows (tokens) of the request, the first of them in the packed call
+  int rows, row, len;      // rows (tokens) of the request, the first of them in the packed call, its tokens
 };
 
 // The item of unit u: units run over requests (pre[s] of a head of the earlier ones), heads, row tiles, steps.
@@ -237,7 +248,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   const long long per = pre[lo + 1] - pre[lo], rest = u - pre[lo] * c.H, h = quotient(rest, per);
   g.h = (int)h;
   g.rows = tile_rows(d, starts, lo, g.row, stt);
-  const int len = pages_len(c, lo), lane = threadIdx.x & 31, tiles = (g.rows * d.G + rows - 1) / rows;
+  const int len = g.len = pages_len(c, lo), lane = threadIdx.x & 31, tiles = (g.rows * d.G + rows - 1) / rows;
   int at = (int)(rest - h * per);
   for (int t0 = 0;; t0 += 32) {   // the tile, 32 at a time
     const int mine = t0 + lane < tiles ? tile_steps(d, len, g.rows, t0 + lane, rows) : 0;
@@ -327,21 +338,23 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     pages_tiles_kernel(const arckv_pages4 c, TileShape d, const bf16* Q, PackedStrides qs, float scale, const int* starts, bf16* O,
                        PackedStrides os, float* parts, int4* cuts, DevStatus* stt) {
   using Cfg = TileCfg<kT>;
-  constexpr int kSoft = Cfg::kSoft, kRows = Cfg::kRows, kRaw = Cfg::kRaw;
+  constexpr int kSoft = Cfg::kSoft, kMma = Cfg::kMma, kRows = Cfg::kRows, kRaw = Cfg::kRaw, kStages = Cfg::kStages, kBuf = Cfg::kBuf;
   extern __shared__ unsigned char smraw[];
   unsigned char* sQ = smraw + ((1024u - (tc::smem_u32(smraw) & 1023u)) & 1023u);   // [tile][half][128][128 B]
   unsigned char* sKV = sQ + kT * 2 * kHalf;                                        // [stage][K halves, V]
   unsigned char* sRaw = sKV + kStages * kStageBytes;                               // [raw stage] page
   long long* pre = (long long*)(sRaw + kRaw * ARCKV_PAGE_BYTES);                   // [S + 1] pages of a head's tiles
-  // of buffer (parity of the tile's page) 0 and 1: S written, P written, P V done
-  __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][2], pfull[kT][2], odone[kT][2], drain;
+  // of each buffer of a tile: S written, P written, P V done
+  __shared__ __align__(8) uint64_t qfull, full[kStages], empty[kStages], sfull[kT][kBuf], pfull[kT][kBuf], odone[kT][kBuf], drain;
   __shared__ __align__(8) uint64_t raw_full[kRaw], raw_empty[kRaw], scaled[kRaw];
-  __shared__ Meta meta[2 * kStages];
+  constexpr int kMetas = kRaw + kStages;
+  __shared__ Meta meta[kMetas];   // of the pages that have come and are not done
   __shared__ Units units[kRaw];
   __shared__ int raw_page[kRaw];
   __shared__ uint32_t tmem_slot;
   __shared__ long long s_share[2];
-  __shared__ Segment s_first;
+  __shared__ __align__(8) uint64_t seg_full[kSegments], seg_empty[kSegments];
+  __shared__ Segment s_first, s_seg[kSegments];   // the CTA's first item; the later ones, in turn
   __shared__ int abort_flag, stop_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abortp = &abort_flag;
@@ -349,11 +362,11 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   if (tid == 0) {
     tc::mbar_init(&qfull, kSoft);
     for (int i = 0; i < kStages; ++i) {
-      tc::mbar_init(&full[i], 5);   // four converters and the scales
+      tc::mbar_init(&full[i], 4);   // converters
       tc::mbar_init(&empty[i], 1);
     }
     for (int t = 0; t < kT; ++t)
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kBuf; ++i) {
         tc::mbar_init(&sfull[t][i], 1);
         tc::mbar_init(&pfull[t][i], 8);
         tc::mbar_init(&odone[t][i], 1);
@@ -363,11 +376,15 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       tc::mbar_init(&raw_empty[i], 5);
       tc::mbar_init(&scaled[i], 1);
     }
+    for (int i = 0; i < kSegments; ++i) {
+      tc::mbar_init(&seg_full[i], 1);
+      tc::mbar_init(&seg_empty[i], kSoft + 3);   // softmax, MMA, scales, pages
+    }
     tc::mbar_init(&drain, 1);
     abort_flag = 0;
     tc::mbar_fence_init();
   }
-  if (warp == kSoft + 4) tc::tmem_alloc(&tmem_slot, 256 * kT);
+  if (warp == kMma) tc::tmem_alloc(&tmem_slot, 512);
   pdl_trigger();
   pdl_wait();
   for (int s = tid; s < c.S; s += Cfg::kThreads) {   // pages of one head's tiles of each request
@@ -413,32 +430,52 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = tmem_slot;   // tile t: two buffers of S / P at columns 256 t, O at 256 t + 128
+  const uint32_t tmem = tmem_slot;   // tile t: buffers of S / P from column 256 t on, O behind them
   const long long u0 = s_share[0], u1 = s_share[1];
-  auto next_segment = [&](long long u) { return segment_of(u, d, c, starts, pre, kRows, stt); };
+  // The CTA's item behind its k-th, which the last warp has found.
+  auto next_segment = [&](int k, Segment& g) {
+    const int at = k % kSegments;
+    const bool ok = __all_sync(0xffffffffu, tc::mbar_wait(&seg_full[at], (k / kSegments) & 1, abortp, stt));
+    if (ok) g = s_seg[at];
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&seg_empty[at]);
+    return ok;
+  };
   // whether the second tile of an item has rows
   auto both = [&](const Segment& g) { return kT == 2 && g.tile * kRows + 128 < g.rows * d.G; };
 
-  if (warp == kSoft + 7) {
-    // ------------------------ the item that begins here and goes on in other CTAs
+  if (warp == kMma + 3) {
+    // ------------- the CTA's items, ahead of the others; the one that begins here and goes on in other CTAs
     regs_dec<Cfg::kRegsMma>();
     int4 cut = make_int4(0, 0, -1, 0);
     if (u0 < u1) {
-      const CacheShares sh(pre[c.S] * c.H, gridDim.x);
       Segment g = s_first;
-      if (g.first + g.count < u1) g = next_segment(u1 - 1);
+      bool ok = true;
+      int k = 0;
+      for (long long u = g.first + g.count; u < u1; u = g.first + g.count, ++k) {
+        g = segment_of(u, d, c, starts, pre, kRows, stt);
+        const int at = k % kSegments;
+        if (k >= kSegments) ok = __all_sync(0xffffffffu, tc::mbar_wait(&seg_empty[at], ((k / kSegments) - 1) & 1, abortp, stt));
+        if (!ok) break;
+        if (lane == 0) {
+          s_seg[at] = g;
+          tc::mbar_arrive(&seg_full[at]);
+        }
+      }
+      const CacheShares sh(pre[c.S] * c.H, gridDim.x);
       const long long end = g.first + g.count;
-      if (end > u1 && g.first >= u0) cut = make_int4(g.s * c.H + g.h, g.tile, sh.owner(end - 1), 0);
+      if (ok && end > u1 && g.first >= u0) cut = make_int4(g.s * c.H + g.h, g.tile, sh.owner(end - 1), 0);
     }
     if (lane == 0) cuts[blockIdx.x] = cut;
-  } else if (warp == kSoft + 6) {
+  } else if (warp == kMma + 2) {
     // ---------------------------------------------------------------- pages
     regs_dec<Cfg::kRegsMma>();
     bool ok = true;
     int q = 0;   // pages issued
     Segment g = s_first;
+    int seg = 0;
     for (long long u = u0; u < u1 && ok;) {
-      const int n = (int)min((long long)(g.count - g.step), u1 - u), held = pages_of(pages_len(c, g.s));
+      const int n = (int)min((long long)(g.count - g.step), u1 - u), held = pages_of(g.len);
       int page = -1;
       for (int i = 0; i < n; ++i, ++q) {
         const int st = q % kRaw;
@@ -464,23 +501,23 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         __syncwarp();
       }
       u += n;
-      if (u < u1) g = next_segment(u);
+      if (u < u1 && ok) ok = next_segment(seg++, g);
     }
     if (!ok) {   // let the copies in flight land before the CTA's memory goes
       volatile int never = 0;
       for (int p = max(0, q - kRaw); p < q; ++p) tc::mbar_wait(&raw_full[p % kRaw], (p / kRaw) & 1, &never, stt);
     }
-  } else if (warp == kSoft + 5) {
+  } else if (warp == kMma + 1) {
     // ---------------------------------------------------------------- scales
     regs_dec<Cfg::kRegsMma>();
     bool ok = true;
-    int q = 0;
+    int q = 0, seg = 0;
     Segment g = s_first;
     for (long long u = u0; u < u1 && ok;) {
-      const int n = (int)min((long long)(g.count - g.step), u1 - u), len = pages_len(c, g.s);
+      const int n = (int)min((long long)(g.count - g.step), u1 - u), len = g.len;
       int eref = -1000;
       for (int i = 0; i < n && ok; ++i, ++q) {
-        const int st = q % kStages, rs = q % kRaw;
+        const int rs = q % kRaw;
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&raw_full[rs], (q / kRaw) & 1, abortp, stt));
         if (!ok) break;
         const int page = raw_page[rs], held = page < 0 ? 0 : min(kPT, max(0, len - (g.step + i) * kPT));
@@ -511,28 +548,24 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         m.undo = pow2(eref - ev);
         m.unit = pow2(eref + kDown);
         m.page = page;
-        if (lane == 0) {
+        if (lane == 0) {   // (the page has come, so the one kRaw before it is converted, and P V of the one kStages before that done)
+          meta[q % kMetas] = m;
           units[rs] = Units{pow2(-ek - kDown), pow2(-ev - kDown), held};
           tc::mbar_arrive(&scaled[rs]);
           tc::mbar_arrive(&raw_empty[rs]);
         }
-        if (q >= kStages) ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt));
-        if (ok && lane == 0) {
-          meta[q % (2 * kStages)] = m;
-          tc::mbar_arrive(&full[st]);
-        }
       }
       u += n;
-      if (u < u1) g = next_segment(u);
+      if (u < u1 && ok) ok = next_segment(seg++, g);
     }
-  } else if (warp == kSoft + 4) {
+  } else if (warp == kMma) {
     // ------------------------------------------------------------ MMA issuer
     regs_dec<Cfg::kRegsMma>();
     bool ok = true;
-    int st = 0, sp = 0, phase = 0;   // stages of this page and of the one before
-    int qt[kT];                      // pages of each tile so far
+    int st = 0, sp = 0, phase = 0;   // stages of the next page for S, for P V
+    int base[kT];                    // pages of each tile in earlier items
 #pragma unroll
-    for (int t = 0; t < kT; ++t) qt[t] = 0;
+    for (int t = 0; t < kT; ++t) base[t] = 0;
     // warp-wide reductions leave their result in uniform registers
     const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
     const uint64_t q_desc = tc::sdesc_k128(tc::smem_u32(sQ)), kv_desc = tc::sdesc_k128(tc::smem_u32(sKV));
@@ -550,41 +583,41 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             if (t < nt) {
-              mma_qk(tm + 256 * t + (qt[t] & 1) * 64, q_desc + t * (2 * kHalf >> 4), kv_desc + (st * kStageBytes >> 4), idesc_f16(64));
-              commit_elected(&sfull[t][qt[t] & 1]);
+              const int b = (base[t] + i) % kBuf;
+              mma_qk(tm + 256 * t + b * 64, q_desc + t * (2 * kHalf >> 4), kv_desc + (st * kStageBytes >> 4), idesc_f16(64));
+              commit_elected(&sfull[t][b]);
             }
+          }
+          if (++st == kStages) {
+            st = 0;
+            phase ^= 1;
           }
         }
         if (i > 0) {
 #pragma unroll
           for (int t = 0; t < kT; ++t) {
             if (t >= nt) break;
-            const int p = qt[t] - 1;
-            ok = __all_sync(0xffffffffu, ok && tc::mbar_wait(&pfull[t][p & 1], (p >> 1) & 1, abortp, stt));
+            const int p = base[t] + i - 1, b = p % kBuf;
+            ok = __all_sync(0xffffffffu, ok && tc::mbar_wait(&pfull[t][b], (p / kBuf) & 1, abortp, stt));
             if (!ok) break;
             tc::fence_after_sync();
-            mma_pv(tm + 256 * t + 128, tm + 256 * t + (p & 1) * 64, kv_desc + ((sp * kStageBytes + 2 * kKTile) >> 4), idesc_f16(128),
+            mma_pv(tm + 256 * t + Cfg::kO, tm + 256 * t + b * 64, kv_desc + ((sp * kStageBytes + 2 * kKTile) >> 4), idesc_f16(128),
                    i > 1);
-            commit_elected(&odone[t][p & 1]);
+            commit_elected(&odone[t][b]);
           }
           if (!ok) break;
-          commit_elected(&empty[sp]);
-        }
-        if (i < n) {
-          sp = st;
-          if (++st == kStages) {
-            st = 0;
-            phase ^= 1;
-          }
-#pragma unroll
-          for (int t = 0; t < kT; ++t)
-            if (t < nt) ++qt[t];
+          if (kT == 2) commit_elected(&empty[sp]);   // (of one tile, P V)
+          if (++sp == kStages) sp = 0;
         }
       }
+#pragma unroll
+      for (int t = 0; t < kT; ++t)
+        if (t < nt) base[t] += n;
       left -= n;
       u += n;
-      if (left > 0) {
-        const Segment next = next_segment(u);
+      if (left > 0 && ok) {
+        Segment next = {};
+        ok = next_segment(seg, next);
         steps = next.count - next.step;
         tiles = both(next) ? 2 : 1;
       }
@@ -611,7 +644,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const int st = q % kStages, rs = q % kRaw;
       bool ok = tc::mbar_wait(&scaled[rs], (q / kRaw) & 1, abortp, stt);
       if (ok) ok = tc::mbar_wait(&raw_full[rs], (q / kRaw) & 1, abortp, stt);   // (long done: for the copy's visibility)
-      if (ok && q >= kStages) ok = tc::mbar_wait(&empty[st], ((q / kStages) - 1) & 1, abortp, stt);
+      // (with one tile and as many stages as buffers, P V is done with both at once)
+      if (ok && q >= kStages) ok = tc::mbar_wait(kT == 1 ? &odone[0][st] : &empty[st], ((q / kStages) - 1) & 1, abortp, stt);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       const unsigned char* raw = sRaw + rs * ARCKV_PAGE_BYTES;
@@ -666,20 +700,20 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     regs_inc<Cfg::kRegsSoft>();
     const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;   // (a warp reaches the lanes of its quarter)
     const int r_warp = 16 * (warp & 7), cl = 2 * (lane & 3);
-    const uint32_t Sb = tmem + 256 * t + ((uint32_t)(quarter * 32 + half * 16) << 16), Ot = Sb + 128;
+    const uint32_t Sb = tmem + 256 * t + ((uint32_t)(quarter * 32 + half * 16) << 16), Ot = Sb + Cfg::kO;
     bool ok = true;
     // P V of page q is in O.  (The one before it, whose phase this could be taken for, is known to be: S of page
     // q + 1 was issued after it and has come in.)
     auto product_done = [&](int q) {
-      ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][q & 1], (q >> 1) & 1, abortp, stt));
+      ok = __all_sync(0xffffffffu, tc::mbar_wait(&odone[t][q % kBuf], (q / kBuf) & 1, abortp, stt));
       tc::fence_after_sync();
       return ok;
     };
-    int it = 0, all = 0;   // pages of this tile, of the CTA, in earlier items
+    int it = 0, all = 0, seg = 0;   // pages of this tile, of the CTA, in earlier items; their number
     Segment g = s_first;
     for (long long u = u0; u < u1;) {
       const int n = (int)min((long long)(g.count - g.step), u1 - u);
-      const int row0 = g.tile * kRows + t * 128, len = pages_len(c, g.s), nrows = g.rows * d.G;
+      const int row0 = g.tile * kRows + t * 128, len = g.len, nrows = g.rows * d.G;
       const bool idle = t == 1 && !both(g);
       const bf16* Qh = Q + g.row * qs.i + g.h * qs.h;
       // the products' factor (for powers of two without biases, of e with them) and sight of this thread's two rows
@@ -738,18 +772,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       const bool any_row = row0 + r_warp < nrows;
       for (int i = 0; i < n && !idle; ++i) {
         const int q = it + i, j0 = (g.step + i) * kPT + cl;
-        const uint32_t S = Sb + (q & 1) * 64;
-        // S is in, and with it the page's scales (written before `full`, which the MMA warp waited for)
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q & 1], (q >> 1) & 1, abortp, stt));
+        const uint32_t S = Sb + (q % kBuf) * 64;
+        // S is in, and with it the page's scales (written before the page was converted)
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(&sfull[t][q % kBuf], (q / kBuf) & 1, abortp, stt));
         if (!ok) break;
         if (!any_row) {   // (uniform)
-          if (lane == 0) tc::mbar_arrive(&pfull[t][q & 1]);
+          if (lane == 0) tc::mbar_arrive(&pfull[t][q % kBuf]);
           continue;
         }
         tc::fence_after_sync();
         float v[32];
         tmem_ld_rows64(S, v);
-        const Meta m = meta[(all + i) % (2 * kStages)];
+        const Meta m = meta[(all + i) % kMetas];
         // (never zero: a masked product is -inf)
         const float f = fmaxf(fac * m.ks, 0x1p-126f);
         unit = m.unit;
@@ -858,7 +892,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tmem_wait_st();
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&pfull[t][q & 1]);
+        if (lane == 0) tc::mbar_arrive(&pfull[t][q % kBuf]);
       }
       all += n;
       if (!idle) {
@@ -930,14 +964,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       }
       tc::fence_before_sync();
       u += n;
-      if (u < u1) g = next_segment(u);
+      if (u < u1 && !next_segment(seg++, g)) {   // a wait gave up: once to the barrier, as the others
+        if (tid == 0) stop_flag = *abortp;
+        asm volatile("bar.sync 1, %0;" ::"r"(Cfg::kSoftThreads) : "memory");
+        break;
+      }
     }
   }
   tc::fence_before_sync();
   __syncthreads();
-  if (warp == kSoft + 4) {
+  if (warp == kMma) {
     tc::fence_after_sync();
-    tc::tmem_dealloc(tmem, 256 * kT);
+    tc::tmem_dealloc(tmem, 512);
   }
 }
 
