@@ -35,7 +35,7 @@
 namespace arckv {
 namespace {
 
-constexpr int kRowsMax = 16;                 // rows of a head in this kernel
+constexpr int kRowsMax = 32;                 // rows of a request and head in this kernel
 constexpr int kRowO = 132;                   // floats of an output row in shared memory (four: rows in other banks)
 constexpr float kGrow = 8.f, kLift = 7.f;    // weights reach 2^15: the range of f16
 
@@ -137,24 +137,29 @@ __device__ __forceinline__ void bar_consumers(int threads) { asm volatile("bar.s
 
 // A run of pages of one item.
 struct Run {
-  int s, h;
+  int s, h, part;         // part: kR rows of the request's
   int blk, n;             // pages blk .. blk + n - 1 of the request
   int first, last;        // the takers that share the item
 };
 
 // The runs of a taker, in order: a CTA, which has one part of an item, or a warp, which has a share of all pages.
-// Items are numbered over requests, then heads; pre[s] are the pages (or parts) before request s of one head.
+// Items are numbered over requests, heads, then kR rows at a time; pre[s] are the pages (or parts) of one head before request s,
+// times as often as its rows want.
+template <int kR>
 struct Walk {
   const arckv_pages4& c;
   const int* pre;
   const int* known;       // [kKnown] first row, rows, tokens
+  const int* starts;
+  int G, N;
   bool parts;             // items are cut into equal parts
   int id;                 // of the taker
   int u, u1;              // parts: this CTA's part of all; else units (pages) of its share
   int q, r;               // shares: q units each, one more for the first r takers
 
-  __device__ Walk(const arckv_pages4& c, const int* pre, const int* known, bool parts, int id, int takers)
-      : c(c), pre(pre), known(known), parts(parts), id(id) {
+  __device__ Walk(const arckv_pages4& c, const int* pre, const int* known, const int* starts, int G, int N, bool parts,
+                  int id, int takers)
+      : c(c), pre(pre), known(known), starts(starts), G(G), N(N), parts(parts), id(id) {
     const int total = pre[c.S] * c.H;
     // a page a taker, or shares of two at least (64 x 300 tokens: 13.5 us, 14.6 with shares of one and two)
     const int n = max(1, total <= takers ? total : min(takers, total - total / 2));
@@ -176,9 +181,19 @@ struct Walk {
       else hi = mid;
     }
     p.s = lo;
-    const int cut = pre[lo + 1] - pre[lo], rest = u - pre[lo] * c.H;
-    p.h = rest / cut;
-    const int k = rest - p.h * cut;
+    const int span = pre[lo + 1] - pre[lo], rest = u - pre[lo] * c.H;
+    p.h = rest / span;
+    int cut = span, k = rest - p.h * span;
+    p.part = 0;
+    if (kR > 8) {
+      const int first = lo < kKnown ? 0 : min(max(starts[lo], 0), N);
+      const int rows = (lo < kKnown ? known[3 * lo + 1] : min(max(starts[lo + 1], first), N) - first) * G;
+      if (rows > kR) {
+        cut = span / ((rows + kR - 1) / kR);
+        p.part = k / cut;
+        k -= p.part * cut;
+      }
+    }
     if (parts) {
       const int nb = max(1, pages_of(p.s < kKnown ? known[3 * p.s + 2] : pages_len(c, p.s)));
       p.blk = (int)((long long)nb * k / cut);
@@ -245,7 +260,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       int run = 0;
       for (int s0 = 0; s0 < c.S; s0 += 32) {
         const int s = s0 + lane;
-        int x = 0;
+        int x = 0, rows = 0;
         if (s < c.S) {
           int first, n, len;
           if (cut > 0 && s < kKnown) {
@@ -260,9 +275,12 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
             known[3 * s + 2] = len;
           }
           if (n > 0) x = max(1, pages_of(len));
+          rows = n;
         }
-        if (cut == 0) items += __popc(__ballot_sync(0xffffffffu, x > 0));
+        const int times = x > 0 ? (rows * d.G + kR - 1) / kR : 0;
+        if (cut == 0) items += __reduce_add_sync(0xffffffffu, times);
         if (cut > 0 && x > 0) x = max(1, min((x + cut - 1) / cut, x / kPartMin));
+        x *= times;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -294,7 +312,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   const bool parts_mode = s_cut > 0;
   // Warps of the launch are numbered over CTAs first, so that few of them are spread over the SMs.
   auto walk_of = [&](int w) {
-    return Walk(c, pre, known, parts_mode, parts_mode ? (int)blockIdx.x : w * (int)gridDim.x + (int)blockIdx.x,
+    return Walk<kR>(c, pre, known, starts, d.G, d.N, parts_mode, parts_mode ? (int)blockIdx.x : w * (int)gridDim.x + (int)blockIdx.x,
                 (int)gridDim.x * (parts_mode ? 1 : kW));
   };
 
@@ -304,7 +322,7 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     // slowest warp held up the others' pages: 104 us instead of 97 for 64 x 8K).
     const bool feeds = lane < kW;
     constexpr int kOwn = Cfg::kOwn;
-    Walk walk = walk_of(min(lane, kW - 1));
+    Walk<kR> walk = walk_of(min(lane, kW - 1));
     Run p;
     int i = 0, issued = 0, entry = -1, held = 0;
     const int step = parts_mode ? kW : 1;   // the warps of a CTA with a part take its pages in turn
@@ -379,14 +397,14 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
   const int g = lane >> 2, t = lane & 3;
   constexpr int kT = Cfg::kTiles, kMt = 4 / kT;   // tiles, and 16s of tokens of a pass
   const int step = parts_mode ? kW : 1;
-  Walk walk = walk_of(warp);
+  Walk<kR> walk = walk_of(warp);
   int taken = 0;                 // pages so far
   bool ok = true;
   Run p;
   while (ok && walk.next(p)) {
     int first, count, len;
     request(p.s, first, count, len);
-    const int n = p.n, h = p.h, nrows = count * d.G;
+    const int n = p.n, h = p.h, row0 = kR * p.part, nrows = min(kR, count * d.G - row0);
     // query rows: column n is row n of the tile
     uint32_t qf[kT][8][2];
     // what a token's least values multiply beside the codes' sums: the sum of a group's elements as two bf16, row g, group t, and
@@ -396,8 +414,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
     int see[kT][2], see_min = 0x7fffffff; // tokens that they see
 #pragma unroll
     for (int tt = 0; tt < kT; ++tt) {
-      const int r = 8 * tt + g, i = r / d.G;
-      const bf16* mine = Q + (first + i) * qs.i + h * qs.h + (r - i * d.G) * 128;
+      const int r = 8 * tt + g, i = (row0 + r) / d.G;
+      const bf16* mine = Q + (first + i) * qs.i + h * qs.h + (row0 + r - i * d.G) * 128;
       uint4 x[4];
       float amax = 0.f;
 #pragma unroll
@@ -730,8 +748,8 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
         for (int k = 0; k < 2; ++k) {
           const int r = 8 * tt + 2 * t + k;
           if (r >= nrows) continue;   // (a tile without rows masks nothing: it may have met anything behind the end)
-          const int i = r / d.G;
-          bf16* to = O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + g;
+          const int i = (row0 + r) / d.G;
+          bf16* to = O + (first + i) * os.i + h * os.h + (row0 + r - i * d.G) * 128 + g;
           const float inv = l[tt][k] == 0.f ? 0.f : 1.f / l[tt][k];
           bool fine = true;
 #pragma unroll
@@ -770,9 +788,9 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       const float inv = z == 0.f ? 0.f : 1.f / z;
       v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
       if (r >= nrows) return;
-      const int i = r / d.G;
+      const int i = (row0 + r) / d.G;
       __nv_bfloat162 y[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-      *(uint2*)(O + (first + i) * os.i + h * os.h + (r - i * d.G) * 128 + dim) = *(const uint2*)&y[0];
+      *(uint2*)(O + (first + i) * os.i + h * os.h + (row0 + r - i * d.G) * 128 + dim) = *(const uint2*)&y[0];
       if (!(fabsf(v.x) <= kBig && fabsf(v.y) <= kBig && fabsf(v.z) <= kBig && fabsf(v.w) <= kBig))
         set_status(stt, ARCKV_ERR_NONFINITE);
     };
@@ -853,22 +871,31 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
 
 }  // namespace
 
-size_t pages_attend_scratch(int, int, int, int max_count, int G) {
+// Whether requests of so many rows of a head are all for pages_rows_kernel.  Up to 32: its items are 16 rows, whose pages' second
+// reading L2 serves, and a change of items costs it next to nothing (32 rows, 250 x 8 x up to 500: 116 us, where the kernel for many
+// rows takes 176; 20 rows, 64 x 8 x up to 8192: 225 and 264; 32 over one request of 300: 8.9 and 13.6), while their units are numbers of 31 bits.
+static bool few_rows(int S, int H, int M, long long rows) {
+  return rows <= 16 || (rows <= kRowsMax && (long long)S * H * M < (1LL << 30));
+}
+
+size_t pages_attend_scratch(int S, int H, int M, int max_count, int G) {
   // partial results of CTAs, or of the warps of each
   const long long all = (long long)max_count * G;
-  const int slots = all > 8 && all <= kRowsMax ? 2 * RowsCfg<16, false>::kW : kWarpsMost;
-  const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(kRowsMax * 132, slots * kTileSlot) * sizeof(float);
-  return (long long)max_count * G > kRowsMax ? std::max(rows, pages_tiles_scratch((long long)max_count * G)) : rows;
+  const bool few = few_rows(S, H, M, all);
+  const int slots = all > 8 && few ? 2 * RowsCfg<16, false>::kW : kWarpsMost;
+  const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(16 * 132, slots * kTileSlot) * sizeof(float);
+  return few ? rows : std::max(rows, pages_tiles_scratch(all));
 }
 
 int launch_pages_attend(const arckv_pages4& p, const PagesQuery& q, float scale, void* ws, cudaStream_t st) {
   const long long rows = (long long)q.max_count * q.G;
-  // Beside requests of more rows, those of 9 to 16 go with them (a mixed batch of one chunk and 16 single tokens: 115 us with
+  const bool few = few_rows(p.S, p.H, p.M, rows);
+  // Beside requests of more rows, those of 9 and more go with them (a mixed batch of one chunk and 16 single tokens: 115 us with
   // 16 rows a request here)
-  const int limit = (int)std::min<long long>(rows, rows <= kRowsMax ? kRowsMax : 8);
+  const int limit = few ? (int)rows : (int)std::min(rows, 8LL);
   const int n = limit <= 8 ? (p.bias ? launch_rows<8, true>(p, q, scale, limit, ws, st) : launch_rows<8, false>(p, q, scale, limit, ws, st))
                            : (p.bias ? launch_rows<16, true>(p, q, scale, limit, ws, st) : launch_rows<16, false>(p, q, scale, limit, ws, st));
-  if (n < 0 || rows <= kRowsMax) return n;
+  if (n < 0 || few) return n;
   const int more = launch_pages_tiles(p, q, scale, limit, ws, st);
   return more < 0 ? -1 : n + more;
 }

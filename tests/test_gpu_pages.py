@@ -435,7 +435,7 @@ def test_a_long_request(n):
 
 
 @pytest.mark.parametrize("bias", [False, True])
-@pytest.mark.parametrize("G", [2, 3, 5])
+@pytest.mark.parametrize("G", [2, 3, 5, 10])
 def test_a_long_request_among_many_short_ones(G, bias):
     """Shares of all pages: a request's end, the next ones' whole and another's beginning; rows of both tiles or of one."""
     S, H = 60, 4
