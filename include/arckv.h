@@ -542,6 +542,8 @@ size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32
  *      records ARCKV_ERR_SHAPE
  *   O  out bf16, addressed as Q with o_strides; rows do not overlap.  Rows of no
  *      request are left as they are.
+ * ARCKV_ERR_SHAPE at once for calls too long to be counted: H M (N G / R + S) from
+ * 2^38 on, with R = 128 (256 where max_count G > 128).
  * Softmax weights and sums are fp32; weights, and with many rows keys and values,
  * enter the products as f16 (2^-11 of each), where an output's rounding to bf16
  * takes 2^-8.  Pages that

@@ -46,6 +46,9 @@ struct PagesQuery {
   PackedStrides os;
 };
 
+// Rows of a row tile of the many-row kernel where a request has up to `rows` rows of a head.
+inline int pages_tile_rows(long long rows) { return rows <= 128 ? 128 : 256; }
+
 // ---- launchers (each returns the kernels it enqueued, or -1) ---------------
 int launch_pages_extend(const arckv_pages4& p, const int* counts, int N, int* starts, int* slots, int* positions,
                         cudaStream_t st);

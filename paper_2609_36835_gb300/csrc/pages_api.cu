@@ -47,6 +47,12 @@ bool attend_ok(int32_t S, int32_t H, int32_t M, int32_t max_count, int32_t G) {
   return sizes_ok(S, H, M) && max_count >= 1 && max_count <= (1 << 24) && G >= 1 && G <= (1 << 12) &&
          (long long)max_count * G < (1LL << 28);
 }
+// A CTA counts the pages of its share in 31 bits; the many-row kernel has one CTA on each of 128 SMs at least.  (A share that
+// long is a call of half an hour.)
+bool shares_ok(const arckv_pages4& p, int32_t N, int32_t G, int32_t max_count) {
+  const double rows = pages_tile_rows((long long)max_count * G);
+  return (double)p.H * p.M * ((double)N * G / rows + p.S) < 128.0 * 2147483648.0;
+}
 
 }  // namespace
 
@@ -118,7 +124,8 @@ arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int
   if (flags & ~(ARCKV_FLAG_NONBLOCKING | ARCKV_FLAG_CAUSAL)) return ARCKV_ERR_INVALID_ARG;
   const arckv_status e = check_pages(p);
   if (e != ARCKV_OK) return e;
-  if (N < 1 || N >= (1 << 30) || !attend_ok(p->S, p->H, p->M, max_count, G)) return ARCKV_ERR_SHAPE;
+  if (N < 1 || N >= (1 << 30) || !attend_ok(p->S, p->H, p->M, max_count, G) || !shares_ok(*p, N, G, max_count))
+    return ARCKV_ERR_SHAPE;
   PagesQuery q;
   if (!Q || !O || !starts || misaligned(starts, 4) ||
       !packed_strides(Q, q_strides, (int64_t)p->H * G * 128, (int64_t)G * 128, 2, &q.qs) ||

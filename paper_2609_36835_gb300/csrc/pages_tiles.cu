@@ -249,7 +249,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   g.h = (int)h;
   g.rows = tile_rows(d, starts, lo, g.row, stt);
   const int len = g.len = pages_len(c, lo), lane = threadIdx.x & 31, tiles = (g.rows * d.G + rows - 1) / rows;
-  int at = (int)(rest - h * per);
+  long long at = rest - h * per;   // (a head's tiles times its pages: up to 2^40; 32 tiles have 2^25 steps at most)
   for (int t0 = 0;; t0 += 32) {   // the tile, 32 at a time
     const int mine = t0 + lane < tiles ? tile_steps(d, len, g.rows, t0 + lane, rows) : 0;
     int x = mine;
@@ -262,7 +262,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
     if (past) {
       const int w = __ffs(past) - 1;
       g.count = __shfl_sync(0xffffffffu, mine, w);
-      g.step = at - (__shfl_sync(0xffffffffu, x, w) - g.count);
+      g.step = (int)at - (__shfl_sync(0xffffffffu, x, w) - g.count);
       g.tile = t0 + w;
       break;
     }
@@ -1108,11 +1108,11 @@ int launch_tiles(const arckv_pages4& p, const PagesQuery& q, float scale, int ab
 }  // namespace
 
 size_t pages_tiles_scratch(long long rows) {
-  return kCacheMaxCtas * (2 * (rows <= 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot) * sizeof(float) + sizeof(int4));
+  return kCacheMaxCtas * (2 * (pages_tile_rows(rows) == 128 ? TileCfg<1>::kSlot : TileCfg<2>::kSlot) * sizeof(float) + sizeof(int4));
 }
 
 int launch_pages_tiles(const arckv_pages4& p, const PagesQuery& q, float scale, int above, void* ws, cudaStream_t st) {
-  if ((long long)q.max_count * q.G <= 128)   // one tile where it holds all rows
+  if (pages_tile_rows((long long)q.max_count * q.G) == 128)   // one tile where it holds all rows
     return p.bias ? launch_tiles<1, true>(p, q, scale, above, ws, st) : launch_tiles<1, false>(p, q, scale, above, ws, st);
   return p.bias ? launch_tiles<2, true>(p, q, scale, above, ws, st) : launch_tiles<2, false>(p, q, scale, above, ws, st);
 }
