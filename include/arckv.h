@@ -410,6 +410,8 @@ size_t arckv_cache_workspace_bytes(int32_t S, int32_t H, int32_t cap, int32_t d,
  *      only ones that position p of head h reads (arckv_cache_select writes
  *      them; distinct, in any order, -1 for none; an index past the cache
  *      records ARCKV_ERR_INVALID_ARG and is passed over)
+ * Without blocks, calls too long to be counted are refused (ARCKV_ERR_SHAPE):
+ * S H (n_pos G / 256 + 1) cap / 64 from 2^38 on.
  */
 arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G, float logit_scale, const void* Q,
                                 const int64_t* q_strides, const int32_t* blocks, int32_t m, float* O,

@@ -127,6 +127,9 @@ arckv_status arckv_cache_attend(const arckv_cache8* c, int32_t n_pos, int32_t G,
   // blocks read in all are counted in 32 bits
   if (blocks && (m < 1 || m > c->cap / kCB + 8192 || (long long)c->S * c->H * n_pos * ((G + 3) / 4) * m >= (1LL << 31)))
     return ARCKV_ERR_SHAPE;
+  // without them a CTA counts its share of a head's row tiles times its blocks in 31 bits (the kernel of many rows has one CTA
+  // on each of 128 SMs at least; a share that long is a call of half an hour)
+  if (!blocks && (double)c->S * c->H * ((double)n_pos * G / 256 + 1) * (c->cap / kCB) >= 128.0 * 2147483648.0) return ARCKV_ERR_SHAPE;
   if (!(logit_scale >= 0.f) || !isfinite(logit_scale)) return ARCKV_ERR_INVALID_ARG;
   const float scale = logit_scale > 0.f ? logit_scale : 1.0f / sqrtf((float)c->d);
   cudaGetLastError();

@@ -245,7 +245,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
   const long long per = pre[lo + 1] - pre[lo], rest = u - pre[lo] * d.H, h = quotient(rest, per);
   g.sh = (long long)lo * d.H + h;
   const int len = cache_len(c, lo), lane = threadIdx.x & 31;
-  int at = (int)(rest - h * per);
+  long long at = rest - h * per;   // (a head's tiles times its blocks: past 31 bits in the longest calls; 32 tiles have 2^25 steps)
   for (int t0 = 0;; t0 += 32) {   // the tile, 32 at a time
     const int mine = t0 + lane < d.tiles ? tile_steps(d, len, t0 + lane, rows) : 0;
     int x = mine;
@@ -258,7 +258,7 @@ __device__ __forceinline__ Segment segment_of(long long u, const TileShape& d, c
     if (past) {
       const int w = __ffs(past) - 1;
       g.count = __shfl_sync(0xffffffffu, mine, w);
-      g.step = at - (__shfl_sync(0xffffffffu, x, w) - g.count);
+      g.step = (int)at - (__shfl_sync(0xffffffffu, x, w) - g.count);
       g.tile = t0 + w;
       break;
     }
