@@ -879,12 +879,12 @@ static bool few_rows(int S, int H, int M, long long rows) {
 }
 
 size_t pages_attend_scratch(int S, int H, int M, int max_count, int G) {
-  // partial results of CTAs, or of the warps of each
+  // partial results of CTAs, or of the warps of each: of 7 warps with two tiles, or 11 with one.  A workspace serves calls of fewer
+  // rows too, so the size never falls as rows become more.
   const long long all = (long long)max_count * G;
-  const bool few = few_rows(S, H, M, all);
-  const int slots = all > 8 && few ? 2 * RowsCfg<16, false>::kW : kWarpsMost;
+  const int slots = all > 8 ? std::max(2 * RowsCfg<16, false>::kW, kWarpsMost) : kWarpsMost;
   const size_t rows = (size_t)2 * kCacheMaxCtas * std::max(16 * 132, slots * kTileSlot) * sizeof(float);
-  return few ? rows : std::max(rows, pages_tiles_scratch(all));
+  return few_rows(S, H, M, all) ? rows : std::max(rows, pages_tiles_scratch(all));
 }
 
 int launch_pages_attend(const arckv_pages4& p, const PagesQuery& q, float scale, void* ws, cudaStream_t st) {

@@ -30,3 +30,15 @@ def test_a_heads_pages_are_counted_in_64_bits():
     tokens have 2^31.  (Narrowed, a step is negative, and the table is read in front of its beginning.)"""
     body = re.search(r"Segment segment_of\(.*?\n}\n", (CSRC / "pages_tiles.cu").read_text(), re.S).group(0)
     assert re.search(r"long long at = rest - h \* per;", body) and "int at" not in body
+
+
+@pytest.mark.parametrize("S,H,M", [(4, 8, 128), (1, 1, 1), (4096, 8, 60), (4096, 16, 20000)])
+def test_a_workspace_serves_calls_of_fewer_rows(lib, S, H, M):
+    """The size never falls as max_count or the query heads of a KV head become more."""
+    size = lambda most, G: lib.arckv_pages_attend_workspace_bytes(S, H, M, 128, most, G)
+    for G in (1, 2, 3, 4, 8, 9, 16, 33, 128):
+        sizes = [size(most, G) for most in list(range(1, 140)) + [255, 256, 257, 1000, 100000]]
+        assert sizes[0] > 0 and sizes == sorted(sizes)
+    for most in (1, 2, 3, 4, 5, 8, 16, 32, 33, 128, 129):
+        sizes = [size(most, G) for G in range(1, 140)]
+        assert sizes == sorted(sizes)
