@@ -71,7 +71,7 @@ struct TileCfg {
   static_assert(kT == 2 || kBuf == kStages, "see the converters");
   static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + kRaw * ARCKV_PAGE_BYTES + 1024;
   static_assert(kSmem + 4097 * 8 + 2048 <= 227 * 1024, "shared memory");
-  // 32-bit words of a partial result: 64 outputs as f16, twice (ref, sum), and the unit, of each softmax thread
+  // 32-bit words of a partial result: 64 outputs as f16, of two rows (ref, sum) and what a unit stands for, of each softmax thread
   static constexpr int kSlot = 40 * kSoftThreads;
 };
 
@@ -914,10 +914,36 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const int q1 = q0 + 8;
         const long long at0 = (g.row + q0 / d.G) * os.i + (q0 % d.G) * 128, at1 = (g.row + q1 / d.G) * os.i + (q1 % d.G) * 128;
         const float inv0 = l[0] == 0.f ? 0.f : 1.f / l[0], inv1 = l[1] == 0.f ? 0.f : 1.f / l[1];
-        // A part goes to memory divided by its sum, as f16 in O's units, in which it is 2^-6 at most: half a step is 2^-11 of a
-        // part, and parts as fp32 took twice the time to write and read (half of them 13.8 us to join)
+        // A part goes to memory divided by its sum, as f16 (parts as fp32 took twice the time to write and read, half of them
+        // 13.8 us to join).  Each row is taken in a power of two of its own that leaves its largest element in [2^14, 2^15): half a
+        // step is 2^-11 of an element, down to 2^-28 of the row's largest.  (O's units would not do: they follow the largest value,
+        // and the mean of thousands of values lies far below it.)
         float* slot = parts + (2ll * blockIdx.x + (g.step == 0 ? 1 : 0)) * Cfg::kSlot + tid * 4;
         if (any_row) {
+          float2 up = make_float2(inv0, inv1), down = make_float2(unit, unit);
+          if (!whole) {
+            float most[2] = {0.f, 0.f};
+#pragma unroll 1
+            for (int ch = 0; ch < 4; ++ch) {
+              float v[16];
+              tmem_ld_rows32(Ot + ch * 32, v);
+              tmem_wait_ld();
+              settle(v);
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) most[(e >> 1) & 1] = max3(most[(e >> 1) & 1], fabsf(v[e]), fabsf(v[e + 1]));
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float a = most[k] * (k ? inv1 : inv0);
+              a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+              a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+              const int e_unit = (int)(__float_as_uint(unit) >> 23) - 127;
+              // (what a part's elements stand for stays a multiple of 2^-126)
+              const int ex = min(max((int)(__float_as_uint(a) >> 23) - 127, max(-100, -112 - e_unit)), 127);
+              (k ? up.y : up.x) *= pow2(14 - ex);
+              (k ? down.y : down.x) *= pow2(ex - 14);
+            }
+          }
 #pragma unroll 1
           for (int ch = 0; ch < 4; ++ch) {
             float v[16];
@@ -949,8 +975,8 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
                 __half2 y[4];
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
-                  const float inv = f & 1 ? inv1 : inv0;
-                  y[f] = __floats2half2_rn(v[8 * e + 2 * f] * inv, v[8 * e + 2 * f + 1] * inv);
+                  const float by = f & 1 ? up.y : up.x;
+                  y[f] = __floats2half2_rn(v[8 * e + 2 * f] * by, v[8 * e + 2 * f + 1] * by);
                 }
                 __stcg((uint4*)(slot + (long long)(ch * 2 + e) * Cfg::kSoftThreads * 4), *(const uint4*)&y[0]);
               }
@@ -958,7 +984,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
           }
           if (!whole) {   // joined by the kernel behind this one
             __stcg((float4*)(slot + 8ll * Cfg::kSoftThreads * 4), make_float4(ref[0], l[0], ref[1], l[1]));
-            __stcg(slot + 9ll * Cfg::kSoftThreads * 4, unit);
+            __stcg((float2*)(slot + 9ll * Cfg::kSoftThreads * 4), down);
           }
         }
       }
@@ -1033,7 +1059,7 @@ __global__ void __launch_bounds__(kJoinThreads) pages_join_kernel(int H, TileSha
     load(0);
     {   // weights of the parts for row tid / 16, sixteen parts at a time
       const int r = tid >> 4, l16 = tid & 15;
-      const long long at = 8ll * Cfg::kSoftThreads * 4 + (r & 7) * 16 + (r >> 3) * 2, unit = 9ll * Cfg::kSoftThreads * 4 + (r & 7) * 16;
+      const long long at = 8ll * Cfg::kSoftThreads * 4 + (r & 7) * 16 + (r >> 3) * 2, unit = 9ll * Cfg::kSoftThreads * 4 + (r & 7) * 16 + (r >> 3);
       float top = -INFINITY;
       float2 mine = make_float2(-INFINITY, 0.f);   // of the first sixteen parts
       if (l16 < n) mine = __ldcg((const float2*)(part(l16) + at));

@@ -1,0 +1,82 @@
+"""How far outputs of the paged cache's attention are off, row by row, where single elements say little: attention spread over
+thousands of tokens, whose outputs are far smaller than the values, values and queries of very different sizes side by side.
+
+The error of a row is the norm of its difference from the plain form in 64 bits (over what the pages hold), relative to the
+row's norm.  An output is a bf16: half a step is 2^-8 of an element, so 2^-8 of the norm at most.  Every rounding before it
+(weights 2^-11; values 2^-11, in units of their page twice 2^-25, 2^-10 of an ordinary value beside one 2^6 to 2^7 larger; parts
+of an item 2^-11; keys, which move a logit x by 2^-11 of sum |q k|) is independent of the others over thousands of
+tokens, so that their norms add up in squares: below 2^-9 in all."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages4 as ref
+import paper_2609_36835_gb300 as pk
+
+pytestmark = pytest.mark.gpu
+SC = 1.0 / np.sqrt(128.0)
+BOUND = 2.0 ** -8 + 2.0 ** -9
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu(lib):
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    torch.cuda.set_device(0)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=gen(seed))
+
+
+def host(x):
+    return x.detach().float().cpu().numpy()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def pages_of(k, v, bias=None):
+    """Pages of one request that hold k, v [T, H, 128] and biases [T, H]."""
+    T, H, _ = k.shape
+    p = pk.pages_alloc(1, H, -(-T // 64), T, bias=bias is not None)
+    _, slots, _ = pk.pages_extend(p, i32([T]), T)
+    pk.pages_append(p, k.cuda(), v.cuda(), slots, bias=None if bias is None else bias.cuda())
+    return p
+
+
+def errors(O, Q, k, v, bias=None, rows=None, dims=slice(None), causal=True):
+    """Relative errors of the (listed) rows of O [n, H, G, 128] over the given dims."""
+    n, H, G, _ = O.shape
+    T, out = len(k), []
+    for h in range(H):
+        K, V = ref.held_rows(host(k[:, h]), host(v[:, h]))
+        for i in range(n) if rows is None else rows:
+            sees = [T - n + 1 + i if causal else T] * G
+            want = ref.attend(host(Q[i, h]), K, V, SC, sees, None if bias is None else host(bias[:, h]))[0][:, dims]
+            diff = host(O[i, h]).astype(np.float64)[:, dims] - want
+            out.append(np.linalg.norm(diff, axis=1) / np.linalg.norm(want, axis=1))
+    return np.concatenate(out)
+
+
+def attend(p, Q, n, **kw):
+    return pk.pages_attend(p, Q, i32([0, n]), max_count=n, **kw)
+
+
+ORDINARY = [i for i in range(128) if i != 7]
+
+
+@pytest.mark.parametrize("outlier", [1, 16, 64])
+@pytest.mark.parametrize("n,T", [(40, 8192), (40, 32768), (300, 8192), (300, 32768)])
+def test_spread_attention_of_many_rows(n, T, outlier):
+    """Items that many CTAs share; one channel of the values larger than the others, which are the ones that count."""
+    k, v = randn(T, T, 2, 128), randn(T + 1, T, 2, 128)
+    v[..., 7] *= outlier
+    Q = (randn(n, n, 2, 1, 128) * 0.05).bfloat16().cuda()
+    O = attend(pages_of(k, v), Q, n)
+    assert errors(O, Q, k, v, rows=range(0, n, max(1, n // 20)), dims=ORDINARY).max() <= BOUND
