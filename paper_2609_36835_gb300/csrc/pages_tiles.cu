@@ -70,7 +70,7 @@ struct TileCfg {
   static constexpr int kO = kBuf * 64;                   // first column of O
   static_assert(kT == 2 || kBuf == kStages, "see the converters");
   static constexpr int kSmem = kT * 2 * kHalf + kStages * kStageBytes + kRaw * ARCKV_PAGE_BYTES + 1024;
-  static_assert(kSmem + 4097 * 8 + 2048 <= 227 * 1024, "shared memory");
+  static_assert(kSmem + 4097 * 8 + 4 * kSoftThreads + 2048 <= 227 * 1024, "shared memory");
   // 32-bit words of a partial result: 64 outputs as f16, of two rows (ref, sum) and what a unit stands for, of each softmax thread
   static constexpr int kSlot = 40 * kSoftThreads;
 };
@@ -356,6 +356,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
   __shared__ __align__(8) uint64_t seg_full[kSegments], seg_empty[kSegments];
   __shared__ Segment s_first, s_seg[kSegments];   // the CTA's first item; the later ones, in turn
   __shared__ int abort_flag, stop_flag;
+  __shared__ uint32_t s_beyond[Cfg::kSoftThreads];   // a softmax thread's own: what its two rows' products are short of, as powers of two
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abortp = &abort_flag;
 
@@ -719,12 +720,15 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       // the products' factor (for powers of two without biases, of e with them) and sight of this thread's two rows
       float fac = 0.f;
       int see[2];
+      bool far = false;   // see below
       if (!idle) {
         // This warp's 16 queries as f16, scaled by a power of two that leaves the largest element of all in [2^14, 2^15): a bf16
         // is exact down to 2^-31 of it, and next to nothing below 2^-39.  16 lanes have a row, two rows at a time.
+        // Where some four dims of a row are all 2^-12 of that or less, each row gets a power of its own, so that what one row
+        // holds, however large or not finite, is nothing to the others.  (A change of items waits for its code, some 20 ns an
+        // instruction: powers for each row in every case took 686 us for 8192 positions, 657 with this.)
         uint4 x[8];
         int row = row0 + r_warp + (lane >> 4), i = row / d.G, gq = row - i * d.G;
-        uint32_t amax = 0u;   // magnitudes of two elements, as integers
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = make_uint4(0u, 0u, 0u, 0u);
@@ -736,14 +740,53 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
             ++i;
           }
         }
+        auto largest = [](const uint4& y) {   // magnitudes of four even and four odd elements, as integers
+          return __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu));
+        };
+        auto exponent = [](uint32_t m) { return min(max((int)(m >> 7) - 127, -100), 127); };
+        uint32_t amax = 0u, amin = 0u;   // of all fours; and of the smallest that is not zero, 0x8000 less it
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t y[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) amax = __vmaxu2(amax, y[k] & 0x7fff7fffu);
+          const uint32_t m = largest(x[e]);
+          amax = __vmaxu2(amax, m);
+          amin = __vmaxu2(amin, (0x80008000u - m) & 0x7fff7fffu);
         }
         amax = __reduce_max_sync(0xffffffffu, max(amax & 0xffffu, amax >> 16));
-        const int ex = min(max((int)(amax >> 7) - 127, -100), 127);
+        amin = __reduce_max_sync(0xffffffffu, max(amin & 0xffffu, amin >> 16));
+        int ex = exponent(amax);
+        far = (int)(amax + amin) > 0x8000 + (12 << 7);
+        s_beyond[tid] = 0u;
+        if (far) {   // (rare) all rows to the smallest one's power; their products get the rest, 2^beyond, when they come
+          ex = 1000;
+          uint32_t own = 0u;   // largest magnitudes of rows lane / 4 and lane / 4 + 8
+#pragma unroll 1
+          for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              uint32_t m = largest(x[e]);
+              m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+              for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+              if (pass == 0) {
+                const uint32_t y = __shfl_sync(0xffffffffu, m, (lane & 4) << 2);
+                if (lane >> 3 == (e & 3)) own |= y << (e < 4 ? 0 : 16);
+                ex = min(ex, (int)__reduce_min_sync(0xffffffffu, m ? exponent(m) : 1000));
+              } else {   // (in two steps: each power is within fp32's normal range)
+                const int by = m ? ex - exponent(m) : 0;
+                const float by0 = pow2(by / 2), by1 = pow2(by - by / 2);
+                uint32_t y[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const __nv_bfloat162 z = __floats2bfloat162_rn(bf16_lo(y[k]) * by0 * by1, bf16_hi(y[k]) * by0 * by1);
+                  y[k] = *(const uint32_t*)&z;
+                }
+                x[e] = make_uint4(y[0], y[1], y[2], y[3]);
+              }
+            }
+          }
+          const uint32_t o0 = own & 0xffffu, o1 = own >> 16;
+          s_beyond[tid] = (o0 ? exponent(o0) - ex : 0) | (o1 ? exponent(o1) - ex : 0) << 16;
+        }
         const float up = pow2(14 - ex);
         fac = pow2(ex - 14) * scale * (kBias ? 1.f : kLog2e);
         const int c16 = lane & 15;   // chunk of 8 dims
@@ -766,7 +809,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const int row = row0 + r_warp + (lane >> 2) + 8 * i;
         see[i] = row < nrows ? row_sees(d.causal, len, g.rows, row / d.G) : 0;
       }
-      const int see_min = __reduce_min_sync(0xffffffffu, min(see[0], see[1]));
+      const int see_min = far ? 0 : __reduce_min_sync(0xffffffffu, min(see[0], see[1]));   // (zero: every page has an edge)
       // references of O (with biases the logit), sums of weights
       float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, unit = 1.f;
       const bool any_row = row0 + r_warp < nrows;
@@ -790,6 +833,18 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         tmem_wait_ld();
         settle(v);
         const bool edge = j0 - cl + kPT > see_min || m.page < 0;
+        if (edge && s_beyond[tid] != 0u) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int by = (int)(s_beyond[tid] >> (16 * k) & 0xffffu);
+            const float by0 = pow2(by / 2), by1 = pow2(by - by / 2);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[4 * j + 2 * k] = v[4 * j + 2 * k] * by0 * by1;
+              v[4 * j + 2 * k + 1] = v[4 * j + 2 * k + 1] * by0 * by1;
+            }
+          }
+        }
         if (kBias && m.page >= 0) {   // logits
           const float* bias = c.bias + ((long long)m.page * c.H + g.h) * kPT + cl;
 #pragma unroll

@@ -80,3 +80,22 @@ def test_spread_attention_of_many_rows(n, T, outlier):
     Q = (randn(n, n, 2, 1, 128) * 0.05).bfloat16().cuda()
     O = attend(pages_of(k, v), Q, n)
     assert errors(O, Q, k, v, rows=range(0, n, max(1, n // 20)), dims=ORDINARY).max() <= BOUND
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan"), 2.0 ** 60, 2.0 ** -60])
+@pytest.mark.parametrize("n", [2, 12, 40, 300])
+def test_a_row_is_nothing_to_the_others(n, bad):
+    """A row that holds an infinity, a NaN or an element far from the others' size: the other rows are what they are without it."""
+    T = 1000
+    k, v = randn(1, T, 2, 128), randn(2, T, 2, 128)
+    p, Q = pages_of(k, v), randn(3, n, 2, 4, 128).bfloat16()
+    ws, plain = pk.pages_workspace(p, n, 4), attend(p, Q.cuda(), n)
+    Q[1, 0, 2], Q[n // 2, 1, 3, 9] = bad, bad
+    O = attend(p, Q.cuda(), n, ws=ws, check=False)
+    status = pk.arckv_query_status(ws)
+    assert status == (5 if not np.isfinite(bad) else 0) or bad > 1
+    keep = torch.ones(n, 2, 4, dtype=torch.bool)
+    keep[1, 0, 2] = keep[n // 2, 1, 3] = False
+    assert torch.equal(O[keep], plain[keep])
+    if bad < 1:                                              # (a row of next to nothing sees all tokens alike)
+        assert errors(O, Q, k, v, rows=[1, n // 2]).max() <= BOUND
