@@ -21,10 +21,11 @@
 // 2^-11 of an element, an eighth of what the bf16 outputs round to, and elements below 2^-8 of the largest are off by up to
 // 2^-17 of it.  K's unit goes into the factor of its page's logits.  V's goes into the exponent of the weights:
 //   w_j = 2^{x_j - ref + ev - eref},  O = 2^eref sum_j w_j v_j 2^-ev / sum_b 2^{eref - ev} sum_{j in b} w_j
-// where eref is at least every ev so far (when it grows, O is scaled down, as for a maximum that grows) and ev at least
-// eref - 20: a page of smaller values has them as f16 below the normal range, off by 2^-36 of the largest at most.
+// where eref is at least every page's ev and at most 6 above it: O, whose fp32 sums have the range, is scaled whenever the values'
+// size leaves that, up or down (down as far as 2^-60 of the largest size met; what lies below that counts as zero).  With a unit that
+// only grew, pages behind one of values 2^20 times theirs lost 0.16 of their output, whether or not that one had any weight.
 // Weights enter as one f16, 2^-11 of each, and ref follows the running maximum only when that has grown by more than 15: to
-// scale O is to wait for its products, and with 8 some warp of a tile did on most pages (512 positions over 8K 97 us, 91 now;
+// scale O is to wait for its products, and with 8 some warp of a tile did on most pages (512 positions over 8K 97 us, 91 then;
 // one jump a row, of its own token, is common).  Weights then reach 2^15, and lose bits where they are below 2^-12 of the
 // page's largest.  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
 //
@@ -516,7 +517,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
     Segment g = s_first;
     for (long long u = u0; u < u1 && ok;) {
       const int n = (int)min((long long)(g.count - g.step), u1 - u), len = g.len;
-      int eref = -1000;
+      int eref = -1000, largest_ref = -1000;
       for (int i = 0; i < n && ok; ++i, ++q) {
         const int rs = q % kRaw;
         ok = __all_sync(0xffffffffu, tc::mbar_wait(&raw_full[rs], (q / kRaw) & 1, abortp, stt));
@@ -539,11 +540,15 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         const int ek = min(max((int)(k >> 23) - 127, -100), 70), own = min(max((int)(v >> 23) - 127, -100), 70);
         Meta m;
         m.shrink = 1.f;
-        if (own > eref) {   // two bits of room, so that few pages raise it
-          if (i > 0) m.shrink = pow2(eref - own - 2);
-          eref = own + 2;
+        // two bits of room, so that few pages raise it; where a page needs less than 2^-6 of it, it follows down, as far as O's
+        // range goes (values of zero need nothing)
+        if (own > eref || (own < eref - 6 && v != 0u)) {
+          const int to = max(own + 2, largest_ref - 60);
+          if (i > 0) m.shrink = pow2(eref - to);
+          eref = to;
+          largest_ref = max(largest_ref, eref);
         }
-        const int ev = max(own, eref - 20);
+        const int ev = max(own, eref - 6);
         m.ks = pow2(ek + kDown);
         m.dv = (float)(ev - eref);
         m.undo = pow2(eref - ev);

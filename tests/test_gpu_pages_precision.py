@@ -99,3 +99,42 @@ def test_a_row_is_nothing_to_the_others(n, bad):
     assert torch.equal(O[keep], plain[keep])
     if bad < 1:                                              # (a row of next to nothing sees all tokens alike)
         assert errors(O, Q, k, v, rows=[1, n // 2]).max() <= BOUND
+
+
+def requests(S, k, v, n, bias=None):
+    """Pages of S requests that hold k, v [T, H, 128] and biases [T, H] each, and starts of n rows for each: with as many items as SMs
+    none is cut into many parts, which would each see little of what the others do."""
+    T, H, _ = k.shape
+    p = pk.pages_alloc(S, H, S * -(-T // 64), T, bias=bias is not None)
+    _, slots, _ = pk.pages_extend(p, i32([T] * S), S * T)
+    pk.pages_append(p, k.cuda().repeat(S, 1, 1), v.cuda().repeat(S, 1, 1), slots, bias=None if bias is None else bias.cuda().repeat(S, 1))
+    return p, i32([n * s for s in range(S + 1)])
+
+
+def check_requests(S, k, v, Q, bound, bias=None):
+    """Q [n, H, G, 128], the same for every request."""
+    n = len(Q)
+    p, starts = requests(S, k, v, n, bias)
+    O = pk.pages_attend(p, Q.cuda().repeat(S, 1, 1, 1), starts, max_count=n)
+    for s in (0, S // 3, S - 1):
+        e = errors(O[s * n:(s + 1) * n], Q, k, v, bias, rows=range(0, n, max(1, n // 5)))
+        assert e.max() <= bound, (s, e.max())
+
+
+@pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 20, 2.0 ** 40, 2.0 ** -20])
+@pytest.mark.parametrize("n,H", [(40, 8), (300, 4)])
+def test_values_behind_a_page_of_another_size(n, H, size):
+    """The first page's values are larger (or smaller) and have next to no weight.  Behind it the peak is a token whose value is zero;
+    the others of its page, 2^-6 of its weight each, are the output, and then pages 2^-12 of it."""
+    T = 640
+    k, v, b = randn(1, T, H, 128), randn(2, T, H, 128), torch.zeros(T, H)
+    v[:64] *= size
+    v[64] = 0.0
+    b[:64], b[64], b[128:] = -100.0, 6 * np.log(2.0), -6 * np.log(2.0)
+    check_requests(40, k, v, (randn(3, n, H, 1, 128) * 0.05).bfloat16(), BOUND, b)
+    # the same without biases: by one dimension of the keys, whose rounding to f16, twice, moves logits of up to 4.2 by 2^-10 of them
+    k[..., 0] = SC ** -1 / 16 * b
+    k[:64, :, 1:] = 0.0
+    q = randn(4, n, H, 1, 128) * 0.05
+    q[..., 0] = 16.0
+    check_requests(40, k, v, q.bfloat16(), BOUND + 2.0 ** -10 * 5)
