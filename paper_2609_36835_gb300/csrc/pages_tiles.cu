@@ -20,14 +20,16 @@
 // A key or value m + c s enters the products as f16, in units of a power of two near its page's largest: half a step is
 // 2^-11 of an element, an eighth of what the bf16 outputs round to, and elements below 2^-8 of the largest are off by up to
 // 2^-17 of it.  K's unit goes into the factor of its page's logits.  V's goes into the exponent of the weights:
-//   w_j = 2^{x_j - ref + ev - eref},  O = 2^eref sum_j w_j v_j 2^-ev / sum_b 2^{eref - ev} sum_{j in b} w_j
+//   w_j = 2^{x_j - ref + 7 + ev - eref},  O = 2^eref sum_j w_j v_j 2^-ev / sum_b 2^{eref - ev} sum_{j in b} w_j
 // where eref is at least every page's ev and at most 6 above it: O, whose fp32 sums have the range, is scaled whenever the values'
 // size leaves that, up or down (down as far as 2^-60 of the largest size met; what lies below that counts as zero).  With a unit that
 // only grew, pages behind one of values 2^20 times theirs lost 0.16 of their output, whether or not that one had any weight.
-// Weights enter as one f16, 2^-11 of each, and ref follows the running maximum only when that has grown by more than 15: to
-// scale O is to wait for its products, and with 8 some warp of a tile did on most pages (512 positions over 8K 97 us, 91 then;
-// one jump a row, of its own token, is common).  Weights then reach 2^15, and lose bits where they are below 2^-12 of the
-// page's largest.  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
+// Weights enter as one f16, 2^-11 of each down to 2^-15 of ref's (2^-26 of ref's weight below, where values are 2^-6 of the unit),
+// so that what lies 20 nats below an early token still counts.  They begin at 2^7 and reach 2^15: ref follows the running maximum
+// when that has grown by more than 8, and then for all rows that have grown by more than 1, as to scale O is to wait for
+// its products.  (Room below costs what jumps of 8 to 15 cost: from one on, 8192 positions 660 us, 695 from 2^7, 706 if rows
+// follow by themselves; but 16 nats below a token of no value 0.3 to 0.7 of the output were lost, 4e-3 now, most of which is
+// the keys' rounding.)  The pipe's fp32 sums round towards zero: O shrinks by 7e-8 a page.
 //
 // Bound by shared memory, which the N = 64 products of S read Q from once a page, and by the softmax's issue (a page and 256
 // rows take 0.93 us, of which the pipe needs 0.54; steps of two pages with one buffer of S took longer, 295 us against 237;
@@ -45,7 +47,7 @@ constexpr int kHalf = 128 * 128;              // bytes of a 128 x 64 f16 operand
 constexpr int kKTile = 64 * 128;              // of a 64 x 64 one
 constexpr int kSegments = 4;                  // items that are found ahead
 constexpr int kStageBytes = 2 * kKTile + kHalf;   // a page (K, V) as operands
-constexpr float kGrow = 15.f;                // see above
+constexpr float kGrow = 8.f, kLift = 7.f, kFollow = 1.f;   // see above
 
 struct TileShape {
   int G, N, above, max_count;   // requests of more than `above` rows of a head
@@ -898,7 +900,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
               const float to = kBias ? top[k] : top[k] * f;
               // what the sums shrink by, as a power of two
               const float by = ref[k] == -INFINITY ? -INFINITY : kBias ? (ref[k] - to) * kLog2e : ref[k] - to;
-              if (to != -INFINITY && -by > kGrow) {
+              if (to != -INFINITY && -by > kFollow) {
                 const float x = ex2_approx(by);
                 alpha[k] *= x;
                 l[k] *= x;
@@ -923,7 +925,7 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
         float2 base[2], add[2], sum[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float b = ref[k] == -INFINITY ? 0.f : ref[k], a = (kBias ? 0.f : -b) + m.dv;
+          const float b = ref[k] == -INFINITY ? 0.f : ref[k], a = (kBias ? 0.f : -b) + m.dv + kLift;
           base[k] = make_float2(-b, -b);
           add[k] = make_float2(a, a);
           sum[k] = make_float2(0.f, 0.f);

@@ -121,6 +121,21 @@ def check_requests(S, k, v, Q, bound, bias=None):
         assert e.max() <= bound, (s, e.max())
 
 
+@pytest.mark.parametrize("nats", [8, 12, 16])
+@pytest.mark.parametrize("n,H", [(1, 8), (12, 8), (40, 8), (300, 4)])
+def test_what_lies_far_below_a_token_of_no_value(n, H, nats):
+    """An attention sink: its weight is e^nats of another token's, its value zero, so that the others are the output.  Keys as f16
+    (many rows) move its logit, sum q k > 0, by 2^-11 of it twice, for their least values and for themselves, and so the sum."""
+    T = 4096
+    k, v = randn(1, T, H, 128) * 0.3, randn(2, T, H, 128) + 1.0
+    d = torch.sign(randn(3, H, 128)) / 128 ** 0.5
+    k -= (k * d).sum(-1, keepdim=True) * d
+    k[0], v[0] = d * 8, 0.0
+    q = randn(4, n, H, 1, 128) * 0.05
+    q += (nats / 8 / SC - (q * d[:, None]).sum(-1, keepdim=True)) * d[:, None]
+    check_requests(40, k, v, q.bfloat16(), BOUND + 2 * nats * 2.0 ** -11)
+
+
 @pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 20, 2.0 ** 40, 2.0 ** -20])
 @pytest.mark.parametrize("n,H", [(40, 8), (300, 4)])
 def test_values_behind_a_page_of_another_size(n, H, size):
