@@ -22,8 +22,8 @@
 //    requests of up to 1000 tokens.)  With fewer items they are cut into equal parts, a CTA each, whose warps take pages in
 //    turn.  An item in several places is finished by the one that comes last (a ticket), which adds the parts up in order.
 //  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
-//    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow
-//    without limit from page to page: the output is then scaled down, as for a maximum that grows.
+//    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow or
+//    shrink from page to page: the output is then scaled, as for a maximum that grows.
 //
 // Bound by HBM and by the warps at once: a page is 860 instructions with one tile of 8 rows, 320 of
 // them the shifts and masks, and some 1330 with two.
@@ -599,8 +599,13 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
           }
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
-          if (most > v_ref) {   // (uniform) a larger unit: between two and four times the scale, so that few pages raise it
-            const float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23)), by = v_ref / to;
+          // (uniform) another unit: between two and four times the scale, so that few pages raise it, and again where a page needs less
+          // than 2^-8 of it (one that only grew lost the pages behind larger values, whether or not those had weight).  Sums have
+          // fp32's range, which it leaves below 2^-30: down from there it does not follow.
+          if (most > v_ref || (most < v_ref * 0x1p-8f && most > 0.f && v_ref > 0x1p-30f)) {
+            float to = __uint_as_float((__float_as_uint(most) & 0x7f800000u) + (2u << 23));
+            if (most < v_ref) to = fmaxf(to, 0x1p-30f);
+            const float by = v_ref / to;
 #pragma unroll
             for (int tt = 0; tt < kT; ++tt)
 #pragma unroll

@@ -137,7 +137,7 @@ def test_what_lies_far_below_a_token_of_no_value(n, H, nats):
 
 
 @pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 20, 2.0 ** 40, 2.0 ** -20])
-@pytest.mark.parametrize("n,H", [(40, 8), (300, 4)])
+@pytest.mark.parametrize("n,H", [(1, 8), (12, 8), (40, 8), (300, 4)])
 def test_values_behind_a_page_of_another_size(n, H, size):
     """The first page's values are larger (or smaller) and have next to no weight.  Behind it the peak is a token whose value is zero;
     the others of its page, 2^-6 of its weight each, are the output, and then pages 2^-12 of it."""
