@@ -550,7 +550,9 @@ size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32
  * enter the products as f16 (2^-11 of each), where an output's rounding to bf16
  * takes 2^-8.  Pages that
  * the table names past the pool record ARCKV_ERR_INVALID_ARG and are passed over,
- * as are missing ones.  Outputs that are not finite record ARCKV_ERR_NONFINITE.
+ * as are missing ones.  Outputs that are not finite record ARCKV_ERR_NONFINITE, and
+ * so do logits that pass 2^22 in magnitude as a row's largest (of pages without biases):
+ * fp32 holds their differences no more, and the row may hold anything.
  */
 arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int32_t max_count, float logit_scale,
                                 const void* Q, const int64_t* q_strides, const int32_t* starts, void* O,

@@ -17,6 +17,7 @@ constexpr int kPageV = 4096, kPageKp = 8192, kPageVp = 9216;
 constexpr float kScaleFloor = 7.888609052210118e-31f;   // 2^-100: least scale, so that 1 / s stays finite
 constexpr float kInv15 = 0.06666667014360428f;          // fl(1 / 15)
 constexpr float kPagesMost = 1.8446744073709552e19f;     // 2^64: largest magnitude held, so that sums of 2^41 values times weights stay finite
+constexpr float kLogitMost = 8388608.f;                  // 2^23: largest logit times log2 e that a reference of the softmax may take
 static_assert(kPageVp + kPT * 4 == ARCKV_PAGE_BYTES && ARCKV_PAGE_BYTES % 16 == 0, "a page is copied in one piece");
 
 __host__ __device__ inline int page_v_word(int pair, int g, int i) {   // byte offset of word i of chunk g

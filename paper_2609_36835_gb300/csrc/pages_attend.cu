@@ -669,6 +669,14 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
       if (lane == 0) tc::mbar_arrive(&empty[st]);
     }
     // ---- the run's end
+    if (!kBias) {   // (a product is exact in its difference from the reference, which is rounded: by half of a power of two at most up to here)
+      float most = 0.f;
+#pragma unroll
+      for (int tt = 0; tt < kT; ++tt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) most = fmaxf(most, mx[tt][k] == -INFINITY ? 0.f : fabsf(mx[tt][k]));
+      if (most > kLogitMost) set_status(stt, ARCKV_ERR_NONFINITE);
+    }
 #pragma unroll
     for (int tt = 0; tt < kT; ++tt) {
 #pragma unroll

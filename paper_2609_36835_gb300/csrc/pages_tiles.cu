@@ -966,6 +966,9 @@ __global__ void __launch_bounds__(TileCfg<kT>::kThreads, 1)
       if (stop_flag) break;
       if (!idle) {
         const bool whole = g.step == 0 && n == g.count;
+        // (a product is exact in its difference from the reference, which is rounded: by half of a power of two at most up to here)
+        if (!kBias && ((fabsf(ref[0]) > kLogitMost && ref[0] != -INFINITY) || (fabsf(ref[1]) > kLogitMost && ref[1] != -INFINITY)))
+          set_status(stt, ARCKV_ERR_NONFINITE);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
