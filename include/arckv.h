@@ -500,6 +500,8 @@ arckv_status arckv_pages_extend(const arckv_pages4* p, const int32_t* counts, in
  * pages behind them back, such that an extension and this call that takes it
  * back leave the free list as it was.  A request with lens[s] < 0 or past its
  * length is left as it is and records ARCKV_ERR_INVALID_ARG.
+ * Pages that the table lacks (entries below zero) are not given back, nor are
+ * entries past the pool, which record ARCKV_ERR_INVALID_ARG.
  */
 arckv_status arckv_pages_truncate(const arckv_pages4* p, const int32_t* lens, uint32_t flags, void* stream);
 

@@ -85,7 +85,8 @@ class Tables:
             if not 0 <= to <= self.len[s]:
                 continue
             for j in range(-(-int(to) // PAGE), -(-int(self.len[s]) // PAGE)):
-                back.append(int(self.table[s, j]))
+                if 0 <= self.table[s, j] < self.P:           # (a page that is missing is not given back)
+                    back.append(int(self.table[s, j]))
                 self.table[s, j] = -1
             self.len[s] = to
         self.free += back[::-1]

@@ -175,13 +175,53 @@ __global__ void __launch_bounds__(kTT) pages_truncate_kernel(const arckv_pages4 
   __syncthreads();
   const int total = (int)min(block_scan(S, [&](int s) { return back[s]; }, before, 0x7fffffff), (long long)0x7fffffff);
   const int room = p.P - n_free;   // more pages than the pool has are not given back (a damaged table)
-  if (tid == 0 && total > room) set_status(stt, ARCKV_ERR_INVALID_ARG);
-  const int n = min(total, room);
-  for (int k = tid; k < total; k += kTT) {
+  auto entry_of = [&](int k) {
     const int s = last_at(before, S, k);
-    int* entry = p.table + (long long)s * p.M + keep[s] + k - before[s];
-    if (k < n) p.free[n_free + n - 1 - k] = *entry;
-    *entry = -1;
+    return p.table + (long long)s * p.M + keep[s] + k - before[s];
+  };
+  // Entries without a page of the pool are passed over.  They are rare: all are looked at first, a thread's first one kept.
+  int first = -1, held = 0;
+  bool rare = total > room;
+  for (int k = tid; k < total; k += kTT) {
+    const int page = *entry_of(k);
+    if (k == tid) first = page;
+    if (page >= p.P) set_status(stt, ARCKV_ERR_INVALID_ARG);
+    if (page >= 0 && page < p.P) ++held;
+    else rare = true;
+  }
+  if (!__syncthreads_or(rare)) {
+    for (int k = tid; k < total; k += kTT) {
+      int* entry = entry_of(k);
+      p.free[n_free + total - 1 - k] = k == tid ? first : *entry;
+      *entry = -1;
+    }
+    if (tid == 0) p.n_free[0] = n_free + total;
+    return;
+  }
+  __shared__ int s_held, s_warp[kTT / 32];
+  if (tid == 0) s_held = 0;
+  __syncthreads();
+  atomicAdd(&s_held, held);
+  __syncthreads();
+  const int n = min(s_held, room), lane = tid & 31, warp = tid >> 5;
+  if (tid == 0 && s_held > room) set_status(stt, ARCKV_ERR_INVALID_ARG);
+  int done = 0;   // pages of earlier rounds
+  for (int k0 = 0; k0 < total; k0 += kTT) {
+    const int k = k0 + tid;
+    int* entry = k < total ? entry_of(k) : nullptr;
+    const int page = entry ? *entry : -1;
+    const bool held_one = page >= 0 && page < p.P;
+    const unsigned int mine = __ballot_sync(0xffffffffu, held_one);
+    if (lane == 0) s_warp[warp] = __popc(mine);
+    __syncthreads();
+    int at = done + __popc(mine & ((1u << lane) - 1u));
+    for (int w = 0; w < kTT / 32; ++w) {
+      if (w < warp) at += s_warp[w];
+      done += s_warp[w];
+    }
+    if (held_one && at < n) p.free[n_free + n - 1 - at] = page;
+    if (entry) *entry = -1;
+    __syncthreads();
   }
   if (tid == 0) p.n_free[0] = n_free + n;
 }

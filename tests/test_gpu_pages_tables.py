@@ -1,0 +1,84 @@
+"""Page tables of the paged cache in states that a run of extensions does not make: missing pages, entries past the pool, requests
+that do not fit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages4 as ref
+import paper_2609_36835_gb300 as pk
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu(lib):
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    torch.cuda.set_device(0)
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def same_tables(p, t):
+    assert p.table.tolist() == t.table.tolist() and p.len.tolist() == t.len.tolist()
+    n = int(p.n_free[0])
+    assert p.free[:n].tolist() == [int(x) for x in t.free]
+
+
+@pytest.mark.parametrize("S,M,longest,gone", [(1, 4, 256, 1), (3, 5, 300, 2), (40, 40, 2560, 9), (300, 9, 500, 60), (7, 300, 19000, 500)])
+def test_missing_pages_are_not_given_back(S, M, longest, gone):
+    """More than a round of 512 entries among them; then an extension that takes every page there is."""
+    g = np.random.default_rng(S)
+    lens = g.integers(1, longest + 1, S)
+    P = int((-(-lens // 64)).sum()) + 5
+    p, t = pk.pages_alloc(S, 1, P, M * 64), ref.Tables(S, M, P)
+    pk.pages_extend(p, i32(lens.tolist()), int(lens.sum()))
+    t.extend(lens, int(lens.sum()))
+    for _ in range(gone):
+        s = int(g.integers(S))
+        j = int(g.integers(-(-lens[s] // 64)))
+        t.table[s, j] = -1
+        p.table[s, j] = -1
+    to = np.where(g.random(S) < 0.5, 0, (lens * g.random(S)).astype(int))
+    pk.pages_truncate(p, i32(to.tolist()))                   # (raises where something is recorded: nothing is)
+    t.truncate(to)
+    same_tables(p, t)
+    free = p.free[:int(p.n_free[0])]
+    assert int(free.min()) >= 0 and len(free.unique()) == len(free)
+    pk.pages_truncate(p, i32([0] * S))
+    t.truncate([0] * S)
+    same_tables(p, t)
+    counts = [min(64 * M, 64 * len(t.free))] + [0] * (S - 1)
+    for got, want in zip(pk.pages_extend(p, i32(counts), counts[0]), t.extend(counts, counts[0])):
+        assert got.tolist() == list(want)
+    same_tables(p, t)
+
+
+def test_entries_past_the_pool_are_recorded_and_not_given_back():
+    p, t = pk.pages_alloc(2, 1, 9, 256), ref.Tables(2, 4, 9)
+    pk.pages_extend(p, i32([200, 130]), 330)
+    t.extend([200, 130], 330)
+    for s, j, page in ((0, 1, 9), (1, 2, 10 ** 6), (0, 3, -1)):
+        t.table[s, j] = page
+        p.table[s, j] = page
+    pk.pages_truncate(p, i32([64, 0]), check=False)
+    t.truncate([64, 0])
+    assert pk.arckv_query_status(p.state) == 1
+    same_tables(p, t)
+
+
+def test_a_length_whose_pages_are_nearly_all_missing():
+    """As many entries as the pool has no room for, of which one is a page."""
+    p, t = pk.pages_alloc(1, 1, 4, 640), ref.Tables(1, 10, 4)
+    pk.pages_extend(p, i32([10]), 10)
+    t.extend([10], 10)
+    p.table[0, 7], p.table[0, 0] = p.table[0, 0].clone(), -1
+    t.table[0, 7], t.table[0, 0] = t.table[0, 0], -1
+    p.len.fill_(640)
+    t.len[0] = 640
+    pk.pages_truncate(p, i32([0]))
+    t.truncate([0])
+    same_tables(p, t)
+    assert int(p.n_free[0]) == 4
