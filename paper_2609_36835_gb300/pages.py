@@ -140,7 +140,10 @@ def _raise_for(st: int, entry: str) -> None:
 def pages_extend(pages: Pages4, counts, n_rows: int, *, stream=None, check: bool = True):
     """Make room for counts[s] (int32 [S]) new tokens of every request.  Returns starts [S + 1], the first row of each
     request among the call's packed n_rows rows, and for each row its slot and its position [n_rows]; rows behind the last
-    request have -1.  A request that does not fit (table, pool or rows) is left as it is, with slots of -1.
+    request have -1.  A request that does not fit (table, pool or rows) is left as it is, with slots of -1; it keeps its rows
+    in starts, and what ``pages_attend`` writes there means nothing.  The others are extended all the same: the error that
+    this raises then has the three results as its `rows` (to go on with those that fit, or to take them back with
+    ``pages_truncate``).
     With check=False the call only enqueues, and ``arckv_query_status(pages.state)`` reports errors."""
     import torch
     c, dev = pages._c, pages.data.device
@@ -154,10 +157,20 @@ def pages_extend(pages: Pages4, counts, n_rows: int, *, stream=None, check: bool
     i32 = torch.int32   # (half of the call's host time; new_empty takes twice as long, one allocation cut in three too)
     starts = torch.empty((c.S + 1,), dtype=i32, device=dev)
     slots, positions = torch.empty((n_rows,), dtype=i32, device=dev), torch.empty((n_rows,), dtype=i32, device=dev)
-    _raise_for(pages._entry("arckv_pages_extend")(
+    st = pages._entry("arckv_pages_extend")(
         pages._ref, counts_ptr, n_rows, starts.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-        0 if check else _pk.FLAG_NONBLOCKING, _pk._current_handle(dev)), "arckv_pages_extend")
+        0 if check else _pk.FLAG_NONBLOCKING, _pk._current_handle(dev))
+    if st != 0:
+        error = _pk.ArckvError(st, "arckv_pages_extend")
+        error.rows = (starts, slots, positions) if check and st in (1, 2) and _sound(c) else None
+        raise error
     return starts, slots, positions
+
+
+def _sound(c: _Pages4) -> bool:
+    """Whether the library takes these pages at all: an error of a call on them was then found by its kernel."""
+    sizes = _pk.load_library().arckv_pages_attend_workspace_bytes(c.S, c.H, c.M, c.d, 1, 1) > 0 and 1 <= c.P <= 1 << 24
+    return sizes and not any((getattr(c, n) or 0) % to for n, to in (("data", 16), ("bias", 16), ("state", 256)))
 
 
 def pages_truncate(pages: Pages4, lens, *, stream=None, check: bool = True) -> None:

@@ -82,3 +82,20 @@ def test_a_length_whose_pages_are_nearly_all_missing():
     t.truncate([0])
     same_tables(p, t)
     assert int(p.n_free[0]) == 4
+
+
+def test_an_extension_that_does_not_fit_hands_its_rows_over():
+    """The requests that fit are extended, and the error has what the call returned: on with them, or back to where they were."""
+    p, t = pk.pages_alloc(3, 1, 6, 256), ref.Tables(3, 4, 6)
+    pk.pages_extend(p, i32([60, 200, 10]), 270)
+    t.extend([60, 200, 10], 270)
+    before = p.len.clone()
+    with pytest.raises(pk.ArckvError) as e:
+        pk.pages_extend(p, i32([3, 100, 2]), 105)
+    for got, want in zip(e.value.rows, t.extend([3, 100, 2], 105)):
+        assert got.tolist() == list(want)
+    same_tables(p, t)
+    assert e.value.code == 2 and p.len.tolist() == [63, 200, 12]
+    pk.pages_truncate(p, before)
+    t.truncate(before.tolist())
+    same_tables(p, t)

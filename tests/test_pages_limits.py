@@ -42,3 +42,29 @@ def test_a_workspace_serves_calls_of_fewer_rows(lib, S, H, M):
     for most in (1, 2, 3, 4, 5, 8, 16, 32, 33, 128, 129):
         sizes = [size(most, G) for G in range(1, 140)]
         assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("code,S,rows", [(2, 3, True), (1, 3, True), (7, 3, False), (2, 5000, False)])
+def test_an_error_found_by_the_extensions_kernel_has_its_rows(lib, monkeypatch, code, S, rows):
+    """(the library is a stand-in but for its sizes; 5000 requests it refuses before it runs)"""
+    import types
+
+    import torch
+
+    import paper_2609_36835_gb300 as pk
+    real = pk.load_library()
+    stand_in = types.SimpleNamespace(arckv_pages_extend=lambda *args: code, arckv_status_string=real.arckv_status_string,
+                                     arckv_pages_attend_workspace_bytes=real.arckv_pages_attend_workspace_bytes)
+    monkeypatch.setattr(pk, "load_library", lambda: stand_in)
+    monkeypatch.setattr(pk, "_on_one_cuda_device", lambda **tensors: None)
+    monkeypatch.setattr(pk, "_current_handle", lambda device: 11)
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 1)
+    room = torch.zeros(1024, dtype=torch.uint8)
+    state = room[-room.data_ptr() % 256:][:256]
+    i32 = lambda *shape: torch.zeros(*shape, dtype=torch.int32)
+    p = pk.Pages4(data=torch.zeros(4, 2, pk.PAGE_BYTES, dtype=torch.uint8), table=i32(S, 4), len=i32(S), free=i32(4), n_free=i32(1), state=state)
+    with pytest.raises(pk.ArckvError) as e:
+        pk.pages_extend(p, i32(S), 7)
+    assert e.value.code == code and (e.value.rows is not None) == rows
+    if rows:
+        assert [len(x) for x in e.value.rows] == [S + 1, 7, 7]
