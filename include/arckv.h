@@ -489,8 +489,10 @@ typedef struct {
  * 0 <= N < 2^30.  A request whose new length passes 64 M, whose rows pass N, or
  * that the free pages do not suffice for (then every later one that needs a page
  * too) is left as it is: its rows have slots and positions of -1, and
- * ARCKV_ERR_SHAPE is recorded.  A negative count is taken as zero and records
- * ARCKV_ERR_INVALID_ARG.
+ * ARCKV_ERR_SHAPE is recorded; the others are extended all the same.  It keeps its rows
+ * in starts.  arckv_pages_attend takes them for its newest tokens, which they are
+ * not: what it writes there means nothing, and its own status tells nothing of it.
+ * A negative count is taken as zero and records ARCKV_ERR_INVALID_ARG.
  */
 arckv_status arckv_pages_extend(const arckv_pages4* p, const int32_t* counts, int32_t N, int32_t* starts, int32_t* slots,
                                 int32_t* positions, uint32_t flags, void* stream);

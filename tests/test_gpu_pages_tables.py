@@ -99,3 +99,30 @@ def test_an_extension_that_does_not_fit_hands_its_rows_over():
     pk.pages_truncate(p, before)
     t.truncate(before.tolist())
     same_tables(p, t)
+
+
+@pytest.mark.parametrize("n", [2, 12, 40])
+def test_a_request_that_did_not_fit_leaves_the_others_right(n):
+    """Its rows are attended over as well, to no purpose; those of the others are what they are without it."""
+    H, G = 2, 4
+    p = pk.pages_alloc(3, H, 9, 256)
+    gen = torch.Generator().manual_seed(n)
+    x = [torch.randn(300, H, 128, generator=gen).bfloat16().cuda() for _ in range(2)]
+    _, slots, _ = pk.pages_extend(p, i32([70, 220, 10]), 300)
+    pk.pages_append(p, *x, slots)
+    starts, slots, positions = pk.pages_extend(p, i32([n, n, n]), 3 * n, check=False)
+    fits = 220 + n <= 256
+    assert pk.arckv_query_status(p.state) == (0 if fits else 2) and p.len.tolist() == [70 + n, 220 + n * fits, 10 + n]
+    assert bool((slots[n:2 * n] >= 0).all() if fits else (slots[n:2 * n] == -1).all())
+    new = [torch.randn(3 * n, H, 128, generator=gen).bfloat16().cuda() for _ in range(2)]
+    pk.pages_append(p, *new, slots)
+    Q = torch.randn(3 * n, H, G, 128, generator=gen).bfloat16().cuda()
+    O = pk.pages_attend(p, Q, starts, max_count=n)
+    two = pk.pages_alloc(2, H, 9, 256)
+    _, slots, _ = pk.pages_extend(two, i32([70 + n, 10 + n]), 80 + 2 * n)
+    pk.pages_append(two, *[torch.cat([a[:70], b[:n], a[290:], b[2 * n:]]) for a, b in zip(x, new)], slots)
+    keep = torch.cat([torch.arange(n), torch.arange(2 * n, 3 * n)]).cuda()
+    want = pk.pages_attend(two, Q[keep], i32([0, n, 2 * n]), max_count=n).float()
+    # The same tokens, cut into items elsewhere.  Each is off by half a bf16 step and by 2^-10 (A + B) + 2 d A, where weights sum
+    # A <= 1 of the values' magnitudes, B <= 4 of a token's largest, and keys' roundings move logits by d <= 2^-11 * 9.
+    assert bool(((O[keep].float() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -5).all())
