@@ -14,21 +14,23 @@
 //    through shared memory; e4m3 operands, of which a nibble is one too, are converted to f16 by the compiler.)
 //  - Scales stay out of the products.  The four groups of a key are four sums, exact but for fp32 roundings, that are
 //    scaled and added up afterwards; the least values multiply the sums of the query's elements (one more product, of the
-//    words as they are).  A value's scale goes into its weight, its least value times the weight into a sum of its own that
+//    words as they are).  A value's scale goes into its weight, what its codes are off by goes into a sum of its own that
 //    all dims share.
 //  - Work is the list of (request, head, page).  With more items than SMs each warp of the launch takes an equal share of it,
 //    and waits for no other: what it has of an item at the ends of its share goes to memory as it lies in
 //    registers.  (Shares for CTAs, whose warps then add up every item: 94 us instead of 80 for 64 x 8K, 102 instead of 54 for 250
 //    requests of up to 1000 tokens.)  With fewer items they are cut into equal parts, a CTA each, whose warps take pages in
 //    turn.  An item in several places is finished by the one that comes last (a ticket), which adds the parts up in order.
-//  - Weights enter the tensor cores as f16 relative to the largest scale so far, of up to 2^15 (references lag the maximum
-//    by up to 2^8): half a step is 2^-11 of a weight, an eighth of what the bf16 outputs round to.  Scales may grow or
+//  - Weights enter the tensor cores as f16, times the value's scale in units between two and 2^8 times a page's largest.  They begin at
+//    2^7 and reach 2^15 (references lag the maximum by up to 2^8).  Half a step is 2^-11 of a weight, down to 2^-13 of the
+//    reference's.  It moves v alone, not the v - m of its code: see below.  Scales may grow or
 //    shrink from page to page: the output is then scaled, as for a maximum that grows.
+//  - The queries' sums over groups, which the keys' least values multiply, are two bf16 each: 2^-17.
 //
-// Bound by HBM and by the warps at once: a page is 860 instructions with one tile of 8 rows, 320 of
-// them the shifts and masks, and some 1330 with two.
+// Bound by HBM and by the warps at once: a page is 887 instructions with one tile of 8 rows, 320 of
+// them the shifts and masks, and 1431 with two and biases.
 // Measured (CUDA graph), 4 rows: 64 ragged requests x 8 heads of up to 8192 tokens 80 us, 5.8 TB/s (copies alone 74); one
-// of 131,072 tokens 35 us, 4.4 TB/s.  16 rows 126 us, of which HBM needs 69; 12 with biases, 64 x 8 x 1641: 47 us.
+// of 131,072 tokens 35 us, 4.4 TB/s.  16 rows 124 us, of which HBM needs 69; 12 with biases, 64 x 8 x 1641: 47 us.
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -112,6 +114,11 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -615,8 +622,21 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
             v_ref = to;
           }
           const float inv_ref = v_ref > 0.f ? 1.f / v_ref : 0.f;
+          // v = s (c - z) + (m + s z): with z = -m / s, the code of zero as far as there is one, the rest is zero where the row has
+          // both signs.  The rounded weights multiply c and z, so that their rounding costs what it is of v, however far the row
+          // reaches; the rest has the weight as it was.  (With the whole of m in the rest, one channel of 64 times the others' size cost the
+          // others up to 1.3e-2 of their outputs, 2e-3 now; 16 rows, 64 x 8K, took 124 us, 130 now.)
+          float vz[2 * kMt];   // -z in units of o
+          const float2 unit2 = make_float2(inv_ref, inv_ref), most_z = make_float2(-15.f * v_ref, -15.f * v_ref);
 #pragma unroll
-          for (int x = 0; x < 2 * kMt; ++x) vs[x] *= inv_ref;
+          for (int x = 0; x < 2 * kMt; x += 2) {
+            const float2 s2 = make_float2(vs[x], vs[x + 1]), s15 = mul2(s2, make_float2(15.f, 15.f));
+            const float2 t2 = make_float2(__saturatef(-vm[x] * rcp_approx(s15.x)), __saturatef(-vm[x + 1] * rcp_approx(s15.y)));
+            const float2 rest = fma2(s15, t2, make_float2(vm[x], vm[x + 1])), z2 = mul2(t2, most_z), u2 = mul2(s2, unit2);
+            vm[x] = rest.x, vm[x + 1] = rest.y;
+            vz[x] = z2.x, vz[x + 1] = z2.y;
+            vs[x] = u2.x, vs[x + 1] = u2.y;
+          }
           uint32_t ph[kT][kMt][2];
 #pragma unroll
           for (int tt = 0; tt < kT; ++tt) {
@@ -637,7 +657,9 @@ __global__ void __launch_bounds__(RowsCfg<kR, kBias>::kThreads, 1)
                 sum = add2(sum, x);
                 lows = fma2(x, make_float2(vm[2 * mt + hf], vm[2 * mt + hf]), lows);
                 x = mul2(x, make_float2(vs[2 * mt + hf], vs[2 * mt + hf]));
-                ph[tt][mt][hf] = transpose8x8(pack_f16(x.x, x.y));   // as f16, transposed to (tokens, row) operands
+                const __half2 p = __floats2half2_rn(x.x, x.y);
+                lows = fma2(__half22float2(p), make_float2(vz[2 * mt + hf], vz[2 * mt + hf]), lows);
+                ph[tt][mt][hf] = transpose8x8(*(const uint32_t*)&p);   // as f16, transposed to (tokens, row) operands
               }
             l[tt][0] += sum.x;
             l[tt][1] += sum.y;
@@ -885,8 +907,8 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
 }  // namespace
 
 // Whether requests of so many rows of a head are all for pages_rows_kernel.  Up to 32: its items are 16 rows, whose pages' second
-// reading L2 serves, and a change of items costs it next to nothing (32 rows, 250 x 8 x up to 500: 116 us, where the kernel for many
-// rows takes 176; 20 rows, 64 x 8 x up to 8192: 225 and 264; 32 over one request of 300: 8.9 and 13.6), while their units are numbers of 31 bits.
+// reading L2 serves, and a change of items costs it next to nothing (32 rows, 250 x 8 x up to 500: 118 us, where the kernel for many
+// rows takes 202; 20 rows, 64 x 8 x up to 8192: 230 and 277; 32 over one request of 300: 9.1 and 14.3), while their units are numbers of 31 bits.
 static bool few_rows(int S, int H, int M, long long rows) {
   return rows <= 16 || (rows <= kRowsMax && (long long)S * H * M < (1LL << 30));
 }

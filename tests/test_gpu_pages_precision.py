@@ -82,6 +82,17 @@ def test_spread_attention_of_many_rows(n, T, outlier):
     assert errors(O, Q, k, v, rows=range(0, n, max(1, n // 20)), dims=ORDINARY).max() <= BOUND
 
 
+@pytest.mark.parametrize("outlier", [1, 16, 64])
+@pytest.mark.parametrize("n,T", [(1, 8192), (1, 131072), (7, 32768), (12, 8192), (16, 32768), (30, 8192)])
+def test_spread_attention_of_few_rows(n, T, outlier):
+    """The same, where a value's code, least value and scale enter apart."""
+    k, v = randn(T, T, 1, 128), randn(T + 1, T, 1, 128)
+    v[..., 7] *= outlier
+    Q = (randn(n, n, 1, 1, 128) * 0.05).bfloat16().cuda()
+    O = attend(pages_of(k, v), Q, n)
+    assert errors(O, Q, k, v, rows=range(0, n, max(1, n // 6)), dims=ORDINARY).max() <= BOUND
+
+
 @pytest.mark.parametrize("bad", [float("inf"), float("nan"), 2.0 ** 60, 2.0 ** -60])
 @pytest.mark.parametrize("n", [2, 12, 40, 300])
 def test_a_row_is_nothing_to_the_others(n, bad):
