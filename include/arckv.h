@@ -530,8 +530,8 @@ arckv_status arckv_pages_read(const arckv_pages4* p, int32_t N, const int32_t* s
                               uint32_t flags, void* stream);
 
 /* Workspace bytes of arckv_pages_attend for up to max_count rows of a request
- * (0 if the sizes are invalid).  Host-only.  As for the 8-bit cache, the first
- * ARCKV_CACHE_WS_HEADER bytes must be zeroed once before the first use. */
+ * (0 if the sizes are invalid); it serves calls of fewer rows too.  Host-only.  As for the 8-bit cache,
+ * the first ARCKV_CACHE_WS_HEADER bytes must be zeroed once before the first use, and after ARCKV_ERR_TIMEOUT. */
 size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32_t d, int32_t max_count, int32_t G);
 
 /*
@@ -550,10 +550,20 @@ size_t arckv_pages_attend_workspace_bytes(int32_t S, int32_t H, int32_t M, int32
  *      request are left as they are.
  * ARCKV_ERR_SHAPE at once for calls too long to be counted: H M (N G / R + S) from
  * 2^38 on, with R = 128 (256 where max_count G > 128).
- * Softmax weights and sums are fp32; weights, and with many rows keys and values,
- * enter the products as f16 (2^-11 of each), where an output's rounding to bf16
- * takes 2^-8.  Pages that
- * the table names past the pool record ARCKV_ERR_INVALID_ARG and are passed over,
+ * Logits, softmax weights and sums are fp32.  What enters the products with fewer
+ * bits, where an output's rounding to bf16 takes 2^-8 of it:
+ *   weights   f16, times the value's size relative to its page's largest: 2^-11 of what
+ *             is then at least 2^-13 of the row's largest weight, below that 2^-24 of
+ *             the row's largest weight times the page's largest value.
+ *   q         with up to 32 rows sums over 32 dims, as two bf16 (2^-17), for the
+ *             least elements of k_j
+ *   k, v      with more rows f16: 2^-11 of an element, or 2^-17 of its page's largest
+ *             if that is more; keys move a logit by as much of its sum of |q k|
+ *   parts     with more rows, of a row that several CTAs share: f16, 2^-11 of each
+ * and fp32 sums of products round towards zero (7e-8 of them a page).  The sizes of
+ * values may differ from page to page: by 2^60 with more than 32 rows, down to 2^-38
+ * behind larger ones with fewer; what lies below counts for less, or as zero.
+ * Pages that the table names past the pool record ARCKV_ERR_INVALID_ARG and are passed over,
  * as are missing ones.  Outputs that are not finite record ARCKV_ERR_NONFINITE, and
  * so do logits that pass 2^22 in magnitude as a row's largest (of pages without biases):
  * fp32 holds their differences no more, and the row may hold anything.
@@ -567,7 +577,8 @@ arckv_status arckv_pages_attend(const arckv_pages4* p, int32_t N, int32_t G, int
  * a = 2 pi positions[n] turns[i] / 2^64:
  *   y1 = f (x1 cos a - x2 sin a),  y2 = f (x2 cos a + x1 sin a)
  * (products in fp32, rounded once at the end); the other d - r are copied.
- * Angles are reduced exactly, so they are as good at any position as at zero.
+ * Angles are reduced exactly, so they are as good at any position as at zero, and
+ * then rounded to 24 bits of half a turn (2^-32 of a turn at least).
  *   turns      uint64 [r/2] device: turns a position, in units of 2^-64
  *   positions  int32 [N] device; rows with one below zero are copied
  *   X, Y       rows (n, head) of the given number of heads, bf16 or fp32 with ARCKV_FLAG_F32; row (n, h)

@@ -27,10 +27,10 @@
 //    shrink from page to page: the output is then scaled, as for a maximum that grows.
 //  - The queries' sums over groups, which the keys' least values multiply, are two bf16 each: 2^-17.
 //
-// Bound by HBM and by the warps at once: a page is 887 instructions with one tile of 8 rows, 320 of
-// them the shifts and masks, and 1431 with two and biases.
+// Bound by HBM and by the warps at once: a page is 933 instructions with one tile of 8 rows, 320 of
+// them the shifts and masks, and 1519 with two and biases.
 // Measured (CUDA graph), 4 rows: 64 ragged requests x 8 heads of up to 8192 tokens 80 us, 5.8 TB/s (copies alone 74); one
-// of 131,072 tokens 35 us, 4.4 TB/s.  16 rows 124 us, of which HBM needs 69; 12 with biases, 64 x 8 x 1641: 47 us.
+// of 131,072 tokens 35 us, 4.4 TB/s.  16 rows 130 us, of which HBM needs 69; 12 with biases, 64 x 8 x 1641: 48 us.
 #include "pages.cuh"
 #include "tc.cuh"
 
@@ -907,8 +907,8 @@ int launch_rows(const arckv_pages4& p, const PagesQuery& q, float scale, int lim
 }  // namespace
 
 // Whether requests of so many rows of a head are all for pages_rows_kernel.  Up to 32: its items are 16 rows, whose pages' second
-// reading L2 serves, and a change of items costs it next to nothing (32 rows, 250 x 8 x up to 500: 118 us, where the kernel for many
-// rows takes 202; 20 rows, 64 x 8 x up to 8192: 230 and 277; 32 over one request of 300: 9.1 and 14.3), while their units are numbers of 31 bits.
+// reading L2 serves, and a change of items costs it next to nothing (32 rows, 250 x 8 x up to 500: 122 us, where the kernel for many
+// rows takes 202; 20 rows, 64 x 8 x up to 8192: 241 and 277; 32 over one request of 300: 9.2 and 14.3), while their units are numbers of 31 bits.
 static bool few_rows(int S, int H, int M, long long rows) {
   return rows <= 16 || (rows <= kRowsMax && (long long)S * H * M < (1LL << 30));
 }

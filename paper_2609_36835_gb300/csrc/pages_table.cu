@@ -7,8 +7,8 @@
 // by itself in shared memory and fills its share of the rows from the state
 // before the call; the CTA that comes last (a ticket) then writes the new state.
 // One launch, bound by its chain of dependent loads.  Measured (CUDA graph): with
-// the truncation behind it 5.3 us for 64 requests of a token each, 8.5 for 250
-// requests and 16,000 rows.
+// the truncation behind it 5.5 us for 64 requests of a token each, 9.0 for 250
+// requests and 16,000 rows (of which the look for missing pages takes 0.5).
 #include "pages.cuh"
 
 namespace arckv {

@@ -34,9 +34,8 @@
 // Bound by shared memory, which the N = 64 products of S read Q from once a page, and by the softmax's issue (a page and 256
 // rows take 0.93 us, of which the pipe needs 0.54; steps of two pages with one buffer of S took longer, 295 us against 237;
 // a warp for S and one for P V 265).  With one tile a page takes 0.8 us: a chain of waits, whatever the rows.
-// Measured (CUDA graph): 2048 rows of 8 heads over 32,768 tokens 234 us, 1.16 PFLOP/s; 256 rows over 8192 34 us with the join;
-// 32 rows, 250 x 8 x up to 500 (which pages_attend.cu takes in 116): 177 us, most of it changes of items (207 where each warp
-// looked up its next item itself).
+// Measured (CUDA graph): 2048 rows of 8 heads over 32,768 tokens 242 us, 1.13 PFLOP/s; 256 rows over 8192 34 us with the join;
+// 32 rows, 250 x 8 x up to 500 (which pages_attend.cu takes in 122): 202 us, most of it changes of items.
 #include "pages.cuh"
 #include "tc.cuh"
 
